@@ -353,6 +353,90 @@ mlip_status mlip_md_second_half(mlip_ctx* ctx, double* vel_dev, const double* fo
 /* Kinetic energy sum_i m_i |v_i|^2 / 2 in eV into *ke_host (synchronises). */
 mlip_status mlip_md_kinetic(mlip_ctx* ctx, const double* vel_dev, double* ke_host);
 
+/*
+ * Learning operators: what the tables of the potential are learned with.
+ * Training is outside the paper's runtime (its models are fitted to energies
+ * and forces beforehand); these calls are the parts of a training step that
+ * run per atom or per weight, and the heads they train can be chosen by the
+ * environment of an atom instead of by its species alone (Section 3.2).
+ *
+ * A mlip_learn context holds the stream, the workspace and the error text of
+ * the calls made with it.  Work is enqueued on its stream; buffers are the
+ * caller's, as above.  A call may enlarge the workspace (hipMalloc, and a
+ * wait for the stream where an older one is freed) the first time it meets a
+ * size; later calls of that size or smaller allocate nothing.  All results
+ * are the same from run to run: nothing is summed in an order that depends on
+ * the scheduling of work-groups.
+ */
+typedef struct mlip_learn mlip_learn;
+typedef enum { MLIP_F32 = 0, MLIP_BF16 = 1 } mlip_dtype;
+
+/* Create a context on the current HIP device.  Errors: MLIP_E_ARG,
+   MLIP_E_OOM, MLIP_E_HIP; mlip_learn_last_error(NULL) then says why. */
+mlip_status mlip_learn_create(void* hip_stream, mlip_learn** out);
+const char* mlip_learn_last_error(const mlip_learn* ctx);
+mlip_status mlip_learn_memory_bytes(const mlip_learn* ctx, size_t* bytes);
+/* Release the context after its stream's work (NULL is ignored). */
+void mlip_learn_destroy(mlip_learn* ctx);
+
+/*
+ * Route n rows (atoms) to top_k of n_experts experts (energy heads).
+ *   logits_dev  f32 or bf16 [n][n_experts], rows row_stride values apart
+ *   kinds_dev   int32 [n] and allowed_dev uint8 [n_kinds][n_experts], or both
+ *               NULL: row i may use expert e only where
+ *               allowed[kinds[i]][e] != 0; a row whose kind is outside
+ *               [0, n_kinds) uses none.  A logit of -infinity takes its expert
+ *               out too.  What stands at places that are out is not looked at
+ *               (it may be NaN)
+ *   experts_dev int32 [n][top_k], the experts of the largest logits in falling
+ *               order (equal logits: the lower index first), -1 where fewer
+ *               are left
+ *   gates_dev   f32 [n][top_k], 0 at -1: with MLIP_GATES_CHOSEN the softmax
+ *               over the chosen experts' logits, with MLIP_GATES_ALL their
+ *               probabilities p_ie, the softmax over all that the row may use
+ *   counts_dev  int32 [n_experts + 1], entries per expert, then the number of
+ *               rows that have any expert
+ *   loss_dev    f32 [1], the balance loss n_experts sum_e f_e P_e with f_e =
+ *               counts_e / sum counts and P_e the mean of p_ie over the rows
+ *               that have any expert: 1 where all experts are used alike, up to
+ *               n_experts where one is; 0 without such rows
+ * A NaN (or +infinity) among the logits a row may use makes its gates NaN.
+ * mlip_route_backward writes the logits' gradient (their type, [n][n_experts]
+ * contiguous) of sum(dgates gates) + dloss loss: the choice of experts and the
+ * shares f_e are constants of it.  dgates_dev [n][top_k] (not looked at where
+ * experts is -1) or NULL, dloss_dev [1] or NULL: none.
+ * n in [0, 2^31 / top_k), n_experts 1..256, top_k 1..16 and <= n_experts.
+ * Errors: MLIP_E_ARG, MLIP_E_OOM, MLIP_E_HIP.
+ */
+typedef enum { MLIP_GATES_CHOSEN = 0, MLIP_GATES_ALL = 1 } mlip_gates;
+typedef struct {
+  int32_t n_experts;
+  int32_t top_k;
+  int32_t n_kinds;     /* rows of allowed_dev; 0 without it */
+  int32_t gates;       /* mlip_gates */
+  int32_t dtype;       /* mlip_dtype of the logits and their gradient */
+  int64_t row_stride;  /* values between rows of the logits, >= n_experts */
+} mlip_route_params;
+
+mlip_status mlip_route(mlip_learn* ctx, const mlip_route_params* p, int64_t n, const void* logits_dev,
+                       const int32_t* kinds_dev, const uint8_t* allowed_dev, int32_t* experts_dev, float* gates_dev,
+                       int32_t* counts_dev, float* loss_dev);
+mlip_status mlip_route_backward(mlip_learn* ctx, const mlip_route_params* p, int64_t n, const void* logits_dev,
+                                const int32_t* kinds_dev, const uint8_t* allowed_dev, const int32_t* experts_dev,
+                                const int32_t* counts_dev, const float* dgates_dev, const float* dloss_dev,
+                                void* dlogits_dev);
+
+/*
+ * Group n_entries routed entries (experts_dev, [n][top_k] flat, or one species
+ * per atom) by expert: order_dev int32 [n_entries] receives the entries'
+ * indices, those of expert e at offsets_dev[e] .. offsets_dev[e + 1] - 1 in
+ * rising order, and after offsets_dev[n_experts] those whose id is outside
+ * [0, n_experts).  offsets_dev int32 [n_experts + 1].
+ * n_entries in [0, 2^31), n_experts 1..256.  Errors: MLIP_E_ARG, MLIP_E_OOM, MLIP_E_HIP.
+ */
+mlip_status mlip_group(mlip_learn* ctx, int64_t n_entries, int32_t n_experts, const int32_t* experts_dev,
+                       int32_t* offsets_dev, int32_t* order_dev);
+
 #ifdef __cplusplus
 }
 #endif

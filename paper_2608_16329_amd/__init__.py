@@ -12,8 +12,9 @@ import numpy as np
 
 from . import binding
 from .binding import MlipError, mlip_hparams
+from .learn import Learner
 
-__all__ = ["binding", "MlipError", "mlip_hparams", "Potential"]
+__all__ = ["binding", "MlipError", "mlip_hparams", "Potential", "Learner"]
 
 
 class Potential:

@@ -25,13 +25,17 @@ STATUS = {0: "MLIP_OK", -1: "MLIP_E_ARG", -2: "MLIP_E_OOM", -3: "MLIP_E_HIP", -4
 EXPORTED = ["mlip_weight_count", "mlip_create", "mlip_build_neighbors", "mlip_compute", "mlip_get_neighbors",
             "mlip_memory_bytes", "mlip_get_stats", "mlip_last_error", "mlip_destroy", "mlip_md_set_masses",
             "mlip_md_first_half", "mlip_md_second_half", "mlip_md_kinetic", "mlip_set_fusion",
-            "mlip_get_neighbor_rows", "mlip_compute_noalloc", "mlip_set_scatter", "mlip_set_list_format"]
+            "mlip_get_neighbor_rows", "mlip_compute_noalloc", "mlip_set_scatter", "mlip_set_list_format",
+            "mlip_learn_create", "mlip_learn_last_error", "mlip_learn_memory_bytes", "mlip_learn_destroy",
+            "mlip_route", "mlip_route_backward", "mlip_group"]
 
 MLIP_STATIC_SCRATCH_BYTES = 256 * 1024 * 1024
 
 MLIP_FUSION_CACHED, MLIP_FUSION_RECOMPUTE, MLIP_FUSION_PARTIAL, MLIP_FUSION_UNFUSED = 0, 1, 2, 3
 MLIP_SCATTER_ATOMIC, MLIP_SCATTER_TILE = 0, 1
 MLIP_LIST_AUTO, MLIP_LIST_INDEX = 0, 1
+MLIP_F32, MLIP_BF16 = 0, 1
+MLIP_GATES_CHOSEN, MLIP_GATES_ALL = 0, 1
 
 
 class mlip_hparams(ctypes.Structure):
@@ -51,6 +55,11 @@ class mlip_stats(ctypes.Structure):
 
     def as_dict(self):
         return {name: getattr(self, name) for name, _ in self._fields_}
+
+
+class mlip_route_params(ctypes.Structure):
+    _fields_ = [("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("n_kinds", ctypes.c_int32),
+                ("gates", ctypes.c_int32), ("dtype", ctypes.c_int32), ("row_stride", ctypes.c_int64)]
 
 
 class MlipError(RuntimeError):
@@ -86,6 +95,13 @@ def _load() -> ctypes.CDLL:
         "mlip_set_fusion": (st, [vp, ctypes.c_int32]),
         "mlip_set_scatter": (st, [vp, ctypes.c_int32]),
         "mlip_set_list_format": (st, [vp, ctypes.c_int32]),
+        "mlip_learn_create": (st, [vp, ctypes.POINTER(vp)]),
+        "mlip_learn_last_error": (ctypes.c_char_p, [vp]),
+        "mlip_learn_memory_bytes": (st, [vp, ctypes.POINTER(ctypes.c_size_t)]),
+        "mlip_learn_destroy": (None, [vp]),
+        "mlip_route": (st, [vp, ctypes.POINTER(mlip_route_params), ctypes.c_int64] + [vp] * 7),
+        "mlip_route_backward": (st, [vp, ctypes.POINTER(mlip_route_params), ctypes.c_int64] + [vp] * 8),
+        "mlip_group": (st, [vp, ctypes.c_int64, ctypes.c_int32, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -222,6 +238,47 @@ def mlip_md_kinetic(ctx: int, vel_ptr: int) -> float:
     out = np.zeros(1)
     _check(ctx, _lib.mlip_md_kinetic(ctx, vel_ptr, _dp(out)))
     return float(out[0])
+
+
+def _check_learn(ctx, status: int):
+    if status != MLIP_OK:
+        raise MlipError(status, _lib.mlip_learn_last_error(ctx).decode())
+
+
+def mlip_learn_create(hip_stream: int = 0) -> int:
+    ctx = ctypes.c_void_p()
+    _check_learn(None, _lib.mlip_learn_create(hip_stream or None, ctypes.byref(ctx)))
+    return ctx.value
+
+
+def mlip_learn_last_error(ctx: int) -> str:
+    return _lib.mlip_learn_last_error(ctx).decode()
+
+
+def mlip_learn_memory_bytes(ctx: int) -> int:
+    b = ctypes.c_size_t()
+    _check_learn(ctx, _lib.mlip_learn_memory_bytes(ctx, ctypes.byref(b)))
+    return int(b.value)
+
+
+def mlip_learn_destroy(ctx: int) -> None:
+    _lib.mlip_learn_destroy(ctx)
+
+
+def mlip_route(ctx: int, params: mlip_route_params, n: int, logits_ptr, kinds_ptr, allowed_ptr, experts_ptr, gates_ptr,
+               counts_ptr, loss_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_route(ctx, ctypes.byref(params), n, logits_ptr, kinds_ptr, allowed_ptr, experts_ptr,
+                                      gates_ptr, counts_ptr, loss_ptr))
+
+
+def mlip_route_backward(ctx: int, params: mlip_route_params, n: int, logits_ptr, kinds_ptr, allowed_ptr, experts_ptr,
+                        counts_ptr, dgates_ptr, dloss_ptr, dlogits_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_route_backward(ctx, ctypes.byref(params), n, logits_ptr, kinds_ptr, allowed_ptr,
+                                               experts_ptr, counts_ptr, dgates_ptr, dloss_ptr, dlogits_ptr))
+
+
+def mlip_group(ctx: int, n_entries: int, n_experts: int, experts_ptr, offsets_ptr, order_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_group(ctx, n_entries, n_experts, experts_ptr, offsets_ptr, order_ptr))
 
 
 def exported_symbols():

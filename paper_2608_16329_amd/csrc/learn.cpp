@@ -1,0 +1,184 @@
+// C ABI of the learning operators (declared in include/mlip.h): contexts,
+// argument checks, workspace, and the launches of their kernels.
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <string>
+
+#include "learn.h"
+
+using namespace mlip;
+
+namespace {
+
+thread_local std::string t_learn_err;
+
+mlip_status fail(mlip_learn* ctx, mlip_status st, const char* msg) {
+  // no exception crosses the ABI: without memory for it the text is dropped
+  try {
+    (ctx ? ctx->err : t_learn_err) = msg;
+  } catch (...) {
+    (ctx ? ctx->err : t_learn_err).clear();
+  }
+  return st;
+}
+
+mlip_status fail_hip(mlip_learn* ctx, hipError_t e) {
+  (void)hipGetLastError();
+  return fail(ctx, MLIP_E_HIP, hipGetErrorString(e));
+}
+
+#define LEARN_HIP(ctx, expr)                          \
+  do {                                                \
+    const hipError_t e_ = (expr);                     \
+    if (e_ != hipSuccess) return fail_hip((ctx), e_); \
+  } while (0)
+
+// The workspace holds at least `need` bytes; it is freed and allocated anew
+// where it is smaller, after the stream's work that may still use it.
+mlip_status workspace(mlip_learn* ctx, size_t need) {
+  if (need <= ctx->cap_ws) return MLIP_OK;
+  if (ctx->d_ws) {
+    LEARN_HIP(ctx, hipStreamSynchronize(ctx->stream));
+    (void)hipFree(ctx->d_ws);
+    ctx->d_ws = nullptr;
+    ctx->cap_ws = 0;
+  }
+  const size_t size = (need + need / 4 + 255) / 256 * 256;
+  if (hipMalloc(reinterpret_cast<void**>(&ctx->d_ws), size) != hipSuccess) {
+    ctx->d_ws = nullptr;
+    (void)hipGetLastError();
+    return fail(ctx, MLIP_E_OOM, "device allocation failed: workspace");
+  }
+  ctx->cap_ws = size;
+  return MLIP_OK;
+}
+
+mlip_status check_route(mlip_learn* ctx, const mlip_route_params* p, int64_t n, const void* logits,
+                        const int32_t* kinds, const uint8_t* allowed) {
+  if (!p) return fail(ctx, MLIP_E_ARG, "NULL parameters");
+  if (p->n_experts < 1 || p->n_experts > kMaxExperts) return fail(ctx, MLIP_E_ARG, "n_experts must be in 1..256");
+  if (p->top_k < 1 || p->top_k > kMaxTopK || p->top_k > p->n_experts)
+    return fail(ctx, MLIP_E_ARG, "top_k must be in 1..16 and at most n_experts");
+  if (p->gates != MLIP_GATES_CHOSEN && p->gates != MLIP_GATES_ALL) return fail(ctx, MLIP_E_ARG, "unknown gates");
+  if (p->dtype != MLIP_F32 && p->dtype != MLIP_BF16) return fail(ctx, MLIP_E_ARG, "unknown dtype");
+  if (n < 0 || n >= (int64_t(1) << 31) / p->top_k) return fail(ctx, MLIP_E_ARG, "n outside [0, 2^31 / top_k)");
+  if (p->row_stride < p->n_experts || p->row_stride > (int64_t(1) << 31))
+    return fail(ctx, MLIP_E_ARG, "row_stride must be in n_experts..2^31");
+  if (!kinds != !allowed) return fail(ctx, MLIP_E_ARG, "kinds and allowed go together");
+  if (kinds ? p->n_kinds < 1 : p->n_kinds != 0) return fail(ctx, MLIP_E_ARG, "n_kinds must fit allowed");
+  if (n > 0 && !logits) return fail(ctx, MLIP_E_ARG, "NULL logits");
+  return MLIP_OK;
+}
+
+RouteArgs route_args(const mlip_route_params* p, int64_t n, const void* logits, const int32_t* kinds,
+                     const uint8_t* allowed) {
+  RouteArgs a{};
+  a.n = n;
+  a.stride = p->row_stride;
+  a.E = p->n_experts;
+  a.K = p->top_k;
+  a.n_kinds = p->n_kinds;
+  a.bf16 = p->dtype == MLIP_BF16;
+  a.all = p->gates == MLIP_GATES_ALL;
+  a.logits = logits;
+  a.kinds = kinds;
+  a.allowed = allowed;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+mlip_status mlip_learn_create(void* hip_stream, mlip_learn** out) {
+  t_learn_err.clear();
+  if (!out) return fail(nullptr, MLIP_E_ARG, "NULL output pointer");
+  *out = nullptr;
+  mlip_learn* ctx = new (std::nothrow) mlip_learn();
+  if (!ctx) return fail(nullptr, MLIP_E_OOM, "host allocation failed");
+  ctx->stream = reinterpret_cast<hipStream_t>(hip_stream);
+  if (hipGetDevice(&ctx->device) != hipSuccess ||
+      hipDeviceGetAttribute(&ctx->n_cu, hipDeviceAttributeMultiprocessorCount, ctx->device) != hipSuccess) {
+    (void)hipGetLastError();
+    delete ctx;
+    return fail(nullptr, MLIP_E_HIP, "no current HIP device");
+  }
+  *out = ctx;
+  return MLIP_OK;
+}
+
+const char* mlip_learn_last_error(const mlip_learn* ctx) { return ctx ? ctx->err.c_str() : t_learn_err.c_str(); }
+
+mlip_status mlip_learn_memory_bytes(const mlip_learn* ctx, size_t* bytes) {
+  if (!ctx || !bytes) return MLIP_E_ARG;
+  *bytes = ctx->cap_ws;
+  return MLIP_OK;
+}
+
+void mlip_learn_destroy(mlip_learn* ctx) {
+  if (!ctx) return;
+  (void)hipStreamSynchronize(ctx->stream);
+  if (ctx->d_ws) (void)hipFree(ctx->d_ws);
+  (void)hipGetLastError();
+  delete ctx;
+}
+
+mlip_status mlip_route(mlip_learn* ctx, const mlip_route_params* p, int64_t n, const void* logits_dev,
+                       const int32_t* kinds_dev, const uint8_t* allowed_dev, int32_t* experts_dev, float* gates_dev,
+                       int32_t* counts_dev, float* loss_dev) {
+  if (!ctx) return MLIP_E_ARG;
+  ctx->err.clear();
+  const mlip_status st = check_route(ctx, p, n, logits_dev, kinds_dev, allowed_dev);
+  if (st != MLIP_OK) return st;
+  if (!counts_dev || !loss_dev || (n > 0 && (!experts_dev || !gates_dev))) return fail(ctx, MLIP_E_ARG, "NULL output");
+  RouteArgs a = route_args(p, n, logits_dev, kinds_dev, allowed_dev);
+  a.experts = experts_dev;
+  a.gates = gates_dev;
+  a.counts = counts_dev;
+  a.loss = loss_dev;
+  const int blocks = route_blocks(n, a.E, ctx->n_cu);
+  if (blocks > 1) {
+    const mlip_status w = workspace(ctx, size_t(blocks) * size_t(2 * a.E + 1) * sizeof(float));
+    if (w != MLIP_OK) return w;
+    a.part_p = reinterpret_cast<float*>(ctx->d_ws);
+    a.part_c = reinterpret_cast<int32_t*>(ctx->d_ws) + size_t(blocks) * size_t(a.E);
+  }
+  LEARN_HIP(ctx, launch_route(a, blocks, ctx->stream));
+  return MLIP_OK;
+}
+
+mlip_status mlip_route_backward(mlip_learn* ctx, const mlip_route_params* p, int64_t n, const void* logits_dev,
+                                const int32_t* kinds_dev, const uint8_t* allowed_dev, const int32_t* experts_dev,
+                                const int32_t* counts_dev, const float* dgates_dev, const float* dloss_dev,
+                                void* dlogits_dev) {
+  if (!ctx) return MLIP_E_ARG;
+  ctx->err.clear();
+  const mlip_status st = check_route(ctx, p, n, logits_dev, kinds_dev, allowed_dev);
+  if (st != MLIP_OK) return st;
+  if (n == 0) return MLIP_OK;
+  if (!experts_dev || !counts_dev || !dlogits_dev) return fail(ctx, MLIP_E_ARG, "NULL argument");
+  RouteArgs a = route_args(p, n, logits_dev, kinds_dev, allowed_dev);
+  a.experts = const_cast<int32_t*>(experts_dev);
+  a.counts = const_cast<int32_t*>(counts_dev);
+  a.dgates = dgates_dev;
+  a.dloss = dloss_dev;
+  a.dlogits = dlogits_dev;
+  LEARN_HIP(ctx, launch_route_backward(a, ctx->n_cu, ctx->stream));
+  return MLIP_OK;
+}
+
+mlip_status mlip_group(mlip_learn* ctx, int64_t n_entries, int32_t n_experts, const int32_t* experts_dev,
+                       int32_t* offsets_dev, int32_t* order_dev) {
+  if (!ctx) return MLIP_E_ARG;
+  ctx->err.clear();
+  if (n_experts < 1 || n_experts > kMaxExperts) return fail(ctx, MLIP_E_ARG, "n_experts must be in 1..256");
+  if (n_entries < 0 || n_entries >= (int64_t(1) << 31)) return fail(ctx, MLIP_E_ARG, "n_entries outside [0, 2^31)");
+  if (!offsets_dev || (n_entries > 0 && (!experts_dev || !order_dev))) return fail(ctx, MLIP_E_ARG, "NULL argument");
+  const mlip_status w = workspace(ctx, group_ws_bytes(n_entries, n_experts));
+  if (w != MLIP_OK) return w;
+  LEARN_HIP(ctx, launch_group(experts_dev, n_entries, n_experts, offsets_dev, order_dev, ctx->d_ws, ctx->stream));
+  return MLIP_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,54 @@
+// Internal declarations of the learning operators: the context they share and
+// the host-side launchers of their kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+#include <string>
+
+#include "../../include/mlip.h"
+
+struct mlip_learn {
+  hipStream_t stream = nullptr;
+  int device = 0;
+  int n_cu = 0;
+  std::string err;
+  unsigned char* d_ws = nullptr;  // workspace of the calls, in the order of the stream
+  size_t cap_ws = 0;
+};
+
+namespace mlip {
+
+constexpr int kMaxExperts = 256;   // heads a row can be routed to
+constexpr int kMaxTopK = 16;
+
+// Arguments of the routing kernels (mlip_route, mlip_route_backward).
+struct RouteArgs {
+  int64_t n;
+  int64_t stride;             // values between rows of the logits
+  int E, K, n_kinds;
+  bool bf16, all;             // logits' type; gates are the probabilities themselves
+  const void* logits;
+  const int32_t* kinds;       // [n] or null
+  const uint8_t* allowed;     // [n_kinds][E] (with kinds)
+  int32_t* experts;           // [n][K]
+  float* gates;               // [n][K]
+  int32_t* counts;            // [E + 1]
+  float* loss;                // [1]
+  const float* dgates;        // [n][K] or null
+  const float* dloss;         // [1] or null
+  void* dlogits;              // [n][E], the logits' type
+  float* part_p;              // [blocks][E] sums of probabilities
+  int32_t* part_c;            // [blocks][E + 1] counts, routed rows
+};
+int route_blocks(int64_t n, int E, int n_cu);
+hipError_t launch_route(const RouteArgs& a, int blocks, hipStream_t s);
+hipError_t launch_route_backward(const RouteArgs& a, int n_cu, hipStream_t s);
+
+// Stable counting sort of m entries by expert; ids outside [0, E) come last.
+size_t group_ws_bytes(int64_t m, int E);
+hipError_t launch_group(const int32_t* experts, int64_t m, int E, int32_t* offsets, int32_t* order, void* ws, hipStream_t s);
+
+}  // namespace mlip

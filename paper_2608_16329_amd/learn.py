@@ -1,0 +1,153 @@
+"""The learning operators over PyTorch-ROCm tensors (C ABI in include/mlip.h).
+
+`Learner` wraps one mlip_learn context.  Every tensor is the caller's, outputs
+too; the arithmetic runs in the library's HIP kernels, and there is no fallback.
+"""
+from __future__ import annotations
+
+from contextlib import contextmanager
+from typing import Optional
+
+from . import binding as b
+
+_GATES = {"chosen": b.MLIP_GATES_CHOSEN, "all": b.MLIP_GATES_ALL}
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _ptr(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+class _OnStream:
+    """A stream of its own that is put in order with the caller's current one."""
+
+    def _bind(self, stream) -> None:
+        import torch
+        if not torch.cuda.is_available():
+            raise RuntimeError("no GPU visible: the MLIP library runs only on the GPU")
+        self.torch = torch
+        self.stream = stream if stream is not None else torch.cuda.current_stream()
+        self.device = self.stream.device
+        self._dtypes = {torch.float32: b.MLIP_F32, torch.bfloat16: b.MLIP_BF16}
+
+    @contextmanager
+    def _ordered(self):
+        """The call's work after what the current stream has, and what it gets next after the call's."""
+        current = self.torch.cuda.current_stream(self.device)
+        if current == self.stream:
+            yield
+            return
+        self.stream.wait_stream(current)
+        yield
+        current.wait_stream(self.stream)
+
+    def _dense(self, t, name: str, dtype, *shape):
+        _need(t.device == self.device, f"{name} is on {t.device}, not {self.device}")
+        _need(t.dtype == dtype, f"{name} is {t.dtype}, not {dtype}")
+        _need(tuple(t.shape) == shape, f"{name} has shape {tuple(t.shape)}, not {shape}")
+        _need(t.is_contiguous(), f"{name} is not contiguous")
+
+    def _rows(self, t, name: str) -> int:
+        """The values between the rows of a 2-d f32 or bf16 tensor."""
+        _need(t.device == self.device, f"{name} is on {t.device}, not {self.device}")
+        _need(t.dtype in self._dtypes, f"{name} is {t.dtype}, not float32 or bfloat16")
+        _need(t.dim() == 2, f"{name} has {t.dim()} dimensions, not 2")
+        n, m = t.shape
+        _need(m == 0 or t.stride(1) == 1 or m == 1, f"{name} has rows of values that are not next to each other")
+        stride = t.stride(0) if n > 1 else m
+        _need(stride >= m, f"{name} has rows that overlap")
+        return stride
+
+
+class Learner(_OnStream):
+    """One mlip_learn context bound to a stream (default: the current one).
+
+    A call made while another stream is current waits for that stream's work,
+    and the work that stream gets afterwards waits for the call's."""
+
+    def __init__(self, stream=None):
+        self.ctx = None
+        self._bind(stream)
+        with self.torch.cuda.device(self.device):
+            self.ctx = b.mlip_learn_create(self.stream.cuda_stream)
+
+    def close(self) -> None:
+        if self.ctx:
+            b.mlip_learn_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def memory_bytes(self) -> int:
+        return b.mlip_learn_memory_bytes(self.ctx)
+
+    # -- routing ---------------------------------------------------------------
+
+    def _route_params(self, logits, top_k: int, kinds, allowed, gates_of: str):
+        t = self.torch
+        stride = self._rows(logits, "logits")
+        n, n_experts = logits.shape
+        _need(gates_of in _GATES, f"gates_of is {gates_of!r}, not 'chosen' or 'all'")
+        _need((kinds is None) == (allowed is None), "kinds and allowed go together")
+        if kinds is not None:
+            self._dense(kinds, "kinds", t.int32, n)
+            _need(allowed.dim() == 2, "allowed is not 2-d")
+            self._dense(allowed, "allowed", t.uint8, allowed.shape[0], n_experts)
+        return b.mlip_route_params(n_experts, top_k, 0 if kinds is None else allowed.shape[0], _GATES[gates_of],
+                                   self._dtypes[logits.dtype], max(stride, n_experts))
+
+    def route(self, logits, experts, gates, counts, loss, *, kinds=None, allowed=None, gates_of: str = "chosen") -> None:
+        """Route the rows of `logits` (f32 or bf16 [n, E], rows may be apart) to
+        their experts.shape[1] largest experts: experts int32 [n, k], gates f32
+        [n, k], counts int32 [E + 1], loss f32 [1] (mlip_route).  kinds int32 [n]
+        and allowed uint8 [kinds, E] say which experts a row may use."""
+        t = self.torch
+        _need(experts.dim() == 2, "experts is not 2-d")
+        p = self._route_params(logits, experts.shape[1], kinds, allowed, gates_of)
+        n, n_experts = logits.shape
+        self._dense(experts, "experts", t.int32, n, p.top_k)
+        self._dense(gates, "gates", t.float32, n, p.top_k)
+        self._dense(counts, "counts", t.int32, n_experts + 1)
+        self._dense(loss, "loss", t.float32, 1)
+        with self._ordered():
+            b.mlip_route(self.ctx, p, n, _ptr(logits), _ptr(kinds), _ptr(allowed), _ptr(experts), _ptr(gates),
+                         _ptr(counts), _ptr(loss))
+
+    def route_backward(self, logits, experts, counts, dlogits, *, dgates=None, dloss=None, kinds=None, allowed=None,
+                       gates_of: str = "chosen") -> None:
+        """dlogits (the logits' type, [n, E]) of sum(dgates gates) + dloss loss,
+        from what `route` was given and what it wrote (mlip_route_backward)."""
+        t = self.torch
+        _need(experts.dim() == 2, "experts is not 2-d")
+        p = self._route_params(logits, experts.shape[1], kinds, allowed, gates_of)
+        n, n_experts = logits.shape
+        self._dense(experts, "experts", t.int32, n, p.top_k)
+        self._dense(counts, "counts", t.int32, n_experts + 1)
+        self._dense(dlogits, "dlogits", logits.dtype, n, n_experts)
+        if dgates is not None:
+            self._dense(dgates, "dgates", t.float32, n, p.top_k)
+        if dloss is not None:
+            self._dense(dloss, "dloss", t.float32, 1)
+        with self._ordered():
+            b.mlip_route_backward(self.ctx, p, n, _ptr(logits), _ptr(kinds), _ptr(allowed), _ptr(experts), _ptr(counts),
+                                  _ptr(dgates), _ptr(dloss), _ptr(dlogits))
+
+    def group(self, experts, offsets, order) -> None:
+        """The entries of `experts` (int32, any shape: [n, k] or one species per
+        atom) by expert: offsets int32 [E + 1], order int32 [entries] (mlip_group)."""
+        t = self.torch
+        m = experts.numel()
+        _need(offsets.dim() == 1 and offsets.shape[0] >= 2, "offsets is not 1-d with at least 2 places")
+        self._dense(experts, "experts", t.int32, *experts.shape)
+        self._dense(offsets, "offsets", t.int32, offsets.shape[0])
+        self._dense(order, "order", t.int32, m)
+        with self._ordered():
+            b.mlip_group(self.ctx, m, offsets.shape[0] - 1, _ptr(experts), _ptr(offsets), _ptr(order))
