@@ -437,6 +437,43 @@ mlip_status mlip_route_backward(mlip_learn* ctx, const mlip_route_params* p, int
 mlip_status mlip_group(mlip_learn* ctx, int64_t n_entries, int32_t n_experts, const int32_t* experts_dev,
                        int32_t* offsets_dev, int32_t* order_dev);
 
+/*
+ * The energy heads (Eq. 6; layout and formula of a head table at
+ * mlip_weight_count, hidden width 64) of n rows, each through the top_k heads it
+ * is routed to: energy_i = sum_s gate_is v_is with v_is the value of head
+ * experts_is at row i, and gradients of sum_i denergy_i energy_i.
+ *   x_dev       f32 or bf16 [n][width], rows row_stride values apart
+ *   weights_dev f32 [n_experts][values of a head]
+ *   offsets_dev, order_dev  the entries [n][top_k] grouped by head, as
+ *               mlip_group writes them (for species as experts: top_k 1)
+ *   gates_dev   f32 [n][top_k], or NULL: 1.  denergy_dev f32 [n], or NULL: 1
+ * Outputs, each NULL where it is not wanted:
+ *   energy_dev  f32 [n]; entries without a head (-1) add nothing, and a row
+ *               without any has energy and gradients of 0
+ *   dx_dev      x's type, [n][width] contiguous
+ *   dweights_dev f32 [n_experts][values of a head], 0 for heads without rows
+ *   dgates_dev  f32 [n][top_k], denergy_i v_is, 0 at entries without a head
+ * Products, activations and sums are float32 whatever x's type; values of bf16
+ * are rounded to nearest once, at the end.
+ * n in [0, 2^31 / top_k), n_experts 1..256, width 1..1024, hidden 1..8, top_k
+ * 1..16.  Errors: MLIP_E_ARG, MLIP_E_OOM, MLIP_E_HIP.
+ */
+typedef struct {
+  int32_t n_experts;
+  int32_t width;       /* inputs of a head, (lmax + 1) k for descriptors */
+  int32_t hidden;      /* hidden layers */
+  int32_t top_k;
+  int32_t dtype;       /* mlip_dtype of x and dx */
+  int64_t row_stride;  /* values between rows of x, >= width */
+} mlip_heads_params;
+
+/* Values of weights_dev; 0 if the parameters are invalid. */
+size_t mlip_heads_weight_count(const mlip_heads_params* p);
+mlip_status mlip_heads(mlip_learn* ctx, const mlip_heads_params* p, int64_t n, const void* x_dev,
+                       const float* weights_dev, const int32_t* offsets_dev, const int32_t* order_dev,
+                       const float* gates_dev, const float* denergy_dev, float* energy_dev, void* dx_dev,
+                       float* dweights_dev, float* dgates_dev);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,7 @@ EXPORTED = ["mlip_weight_count", "mlip_create", "mlip_build_neighbors", "mlip_co
             "mlip_md_first_half", "mlip_md_second_half", "mlip_md_kinetic", "mlip_set_fusion",
             "mlip_get_neighbor_rows", "mlip_compute_noalloc", "mlip_set_scatter", "mlip_set_list_format",
             "mlip_learn_create", "mlip_learn_last_error", "mlip_learn_memory_bytes", "mlip_learn_destroy",
-            "mlip_route", "mlip_route_backward", "mlip_group"]
+            "mlip_route", "mlip_route_backward", "mlip_group", "mlip_heads_weight_count", "mlip_heads"]
 
 MLIP_STATIC_SCRATCH_BYTES = 256 * 1024 * 1024
 
@@ -60,6 +60,11 @@ class mlip_stats(ctypes.Structure):
 class mlip_route_params(ctypes.Structure):
     _fields_ = [("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("n_kinds", ctypes.c_int32),
                 ("gates", ctypes.c_int32), ("dtype", ctypes.c_int32), ("row_stride", ctypes.c_int64)]
+
+
+class mlip_heads_params(ctypes.Structure):
+    _fields_ = [("n_experts", ctypes.c_int32), ("width", ctypes.c_int32), ("hidden", ctypes.c_int32),
+                ("top_k", ctypes.c_int32), ("dtype", ctypes.c_int32), ("row_stride", ctypes.c_int64)]
 
 
 class MlipError(RuntimeError):
@@ -101,6 +106,8 @@ def _load() -> ctypes.CDLL:
         "mlip_learn_destroy": (None, [vp]),
         "mlip_route": (st, [vp, ctypes.POINTER(mlip_route_params), ctypes.c_int64] + [vp] * 7),
         "mlip_route_backward": (st, [vp, ctypes.POINTER(mlip_route_params), ctypes.c_int64] + [vp] * 8),
+        "mlip_heads_weight_count": (ctypes.c_size_t, [ctypes.POINTER(mlip_heads_params)]),
+        "mlip_heads": (st, [vp, ctypes.POINTER(mlip_heads_params), ctypes.c_int64] + [vp] * 10),
         "mlip_group": (st, [vp, ctypes.c_int64, ctypes.c_int32, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -279,6 +286,16 @@ def mlip_route_backward(ctx: int, params: mlip_route_params, n: int, logits_ptr,
 
 def mlip_group(ctx: int, n_entries: int, n_experts: int, experts_ptr, offsets_ptr, order_ptr) -> None:
     _check_learn(ctx, _lib.mlip_group(ctx, n_entries, n_experts, experts_ptr, offsets_ptr, order_ptr))
+
+
+def mlip_heads_weight_count(params: mlip_heads_params) -> int:
+    return int(_lib.mlip_heads_weight_count(ctypes.byref(params)))
+
+
+def mlip_heads(ctx: int, params: mlip_heads_params, n: int, x_ptr, weights_ptr, offsets_ptr, order_ptr, gates_ptr,
+               denergy_ptr, energy_ptr, dx_ptr, dweights_ptr, dgates_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_heads(ctx, ctypes.byref(params), n, x_ptr, weights_ptr, offsets_ptr, order_ptr,
+                                      gates_ptr, denergy_ptr, energy_ptr, dx_ptr, dweights_ptr, dgates_ptr))
 
 
 def exported_symbols():

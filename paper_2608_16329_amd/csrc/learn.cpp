@@ -87,6 +87,15 @@ RouteArgs route_args(const mlip_route_params* p, int64_t n, const void* logits, 
   return a;
 }
 
+bool heads_valid(const mlip_heads_params* p) {
+  return p->n_experts >= 1 && p->n_experts <= kMaxExperts && p->width >= 1 && p->width <= kMaxHeadInputs &&
+         p->hidden >= 1 && p->hidden <= kMaxHeadLayers;
+}
+
+int64_t head_values(const mlip_heads_params* p) {
+  return 64 * int64_t(p->width) + 64 + int64_t(p->hidden - 1) * (64 * 64 + 64) + 64 + 1;
+}
+
 }  // namespace
 
 extern "C" {
@@ -178,6 +187,56 @@ mlip_status mlip_group(mlip_learn* ctx, int64_t n_entries, int32_t n_experts, co
   const mlip_status w = workspace(ctx, group_ws_bytes(n_entries, n_experts));
   if (w != MLIP_OK) return w;
   LEARN_HIP(ctx, launch_group(experts_dev, n_entries, n_experts, offsets_dev, order_dev, ctx->d_ws, ctx->stream));
+  return MLIP_OK;
+}
+
+size_t mlip_heads_weight_count(const mlip_heads_params* p) {
+  return p && heads_valid(p) ? size_t(p->n_experts) * size_t(head_values(p)) : 0;
+}
+
+mlip_status mlip_heads(mlip_learn* ctx, const mlip_heads_params* p, int64_t n, const void* x_dev,
+                       const float* weights_dev, const int32_t* offsets_dev, const int32_t* order_dev,
+                       const float* gates_dev, const float* denergy_dev, float* energy_dev, void* dx_dev,
+                       float* dweights_dev, float* dgates_dev) {
+  if (!ctx) return MLIP_E_ARG;
+  ctx->err.clear();
+  if (!p) return fail(ctx, MLIP_E_ARG, "NULL parameters");
+  if (!heads_valid(p)) return fail(ctx, MLIP_E_ARG, "n_experts must be in 1..256, width in 1..1024, hidden in 1..8");
+  if (p->top_k < 1 || p->top_k > kMaxTopK) return fail(ctx, MLIP_E_ARG, "top_k must be in 1..16");
+  if (p->dtype != MLIP_F32 && p->dtype != MLIP_BF16) return fail(ctx, MLIP_E_ARG, "unknown dtype");
+  if (n < 0 || n >= (int64_t(1) << 31) / p->top_k) return fail(ctx, MLIP_E_ARG, "n outside [0, 2^31 / top_k)");
+  if (p->row_stride < p->width || p->row_stride > (int64_t(1) << 31))
+    return fail(ctx, MLIP_E_ARG, "row_stride must be in width..2^31");
+  if (n > 0 && !energy_dev && !dx_dev && !dweights_dev && !dgates_dev) return fail(ctx, MLIP_E_ARG, "no output");
+  if (!weights_dev || !offsets_dev || (n > 0 && (!x_dev || !order_dev))) return fail(ctx, MLIP_E_ARG, "NULL argument");
+  HeadsArgs a{};
+  a.n = n;
+  a.m = n * p->top_k;
+  a.stride = p->row_stride;
+  a.E = p->n_experts;
+  a.D = p->width;
+  a.H = p->hidden;
+  a.K = p->top_k;
+  a.bf16 = p->dtype == MLIP_BF16;
+  a.values = head_values(p);
+  a.x = x_dev;
+  a.weights = weights_dev;
+  a.offsets = offsets_dev;
+  a.order = order_dev;
+  a.gates = gates_dev;
+  a.denergy = denergy_dev;
+  a.energy = energy_dev;
+  a.dx = dx_dev;
+  a.dweights = dweights_dev;
+  a.dgates = dgates_dev;
+  const size_t need = heads_plan(&a, ctx->n_cu);
+  const mlip_status w = workspace(ctx, need);
+  if (w != MLIP_OK) return w;
+  float* at = reinterpret_cast<float*>(ctx->d_ws);
+  if (a.dweights) a.slots = at, at += int64_t(a.blocks + a.E) * a.slot;
+  if (a.K > 1 && a.dx) a.entry_dx = at, at += a.m * a.D;
+  if (a.K > 1 && a.energy) a.entry_energy = at;
+  LEARN_HIP(ctx, launch_heads(a, ctx->stream));
   return MLIP_OK;
 }
 

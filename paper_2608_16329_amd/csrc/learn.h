@@ -23,6 +23,8 @@ namespace mlip {
 
 constexpr int kMaxExperts = 256;   // heads a row can be routed to
 constexpr int kMaxTopK = 16;
+constexpr int kMaxHeadInputs = 1024;
+constexpr int kMaxHeadLayers = 8;
 
 // Arguments of the routing kernels (mlip_route, mlip_route_backward).
 struct RouteArgs {
@@ -50,5 +52,34 @@ hipError_t launch_route_backward(const RouteArgs& a, int n_cu, hipStream_t s);
 // Stable counting sort of m entries by expert; ids outside [0, E) come last.
 size_t group_ws_bytes(int64_t m, int E);
 hipError_t launch_group(const int32_t* experts, int64_t m, int E, int32_t* offsets, int32_t* order, void* ws, hipStream_t s);
+
+// Arguments of the energy heads' kernels (mlip_heads).
+struct HeadsArgs {
+  int64_t n;
+  int64_t m;                  // entries, n top_k
+  int64_t stride;             // values between rows of x
+  int E, D, H, K;
+  bool bf16;                  // x and dx
+  int blocks;                 // work-groups that share the tiles
+  int64_t values;             // of one head
+  const void* x;
+  const float* weights;       // [E][values]
+  const int32_t* offsets;     // [E + 1]
+  const int32_t* order;       // [m]
+  const float* gates;         // [m] or null
+  const float* denergy;       // [n] or null (ones)
+  float* energy;              // [n] or null
+  void* dx;                   // [n][D] or null
+  float* dweights;            // [E][values] or null
+  float* dgates;              // [m] or null
+  float* entry_energy;        // [m], with several entries a row
+  float* entry_dx;            // [m][D], with several entries a row and dx
+  float* slots;               // [blocks + E][slot] sums of a work-group for a head
+  int64_t slot;
+};
+// Work-groups, values per slot, and the workspace in bytes (split off in order:
+// slots, entry gradients, entry energies); sets blocks and slot.
+size_t heads_plan(HeadsArgs* a, int n_cu);
+hipError_t launch_heads(const HeadsArgs& a, hipStream_t s);
 
 }  // namespace mlip

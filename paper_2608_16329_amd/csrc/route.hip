@@ -10,23 +10,13 @@
 #include <algorithm>
 
 #include "learn.h"
+#include "learn_math.h"
 
 namespace mlip {
 namespace {
 
 constexpr int kRouteThreads = 256;
 constexpr int kV = 16;              // logits a lane holds
-
-struct __attribute__((packed, aligned(4))) F4 { float v[4]; };
-struct __attribute__((packed, aligned(2))) H4 { uint16_t v[4]; };
-
-__device__ __forceinline__ float from_bf16(uint16_t h) { return __uint_as_float(uint32_t(h) << 16); }
-// round to nearest even; a NaN stays one
-__device__ __forceinline__ uint16_t to_bf16(float f) {
-  const uint32_t u = __float_as_uint(f);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return uint16_t((u >> 16) | 0x40u);
-  return uint16_t((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
-}
 
 // Row i's logits of this lane: expert 4 (c L + l) + q at z[4 c + q]; what the
 // row may not use is -inf, whatever stands there.  True if anything is left in
@@ -44,25 +34,8 @@ __device__ __forceinline__ bool load_row(const RouteArgs& a, int64_t i, int l, f
 #pragma unroll
   for (int c = 0; c < kV / 4; ++c) {
     const int e = 4 * (c * L + l);
-    float t[4] = {0.f, 0.f, 0.f, 0.f};
-    if (live && e < a.E) {
-      const int64_t at = i * a.stride + e;
-      if (e + 4 <= a.E) {
-        if (BF) {
-          const H4 h = *reinterpret_cast<const H4*>(static_cast<const uint16_t*>(a.logits) + at);
-          for (int q = 0; q < 4; ++q) t[q] = from_bf16(h.v[q]);
-        } else {
-          const F4 f = *reinterpret_cast<const F4*>(static_cast<const float*>(a.logits) + at);
-          for (int q = 0; q < 4; ++q) t[q] = f.v[q];
-        }
-      } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (e + q < a.E)
-            t[q] = BF ? from_bf16(static_cast<const uint16_t*>(a.logits)[at + q])
-                      : static_cast<const float*>(a.logits)[at + q];
-      }
-    }
+    float t[4];
+    load4(a.logits, BF, i * a.stride + e, live ? a.E - e : 0, t);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const bool use = live && e + q < a.E && (!ok || ok[e + q]);
@@ -321,25 +294,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
         float t[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) t[q] = any ? z[4 * c + q] * (h[4 * c + q] - mean) + d[4 * c + q] : 0.f;
-        const int64_t at = i * a.E + e;
-        if (e + 4 <= a.E) {
-          if (BF) {
-            H4 o;
-            for (int q = 0; q < 4; ++q) o.v[q] = to_bf16(t[q]);
-            *reinterpret_cast<H4*>(static_cast<uint16_t*>(a.dlogits) + at) = o;
-          } else {
-            F4 o;
-            for (int q = 0; q < 4; ++q) o.v[q] = t[q];
-            *reinterpret_cast<F4*>(static_cast<float*>(a.dlogits) + at) = o;
-          }
-        } else {
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (e + q < a.E) {
-              if (BF) static_cast<uint16_t*>(a.dlogits)[at + q] = to_bf16(t[q]);
-              else static_cast<float*>(a.dlogits)[at + q] = t[q];
-            }
-        }
+        store4(a.dlogits, BF, i * a.E + e, a.E - e, t);
       }
     }
   }

@@ -151,3 +151,34 @@ class Learner(_OnStream):
         self._dense(order, "order", t.int32, m)
         with self._ordered():
             b.mlip_group(self.ctx, m, offsets.shape[0] - 1, _ptr(experts), _ptr(offsets), _ptr(order))
+
+    # -- energy heads ------------------------------------------------------------
+
+    def heads(self, x, weights, offsets, order, *, hidden: int, top_k: int = 1, gates=None, denergy=None, energy=None,
+              dx=None, dweights=None, dgates=None) -> None:
+        """Energy heads `weights` (f32 [E, values], tables as in the potential's
+        blob) over the rows of `x` (f32 or bf16 [n, width], rows may be apart),
+        grouped by `group` (mlip_heads).  Outputs that are given are written:
+        energy f32 [n] and, of sum(denergy energy), dx (x's type, [n, width]),
+        dweights f32 [E, values] and dgates f32 [n, top_k]."""
+        t = self.torch
+        stride = self._rows(x, "x")
+        n, width = x.shape
+        _need(weights.dim() == 2, "weights is not 2-d")
+        n_experts, values = weights.shape
+        p = b.mlip_heads_params(n_experts, width, hidden, top_k, self._dtypes[x.dtype], max(stride, width))
+        count = b.mlip_heads_weight_count(p)
+        _need(count == 0 or values * n_experts == count,
+              f"weights has {values} values a head, {width} inputs and {hidden} layers need {count // max(n_experts, 1)}")
+        self._dense(weights, "weights", t.float32, n_experts, values)
+        self._dense(offsets, "offsets", t.int32, n_experts + 1)
+        self._dense(order, "order", t.int32, n * top_k)
+        for v, name, dtype, shape in ((gates, "gates", t.float32, (n, top_k)), (denergy, "denergy", t.float32, (n,)),
+                                      (energy, "energy", t.float32, (n,)), (dx, "dx", x.dtype, (n, width)),
+                                      (dweights, "dweights", t.float32, (n_experts, values)),
+                                      (dgates, "dgates", t.float32, (n, top_k))):
+            if v is not None:
+                self._dense(v, name, dtype, *shape)
+        with self._ordered():
+            b.mlip_heads(self.ctx, p, n, _ptr(x), _ptr(weights), _ptr(offsets), _ptr(order), _ptr(gates), _ptr(denergy),
+                         _ptr(energy), _ptr(dx), _ptr(dweights), _ptr(dgates))
