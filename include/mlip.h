@@ -474,6 +474,78 @@ mlip_status mlip_heads(mlip_learn* ctx, const mlip_heads_params* p, int64_t n, c
                        const float* gates_dev, const float* denergy_dev, float* energy_dev, void* dx_dev,
                        float* dweights_dev, float* dgates_dev);
 
+/*
+ * AdamW over many tensors at once (the tables of a potential are hundreds to
+ * thousands: eight tensors for every pair of species and ten for every
+ * species), in one launch:
+ *   m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g^2,  g the gradient
+ *   times grad_scale,
+ *   p' = p (1 - lr weight_decay [tensors with decay])
+ *        - lr / (1 - beta1^step) m' / (sqrt(v') / sqrt(1 - beta2^step) + eps)
+ * in float32; bf16 parameters are rounded to nearest at the end.
+ *
+ * A plan holds the tensors' places and the stream, and is made once.  The
+ * moments are the caller's: the tensors' elements back to back in the order of
+ * the plan, float32, or with state_bits 8 one code each and one exponent for
+ * every 256 elements of a tensor (the last block of a tensor is shorter):
+ *   exponent byte e + 127, the block's |values| < 2^e
+ *   m  sign, 4 exponent bits E, 3 mantissa bits: (1 + f/8) 2^(E - 15) 2^e, for
+ *      E = 0 f/8 2^-14 2^e; 0x7f is NaN
+ *   v  4 exponent and 4 mantissa bits: (1 + f/16) 2^(E - 15) 2^e, for E = 0 f/16
+ *      2^-14 2^e; 0xff is NaN
+ * All zero bytes are zero moments.  The update uses m' and v' before they are
+ * rounded.  Rounding is up or down at random, up with the probability of the
+ * part that is cut off (to nearest, v would never change: a step moves it by
+ * less than half of what its codes are apart); the random bits are mixed from
+ * `seed` (another one each step) and the element's place, so a step can be
+ * repeated bit for bit.  A v that is not 0 is not rounded to 0.  An element
+ * whose moment is not finite keeps NaN and leaves its block's others alone.
+ *
+ * mlip_adamw_create  tensors: host array, copied; into_dev, for all tensors or
+ *                    for none: where new parameters go (NULL: param_dev), equal
+ *                    to param_dev or apart from it.  Errors:
+ *                    MLIP_E_ARG, MLIP_E_OOM, MLIP_E_HIP, text from
+ *                    mlip_adamw_last_error(NULL).  Synchronises
+ * mlip_adamw_state_count  elements of each moment, and exponents of each (0
+ *                    with 32 bits)
+ * mlip_adamw_step    reads the state `from` and writes `into` (NULL: `from`
+ *                    again); with into_dev and a second state a step can be
+ *                    dropped by not using what it wrote.  reverse != 0 reads
+ *                    the parameters at into_dev and writes param_dev
+ * mlip_adamw_moments the values 8-bit moments stand for, float32 [elements]
+ */
+typedef struct mlip_adamw mlip_adamw;
+typedef struct {
+  void* param_dev;
+  void* into_dev;
+  const void* grad_dev;
+  int64_t n;
+  int32_t param_dtype;  /* mlip_dtype */
+  int32_t grad_dtype;   /* mlip_dtype */
+  int32_t decay;        /* whether weight_decay applies */
+} mlip_adamw_tensor;
+typedef struct {
+  int64_t step;         /* this step's number, from 1 */
+  double lr, beta1, beta2, eps, weight_decay;
+  double grad_scale;    /* factor on the gradients: 1, a clipping factor, or 1 / loss scale */
+  uint32_t seed;        /* of the rounding of 8-bit moments */
+} mlip_adamw_params;
+typedef struct {
+  void* m_dev;
+  void* v_dev;
+  uint8_t* m_exp_dev;   /* 8 bits only */
+  uint8_t* v_exp_dev;
+} mlip_adamw_state;
+
+mlip_status mlip_adamw_create(const mlip_adamw_tensor* tensors, int64_t n_tensors, int32_t state_bits,
+                              void* hip_stream, mlip_adamw** out);
+const char* mlip_adamw_last_error(const mlip_adamw* plan);
+mlip_status mlip_adamw_state_count(const mlip_adamw* plan, int64_t* elements, int64_t* blocks);
+void mlip_adamw_destroy(mlip_adamw* plan);
+mlip_status mlip_adamw_step(mlip_adamw* plan, const mlip_adamw_params* p, const mlip_adamw_state* from,
+                            const mlip_adamw_state* into, int32_t reverse);
+mlip_status mlip_adamw_moments(mlip_adamw* plan, const mlip_adamw_state* state, float* m_out_dev, float* v_out_dev);
+
 #ifdef __cplusplus
 }
 #endif

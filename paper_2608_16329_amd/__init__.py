@@ -12,9 +12,9 @@ import numpy as np
 
 from . import binding
 from .binding import MlipError, mlip_hparams
-from .learn import Learner
+from .learn import AdamW, Learner
 
-__all__ = ["binding", "MlipError", "mlip_hparams", "Potential", "Learner"]
+__all__ = ["binding", "MlipError", "mlip_hparams", "Potential", "Learner", "AdamW"]
 
 
 class Potential:

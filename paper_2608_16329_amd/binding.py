@@ -27,7 +27,9 @@ EXPORTED = ["mlip_weight_count", "mlip_create", "mlip_build_neighbors", "mlip_co
             "mlip_md_first_half", "mlip_md_second_half", "mlip_md_kinetic", "mlip_set_fusion",
             "mlip_get_neighbor_rows", "mlip_compute_noalloc", "mlip_set_scatter", "mlip_set_list_format",
             "mlip_learn_create", "mlip_learn_last_error", "mlip_learn_memory_bytes", "mlip_learn_destroy",
-            "mlip_route", "mlip_route_backward", "mlip_group", "mlip_heads_weight_count", "mlip_heads"]
+            "mlip_route", "mlip_route_backward", "mlip_group", "mlip_heads_weight_count", "mlip_heads",
+            "mlip_adamw_create", "mlip_adamw_last_error", "mlip_adamw_state_count", "mlip_adamw_destroy",
+            "mlip_adamw_step", "mlip_adamw_moments"]
 
 MLIP_STATIC_SCRATCH_BYTES = 256 * 1024 * 1024
 
@@ -65,6 +67,23 @@ class mlip_route_params(ctypes.Structure):
 class mlip_heads_params(ctypes.Structure):
     _fields_ = [("n_experts", ctypes.c_int32), ("width", ctypes.c_int32), ("hidden", ctypes.c_int32),
                 ("top_k", ctypes.c_int32), ("dtype", ctypes.c_int32), ("row_stride", ctypes.c_int64)]
+
+
+class mlip_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param_dev", ctypes.c_void_p), ("into_dev", ctypes.c_void_p), ("grad_dev", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("decay", ctypes.c_int32)]
+
+
+class mlip_adamw_params(ctypes.Structure):
+    _fields_ = [("step", ctypes.c_int64), ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
+                ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("grad_scale", ctypes.c_double), ("seed", ctypes.c_uint32)]
+
+
+class mlip_adamw_state(ctypes.Structure):
+    _fields_ = [("m_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p), ("m_exp_dev", ctypes.c_void_p),
+                ("v_exp_dev", ctypes.c_void_p)]
 
 
 class MlipError(RuntimeError):
@@ -108,6 +127,13 @@ def _load() -> ctypes.CDLL:
         "mlip_route_backward": (st, [vp, ctypes.POINTER(mlip_route_params), ctypes.c_int64] + [vp] * 8),
         "mlip_heads_weight_count": (ctypes.c_size_t, [ctypes.POINTER(mlip_heads_params)]),
         "mlip_heads": (st, [vp, ctypes.POINTER(mlip_heads_params), ctypes.c_int64] + [vp] * 10),
+        "mlip_adamw_create": (st, [ctypes.POINTER(mlip_adamw_tensor), ctypes.c_int64, ctypes.c_int32, vp, ctypes.POINTER(vp)]),
+        "mlip_adamw_last_error": (ctypes.c_char_p, [vp]),
+        "mlip_adamw_state_count": (st, [vp, ip64, ip64]),
+        "mlip_adamw_destroy": (None, [vp]),
+        "mlip_adamw_step": (st, [vp, ctypes.POINTER(mlip_adamw_params), ctypes.POINTER(mlip_adamw_state),
+                                 ctypes.POINTER(mlip_adamw_state), ctypes.c_int32]),
+        "mlip_adamw_moments": (st, [vp, ctypes.POINTER(mlip_adamw_state), vp, vp]),
         "mlip_group": (st, [vp, ctypes.c_int64, ctypes.c_int32, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -296,6 +322,43 @@ def mlip_heads(ctx: int, params: mlip_heads_params, n: int, x_ptr, weights_ptr, 
                denergy_ptr, energy_ptr, dx_ptr, dweights_ptr, dgates_ptr) -> None:
     _check_learn(ctx, _lib.mlip_heads(ctx, ctypes.byref(params), n, x_ptr, weights_ptr, offsets_ptr, order_ptr,
                                       gates_ptr, denergy_ptr, energy_ptr, dx_ptr, dweights_ptr, dgates_ptr))
+
+
+def _check_adamw(plan, status: int):
+    if status != MLIP_OK:
+        raise MlipError(status, _lib.mlip_adamw_last_error(plan).decode())
+
+
+def mlip_adamw_create(tensors, state_bits: int, hip_stream: int = 0) -> int:
+    """tensors: list of mlip_adamw_tensor."""
+    plan = ctypes.c_void_p()
+    array = (mlip_adamw_tensor * max(len(tensors), 1))(*tensors)
+    _check_adamw(None, _lib.mlip_adamw_create(array, len(tensors), state_bits, hip_stream or None, ctypes.byref(plan)))
+    return plan.value
+
+
+def mlip_adamw_last_error(plan: int) -> str:
+    return _lib.mlip_adamw_last_error(plan).decode()
+
+
+def mlip_adamw_state_count(plan: int):
+    elements, blocks = ctypes.c_int64(), ctypes.c_int64()
+    _check_adamw(plan, _lib.mlip_adamw_state_count(plan, ctypes.byref(elements), ctypes.byref(blocks)))
+    return int(elements.value), int(blocks.value)
+
+
+def mlip_adamw_destroy(plan: int) -> None:
+    _lib.mlip_adamw_destroy(plan)
+
+
+def mlip_adamw_step(plan: int, params: mlip_adamw_params, state: mlip_adamw_state,
+                    into: Optional[mlip_adamw_state] = None, reverse: bool = False) -> None:
+    _check_adamw(plan, _lib.mlip_adamw_step(plan, ctypes.byref(params), ctypes.byref(state),
+                                            ctypes.byref(into) if into is not None else None, int(reverse)))
+
+
+def mlip_adamw_moments(plan: int, state: mlip_adamw_state, m_out_ptr, v_out_ptr) -> None:
+    _check_adamw(plan, _lib.mlip_adamw_moments(plan, ctypes.byref(state), m_out_ptr, v_out_ptr))
 
 
 def exported_symbols():

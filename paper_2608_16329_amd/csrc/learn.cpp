@@ -4,6 +4,7 @@
 #include <cmath>
 #include <new>
 #include <string>
+#include <vector>
 
 #include "learn.h"
 
@@ -13,7 +14,8 @@ namespace {
 
 thread_local std::string t_learn_err;
 
-mlip_status fail(mlip_learn* ctx, mlip_status st, const char* msg) {
+template <typename Ctx>
+mlip_status fail(Ctx* ctx, mlip_status st, const char* msg) {
   // no exception crosses the ABI: without memory for it the text is dropped
   try {
     (ctx ? ctx->err : t_learn_err) = msg;
@@ -23,7 +25,8 @@ mlip_status fail(mlip_learn* ctx, mlip_status st, const char* msg) {
   return st;
 }
 
-mlip_status fail_hip(mlip_learn* ctx, hipError_t e) {
+template <typename Ctx>
+mlip_status fail_hip(Ctx* ctx, hipError_t e) {
   (void)hipGetLastError();
   return fail(ctx, MLIP_E_HIP, hipGetErrorString(e));
 }
@@ -96,22 +99,44 @@ int64_t head_values(const mlip_heads_params* p) {
   return 64 * int64_t(p->width) + 64 + int64_t(p->hidden - 1) * (64 * 64 + 64) + 64 + 1;
 }
 
+// The state arrays of a call: both moments, and exponents with 8 bits.
+bool state_given(const mlip_adamw* h, const mlip_adamw_state* s) {
+  return s && (h->elements == 0 || (s->m_dev && s->v_dev && (h->bits == 32 || (s->m_exp_dev && s->v_exp_dev))));
+}
+
+AdamArgs adam_args(const mlip_adamw* h, const mlip_adamw_state* from, const mlip_adamw_state* into) {
+  AdamArgs a{};
+  a.tensor = reinterpret_cast<const AdamTensor*>(h->d_tables);
+  a.piece = reinterpret_cast<const AdamPiece*>(h->d_tables + h->tensors * sizeof(AdamTensor));
+  a.pieces = h->pieces;
+  a.bits = h->bits;
+  a.m = from->m_dev;
+  a.v = from->v_dev;
+  a.m_exp = from->m_exp_dev;
+  a.v_exp = from->v_exp_dev;
+  a.new_m = into->m_dev;
+  a.new_v = into->v_dev;
+  a.new_m_exp = into->m_exp_dev;
+  a.new_v_exp = into->v_exp_dev;
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
 
 mlip_status mlip_learn_create(void* hip_stream, mlip_learn** out) {
   t_learn_err.clear();
-  if (!out) return fail(nullptr, MLIP_E_ARG, "NULL output pointer");
+  if (!out) return fail<mlip_learn>(nullptr, MLIP_E_ARG, "NULL output pointer");
   *out = nullptr;
   mlip_learn* ctx = new (std::nothrow) mlip_learn();
-  if (!ctx) return fail(nullptr, MLIP_E_OOM, "host allocation failed");
+  if (!ctx) return fail<mlip_learn>(nullptr, MLIP_E_OOM, "host allocation failed");
   ctx->stream = reinterpret_cast<hipStream_t>(hip_stream);
   if (hipGetDevice(&ctx->device) != hipSuccess ||
       hipDeviceGetAttribute(&ctx->n_cu, hipDeviceAttributeMultiprocessorCount, ctx->device) != hipSuccess) {
     (void)hipGetLastError();
     delete ctx;
-    return fail(nullptr, MLIP_E_HIP, "no current HIP device");
+    return fail<mlip_learn>(nullptr, MLIP_E_HIP, "no current HIP device");
   }
   *out = ctx;
   return MLIP_OK;
@@ -237,6 +262,139 @@ mlip_status mlip_heads(mlip_learn* ctx, const mlip_heads_params* p, int64_t n, c
   if (a.K > 1 && a.dx) a.entry_dx = at, at += a.m * a.D;
   if (a.K > 1 && a.energy) a.entry_energy = at;
   LEARN_HIP(ctx, launch_heads(a, ctx->stream));
+  return MLIP_OK;
+}
+
+mlip_status mlip_adamw_create(const mlip_adamw_tensor* tensors, int64_t n_tensors, int32_t state_bits,
+                              void* hip_stream, mlip_adamw** out) {
+  t_learn_err.clear();
+  mlip_adamw* const none = nullptr;
+  if (!out) return fail(none, MLIP_E_ARG, "NULL output pointer");
+  *out = nullptr;
+  if (!tensors || n_tensors < 1) return fail(none, MLIP_E_ARG, "no tensors");
+  if (state_bits != 32 && state_bits != 8) return fail(none, MLIP_E_ARG, "state_bits must be 32 or 8");
+  mlip_adamw* h = nullptr;
+  try {
+    std::vector<AdamTensor> tt;
+    std::vector<AdamPiece> pp;
+    int64_t at = 0, block = 0, into = 0, filled = 0;
+    for (int64_t k = 0; k < n_tensors; ++k) {
+      const mlip_adamw_tensor& t = tensors[k];
+      if (t.n < 0 || t.n > (int64_t(1) << 40) - at) return fail(none, MLIP_E_ARG, "more than 2^40 elements");
+      if (t.n > 0 && (!t.param_dev || !t.grad_dev)) return fail(none, MLIP_E_ARG, "NULL parameter or gradient");
+      if ((t.param_dtype != MLIP_F32 && t.param_dtype != MLIP_BF16) || (t.grad_dtype != MLIP_F32 && t.grad_dtype != MLIP_BF16))
+        return fail(none, MLIP_E_ARG, "unknown dtype");
+      filled += t.n > 0 ? 1 : 0;   // an empty tensor may be nowhere
+      into += t.n > 0 && t.into_dev ? 1 : 0;
+      AdamTensor d{};
+      d.param = t.param_dev;
+      d.into = t.into_dev ? t.into_dev : t.param_dev;
+      d.grad = t.grad_dev;
+      d.at = at;
+      d.block = block;
+      d.param_bf16 = t.param_dtype == MLIP_BF16;
+      d.grad_bf16 = t.grad_dtype == MLIP_BF16;
+      d.decay = t.decay != 0;
+      tt.push_back(d);
+      for (int64_t i = 0; i < t.n; i += kAdamPiece) pp.push_back({k, i, std::min<int64_t>(t.n, i + kAdamPiece)});
+      at += t.n;
+      block += (t.n + 255) / 256;
+    }
+    if (into != 0 && into != filled) return fail(none, MLIP_E_ARG, "into_dev is for all tensors or for none");
+    h = new mlip_adamw();
+    h->stream = reinterpret_cast<hipStream_t>(hip_stream);
+    h->bits = state_bits;
+    h->into = into != 0;
+    h->elements = at;
+    h->blocks = block;
+    h->pieces = int64_t(pp.size());
+    h->tensors = tt.size();
+    h->bytes = tt.size() * sizeof(AdamTensor) + pp.size() * sizeof(AdamPiece);
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess ||
+        hipDeviceGetAttribute(&h->n_cu, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) {
+      (void)hipGetLastError();
+      delete h;
+      return fail(none, MLIP_E_HIP, "no current HIP device");
+    }
+    if (hipMalloc(reinterpret_cast<void**>(&h->d_tables), h->bytes) != hipSuccess) {
+      (void)hipGetLastError();
+      delete h;
+      return fail(none, MLIP_E_OOM, "device allocation failed: tables");
+    }
+    hipError_t e = hipMemcpy(h->d_tables, tt.data(), tt.size() * sizeof(AdamTensor), hipMemcpyHostToDevice);
+    if (e == hipSuccess && !pp.empty())
+      e = hipMemcpy(h->d_tables + tt.size() * sizeof(AdamTensor), pp.data(), pp.size() * sizeof(AdamPiece),
+                    hipMemcpyHostToDevice);
+    if (e != hipSuccess) {
+      (void)hipFree(h->d_tables);
+      delete h;
+      return fail_hip(none, e);
+    }
+  } catch (...) {
+    delete h;
+    return fail(none, MLIP_E_OOM, "host allocation failed");
+  }
+  *out = h;
+  return MLIP_OK;
+}
+
+const char* mlip_adamw_last_error(const mlip_adamw* plan) { return plan ? plan->err.c_str() : t_learn_err.c_str(); }
+
+mlip_status mlip_adamw_state_count(const mlip_adamw* plan, int64_t* elements, int64_t* blocks) {
+  if (!plan || !elements || !blocks) return MLIP_E_ARG;
+  *elements = plan->elements;
+  *blocks = plan->bits == 8 ? plan->blocks : 0;
+  return MLIP_OK;
+}
+
+void mlip_adamw_destroy(mlip_adamw* plan) {
+  if (!plan) return;
+  (void)hipStreamSynchronize(plan->stream);
+  if (plan->d_tables) (void)hipFree(plan->d_tables);
+  (void)hipGetLastError();
+  delete plan;
+}
+
+mlip_status mlip_adamw_step(mlip_adamw* plan, const mlip_adamw_params* p, const mlip_adamw_state* from,
+                            const mlip_adamw_state* into, int32_t reverse) {
+  if (!plan) return MLIP_E_ARG;
+  plan->err.clear();
+  if (!p) return fail(plan, MLIP_E_ARG, "NULL parameters");
+  if (p->step < 1) return fail(plan, MLIP_E_ARG, "step must be 1 or more");
+  if (!(p->beta1 >= 0.0 && p->beta1 < 1.0) || !(p->beta2 >= 0.0 && p->beta2 < 1.0))
+    return fail(plan, MLIP_E_ARG, "beta1 and beta2 must be in [0, 1)");
+  if (!(p->eps >= 0.0) || !std::isfinite(p->eps) || !std::isfinite(p->lr) || !std::isfinite(p->weight_decay) ||
+      !std::isfinite(p->grad_scale))
+    return fail(plan, MLIP_E_ARG, "eps must be at least 0, and lr, weight_decay and grad_scale finite");
+  if (reverse && !plan->into) return fail(plan, MLIP_E_ARG, "reverse needs a plan with into_dev");
+  if (!state_given(plan, from) || (into && !state_given(plan, into))) return fail(plan, MLIP_E_ARG, "NULL state");
+  if (plan->pieces == 0) return MLIP_OK;
+  AdamArgs a = adam_args(plan, from, into ? into : from);
+  a.reverse = reverse != 0;
+  AdamStep h{};
+  h.lr = p->lr;
+  h.beta1 = p->beta1;
+  h.beta2 = p->beta2;
+  h.eps = p->eps;
+  h.weight_decay = p->weight_decay;
+  h.grad_scale = p->grad_scale;
+  h.correction1 = 1.0 - std::pow(p->beta1, double(p->step));
+  h.root_correction2 = std::sqrt(1.0 - std::pow(p->beta2, double(p->step)));
+  h.seed = p->seed;
+  LEARN_HIP(plan, launch_adamw(a, h, plan->n_cu, plan->stream));
+  return MLIP_OK;
+}
+
+mlip_status mlip_adamw_moments(mlip_adamw* plan, const mlip_adamw_state* state, float* m_out_dev, float* v_out_dev) {
+  if (!plan) return MLIP_E_ARG;
+  plan->err.clear();
+  if (plan->bits != 8) return fail(plan, MLIP_E_ARG, "the moments are values already");
+  if (!state_given(plan, state)) return fail(plan, MLIP_E_ARG, "NULL state");
+  if (plan->pieces == 0) return MLIP_OK;
+  if (!m_out_dev || !v_out_dev) return fail(plan, MLIP_E_ARG, "NULL output");
+  const AdamArgs a = adam_args(plan, state, state);
+  LEARN_HIP(plan, launch_moments(a, m_out_dev, v_out_dev, plan->n_cu, plan->stream));
   return MLIP_OK;
 }
 

@@ -10,6 +10,24 @@
 
 #include "../../include/mlip.h"
 
+namespace mlip {
+
+// A tensor of an AdamW plan and a piece of one, as the kernels read them.
+constexpr int kAdamPiece = 2048;   // a multiple of 256: pieces start where blocks of 8-bit moments do
+struct AdamTensor {
+  void* param;
+  void* into;
+  const void* grad;
+  int64_t at;                 // first element among the moments
+  int64_t block;              // first block of 8-bit moments
+  int32_t param_bf16, grad_bf16, decay, pad;
+};
+struct AdamPiece {
+  int64_t tensor, from, to;
+};
+
+}  // namespace mlip
+
 struct mlip_learn {
   hipStream_t stream = nullptr;
   int device = 0;
@@ -17,6 +35,17 @@ struct mlip_learn {
   std::string err;
   unsigned char* d_ws = nullptr;  // workspace of the calls, in the order of the stream
   size_t cap_ws = 0;
+};
+
+struct mlip_adamw {
+  hipStream_t stream = nullptr;
+  int n_cu = 0;
+  int bits = 32;
+  bool into = false;          // the plan has a second set of parameters
+  int64_t elements = 0, blocks = 0, pieces = 0;
+  std::string err;
+  unsigned char* d_tables = nullptr;   // AdamTensor [tensors], then AdamPiece [pieces]
+  size_t tensors = 0, bytes = 0;
 };
 
 namespace mlip {
@@ -81,5 +110,30 @@ struct HeadsArgs {
 // slots, entry gradients, entry energies); sets blocks and slot.
 size_t heads_plan(HeadsArgs* a, int n_cu);
 hipError_t launch_heads(const HeadsArgs& a, hipStream_t s);
+
+// Arguments of the AdamW kernels.
+struct AdamArgs {
+  const AdamTensor* tensor;
+  const AdamPiece* piece;
+  int64_t pieces;
+  int bits;
+  bool reverse;               // reads `into` and writes `param`
+  const void* m;              // float32 or codes [elements]
+  const void* v;
+  const uint8_t* m_exp;       // [blocks], 8 bits: e + 127
+  const uint8_t* v_exp;
+  void* new_m;
+  void* new_v;
+  uint8_t* new_m_exp;
+  uint8_t* new_v_exp;
+};
+struct AdamStep {
+  double lr, beta1, beta2, eps, weight_decay, grad_scale;
+  double correction1;         // 1 - beta1^t
+  double root_correction2;    // sqrt(1 - beta2^t)
+  uint32_t seed;
+};
+hipError_t launch_adamw(const AdamArgs& a, const AdamStep& h, int n_cu, hipStream_t s);
+hipError_t launch_moments(const AdamArgs& a, float* m_out, float* v_out, int n_cu, hipStream_t s);
 
 }  // namespace mlip

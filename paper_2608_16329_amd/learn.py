@@ -1,7 +1,8 @@
 """The learning operators over PyTorch-ROCm tensors (C ABI in include/mlip.h).
 
-`Learner` wraps one mlip_learn context.  Every tensor is the caller's, outputs
-too; the arithmetic runs in the library's HIP kernels, and there is no fallback.
+`Learner` wraps one mlip_learn context, `AdamW` one optimiser plan.  Every
+tensor is the caller's, outputs too (but for the optimiser's moments); the
+arithmetic runs in the library's HIP kernels, and there is no fallback.
 """
 from __future__ import annotations
 
@@ -182,3 +183,96 @@ class Learner(_OnStream):
         with self._ordered():
             b.mlip_heads(self.ctx, p, n, _ptr(x), _ptr(weights), _ptr(offsets), _ptr(order), _ptr(gates), _ptr(denergy),
                          _ptr(energy), _ptr(dx), _ptr(dweights), _ptr(dgates))
+
+
+class AdamW(_OnStream):
+    """AdamW over lists of contiguous tensors (f32 or bf16, gradients of either
+    type in the same order), moments in 32 or 8 bits (mlip_adamw_step).
+
+    The tensors' places are taken once: later gradients have to be written to
+    the same tensors.  decay: one truth value a tensor, whether weight_decay
+    applies (default: to those with two dimensions or more).  The moments are `m`
+    and `v`, flat over the tensors back to back, with 8 bits codes beside
+    `m_exp` and `v_exp`; they start as zeros and may be read and overwritten.
+
+    into: tensors that new parameters go to, like `params`; `new_m`, `new_v`
+    (`new_m_exp`, `new_v_exp`) receive the new moments.  A step then changes
+    nothing that it reads; `accept` makes what it wrote the next step's start
+    and the old values the place to write to."""
+
+    def __init__(self, params, grads, *, bits: int = 32, decay=None, into=None, stream=None):
+        self.plan = None
+        self._bind(stream)
+        t = self.torch
+        params, grads = list(params), list(grads)
+        into = list(into) if into is not None else [None] * len(params)
+        decay = [p.dim() >= 2 for p in params] if decay is None else list(decay)
+        _need(len(params) == len(grads) == len(into) == len(decay), "params, grads, into and decay differ in length")
+        _need(bits in (8, 32), f"bits is {bits}, not 32 or 8")
+        table = []
+        for k, (p, g, q, d) in enumerate(zip(params, grads, into, decay)):
+            for v, name in ((p, "params"), (g, "grads")):
+                _need(v.dtype in self._dtypes, f"{name}[{k}] is {v.dtype}, not float32 or bfloat16")
+            self._dense(p, f"params[{k}]", p.dtype, *p.shape)
+            self._dense(g, f"grads[{k}]", g.dtype, *p.shape)
+            if q is not None:
+                self._dense(q, f"into[{k}]", p.dtype, *p.shape)
+            table.append(b.mlip_adamw_tensor(_ptr(p), _ptr(q), _ptr(g), p.numel(), self._dtypes[p.dtype],
+                                             self._dtypes[g.dtype], int(bool(d))))
+        self._hold = (params, grads, into)
+        self.bits, self._twice, self._reverse = bits, bool(into) and into[0] is not None, False
+        with t.cuda.device(self.device):
+            self.plan = b.mlip_adamw_create(table, bits, self.stream.cuda_stream)
+            n, blocks = b.mlip_adamw_state_count(self.plan)
+
+            def zeros(m, dtype):
+                return t.zeros(m, dtype=dtype, device=self.device)
+            self.m_exp = self.v_exp = self.new_m_exp = self.new_v_exp = None
+            kind = t.float32 if bits == 32 else t.uint8
+            self.m, self.v = zeros(n, kind), zeros(n, kind)
+            if bits == 8:
+                self.m_exp, self.v_exp = zeros(blocks, t.uint8), zeros(blocks, t.uint8)
+            self.new_m, self.new_v = (zeros(n, kind), zeros(n, kind)) if self._twice else (self.m, self.v)
+            if bits == 8:
+                self.new_m_exp, self.new_v_exp = (zeros(blocks, t.uint8), zeros(blocks, t.uint8)) if self._twice \
+                    else (self.m_exp, self.v_exp)
+        # the moments' zeros are written by the current stream
+        self.stream.wait_stream(t.cuda.current_stream(self.device))
+        self._states()
+
+    def _states(self) -> None:
+        self._from = b.mlip_adamw_state(_ptr(self.m), _ptr(self.v), _ptr(self.m_exp), _ptr(self.v_exp))
+        self._into = b.mlip_adamw_state(_ptr(self.new_m), _ptr(self.new_v), _ptr(self.new_m_exp), _ptr(self.new_v_exp))
+
+    def close(self) -> None:
+        if self.plan:
+            b.mlip_adamw_destroy(self.plan)
+            self.plan = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self, step: int, *, lr: float, beta1: float = 0.9, beta2: float = 0.99, eps: float = 1e-8,
+             weight_decay: float = 0.0, grad_scale: float = 1.0, seed: int = 0) -> None:
+        """Step number `step` (from 1).  seed: of the rounding of 8-bit moments, another one each step."""
+        p = b.mlip_adamw_params(step, lr, beta1, beta2, eps, weight_decay, grad_scale, seed & 0xFFFFFFFF)
+        with self._ordered():
+            b.mlip_adamw_step(self.plan, p, self._from, self._into, self._reverse)
+
+    def accept(self) -> None:
+        """With `into`: the next step starts from what the last one wrote."""
+        _need(self._twice, "accept() is for a plan with into")
+        self._reverse = not self._reverse
+        self.m, self.new_m, self.v, self.new_v = self.new_m, self.m, self.new_v, self.v
+        self.m_exp, self.new_m_exp, self.v_exp, self.new_v_exp = self.new_m_exp, self.m_exp, self.new_v_exp, self.v_exp
+        self._states()
+
+    def moments(self, m, v) -> None:
+        """The values that 8-bit moments as the last step wrote them stand for, f32 [elements] each."""
+        self._dense(m, "m", self.torch.float32, self.m.shape[0])
+        self._dense(v, "v", self.torch.float32, self.m.shape[0])
+        with self._ordered():
+            b.mlip_adamw_moments(self.plan, self._into, _ptr(m), _ptr(v))
