@@ -310,6 +310,25 @@ mlip_status mlip_set_scatter(mlip_ctx* ctx, int32_t scatter);
 typedef enum { MLIP_LIST_AUTO = 0, MLIP_LIST_INDEX = 1 } mlip_list_format;
 mlip_status mlip_set_list_format(mlip_ctx* ctx, int32_t format);
 
+/*
+ * The descriptors of the current positions, for heads outside the library's
+ * fused evaluation (mlip_heads): rows_dev float32 [n][(lmax+1) k], x = vec(G_i)
+ * in l-major order (Eq. 5) rounded to float32, in the caller's order of atoms.
+ * pos_dev as in mlip_compute.
+ * mlip_forces_from_descriptors is the other end: forces_dev float64 [n][3] and,
+ * unless NULL, virial_dev float64 [n][9], as mlip_compute writes them, of
+ * energies whose gradient in the descriptors is drows_dev, float32
+ * [n][(lmax+1) k] (Eqs. 7-10): the encoder and the geometry are differentiated
+ * here, the head was by the caller.
+ * Both are the outer kernels of the three-kernel configuration and need it
+ * (mlip_set_fusion(MLIP_FUSION_PARTIAL)).
+ * Errors: MLIP_E_ARG, MLIP_E_STATE (no build, another configuration),
+ * MLIP_E_OOM, MLIP_E_HIP.
+ */
+mlip_status mlip_descriptors(mlip_ctx* ctx, const double* pos_dev, float* rows_dev);
+mlip_status mlip_forces_from_descriptors(mlip_ctx* ctx, const double* pos_dev, const float* drows_dev,
+                                         double* forces_dev, double* virial_dev);
+
 /* Device memory held by the context, in bytes. */
 mlip_status mlip_memory_bytes(const mlip_ctx* ctx, size_t* bytes);
 

@@ -31,6 +31,7 @@ class Potential:
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         self.ctx = binding.mlip_create(hp, weights, self.stream.cuda_stream)
         self.n = 0
+        self.width = (hp.lmax + 1) * hp.k
 
     def close(self):
         if self.ctx:
@@ -76,6 +77,26 @@ class Potential:
         """binding.MLIP_LIST_AUTO (2-byte coded entries where possible, default)
         or MLIP_LIST_INDEX (4-byte indices); applies from the next build."""
         binding.mlip_set_list_format(self.ctx, fmt)
+
+    def descriptors(self, pos, rows) -> None:
+        """Descriptors of `pos` into `rows`, float32 [n, (lmax + 1) k], for heads
+        outside the fused evaluation (mlip_descriptors; needs MLIP_FUSION_PARTIAL)."""
+        assert pos.is_cuda and pos.dtype == self.torch.float64 and pos.is_contiguous()
+        self._check_rows(rows)
+        binding.mlip_descriptors(self.ctx, pos.data_ptr(), rows.data_ptr())
+
+    def forces_from_descriptors(self, pos, drows, forces, virial=None) -> None:
+        """Forces (and virials) of energies whose gradient in the descriptors is
+        `drows` (mlip_forces_from_descriptors; needs MLIP_FUSION_PARTIAL)."""
+        assert pos.is_cuda and pos.dtype == self.torch.float64 and pos.is_contiguous()
+        assert forces.is_cuda and forces.dtype == self.torch.float64 and forces.is_contiguous()
+        self._check_rows(drows)
+        binding.mlip_forces_from_descriptors(self.ctx, pos.data_ptr(), drows.data_ptr(), forces.data_ptr(),
+                                             virial.data_ptr() if virial is not None else None)
+
+    def _check_rows(self, rows) -> None:
+        assert rows.is_cuda and rows.dtype == self.torch.float32 and rows.is_contiguous()
+        assert tuple(rows.shape) == (self.n, self.width), f"rows are {tuple(rows.shape)}, not {(self.n, self.width)}"
 
     def neighbors(self):
         return binding.mlip_get_neighbors(self.ctx)

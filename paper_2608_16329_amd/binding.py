@@ -26,7 +26,7 @@ EXPORTED = ["mlip_weight_count", "mlip_create", "mlip_build_neighbors", "mlip_co
             "mlip_memory_bytes", "mlip_get_stats", "mlip_last_error", "mlip_destroy", "mlip_md_set_masses",
             "mlip_md_first_half", "mlip_md_second_half", "mlip_md_kinetic", "mlip_set_fusion",
             "mlip_get_neighbor_rows", "mlip_compute_noalloc", "mlip_set_scatter", "mlip_set_list_format",
-            "mlip_learn_create", "mlip_learn_last_error", "mlip_learn_memory_bytes", "mlip_learn_destroy",
+            "mlip_descriptors", "mlip_forces_from_descriptors", "mlip_learn_create", "mlip_learn_last_error", "mlip_learn_memory_bytes", "mlip_learn_destroy",
             "mlip_route", "mlip_route_backward", "mlip_group", "mlip_heads_weight_count", "mlip_heads",
             "mlip_adamw_create", "mlip_adamw_last_error", "mlip_adamw_state_count", "mlip_adamw_destroy",
             "mlip_adamw_step", "mlip_adamw_moments"]
@@ -119,6 +119,8 @@ def _load() -> ctypes.CDLL:
         "mlip_set_fusion": (st, [vp, ctypes.c_int32]),
         "mlip_set_scatter": (st, [vp, ctypes.c_int32]),
         "mlip_set_list_format": (st, [vp, ctypes.c_int32]),
+        "mlip_descriptors": (st, [vp, vp, vp]),
+        "mlip_forces_from_descriptors": (st, [vp, vp, vp, vp, vp]),
         "mlip_learn_create": (st, [vp, ctypes.POINTER(vp)]),
         "mlip_learn_last_error": (ctypes.c_char_p, [vp]),
         "mlip_learn_memory_bytes": (st, [vp, ctypes.POINTER(ctypes.c_size_t)]),
@@ -235,6 +237,15 @@ def mlip_set_scatter(ctx: int, scatter: int) -> None:
 
 def mlip_set_list_format(ctx: int, fmt: int) -> None:
     _check(ctx, _lib.mlip_set_list_format(ctx, int(fmt)))
+
+
+def mlip_descriptors(ctx: int, pos_ptr: int, rows_ptr: int) -> None:
+    _check(ctx, _lib.mlip_descriptors(ctx, pos_ptr, rows_ptr))
+
+
+def mlip_forces_from_descriptors(ctx: int, pos_ptr: int, drows_ptr: int, forces_ptr: int,
+                                 virial_ptr: Optional[int] = None) -> None:
+    _check(ctx, _lib.mlip_forces_from_descriptors(ctx, pos_ptr, drows_ptr, forces_ptr, virial_ptr or None))
 
 
 def mlip_memory_bytes(ctx: int) -> int:

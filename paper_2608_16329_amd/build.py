@@ -33,7 +33,8 @@ SOURCES = [("api.cpp", "api", []), ("angular_tables.cpp", "angular_tables", []),
            ("fused.hip", "fused_f64_high_float", ["-DMLIP_FUSED_PART=2", "-DMLIP_FUSED_DIGITS=0"]),
            ("fused.hip", "fused_f32_float", ["-DMLIP_FUSED_PART=3", "-DMLIP_FUSED_DIGITS=0"]),
            ("pack.hip", "pack", []), ("learn.cpp", "learn", []), ("route.hip", "route", []),
-           ("heads.hip", "heads", []), ("adamw.hip", "adamw", []), ("unfused.hip", "unfused", []), ("md.hip", "md", []), ("scratch.hip", "scratch", [])]
+           ("heads.hip", "heads", []), ("adamw.hip", "adamw", []), ("unfused.hip", "unfused", []), ("md.hip", "md", []), ("scratch.hip", "scratch", []),
+           ("descriptors.hip", "descriptors", [])]
 
 
 def hipcc() -> str:

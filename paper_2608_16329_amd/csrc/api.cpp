@@ -347,20 +347,9 @@ mlip_status compute_unfused(mlip_ctx* ctx, FusedArgs& a) {
   return MLIP_OK;
 }
 
-// One evaluation (mlip_compute and mlip_compute_noalloc) with the given
-// scratch.  Allocates only in the three-kernel and unfused configurations.
-mlip_status run_compute(mlip_ctx* ctx, const double* pos_dev, double* energy_dev, double* forces_dev,
-                        double* virial_dev, double* totals_host, const ComputeScratch& sc) {
-  hipStream_t s = ctx->stream;
-  const int64_t n = ctx->n;
-  if (n == 0) {
-    if (totals_host)
-      for (int k = 0; k < 10; ++k) totals_host[k] = 0.0;
-    return MLIP_OK;
-  }
-  if (!pos_dev || !forces_dev) return fail(ctx, MLIP_E_ARG, "NULL positions or forces");
-  MLIP_HIP(ctx, launch_clear_outputs(forces_dev, n, sc.totals, sc.counters, s));
-
+// The fused kernel's arguments for the current neighbour list.
+FusedArgs fused_args(const mlip_ctx* ctx, const double* pos_dev, double* energy_dev, double* forces_dev,
+                     double* virial_dev, const ComputeScratch& sc) {
   FusedArgs a{};
   a.pos = pos_dev;
   a.types = ctx->d_types;
@@ -401,9 +390,32 @@ mlip_status run_compute(mlip_ctx* ctx, const double* pos_dev, double* energy_dev
     a.tile_start[sp_i] = t;
     if (sp_i < a.C) t += (ctx->species_start[sp_i + 1] - ctx->species_start[sp_i] + ctx->tile_atoms - 1) / ctx->tile_atoms;
   }
+  return a;
+}
+
+// The descriptor buffer of the three-kernel and unfused configurations.
+mlip_status ensure_descriptors(mlip_ctx* ctx) {
+  const size_t need = size_t(ctx->n) * size_t((ctx->hp.lmax + 1) * ctx->hp.k) * ctx->elem_bytes;
+  return ensure(ctx, &ctx->d_gbuf, &ctx->cap_gbuf, need, "descriptor buffer");
+}
+
+// One evaluation (mlip_compute and mlip_compute_noalloc) with the given
+// scratch.  Allocates only in the three-kernel and unfused configurations.
+mlip_status run_compute(mlip_ctx* ctx, const double* pos_dev, double* energy_dev, double* forces_dev,
+                        double* virial_dev, double* totals_host, const ComputeScratch& sc) {
+  hipStream_t s = ctx->stream;
+  const int64_t n = ctx->n;
+  if (n == 0) {
+    if (totals_host)
+      for (int k = 0; k < 10; ++k) totals_host[k] = 0.0;
+    return MLIP_OK;
+  }
+  if (!pos_dev || !forces_dev) return fail(ctx, MLIP_E_ARG, "NULL positions or forces");
+  MLIP_HIP(ctx, launch_clear_outputs(forces_dev, n, sc.totals, sc.counters, s));
+
+  FusedArgs a = fused_args(ctx, pos_dev, energy_dev, forces_dev, virial_dev, sc);
   if (ctx->fusion == MLIP_FUSION_PARTIAL || ctx->fusion == MLIP_FUSION_UNFUSED) {
-    const size_t need = size_t(n) * size_t((ctx->hp.lmax + 1) * ctx->hp.k) * ctx->elem_bytes;
-    MLIP_TRY(ensure(ctx, &ctx->d_gbuf, &ctx->cap_gbuf, need, "descriptor buffer"));
+    MLIP_TRY(ensure_descriptors(ctx));
     a.gbuf = ctx->d_gbuf;
   }
   if (ctx->fusion == MLIP_FUSION_UNFUSED && ctx->n_tiles > 0) {
@@ -413,9 +425,9 @@ mlip_status run_compute(mlip_ctx* ctx, const double* pos_dev, double* energy_dev
   if (ctx->n_tiles > 0) {
     const int k = ctx->hp.k, prec = ctx->hp.precision;
     if (ctx->fusion == MLIP_FUSION_PARTIAL) {
-      MLIP_HIP(ctx, launch_fused(k, prec, ctx->acfg, 2, ctx->digits, a, ctx->n_blocks, s));
-      MLIP_HIP(ctx, launch_fused(k, prec, ctx->acfg, 3, ctx->digits, a, ctx->n_blocks, s));
-      MLIP_HIP(ctx, launch_fused(k, prec, ctx->acfg, 4, ctx->digits, a, ctx->n_blocks, s));
+      MLIP_HIP(ctx, launch_fused(k, prec, ctx->acfg, kModeEncode, ctx->digits, a, ctx->n_blocks, s));
+      MLIP_HIP(ctx, launch_fused(k, prec, ctx->acfg, kModeRegress, ctx->digits, a, ctx->n_blocks, s));
+      MLIP_HIP(ctx, launch_fused(k, prec, ctx->acfg, kModeDerive, ctx->digits, a, ctx->n_blocks, s));
     } else {
       const int mode = ctx->fusion == MLIP_FUSION_RECOMPUTE ? 1
                        : (ctx->scatter == MLIP_SCATTER_TILE ? kModeCachedTileFj : 0);
@@ -754,6 +766,42 @@ mlip_status mlip_compute_noalloc(mlip_ctx* ctx, const double* pos_dev, double* e
   if (ctx->n > 0)
     MLIP_HIP(ctx, hipMemcpyAsync(ctx->d_counters, sc.counters, sizeof(unsigned long long), hipMemcpyDeviceToDevice,
                                  ctx->stream));
+  return MLIP_OK;
+}
+
+mlip_status mlip_descriptors(mlip_ctx* ctx, const double* pos_dev, float* rows_dev) {
+  if (!ctx) return MLIP_E_ARG;
+  ctx->err.clear();
+  if (!ctx->built) return fail(ctx, MLIP_E_STATE, "mlip_build_neighbors has not been called");
+  if (ctx->fusion != MLIP_FUSION_PARTIAL) return fail(ctx, MLIP_E_STATE, "the configuration is not MLIP_FUSION_PARTIAL");
+  if (ctx->n == 0) return MLIP_OK;
+  if (!pos_dev || !rows_dev) return fail(ctx, MLIP_E_ARG, "NULL positions or descriptors");
+  MLIP_TRY(ensure_descriptors(ctx));
+  const ComputeScratch sc{ctx->d_totals, ctx->d_counters, ctx->d_ws};
+  FusedArgs a = fused_args(ctx, pos_dev, nullptr, nullptr, nullptr, sc);
+  a.gbuf = ctx->d_gbuf;
+  MLIP_HIP(ctx, launch_fused(ctx->hp.k, ctx->hp.precision, ctx->acfg, kModeEncode, ctx->digits, a, ctx->n_blocks, ctx->stream));
+  MLIP_HIP(ctx, launch_descriptor_rows(ctx->d_gbuf, ctx->hp.precision, ctx->d_perm, ctx->n, (ctx->hp.lmax + 1) * ctx->hp.k,
+                                       rows_dev, true, ctx->stream));
+  return MLIP_OK;
+}
+
+mlip_status mlip_forces_from_descriptors(mlip_ctx* ctx, const double* pos_dev, const float* drows_dev,
+                                         double* forces_dev, double* virial_dev) {
+  if (!ctx) return MLIP_E_ARG;
+  ctx->err.clear();
+  if (!ctx->built) return fail(ctx, MLIP_E_STATE, "mlip_build_neighbors has not been called");
+  if (ctx->fusion != MLIP_FUSION_PARTIAL) return fail(ctx, MLIP_E_STATE, "the configuration is not MLIP_FUSION_PARTIAL");
+  if (ctx->n == 0) return MLIP_OK;
+  if (!pos_dev || !drows_dev || !forces_dev) return fail(ctx, MLIP_E_ARG, "NULL positions, gradient or forces");
+  MLIP_TRY(ensure_descriptors(ctx));
+  const ComputeScratch sc{ctx->d_totals, ctx->d_counters, ctx->d_ws};
+  MLIP_HIP(ctx, launch_clear_outputs(forces_dev, ctx->n, sc.totals, sc.counters, ctx->stream));
+  MLIP_HIP(ctx, launch_descriptor_rows(ctx->d_gbuf, ctx->hp.precision, ctx->d_perm, ctx->n, (ctx->hp.lmax + 1) * ctx->hp.k,
+                                       const_cast<float*>(drows_dev), false, ctx->stream));
+  FusedArgs a = fused_args(ctx, pos_dev, nullptr, forces_dev, virial_dev, sc);
+  a.gbuf = ctx->d_gbuf;
+  MLIP_HIP(ctx, launch_fused(ctx->hp.k, ctx->hp.precision, ctx->acfg, kModeDerive, ctx->digits, a, ctx->n_blocks, ctx->stream));
   return MLIP_OK;
 }
 

@@ -1829,6 +1829,7 @@ __device__ __forceinline__ void stage_first_layer(const FusedArgs& A, Smem<K, TM
 enum Mode { kCached = 0, kRecompute = 1, kEncode = 2, kRegress = 3, kDerive = 4, kRadial = 5, kCachedTileFj = 6 };
 static_assert(kCachedTileFj == kModeCachedTileFj, "mode number of the tile-reduced scatter");
 static_assert(kRegress == kModeRegress && kRadial == kModeRadial, "mode numbers of the unfused configuration");
+static_assert(kEncode == kModeEncode && kDerive == kModeDerive, "mode numbers of the three-kernel split");
 
 template <int K, int TM, typename R, int NW, int DR, int NM, int MODE, bool kDig>
 __global__ __launch_bounds__(64 * NW, 1) void k_fused(FusedArgs A) {

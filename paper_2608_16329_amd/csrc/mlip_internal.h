@@ -317,6 +317,9 @@ hipError_t launch_fused_f64_high_digits(int k, const FusedArgs& a, int n_blocks,
 hipError_t launch_fused_f64_high_float(int k, const FusedArgs& a, int n_blocks, hipStream_t s);
 hipError_t launch_fused_f32_digits(int k, int acfg, int mode, const FusedArgs& a, int n_blocks, hipStream_t s);
 hipError_t launch_fused_f32_float(int k, int acfg, int mode, const FusedArgs& a, int n_blocks, hipStream_t s);
+// The outer kernels of the three-kernel split.
+constexpr int kModeEncode = 2;    // Eqs. 1-5: G to the descriptor buffer
+constexpr int kModeDerive = 4;    // Eqs. 7-10: dE/dG from it to forces
 // Modes of launch_fused used by the unfused configuration.
 constexpr int kModeRegress = 3;   // Eq. 6: G -> E_i, dE/dG
 constexpr int kModeRadial = 5;    // Eq. 2: distances -> g_rad, dg_rad/dr per entry
@@ -329,6 +332,11 @@ constexpr int kModeCachedTileFj = 6;
 // order; k = 32, irreducible basis with l_max <= 3.
 enum UnfusedStage { kUnfSetup, kUnfAngular, kUnfMoment, kUnfDescriptor, kUnfAdjoint, kUnfU, kUnfV, kUnfForce };
 hipError_t launch_unfused(int stage, int precision, const UnfusedArgs& a, hipStream_t s);
+
+// descriptors.hip: the descriptor buffer (nin values a sorted slot) to the
+// caller's float32 rows by atom, or back
+hipError_t launch_descriptor_rows(void* slots, int precision, const int32_t* perm, int64_t n, int nin, float* rows,
+                                  bool out, hipStream_t s);
 
 // scratch.hip: the device address of the fixed scratch on `device`, which
 // must be the current device; resolved on first use and kept per device.
