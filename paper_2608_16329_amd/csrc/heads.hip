@@ -8,16 +8,26 @@
 //   da += d y_{H-1}, dc += d, dgate_is = denergy_i v_is.
 //
 // One kernel takes a row through all of it.  A work-group has a tile of rows
-// of one head, each wavefront 16 of them as the columns of 16x16x4 matrix
-// products in float32: a layer's result is, register by register, the second
-// operand of the next layer's product (the products sum over inputs 16 T + 4 g
-// + i in lane group g, step i, which is where results 4 g + i stand), so y, z
-// and u never leave registers.  The layers' matrices go through LDS one 64x64
-// block at a time, the next block loaded while one is used.  The weights'
-// gradients are products over rows: g and y change places through LDS, each
-// wavefront owns some of the 16 result tiles of every layer and keeps their
-// sums over all of the work-group's tiles of a head, which are written once
-// and added up in order by a second kernel.
+// of one head, each wavefront 16 of them as the columns of its matrix products;
+// y, z and u never leave registers: a layer's result is, register by register,
+// the second operand of the next layer's product (which sums over the inputs in
+// the order in which the lane groups hold them).
+//
+// Products: a float32 is three bfloat16 limbs, exactly (24 bits in 8 + 8 + 8,
+// cut off, not rounded), and the product of two the six limb products above
+// 2^-24 of it, which 16x16x32 bfloat16 matrix instructions add up in float32.
+// That errs no more than float32 products, and six of them take 0.43 of the
+// time of the float32 matrix instructions (2,100 against 150 TFLOP/s in a loop
+// of nothing else).  A first kernel splits the heads' matrices, in the order in
+// which lanes take them, for products with the matrix and with its transpose;
+// the main kernel brings them to LDS one 64x64 block at a time, the next block
+// on its way while one is used.
+//
+// The weights' gradients are products over rows: the limbs of g and y change
+// places through LDS, read transposed, each wavefront owns some of the 16
+// result tiles of every block and keeps their sums over all of the work-group's
+// tiles of a head, which are written once and added up in order by a third
+// kernel.
 #include <algorithm>
 
 #include "learn.h"
@@ -27,14 +37,62 @@ namespace mlip {
 namespace {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
 
 constexpr int kR = 64;                 // hidden width
-constexpr int kWS = kR + 4;            // LDS row of a 64x64 block: 4 mod 64 banks apart
-constexpr int kWBlock = kR * kWS;
-constexpr int kTStride = kR + 16;      // LDS row of g and y: four rows 16 banks apart, as the lane groups read them
+constexpr int kFragBytes = 1024;       // an operand of one limb: 8 values a lane
+constexpr int kBlockBytes = 24 * kFragBytes;   // a 64x64 block: 4 result tiles x 2 steps of 32 inputs x 3 limbs
+constexpr int kRowBytes = 2 * kR;      // a row of one limb of g or y in LDS
 constexpr int kChunksHeld = 2;         // 64-input chunks whose gradient sums stay in registers
 
-__device__ __forceinline__ f4 mfma(float a, float b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f4 mfma(u4 a, u4 b, f4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+}
+
+// The sum of products of two numbers of three limbs, those above 2^-24 of it.
+__device__ __forceinline__ f4 mfma6(const u4 a[3], const u4 b[3], f4 c) {
+  c = mfma(a[2], b[0], c);
+  c = mfma(a[0], b[2], c);
+  c = mfma(a[1], b[1], c);
+  c = mfma(a[1], b[0], c);
+  c = mfma(a[0], b[1], c);
+  return mfma(a[0], b[0], c);
+}
+
+// Limb k of four values, two to a register.
+__device__ __forceinline__ void split4(const f4 v, u2 limb[3]) {
+  float r[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(r[i]);
+    limb[k][0] = __builtin_amdgcn_perm(u[1], u[0], 0x07060302u);
+    limb[k][1] = __builtin_amdgcn_perm(u[3], u[2], 0x07060302u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] -= __uint_as_float(u[i] & 0xffff0000u);
+  }
+}
+
+// 64 values of a column as a product's second operand: step s, limb k.
+struct Limbs {
+  u4 v[2][3];
+  __device__ __forceinline__ void of(const f4 in[4]) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      u2 lo[3], hi[3];
+      split4(in[2 * s], lo);
+      split4(in[2 * s + 1], hi);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) v[s][k] = u4{lo[k][0], lo[k][1], hi[k][0], hi[k][1]};
+    }
+  }
+};
+// Which of a block's 64 inputs value j of lane group g is in step s.
+__device__ __forceinline__ int input_of(int s, int g, int j) { return 32 * s + 16 * (j >> 2) + 4 * g + (j & 3); }
 
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
@@ -110,83 +168,112 @@ __device__ __forceinline__ void column(const float* base, f4 v[4]) {
 // A value that all lanes hold, for the scalar registers.
 __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// A 64 x 64 block of a head's weights on its way to LDS: rows of `ld` values.
-// Of a block with fewer than 64 columns the rest is what follows in the head's
-// table (its rows, then the bias): it is multiplied by zeros.
+// A split block of weights from memory to LDS, 1 KB at a time, without passing
+// registers; landed() waits for the wavefront's part.
 template <int NW>
-struct Staged {
-  static constexpr int kPer = 16 / NW;   // groups of four values a thread
-  f4 v[kPer];
-  __device__ __forceinline__ void load(const float* src, int ld) {
-    const uint32_t tid = here(threadIdx.x), r = tid / NW, q = tid % NW;
+__device__ __forceinline__ void stage(const unsigned char* src, unsigned char* lds) {
+  const int w = uni(threadIdx.x >> 6);
+  const uint32_t lane16 = here(16 * (threadIdx.x & 63));
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) v[j] = vec4(src, 4 * (r * uint32_t(ld) + 4 * q) + 16 * NW * j);
+  for (int k = 0; k < kBlockBytes / kFragBytes / NW; ++k) {
+    const int at = kFragBytes * (w + NW * k);
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + at + lane16),
+                                     (__attribute__((address_space(3))) void*)(lds + at), 16, 0, 0);
   }
-  __device__ __forceinline__ void store(float* lds) const {
-    const int r = threadIdx.x / NW, q = threadIdx.x % NW;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) *reinterpret_cast<f4*>(lds + r * kWS + 4 * (q + NW * j)) = v[j];
-  }
-};
+}
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// out += block in: 64 inputs from registers, 16 at a time, the next group's
-// weights loaded before this one's products (and no further ahead: loads of
-// the whole block at once take the registers that sums need).
-__device__ __forceinline__ void product(const float* w, const f4 in[4], f4 out[4]) {
-  const int c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
-  const float* row = w + here(c * kWS + 4 * g);
-  f4 wa[2][4];
+// out += block in, the next operands loaded before this one's products (and no
+// further ahead: loads of the whole block at once take the registers that sums
+// need).
+__device__ __forceinline__ void product(const unsigned char* block, const Limbs& in, f4 out[4]) {
+  const unsigned char* p = block + here(16 * (threadIdx.x & 63));
+  u4 a[2][3];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) wa[0][t] = *reinterpret_cast<const f4*>(row + 16 * t * kWS);
+  for (int k = 0; k < 3; ++k) a[0][k] = *reinterpret_cast<const u4*>(p + kFragBytes * k);
 #pragma unroll
-  for (int T = 0; T < 4; ++T) {
+  for (int n = 0; n < 8; ++n) {   // step n / 4, result tile n % 4
     __builtin_amdgcn_sched_barrier(0);
-    if (T < 3) {
+    if (n < 7) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) wa[(T + 1) & 1][t] = *reinterpret_cast<const f4*>(row + 16 * t * kWS + 16 * (T + 1));
+      for (int k = 0; k < 3; ++k) a[(n + 1) & 1][k] = *reinterpret_cast<const u4*>(p + kFragBytes * (3 * (n + 1) + k));
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) out[t] = mfma(wa[T & 1][t][i], in[T][i], out[t]);
+    out[n & 3] = mfma6(a[n & 1], in.v[n >> 2], out[n & 3]);
   }
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// out += block^T in.
-__device__ __forceinline__ void product_t(const float* w, const f4 in[4], f4 out[4]) {
-  const int c = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
-  const float* row = w + here(4 * g * kWS + c);
-  float wa[2][2][4];
-  auto fetch = [&](int k) {   // inputs 16 T + 4 g + i for i = 2 (k & 1) and the next, T = k / 2
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) wa[k & 1][j][t] = row[(16 * (k >> 1) + 2 * (k & 1) + j) * kWS + 16 * t];
-  };
-  fetch(0);
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    __builtin_amdgcn_sched_barrier(0);
-    if (k < 7) fetch(k + 1);
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) out[t] = mfma(wa[k & 1][j][t], in[k >> 1][2 * (k & 1) + j], out[t]);
+// The heads' matrices in limbs: block b of head e (64 inputs of A_0 each, then
+// A_1 ..) for products with it and, after it, with its transpose.  Heads
+// without rows are left out.
+__global__ __launch_bounds__(256) void k_split(HeadsArgs a) {
+  __shared__ float m[kR][kR + 1];
+  const int b = blockIdx.x, e = blockIdx.y, chunks = (a.D + 63) / 64;
+  if (a.offsets[e] == a.offsets[e + 1]) return;
+  const float* w = a.weights + e * a.values;
+  const float* src = b < chunks ? w + 64 * b : w + (kR * a.D + kR + (b - chunks) * (kR * kR + kR));
+  const int ld = b < chunks ? a.D : kR, cols = b < chunks ? a.D - 64 * b : kR;
+  for (int at = threadIdx.x; at < kR * kR; at += 256) {
+    const int r = at / kR, c = at % kR;
+    m[r][c] = c < cols ? src[r * ld + c] : 0.f;
   }
-  __builtin_amdgcn_sched_barrier(0);
+  __syncthreads();
+  unsigned char* dst = a.split + (e * int64_t(chunks + a.H - 1) + b) * a.split_block;
+  const int turns = int(a.split_block / kBlockBytes);
+  for (int at = threadIdx.x; at < turns * 512; at += 256) {
+    const int turn = at >> 9, n = (at >> 6) & 7, lane = at & 63, g = lane >> 4, c = lane & 15;
+    f4 v[2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int r = 16 * (n & 3) + c, in = input_of(n >> 2, g, j);
+      v[j >> 2][j & 3] = turn ? m[in][r] : m[r][in];
+    }
+    u2 lo[3], hi[3];
+    split4(v[0], lo);
+    split4(v[1], hi);
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      *reinterpret_cast<u4*>(dst + turn * kBlockBytes + kFragBytes * (3 * n + k) + 16 * lane) =
+          u4{lo[k][0], lo[k][1], hi[k][0], hi[k][1]};
+  }
+}
+
+// Sums over the 16 columns of a wavefront's rows: lane (g, c) gets that of value
+// 16 (c / 4) + 4 g + c % 4.  Each step adds two lanes' halves of what is left.
+template <int CTRL, int N>
+__device__ __forceinline__ void fold_step(float* v, bool upper) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const float send = upper ? v[k] : v[k + N], keep = upper ? v[k + N] : v[k];
+    v[k] = keep + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(send), CTRL, 0xf, 0xf, true));
+  }
+}
+__device__ __forceinline__ float fold16(const f4 in[4]) {
+  const int c = threadIdx.x & 15;
+  float v[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) v[k] = in[k >> 2][k & 3];
+  fold_step<0x140, 8>(v, c & 8);   // row mirror: lane 15 - c
+  fold_step<0x141, 4>(v, c & 4);   // half row mirror
+  fold_step<0x4e, 2>(v, c & 2);    // lane c ^ 2
+  fold_step<0xb1, 1>(v, c & 1);    // lane c ^ 1
+  return v[0];
+}
+__device__ __forceinline__ int fold_value() {
+  const int lane = threadIdx.x & 63, c = lane & 15;
+  return 16 * (c >> 2) + 4 * (lane >> 4) + (c & 3);
 }
 
 // The row of a lane's column in a tile.
 struct Row {
-  int64_t entry;   // -1: none
-  int64_t i;
+  int32_t entry;   // -1: none
+  int32_t i;
   float gate, up;  // gate and denergy
 };
 __device__ __forceinline__ Row row_of(const HeadsArgs& a, int64_t at, int64_t end) {
   Row r{-1, 0, 0.f, 0.f};
   if (at < end) {
-    const int64_t ent = a.order[at];
+    const int32_t ent = a.order[at];
     if (ent >= 0 && ent < a.m) {
       r.entry = ent;
       r.i = a.K == 1 ? ent : ent / a.K;
@@ -216,7 +303,7 @@ __device__ __forceinline__ f4 x4(const void* p, int64_t at) {
 template <bool BF>
 __device__ __forceinline__ void load_x(const HeadsArgs& a, const Row& r, int ch, f4 in[4]) {
   const int g = (threadIdx.x >> 4) & 3;
-  const int64_t row = r.i * a.stride;
+  const int64_t row = int64_t(r.i) * a.stride;
 #pragma unroll
   for (int T = 0; T < 4; ++T) {
     const int c = 64 * ch + 16 * T + 4 * g;
@@ -265,8 +352,8 @@ __device__ __forceinline__ void store_row(void* to, int64_t row, int D, int ch, 
 template <bool BF>
 __device__ __forceinline__ void store_dx(const HeadsArgs& a, const Row& r, int ch, const f4 d[4]) {
   if (r.entry < 0) return;
-  if (a.K == 1) store_row<BF>(a.dx, r.i * a.D, a.D, ch, d);
-  else store_row<false>(a.entry_dx, r.entry * a.D, a.D, ch, d);
+  if (a.K == 1) store_row<BF>(a.dx, int64_t(r.i) * a.D, a.D, ch, d);
+  else store_row<false>(a.entry_dx, int64_t(r.entry) * a.D, a.D, ch, d);
 }
 
 // Value v of the lane's row: energy and the gate's gradient.
@@ -299,71 +386,82 @@ template <int NW, bool BF>
 __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
   constexpr int kRows = 16 * NW;
   __shared__ int32_t s_first[kMaxExperts + 2], s_entry[kMaxExperts + 2];
-  __shared__ __attribute__((aligned(16))) float s_w[2 * kWBlock];
+  __shared__ __attribute__((aligned(16))) unsigned char s_w[2 * kBlockBytes];
   tile_table(a, kRows, s_first, s_entry);
   const int lane = threadIdx.x & 63, w = uni(threadIdx.x >> 6);
   const int tiles = uni(s_first[a.E + 1]);
   const int t_end = share(tiles, blockIdx.x + 1, a.blocks);
-  const int chunks = (a.D + 63) / 64;
+  const int chunks = (a.D + 63) / 64, blocks = chunks + a.H - 1;
   int e = 0;
-  for (int tile = share(tiles, blockIdx.x, a.blocks); tile < t_end; ++tile) {
+  for (int tile = share(tiles, blockIdx.x, a.blocks); tile < t_end;) {
     while (tile >= uni(s_first[e + 1])) ++e;
-    const int64_t at0 = uni(s_entry[e]) + int64_t(tile - uni(s_first[e])) * kRows, end = uni(s_entry[e + 1]);
+    const int stop = min(t_end, uni(s_first[e + 1]));
+    const int64_t begin = uni(s_entry[e]), end = uni(s_entry[e + 1]), t0 = uni(s_first[e]);
     if (e == a.E) {
-      empty_tile<NW, BF>(a, at0, end);
-      continue;
+      for (; tile < stop; ++tile) empty_tile<NW, BF>(a, begin + (tile - t0) * kRows, end);
+      break;
     }
     const float* wt = a.weights + e * a.values;
-    const Row r = row_of(a, at0 + 16 * w + (lane & 15), end);
-    Staged<NW> next;
-    next.load(wt, a.D);
+    const unsigned char* split = a.split + e * int64_t(blocks) * a.split_block;
+    int cur = 0;
+    __syncthreads();
+    stage<NW>(split, s_w);
+    Row r = row_of(a, begin + (tile - t0) * kRows + 16 * w + (lane & 15), end);
     f4 in[4];
     load_x<BF>(a, r, 0, in);
+    landed();
     __syncthreads();
-    next.store(s_w);
-    __syncthreads();
-    int cur = 0;
-    f4 z[4], y[4] = {};
+    // block b is in use: the next one, or the next tile's first, on its way
+    auto ahead = [&](int b) {
+      if (b + 1 < blocks) stage<NW>(split + (b + 1) * a.split_block, s_w + (cur ^ 1) * kBlockBytes);
+      else if (tile + 1 < stop) stage<NW>(split, s_w + (cur ^ 1) * kBlockBytes);
+    };
+    auto turn = [&]() {
+      landed();
+      __syncthreads();
+      cur ^= 1;
+    };
+    for (; tile < stop; ++tile) {
+      Limbs x;
+      f4 z[4], y[4] = {};
       column(wt + kR * a.D, z);
-    for (int ch = 0; ch < chunks; ++ch) {
-      const bool more = ch + 1 < chunks;
-      if (more) next.load(wt + 64 * (ch + 1), a.D);
-      else if (a.H > 1) next.load(layer(wt, a.D, 1), kR);
-      product(s_w + cur * kWBlock, in, z);
-      if (more) load_x<BF>(a, r, ch + 1, in);
-      if (more || a.H > 1) {
-        next.store(s_w + (cur ^ 1) * kWBlock);
-        cur ^= 1;
-        __syncthreads();
+      for (int ch = 0; ch < chunks; ++ch) {
+        ahead(ch);
+        x.of(in);
+        if (ch + 1 < chunks) load_x<BF>(a, r, ch + 1, in);
+        product(s_w + cur * kBlockBytes, x, z);
+        turn();
       }
-    }
-    for (int l = 1;; ++l) {
+      Row next{-1, 0, 0.f, 0.f};
+      if (tile + 1 < stop) {
+        next = row_of(a, begin + (tile + 1 - t0) * kRows + 16 * w + (lane & 15), end);
+        load_x<BF>(a, next, 0, in);
+      }
+      for (int l = 1;; ++l) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[t][i] += z[t][i] * sigmoid(z[t][i]);
+        if (l == a.H) break;
+        ahead(chunks + l - 1);
+        x.of(y);
+        column(layer(wt, a.D, l) + kR * kR, z);
+        product(s_w + cur * kBlockBytes, x, z);
+        turn();
+      }
+      const float* out = layer(wt, a.D, a.H);
+      float v = 0.f;
+      f4 o[4];
+      column(out, o);
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[t][i] += z[t][i] * sigmoid(z[t][i]);
-      if (l == a.H) break;
-      const float* bias = layer(wt, a.D, l) + kR * kR;
-      column(bias, z);
-      if (l + 1 < a.H) next.load(layer(wt, a.D, l + 1), kR);
-      product(s_w + cur * kWBlock, y, z);
-      if (l + 1 < a.H) {
-        next.store(s_w + (cur ^ 1) * kWBlock);
-        cur ^= 1;
-        __syncthreads();
-      }
+        for (int i = 0; i < 4; ++i) v += o[t][i] * y[t][i];
+      v += __shfl_xor(v, 16, 64);
+      v += __shfl_xor(v, 32, 64);
+      store_value(a, r, v + out[kR]);
+      r = next;
     }
-    const float* out = layer(wt, a.D, a.H);
-    float v = 0.f;
-    f4 o[4];
-    column(out, o);
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v += o[t][i] * y[t][i];
-    v += __shfl_xor(v, 16, 64);
-    v += __shfl_xor(v, 32, 64);
-    store_value(a, r, v + out[kR]);
   }
 }
 
@@ -377,66 +475,78 @@ __host__ __device__ __forceinline__ int64_t slot_values(int D, int H) {
 
 // Energies, gradients in the descriptors and (TRAIN) in the weights.
 template <int H, int NW, bool TRAIN, bool BF>
-__global__ __launch_bounds__(NW * 64) void k_gradient(HeadsArgs a) {
+__global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(HeadsArgs a) {
   constexpr int kRows = 16 * NW;
-  constexpr int kTS = kTStride;
   constexpr int kOwn = 16 / NW;          // result tiles of a wavefront in a 64x64 block
-  extern __shared__ __attribute__((aligned(16))) float s_mem[];
-  float* const s_w = s_mem;              // two blocks of weights
-  float* const s_g = s_mem + 2 * kWBlock;
-  float* const s_y = s_g + kRows * kTS;
+  constexpr int kPlane = kRows * kRowBytes;   // a limb of the tile's rows
+  extern __shared__ __attribute__((aligned(16))) unsigned char s_mem[];
+  unsigned char* const s_w = s_mem;                    // two blocks of weights
+  unsigned char* const s_g = s_mem + 2 * kBlockBytes;  // limbs of g, then of y
+  unsigned char* const s_y = s_g + 3 * kPlane;
   __shared__ int32_t s_first[kMaxExperts + 2], s_entry[kMaxExperts + 2];
   tile_table(a, kRows, s_first, s_entry);
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = uni(tid >> 6);
   const int tiles = uni(s_first[a.E + 1]);
   const int t_begin = share(tiles, blockIdx.x, a.blocks), t_end = share(tiles, blockIdx.x + 1, a.blocks);
-  const int chunks = (a.D + 63) / 64;
+  const int chunks = (a.D + 63) / 64, blocks = chunks + H - 1;
   // the wavefront's tiles of a block: outputs 16 ta .., inputs 16 (tb + k) ..
   const int ta = NW == 8 ? w >> 1 : w, tb = NW == 8 ? 2 * (w & 1) : 0;
 
   f4 sum_h[H > 1 ? H - 1 : 1][kOwn], sum_0[kChunksHeld][kOwn];
-  float sum_b[H], sum_a = 0.f, sum_c = 0.f;   // of dc_t and da, value `lane` over the wavefront's rows; of dc
+  float sum_b[H], sum_a = 0.f, sum_c = 0.f;   // of dc_t and da, value fold_value(); of dc
 
+  // Rows are 128 bytes a limb, their four groups of 16 values turned by the
+  // row, so that 16 rows of one group lie in all banks: as they are written
+  // (by column, four values a lane) and as they are read.
+  auto put = [&](unsigned char* to, int t, const u2 limb[3]) {
+    const int at = here((16 * w + c) * kRowBytes + 8 * g + (((c << 4) & 96) ^ (32 * t)));
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<u2*>(to + k * kPlane + at) = limb[k];
+  };
+  // group t of 16 values of rows 32 s .. 32 s + 31 as an operand: lane (g, c)
+  // gets value c at rows 4 g + j and 16 + 4 g + j, j < 4
+  auto get = [&](const unsigned char* from, int t, int s, u4 limb[3]) {
+    const int row = 4 * g + (c >> 2);
+    const int at = here(row * kRowBytes + 8 * (c & 3) + (((row << 4) & 96) ^ (32 * t)));
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      u2 half[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        half[h] = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s4*)(from + k * kPlane + (32 * s + 16 * h) * kRowBytes + at)));
+      limb[k] = u4{half[0][0], half[0][1], half[1][0], half[1][1]};
+    }
+  };
   // sums of g y^T over the tile's rows into the wavefront's tiles
   auto outer = [&](f4 acc[kOwn]) {
-    const int from = here(g * kTS + c);
-    const float* gp = s_g + 16 * ta + from;
-    const float* yp = s_y + 16 * tb + from;
-    float ga[2][4], yb[2][kOwn][4];
-    auto fetch = [&](int s) {   // rows 16 s + 4 i + g
+#pragma unroll 1
+    for (int s = 0; s < NW / 2; ++s) {
+      u4 ga[3], yb[kOwn][3];
+      get(s_g, ta, s, ga);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        ga[s & 1][i] = gp[(16 * s + 4 * i) * kTS];
+      for (int k = 0; k < kOwn; ++k) get(s_y, tb + k, s, yb[k]);
 #pragma unroll
-        for (int k = 0; k < kOwn; ++k) yb[s & 1][k][i] = yp[(16 * s + 4 * i) * kTS + 16 * k];
-      }
-    };
-    fetch(0);
-#pragma unroll
-    for (int s = 0; s < NW; ++s) {
-      __builtin_amdgcn_sched_barrier(0);
-      if (s + 1 < NW) fetch(s + 1);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int k = 0; k < kOwn; ++k) acc[k] = mfma(ga[s & 1][i], yb[s & 1][k][i], acc[k]);
+      for (int k = 0; k < kOwn; ++k) acc[k] = mfma6(ga, yb[k], acc[k]);
     }
-    __builtin_amdgcn_sched_barrier(0);
   };
-  // v[t][i] of the lane's row, value 16 t + 4 g + i, to LDS
-  auto to_lds = [&](int from, const f4 v[4]) {
-    float* const mine = s_g + here((16 * w + c) * kTS + 4 * g);
+  auto put_limbs = [&](unsigned char* to, const Limbs& l) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) *reinterpret_cast<f4*>(mine + from + 16 * t) = v[t];
+    for (int t = 0; t < 4; ++t) {
+      u2 limb[3];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) limb[k] = u2{l.v[t >> 1][k][2 * (t & 1)], l.v[t >> 1][k][2 * (t & 1) + 1]};
+      put(to, t, limb);
+    }
   };
-  // value `lane` of g over the wavefront's own rows, for the bias
-  auto bias_sum = [&]() {
-    const float* const g_own = s_g + here(16 * w * kTS + lane);
-    float v = 0.f;
+  auto put_values = [&](unsigned char* to, const f4 v[4]) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v += g_own[j * kTS];
-    return v;
+    for (int t = 0; t < 4; ++t) {
+      u2 limb[3];
+      split4(v[t], limb);
+      put(to, t, limb);
+    }
   };
   auto clear = [&]() {
 #pragma unroll
@@ -465,22 +575,23 @@ __global__ __launch_bounds__(NW * 64) void k_gradient(HeadsArgs a) {
 #pragma unroll
       for (int t = 1; t < H; ++t) *place(slot, chunks + t - 1, k) = sum_h[t - 1][k];
     }
-    float* tail = slot + slot_block(a.D, chunks + H - 1);
+    float* tail = slot + slot_block(a.D, blocks);
     // dc_t, da and dc over the wavefronts
     constexpr int kSums = (H + 2) * kR;
+    float* const s_sum = reinterpret_cast<float*>(s_g);
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < H; ++t) s_g[w * kSums + t * kR + lane] = sum_b[t];
-    s_g[w * kSums + H * kR + lane] = sum_a;
+    for (int t = 0; t < H; ++t) s_sum[w * kSums + t * kR + fold_value()] = sum_b[t];
+    s_sum[w * kSums + H * kR + fold_value()] = sum_a;
     float v = sum_c;
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) v += __shfl_xor(v, o, 64);
-    if (lane == 0) s_g[w * kSums + (H + 1) * kR] = v;
+    if (lane == 0) s_sum[w * kSums + (H + 1) * kR] = v;
     __syncthreads();
     for (int at = tid; at <= (H + 1) * kR; at += NW * 64) {
       float v = 0.f;
 #pragma unroll
-      for (int u = 0; u < NW; ++u) v += s_g[u * kSums + at];
+      for (int u = 0; u < NW; ++u) v += s_sum[u * kSums + at];
       tail[at] = v;
     }
     __syncthreads();
@@ -496,32 +607,39 @@ __global__ __launch_bounds__(NW * 64) void k_gradient(HeadsArgs a) {
       break;
     }
     const float* wt = a.weights + e * a.values;
+    const unsigned char* split = a.split + e * int64_t(blocks) * a.split_block;
     if (TRAIN) clear();
+    // blocks of weights in LDS: one in use, the next on its way into the other
+    int cur = 0;
+    auto ahead = [&](int b, bool transposed) {
+      stage<NW>(split + b * a.split_block + (transposed ? kBlockBytes : 0), s_w + (cur ^ 1) * kBlockBytes);
+    };
+    auto turn = [&]() {
+      landed();
+      __syncthreads();
+      cur ^= 1;
+    };
+    __syncthreads();
+    cur = 1;
+    ahead(0, false);
+    Row r = row_of(a, begin + (tile - t0) * kRows + 16 * w + c, end);
+    f4 in[4];
+    load_x<BF>(a, r, 0, in);
+    turn();
     for (bool first = true; tile < stop; ++tile, first = false) {
-      const int64_t at0 = begin + (tile - t0) * kRows;
-      const Row r = row_of(a, at0 + 16 * w + c, end);
-      Staged<NW> next;
-      next.load(wt, a.D);
-      f4 in[4];
-      load_x<BF>(a, r, 0, in);
-      __syncthreads();
-      next.store(s_w);
-      __syncthreads();
-      int cur = 0;
       // forward: z_t of every layer and the last y stay
+      Limbs x;
       f4 y[4] = {}, z[H][4];
       column(wt + kR * a.D, z[0]);
       for (int ch = 0; ch < chunks; ++ch) {
         const bool more = ch + 1 < chunks;
-        if (more) next.load(wt + 64 * (ch + 1), a.D);
-        else if (H > 1) next.load(layer(wt, a.D, 1), kR);
-        product(s_w + cur * kWBlock, in, z[0]);
+        if (more) ahead(ch + 1, false);
+        else if (H > 1) ahead(chunks, false);
+        else ahead(0, true);
+        x.of(in);
         if (more) load_x<BF>(a, r, ch + 1, in);
-        if (more || H > 1) {
-          next.store(s_w + (cur ^ 1) * kWBlock);
-          cur ^= 1;
-          __syncthreads();
-        }
+        product(s_w + cur * kBlockBytes, x, z[0]);
+        turn();
       }
 #pragma unroll
       for (int l = 0; l < H; ++l) {
@@ -530,15 +648,11 @@ __global__ __launch_bounds__(NW * 64) void k_gradient(HeadsArgs a) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) y[t][i] += z[l][t][i] * sigmoid(z[l][t][i]);
         if (l + 1 < H) {
-          const float* bias = layer(wt, a.D, l + 1) + kR * kR;
-      column(bias, z[l + 1]);
-          if (l + 2 < H) next.load(layer(wt, a.D, l + 2), kR);
-          product(s_w + cur * kWBlock, y, z[l + 1]);
-          if (l + 2 < H) {
-            next.store(s_w + (cur ^ 1) * kWBlock);
-            cur ^= 1;
-            __syncthreads();
-          }
+          column(layer(wt, a.D, l + 1) + kR * kR, z[l + 1]);
+          ahead(chunks + (l + 2 < H ? l + 1 : l), l + 2 == H);
+          x.of(y);
+          product(s_w + cur * kBlockBytes, x, z[l + 1]);
+          turn();
         }
       }
       const float* out = layer(wt, a.D, H);
@@ -547,75 +661,79 @@ __global__ __launch_bounds__(NW * 64) void k_gradient(HeadsArgs a) {
       {
         float v = 0.f;
         column(out, u);
+        f4 dy[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             v += u[t][i] * y[t][i];
             u[t][i] *= d;
+            dy[t][i] = d * y[t][i];
           }
         if (TRAIN) {
           sum_c += d;
-          to_lds(kRows * kTS, y);
-          const float* const y_own = s_y + here(16 * w * kTS + lane);
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            sum_a += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(d), j)) * y_own[j * kTS];
+          sum_a += fold16(dy);
         }
         v += __shfl_xor(v, 16, 64);
         v += __shfl_xor(v, 32, 64);
         store_value(a, r, v + out[kR]);
       }
-      // g_t = u silu'(z_t), and y_{t-1} from y_t (the sigmoid again: a tenth of the
-      // products' time, where keeping y or silu' of every layer takes 16 registers
-      // a layer that there are not)
+      // g_t = u silu'(z_t), and y_{t-1} from y_t (the sigmoid again: keeping y or
+      // silu' of every layer takes 16 registers a layer that there are not)
       auto back = [&](f4 zl[4], f4 gz[4]) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             // (so that the compiler does not keep the forward pass's sigmoids)
-          asm volatile("" : "+v"(zl[t][i]));
-          const float s = sigmoid(zl[t][i]);
+            asm volatile("" : "+v"(zl[t][i]));
+            const float s = sigmoid(zl[t][i]);
             gz[t][i] = u[t][i] * (s * (1.f + zl[t][i] * (1.f - s)));
             if (TRAIN) y[t][i] -= zl[t][i] * s;
           }
       };
-      // backward: the block in use is A_{H-1} (A_0's last chunk for H = 1)
+      f4 gz[4];
 #pragma unroll
       for (int l = H - 1; l > 0; --l) {
-        f4 gz[4];
+        ahead(l > 1 ? chunks + l - 2 : 0, true);
         back(z[l], gz);
-        if (l > 1) next.load(layer(wt, a.D, l - 1), kR);
-        else next.load(wt, a.D);
+        x.of(gz);
         if (TRAIN) {
-          to_lds(0, gz);
-          to_lds(kRows * kTS, y);
+          sum_b[l] += fold16(gz);
+          put_limbs(s_g, x);
+          put_values(s_y, y);
+        }
+        product(s_w + cur * kBlockBytes, x, u);
+        if (TRAIN) {
           __syncthreads();
           outer(sum_h[l - 1]);
-          sum_b[l] += bias_sum();
         }
-        product_t(s_w + cur * kWBlock, gz, u);
-        next.store(s_w + (cur ^ 1) * kWBlock);
-        cur ^= 1;
-        __syncthreads();
+        turn();
       }
-      f4 gz[4];
+      if (TRAIN) load_x<BF>(a, r, 0, in);
       back(z[0], gz);
+      x.of(gz);
       if (TRAIN) {
-        to_lds(0, gz);
-        __syncthreads();
-        sum_b[0] += bias_sum();
+        sum_b[0] += fold16(gz);
+        put_limbs(s_g, x);
       }
-      // A_0 chunk by chunk; for H = 1 the last chunk is in use, so that one first
-      for (int k = 0; k < chunks; ++k) {
-        const int ch = H > 1 ? k : chunks - 1 - k;
-        const int after = H > 1 ? k + 1 : chunks - 2 - k;
-        const bool more = k + 1 < chunks;
-        if (more) next.load(wt + 64 * after, a.D);
+      const Row now = r;
+      const bool follows = tile + 1 < stop;
+      if (follows) r = row_of(a, begin + (tile + 1 - t0) * kRows + 16 * w + c, end);
+      for (int ch = 0; ch < chunks; ++ch) {
+        const bool more = ch + 1 < chunks;
+        if (more) ahead(ch + 1, true);
+        else if (follows) ahead(0, false);
+        if (TRAIN) put_values(s_y, in);
+        // the next chunk, or the next tile's first
+        if (TRAIN && more) load_x<BF>(a, now, ch + 1, in);
+        else if (!more && follows) load_x<BF>(a, r, 0, in);
+        if (a.dx) {
+          f4 dx[4] = {};
+          product(s_w + cur * kBlockBytes, x, dx);
+          store_dx<BF>(a, now, ch, dx);
+        }
         if (TRAIN) {
-          load_x<BF>(a, r, ch, in);
-          to_lds(kRows * kTS, in);
           __syncthreads();
           if (ch == 0) outer(sum_0[0]);
           else if (ch == 1) outer(sum_0[1]);
@@ -629,16 +747,7 @@ __global__ __launch_bounds__(NW * 64) void k_gradient(HeadsArgs a) {
             for (int j = 0; j < kOwn; ++j) *place(slot, ch, j) = acc[j];
           }
         }
-        if (a.dx) {
-          f4 dx[4] = {};
-          product_t(s_w + cur * kWBlock, gz, dx);
-          store_dx<BF>(a, r, ch, dx);
-        }
-        if (more) {
-          next.store(s_w + (cur ^ 1) * kWBlock);
-          cur ^= 1;
-          __syncthreads();
-        }
+        turn();
       }
     }
     if (TRAIN) flush(e);
@@ -717,11 +826,11 @@ __global__ __launch_bounds__(256) void k_sum_entries(HeadsArgs a) {
 
 // Wavefronts of a work-group: eight, two a SIMD; four where y and silu' of more
 // than four layers and the sums of their gradients need all of a SIMD's registers.
-int heads_waves(const HeadsArgs& a) { return a.dweights && a.H > 4 ? 4 : 8; }
+int heads_waves(const HeadsArgs& a) { return a.dweights && a.H <= 4 ? 8 : 4; }
 
 template <int H, int NW, bool TRAIN, bool BF>
 hipError_t gradient_of(const HeadsArgs& a, hipStream_t s) {
-  constexpr size_t lds = (2 * kWBlock + (TRAIN ? 2 * 16 * NW * kTStride : 0)) * sizeof(float);
+  constexpr size_t lds = 2 * kBlockBytes + (TRAIN ? 2 * 3 * 16 * NW * kRowBytes : 0);
   const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_gradient<H, NW, TRAIN, BF>),
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
   if (ready != hipSuccess) return ready;
@@ -731,16 +840,16 @@ hipError_t gradient_of(const HeadsArgs& a, hipStream_t s) {
 
 template <bool TRAIN, bool BF>
 hipError_t gradient_by_layers(const HeadsArgs& a, hipStream_t s) {
-  constexpr int kDeep = TRAIN ? 4 : 8;
+  constexpr int kShallow = TRAIN ? 8 : 4;
   switch (a.H) {
-    case 1: return gradient_of<1, 8, TRAIN, BF>(a, s);
-    case 2: return gradient_of<2, 8, TRAIN, BF>(a, s);
-    case 3: return gradient_of<3, 8, TRAIN, BF>(a, s);
-    case 4: return gradient_of<4, 8, TRAIN, BF>(a, s);
-    case 5: return gradient_of<5, kDeep, TRAIN, BF>(a, s);
-    case 6: return gradient_of<6, kDeep, TRAIN, BF>(a, s);
-    case 7: return gradient_of<7, kDeep, TRAIN, BF>(a, s);
-    default: return gradient_of<8, kDeep, TRAIN, BF>(a, s);
+    case 1: return gradient_of<1, kShallow, TRAIN, BF>(a, s);
+    case 2: return gradient_of<2, kShallow, TRAIN, BF>(a, s);
+    case 3: return gradient_of<3, kShallow, TRAIN, BF>(a, s);
+    case 4: return gradient_of<4, kShallow, TRAIN, BF>(a, s);
+    case 5: return gradient_of<5, 4, TRAIN, BF>(a, s);
+    case 6: return gradient_of<6, 4, TRAIN, BF>(a, s);
+    case 7: return gradient_of<7, 4, TRAIN, BF>(a, s);
+    default: return gradient_of<8, 4, TRAIN, BF>(a, s);
   }
 }
 
@@ -750,21 +859,33 @@ size_t heads_plan(HeadsArgs* a, int n_cu) {
   const int rows = 16 * heads_waves(*a);
   // at most one more tile than full ones for each head and for entries without
   const int64_t tiles = a->m / rows + a->E + 1;
-  a->blocks = int(std::min<int64_t>(tiles, n_cu));
+  a->blocks = int(std::min<int64_t>(tiles, a->dweights ? n_cu : 2 * n_cu));
   a->slot = slot_values(a->D, a->H);
-  size_t b = 0;
+  a->split_block = (a->dx || a->dweights ? 2 : 1) * kBlockBytes;
+  size_t b = size_t(a->E) * size_t((a->D + 63) / 64 + a->H - 1) * size_t(a->split_block);
   if (a->dweights) b += size_t(a->blocks + a->E) * size_t(a->slot) * sizeof(float);
   if (a->K > 1 && a->energy) b += size_t(a->m) * sizeof(float);
   if (a->K > 1 && a->dx) b += size_t(a->m) * size_t(a->D) * sizeof(float);
   return b;
 }
 
+void heads_workspace(HeadsArgs* a, unsigned char* ws) {
+  a->split = ws;
+  ws += size_t(a->E) * size_t((a->D + 63) / 64 + a->H - 1) * size_t(a->split_block);
+  float* at = reinterpret_cast<float*>(ws);
+  if (a->dweights) a->slots = at, at += int64_t(a->blocks + a->E) * a->slot;
+  if (a->K > 1 && a->dx) a->entry_dx = at, at += a->m * a->D;
+  if (a->K > 1 && a->energy) a->entry_energy = at;
+}
+
 hipError_t launch_heads(const HeadsArgs& a, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.m > 0) {
+    k_split<<<dim3((a.D + 63) / 64 + a.H - 1, a.E), 256, 0, s>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     if (!a.dx && !a.dweights) {
-      if (a.bf16) k_energy<8, true><<<a.blocks, 512, 0, s>>>(a);
-      else k_energy<8, false><<<a.blocks, 512, 0, s>>>(a);
+      if (a.bf16) k_energy<4, true><<<a.blocks, 256, 0, s>>>(a);
+      else k_energy<4, false><<<a.blocks, 256, 0, s>>>(a);
       e = hipGetLastError();
     } else if (a.dweights) {
       e = a.bf16 ? gradient_by_layers<true, true>(a, s) : gradient_by_layers<true, false>(a, s);

@@ -257,10 +257,7 @@ mlip_status mlip_heads(mlip_learn* ctx, const mlip_heads_params* p, int64_t n, c
   const size_t need = heads_plan(&a, ctx->n_cu);
   const mlip_status w = workspace(ctx, need);
   if (w != MLIP_OK) return w;
-  float* at = reinterpret_cast<float*>(ctx->d_ws);
-  if (a.dweights) a.slots = at, at += int64_t(a.blocks + a.E) * a.slot;
-  if (a.K > 1 && a.dx) a.entry_dx = at, at += a.m * a.D;
-  if (a.K > 1 && a.energy) a.entry_energy = at;
+  heads_workspace(&a, ctx->d_ws);
   LEARN_HIP(ctx, launch_heads(a, ctx->stream));
   return MLIP_OK;
 }

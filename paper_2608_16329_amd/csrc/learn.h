@@ -103,12 +103,15 @@ struct HeadsArgs {
   float* dgates;              // [m] or null
   float* entry_energy;        // [m], with several entries a row
   float* entry_dx;            // [m][D], with several entries a row and dx
+  unsigned char* split;       // the heads' matrices in limbs, split_block bytes a block
+  int64_t split_block;
   float* slots;               // [blocks + E][slot] sums of a work-group for a head
   int64_t slot;
 };
-// Work-groups, values per slot, and the workspace in bytes (split off in order:
-// slots, entry gradients, entry energies); sets blocks and slot.
+// Sets blocks, split_block and slot; the workspace in bytes, which
+// heads_workspace divides.
 size_t heads_plan(HeadsArgs* a, int n_cu);
+void heads_workspace(HeadsArgs* a, unsigned char* ws);
 hipError_t launch_heads(const HeadsArgs& a, hipStream_t s);
 
 // Arguments of the AdamW kernels.
