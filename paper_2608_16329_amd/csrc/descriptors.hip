@@ -21,12 +21,12 @@ __global__ __launch_bounds__(256) void k_rows(R* __restrict__ slots, const int32
   F4 f;
   if (OUT) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) f.v[q] = float(s[q]);
+    for (int q = 0; q < 4; ++q) f[q] = float(s[q]);
     *reinterpret_cast<F4*>(r) = f;
   } else {
     f = *reinterpret_cast<const F4*>(r);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) s[q] = R(f.v[q]);
+    for (int q = 0; q < 4; ++q) s[q] = R(f[q]);
   }
 }
 

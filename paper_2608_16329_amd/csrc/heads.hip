@@ -80,15 +80,16 @@ __device__ __forceinline__ void split4(const f4 v, u2 limb[3]) {
 // 64 values of a column as a product's second operand: step s, limb k.
 struct Limbs {
   u4 v[2][3];
+  __device__ __forceinline__ void step(int s, const f4 a, const f4 b) {
+    u2 lo[3], hi[3];
+    split4(a, lo);
+    split4(b, hi);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) v[s][k] = u4{lo[k][0], lo[k][1], hi[k][0], hi[k][1]};
+  }
   __device__ __forceinline__ void of(const f4 in[4]) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u2 lo[3], hi[3];
-      split4(in[2 * s], lo);
-      split4(in[2 * s + 1], hi);
-#pragma unroll
-      for (int k = 0; k < 3; ++k) v[s][k] = u4{lo[k][0], lo[k][1], hi[k][0], hi[k][1]};
-    }
+    step(0, in[0], in[1]);
+    step(1, in[2], in[3]);
   }
 };
 // Which of a block's 64 inputs value j of lane group g is in step s.
@@ -143,11 +144,7 @@ __device__ void tile_table(const HeadsArgs& a, int rows, int32_t* first, int32_t
 __device__ __forceinline__ int share(int64_t tiles, int64_t b, int blocks) { return int(tiles * b / blocks); }
 
 __device__ __forceinline__ f4 vec4(const float* p) {
-  const F4 f = *reinterpret_cast<const F4*>(p);
-  f4 t;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) t[k] = f.v[k];
-  return t;
+  return *reinterpret_cast<const F4*>(p);
 }
 // The same from a place that all lanes share, and the lane's own bytes from there.
 __device__ __forceinline__ f4 vec4(const float* base, uint32_t bytes) {
@@ -183,24 +180,44 @@ __device__ __forceinline__ void stage(const unsigned char* src, unsigned char* l
 }
 __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// out += block in, the next operands loaded before this one's products (and no
-// further ahead: loads of the whole block at once take the registers that sums
-// need).
-__device__ __forceinline__ void product(const unsigned char* block, const Limbs& in, f4 out[4]) {
+// Between two matrix instructions, vector instructions of what stands beside
+// them: 16 cycles of one take four of the other.
+template <int N>
+__device__ __forceinline__ void mixed() {
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+  }
+}
+
+// out += block in, one tile of 16 results after another, the next tile's
+// operands loaded before this one's products; beside(t) is work that goes with
+// the products of tile t, such as what becomes of the results of the tiles before.
+template <typename F>
+__device__ __forceinline__ void product(const unsigned char* block, const Limbs& in, f4 out[4], F beside) {
   const unsigned char* p = block + here(16 * (threadIdx.x & 63));
-  u4 a[2][3];
+  u4 a[2][3];   // of step 0, step 1
+  auto fetch = [&](int t, int s) {
 #pragma unroll
-  for (int k = 0; k < 3; ++k) a[0][k] = *reinterpret_cast<const u4*>(p + kFragBytes * k);
+    for (int k = 0; k < 3; ++k) a[s][k] = *reinterpret_cast<const u4*>(p + kFragBytes * (3 * (4 * s + t) + k));
+  };
+  fetch(0, 0);
+  fetch(0, 1);
 #pragma unroll
-  for (int n = 0; n < 8; ++n) {   // step n / 4, result tile n % 4
+  for (int t = 0; t < 4; ++t) {
     __builtin_amdgcn_sched_barrier(0);
-    if (n < 7) {
-#pragma unroll
-      for (int k = 0; k < 3; ++k) a[(n + 1) & 1][k] = *reinterpret_cast<const u4*>(p + kFragBytes * (3 * (n + 1) + k));
-    }
-    out[n & 3] = mfma6(a[n & 1], in.v[n >> 2], out[n & 3]);
+    f4 sum = mfma6(a[0], in.v[0], out[t]);
+    if (t < 3) fetch(t + 1, 0);
+    out[t] = mfma6(a[1], in.v[1], sum);
+    if (t < 3) fetch(t + 1, 1);
+    beside(t);
+    mixed<12>();
   }
   __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void product(const unsigned char* block, const Limbs& in, f4 out[4]) {
+  product(block, in, out, [](int) {});
 }
 
 // The heads' matrices in limbs: block b of head e (64 inputs of A_0 each, then
@@ -290,7 +307,7 @@ __device__ __forceinline__ f4 x4(const void* p, int64_t at) {
   if (BF) {
     const H4 h = *reinterpret_cast<const H4*>(static_cast<const uint16_t*>(p) + at);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = from_bf16(h.v[i]);
+    for (int i = 0; i < 4; ++i) f[i] = from_bf16(h[i]);
   } else {
     f = vec4(static_cast<const float*>(p) + at);
   }
@@ -424,6 +441,12 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
     for (; tile < stop; ++tile) {
       Limbs x;
       f4 z[4], y[4] = {};
+      // y += silu(z) of one tile, and the next product's operand from two
+      auto activate = [&](int t, Limbs& next) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[t][i] += z[t][i] * sigmoid(z[t][i]);
+        if (t & 1) next.step(t >> 1, y[t - 1], y[t]);
+      };
       column(wt + kR * a.D, z);
       for (int ch = 0; ch < chunks; ++ch) {
         ahead(ch);
@@ -437,16 +460,17 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
         next = row_of(a, begin + (tile + 1 - t0) * kRows + 16 * w + (lane & 15), end);
         load_x<BF>(a, next, 0, in);
       }
-      for (int l = 1;; ++l) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[t][i] += z[t][i] * sigmoid(z[t][i]);
-        if (l == a.H) break;
+      for (int t = 0; t < 4; ++t) activate(t, x);
+      for (int l = 1; l < a.H; ++l) {
         ahead(chunks + l - 1);
-        x.of(y);
         column(layer(wt, a.D, l) + kR * kR, z);
-        product(s_w + cur * kBlockBytes, x, z);
+        Limbs after;
+        product(s_w + cur * kBlockBytes, x, z, [&](int t) {
+          if (t > 0) activate(t - 1, after);
+        });
+        activate(3, after);
+        x = after;
         turn();
       }
       const float* out = layer(wt, a.D, a.H);
@@ -519,18 +543,25 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       limb[k] = u4{half[0][0], half[0][1], half[1][0], half[1][1]};
     }
   };
-  // sums of g y^T over the tile's rows into the wavefront's tiles
-  auto outer = [&](f4 acc[kOwn]) {
-#pragma unroll 1
+  // sums of g y^T over the tile's rows into the wavefront's tiles; beside(s) is
+  // work that goes with the products of the s-th quarter of the rows (half, with
+  // four wavefronts: then it is called for two quarters)
+  auto outer = [&](f4 acc[kOwn], auto beside) {
+#pragma unroll
     for (int s = 0; s < NW / 2; ++s) {
       u4 ga[3], yb[kOwn][3];
+      __builtin_amdgcn_sched_barrier(0);
       get(s_g, ta, s, ga);
 #pragma unroll
       for (int k = 0; k < kOwn; ++k) get(s_y, tb + k, s, yb[k]);
 #pragma unroll
+      for (int q = 0; q < 8 / NW; ++q) beside(8 / NW * s + q);
+#pragma unroll
       for (int k = 0; k < kOwn; ++k) acc[k] = mfma6(ga, yb[k], acc[k]);
     }
+    __builtin_amdgcn_sched_barrier(0);
   };
+  auto nothing = [](int) {};
   auto put_limbs = [&](unsigned char* to, const Limbs& l) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -540,13 +571,10 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       put(to, t, limb);
     }
   };
-  auto put_values = [&](unsigned char* to, const f4 v[4]) {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      u2 limb[3];
-      split4(v[t], limb);
-      put(to, t, limb);
-    }
+  auto put_value = [&](unsigned char* to, int t, const f4 v) {
+    u2 limb[3];
+    split4(v, limb);
+    put(to, t, limb);
   };
   auto clear = [&]() {
 #pragma unroll
@@ -641,19 +669,25 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         product(s_w + cur * kBlockBytes, x, z[0]);
         turn();
       }
+      // y += silu(z_l) of one tile, and the next product's operand from two
+      auto activate = [&](int l, int t, Limbs& next) {
 #pragma unroll
-      for (int l = 0; l < H; ++l) {
+        for (int i = 0; i < 4; ++i) y[t][i] += z[l][t][i] * sigmoid(z[l][t][i]);
+        if (l + 1 < H && (t & 1)) next.step(t >> 1, y[t - 1], y[t]);
+      };
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 4; ++t) activate(0, t, x);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) y[t][i] += z[l][t][i] * sigmoid(z[l][t][i]);
-        if (l + 1 < H) {
-          column(layer(wt, a.D, l + 1) + kR * kR, z[l + 1]);
-          ahead(chunks + (l + 2 < H ? l + 1 : l), l + 2 == H);
-          x.of(y);
-          product(s_w + cur * kBlockBytes, x, z[l + 1]);
-          turn();
-        }
+      for (int l = 1; l < H; ++l) {
+        column(layer(wt, a.D, l) + kR * kR, z[l]);
+        ahead(chunks + (l + 1 < H ? l : l - 1), l + 1 == H);
+        Limbs after;
+        product(s_w + cur * kBlockBytes, x, z[l], [&](int t) {
+          if (t > 0) activate(l, t - 1, after);
+        });
+        activate(l, 3, after);
+        if (l + 1 < H) x = after;
+        turn();
       }
       const float* out = layer(wt, a.D, H);
       f4 u[4];
@@ -678,44 +712,46 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         v += __shfl_xor(v, 32, 64);
         store_value(a, r, v + out[kR]);
       }
-      // g_t = u silu'(z_t), and y_{t-1} from y_t (the sigmoid again: keeping y or
-      // silu' of every layer takes 16 registers a layer that there are not)
-      auto back = [&](f4 zl[4], f4 gz[4]) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            // (so that the compiler does not keep the forward pass's sigmoids)
-            asm volatile("" : "+v"(zl[t][i]));
-            const float s = sigmoid(zl[t][i]);
-            gz[t][i] = u[t][i] * (s * (1.f + zl[t][i] * (1.f - s)));
-            if (TRAIN) y[t][i] -= zl[t][i] * s;
-          }
-      };
+      // g_l = u silu'(z_l) of one tile, its limbs from two, and y_{l-1} from y_l
+      // (the sigmoid again: keeping y or silu' of every layer takes 16 registers
+      // a layer that there are not)
       f4 gz[4];
+      auto back = [&](int l, int t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // (so that the compiler does not keep the forward pass's sigmoids)
+          float zl = z[l][t][i];
+          asm volatile("" : "+v"(zl));
+          const float s = sigmoid(zl);
+          gz[t][i] = u[t][i] * (s * (1.f + zl * (1.f - s)));
+          if (TRAIN && l > 0) y[t][i] -= zl * s;
+        }
+        if (t & 1) x.step(t >> 1, gz[t - 1], gz[t]);
+      };
+#pragma unroll
+      for (int t = 0; t < 4; ++t) back(H - 1, t);
+      if (TRAIN) sum_b[H - 1] += fold16(gz);
 #pragma unroll
       for (int l = H - 1; l > 0; --l) {
         ahead(l > 1 ? chunks + l - 2 : 0, true);
-        back(z[l], gz);
-        x.of(gz);
-        if (TRAIN) {
-          sum_b[l] += fold16(gz);
-          put_limbs(s_g, x);
-          put_values(s_y, y);
-        }
-        product(s_w + cur * kBlockBytes, x, u);
+        if (TRAIN && l == 1) load_x<BF>(a, r, 0, in);   // for the chunks below
+        if (TRAIN) put_limbs(s_g, x);
+        product(s_w + cur * kBlockBytes, x, u, [&](int t) {
+          if (TRAIN) put_value(s_y, t, y[t]);
+        });
         if (TRAIN) {
           __syncthreads();
-          outer(sum_h[l - 1]);
+          outer(sum_h[l - 1], [&](int t) { back(l - 1, t); });
+          sum_b[l - 1] += fold16(gz);
+        } else {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) back(l - 1, t);
         }
         turn();
       }
-      if (TRAIN) load_x<BF>(a, r, 0, in);
-      back(z[0], gz);
-      x.of(gz);
       if (TRAIN) {
-        sum_b[0] += fold16(gz);
         put_limbs(s_g, x);
+        if (H == 1) load_x<BF>(a, r, 0, in);
       }
       const Row now = r;
       const bool follows = tile + 1 < stop;
@@ -724,7 +760,10 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         const bool more = ch + 1 < chunks;
         if (more) ahead(ch + 1, true);
         else if (follows) ahead(0, false);
-        if (TRAIN) put_values(s_y, in);
+        if (TRAIN) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) put_value(s_y, t, in[t]);
+        }
         // the next chunk, or the next tile's first
         if (TRAIN && more) load_x<BF>(a, now, ch + 1, in);
         else if (!more && follows) load_x<BF>(a, r, 0, in);
@@ -735,14 +774,14 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         }
         if (TRAIN) {
           __syncthreads();
-          if (ch == 0) outer(sum_0[0]);
-          else if (ch == 1) outer(sum_0[1]);
+          if (ch == 0) outer(sum_0[0], nothing);
+          else if (ch == 1) outer(sum_0[1], nothing);
           else {
             float* slot = a.slots + (int64_t(blockIdx.x) + e) * a.slot;
             f4 acc[kOwn];
 #pragma unroll
             for (int j = 0; j < kOwn; ++j) acc[j] = first ? f4{0.f, 0.f, 0.f, 0.f} : *place(slot, ch, j);
-            outer(acc);
+            outer(acc, nothing);
 #pragma unroll
             for (int j = 0; j < kOwn; ++j) *place(slot, ch, j) = acc[j];
           }

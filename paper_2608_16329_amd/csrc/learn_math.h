@@ -10,8 +10,10 @@ namespace mlip {
 
 // Four neighbouring values, aligned like one of them (rows and tables start
 // anywhere; the hardware loads and stores them in one access all the same).
-struct __attribute__((packed, aligned(4))) F4 { float v[4]; };
-struct __attribute__((packed, aligned(2))) H4 { uint16_t v[4]; };
+// Vectors, not arrays: of an array's four stores the compiler moves some out of
+// a branch and leaves three.
+typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t H4 __attribute__((ext_vector_type(4), aligned(2)));
 
 __device__ __forceinline__ float from_bf16(uint16_t h) { return __uint_as_float(uint32_t(h) << 16); }
 // round to nearest even; a NaN stays one
@@ -28,11 +30,11 @@ __device__ __forceinline__ void load4(const void* p, bool bf16, int64_t at, int 
     if (bf16) {
       const H4 h = *reinterpret_cast<const H4*>(static_cast<const uint16_t*>(p) + at);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = from_bf16(h.v[q]);
+      for (int q = 0; q < 4; ++q) v[q] = from_bf16(h[q]);
     } else {
       const F4 f = *reinterpret_cast<const F4*>(static_cast<const float*>(p) + at);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = f.v[q];
+      for (int q = 0; q < 4; ++q) v[q] = f[q];
     }
     return;
   }
@@ -48,12 +50,12 @@ __device__ __forceinline__ void store4(void* p, bool bf16, int64_t at, int left,
     if (bf16) {
       H4 h;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) h.v[q] = to_bf16(v[q]);
+      for (int q = 0; q < 4; ++q) h[q] = to_bf16(v[q]);
       *reinterpret_cast<H4*>(static_cast<uint16_t*>(p) + at) = h;
     } else {
       F4 f;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) f.v[q] = v[q];
+      for (int q = 0; q < 4; ++q) f[q] = v[q];
       *reinterpret_cast<F4*>(static_cast<float*>(p) + at) = f;
     }
     return;
