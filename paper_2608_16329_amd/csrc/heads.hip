@@ -287,16 +287,16 @@ struct Row {
   int32_t i;
   float gate, up;  // gate and denergy
 };
-__device__ __forceinline__ Row row_of(const HeadsArgs& a, int64_t at, int64_t end) {
+__device__ __forceinline__ int32_t entry_of(const HeadsArgs& a, int64_t at, int64_t end) {
+  return at < end ? a.order[at] : -1;
+}
+__device__ __forceinline__ Row row_of(const HeadsArgs& a, int32_t ent) {
   Row r{-1, 0, 0.f, 0.f};
-  if (at < end) {
-    const int32_t ent = a.order[at];
-    if (ent >= 0 && ent < a.m) {
-      r.entry = ent;
-      r.i = a.K == 1 ? ent : ent / a.K;
-      r.gate = a.gates ? a.gates[ent] : 1.f;
-      r.up = a.denergy ? a.denergy[r.i] : 1.f;
-    }
+  if (ent >= 0 && ent < a.m) {
+    r.entry = ent;
+    r.i = a.K == 1 ? ent : ent / a.K;
+    r.gate = a.gates ? a.gates[ent] : 1.f;
+    r.up = a.denergy ? a.denergy[r.i] : 1.f;
   }
   return r;
 }
@@ -385,7 +385,7 @@ template <int NW, bool BF>
 __device__ void empty_tile(const HeadsArgs& a, int64_t at0, int64_t end) {
   const int lane = threadIdx.x & 63;
   const int64_t at = at0 + 16 * (threadIdx.x >> 6) + (lane & 15);
-  Row r = row_of(a, at, end);
+  Row r = row_of(a, entry_of(a, at, end));
   r.gate = r.up = 0.f;   // the gate of such an entry may be anything
   store_value(a, r, 0.f);
   if (a.dx) {
@@ -423,7 +423,7 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
     int cur = 0;
     __syncthreads();
     stage<NW>(split, s_w);
-    Row r = row_of(a, begin + (tile - t0) * kRows + 16 * w + (lane & 15), end);
+    Row r = row_of(a, entry_of(a, begin + (tile - t0) * kRows + 16 * w + (lane & 15), end));
     f4 in[4];
     load_x<BF>(a, r, 0, in);
     landed();
@@ -448,6 +448,8 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
         if (t & 1) next.step(t >> 1, y[t - 1], y[t]);
       };
       column(wt + kR * a.D, z);
+      // the next tile's rows, in time for their inputs
+      const int32_t entry = tile + 1 < stop ? entry_of(a, begin + (tile + 1 - t0) * kRows + 16 * w + (lane & 15), end) : -1;
       for (int ch = 0; ch < chunks; ++ch) {
         ahead(ch);
         x.of(in);
@@ -457,7 +459,7 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
       }
       Row next{-1, 0, 0.f, 0.f};
       if (tile + 1 < stop) {
-        next = row_of(a, begin + (tile + 1 - t0) * kRows + 16 * w + (lane & 15), end);
+        next = row_of(a, entry);
         load_x<BF>(a, next, 0, in);
       }
 #pragma unroll
@@ -518,21 +520,24 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
   const int ta = NW == 8 ? w >> 1 : w, tb = NW == 8 ? 2 * (w & 1) : 0;
 
   f4 sum_h[H > 1 ? H - 1 : 1][kOwn], sum_0[kChunksHeld][kOwn];
-  float sum_b[H], sum_a = 0.f, sum_c = 0.f;   // of dc_t and da, value fold_value(); of dc
+  f4 sum_b;                                   // of dc_t, column t: the sums of g_t are products with ones there
+  float sum_a = 0.f, sum_c = 0.f;             // of da, value fold_value(); of dc
 
-  // Rows are 128 bytes a limb, their four groups of 16 values turned by the
-  // row, so that 16 rows of one group lie in all banks: as they are written
-  // (by column, four values a lane) and as they are read.
+  // A limb's row is 128 bytes: four groups of 16 values, turned by the row's
+  // bits 1 and 2, and the halves of a group by bit 3, so that the 32 lanes that
+  // LDS serves at once meet all banks: writing (by column, four values a lane)
+  // and reading.
+  const int put_at = (16 * w + c) * kRowBytes + 8 * (g ^ (c >> 3 << 1)) + ((c << 4) & 96);
+  const int get_at = (4 * g + (c >> 2)) * kRowBytes + 8 * ((c & 3) ^ (g & 2)) + (((4 * g + (c >> 2)) << 4) & 96);
   auto put = [&](unsigned char* to, int t, const u2 limb[3]) {
-    const int at = here((16 * w + c) * kRowBytes + 8 * g + (((c << 4) & 96) ^ (32 * t)));
+    const int at = here(put_at) ^ (32 * t);
 #pragma unroll
     for (int k = 0; k < 3; ++k) *reinterpret_cast<u2*>(to + k * kPlane + at) = limb[k];
   };
   // group t of 16 values of rows 32 s .. 32 s + 31 as an operand: lane (g, c)
   // gets value c at rows 4 g + j and 16 + 4 g + j, j < 4
   auto get = [&](const unsigned char* from, int t, int s, u4 limb[3]) {
-    const int row = 4 * g + (c >> 2);
-    const int at = here(row * kRowBytes + 8 * (c & 3) + (((row << 4) & 96) ^ (32 * t)));
+    const int at = here(get_at) ^ (32 * t);
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
       u2 half[2];
@@ -543,10 +548,12 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       limb[k] = u4{half[0][0], half[0][1], half[1][0], half[1][1]};
     }
   };
-  // sums of g y^T over the tile's rows into the wavefront's tiles; beside(s) is
+  // sums of g y^T over the tile's rows into the wavefront's tiles, and (bias >=
+  // 0) of g into column `bias` of sum_b, for which two wavefronts with the same
+  // outputs take turns; beside(s) is
   // work that goes with the products of the s-th quarter of the rows (half, with
   // four wavefronts: then it is called for two quarters)
-  auto outer = [&](f4 acc[kOwn], auto beside) {
+  auto outer = [&](f4 acc[kOwn], int bias, auto beside) {
 #pragma unroll
     for (int s = 0; s < NW / 2; ++s) {
       u4 ga[3], yb[kOwn][3];
@@ -558,6 +565,12 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       for (int q = 0; q < 8 / NW; ++q) beside(8 / NW * s + q);
 #pragma unroll
       for (int k = 0; k < kOwn; ++k) acc[k] = mfma6(ga, yb[k], acc[k]);
+      if (bias >= 0 && (NW == 4 || (w & 1) == (s & 1))) {
+        const uint32_t one = c == bias ? 0x3f803f80u : 0u;
+        const u4 ones = {one, one, one, one};
+#pragma unroll
+        for (int k = 2; k >= 0; --k) sum_b = mfma(ga[k], ones, sum_b);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -584,8 +597,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
 #pragma unroll
       for (int t = 0; t < kChunksHeld; ++t) sum_0[t][k] = f4{0.f, 0.f, 0.f, 0.f};
     }
-#pragma unroll
-    for (int t = 0; t < H; ++t) sum_b[t] = 0.f;
+    sum_b = f4{0.f, 0.f, 0.f, 0.f};
     sum_a = 0.f;
     sum_c = 0.f;
   };
@@ -604,23 +616,25 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       for (int t = 1; t < H; ++t) *place(slot, chunks + t - 1, k) = sum_h[t - 1][k];
     }
     float* tail = slot + slot_block(a.D, blocks);
-    // dc_t, da and dc over the wavefronts
-    constexpr int kSums = (H + 2) * kR;
+    // dc_t over the two wavefronts that have its value, da and dc over all
     float* const s_sum = reinterpret_cast<float*>(s_g);
+    float* const s_all = s_sum + 2 * H * kR;
     __syncthreads();
+    if (c < H)
 #pragma unroll
-    for (int t = 0; t < H; ++t) s_sum[w * kSums + t * kR + fold_value()] = sum_b[t];
-    s_sum[w * kSums + H * kR + fold_value()] = sum_a;
+      for (int i = 0; i < 4; ++i) s_sum[((NW == 8 ? w & 1 : 0) * H + c) * kR + 16 * ta + 4 * g + i] = sum_b[i];
+    s_all[w * 2 * kR + fold_value()] = sum_a;
     float v = sum_c;
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) v += __shfl_xor(v, o, 64);
-    if (lane == 0) s_sum[w * kSums + (H + 1) * kR] = v;
+    if (lane == 0) s_all[w * 2 * kR + kR] = v;
     __syncthreads();
-    for (int at = tid; at <= (H + 1) * kR; at += NW * 64) {
+    for (int at = tid; at < H * kR; at += NW * 64) tail[at] = NW == 8 ? s_sum[at] + s_sum[H * kR + at] : s_sum[at];
+    if (tid <= kR) {
       float v = 0.f;
 #pragma unroll
-      for (int u = 0; u < NW; ++u) v += s_sum[u * kSums + at];
-      tail[at] = v;
+      for (int u = 0; u < NW; ++u) v += s_all[u * 2 * kR + tid];
+      tail[H * kR + tid] = v;
     }
     __syncthreads();
   };
@@ -650,7 +664,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
     __syncthreads();
     cur = 1;
     ahead(0, false);
-    Row r = row_of(a, begin + (tile - t0) * kRows + 16 * w + c, end);
+    Row r = row_of(a, entry_of(a, begin + (tile - t0) * kRows + 16 * w + c, end));
     f4 in[4];
     load_x<BF>(a, r, 0, in);
     turn();
@@ -659,6 +673,9 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       Limbs x;
       f4 y[4] = {}, z[H][4];
       column(wt + kR * a.D, z[0]);
+      // the next tile's rows, in time for their inputs
+      const bool follows = tile + 1 < stop;
+      const int32_t entry = follows ? entry_of(a, begin + (tile + 1 - t0) * kRows + 16 * w + c, end) : -1;
       for (int ch = 0; ch < chunks; ++ch) {
         const bool more = ch + 1 < chunks;
         if (more) ahead(ch + 1, false);
@@ -730,7 +747,6 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       };
 #pragma unroll
       for (int t = 0; t < 4; ++t) back(H - 1, t);
-      if (TRAIN) sum_b[H - 1] += fold16(gz);
 #pragma unroll
       for (int l = H - 1; l > 0; --l) {
         ahead(l > 1 ? chunks + l - 2 : 0, true);
@@ -741,8 +757,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         });
         if (TRAIN) {
           __syncthreads();
-          outer(sum_h[l - 1], [&](int t) { back(l - 1, t); });
-          sum_b[l - 1] += fold16(gz);
+          outer(sum_h[l - 1], l, [&](int t) { back(l - 1, t); });
         } else {
 #pragma unroll
           for (int t = 0; t < 4; ++t) back(l - 1, t);
@@ -754,8 +769,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         if (H == 1) load_x<BF>(a, r, 0, in);
       }
       const Row now = r;
-      const bool follows = tile + 1 < stop;
-      if (follows) r = row_of(a, begin + (tile + 1 - t0) * kRows + 16 * w + c, end);
+      r = row_of(a, entry);
       for (int ch = 0; ch < chunks; ++ch) {
         const bool more = ch + 1 < chunks;
         if (more) ahead(ch + 1, true);
@@ -774,14 +788,14 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         }
         if (TRAIN) {
           __syncthreads();
-          if (ch == 0) outer(sum_0[0], nothing);
-          else if (ch == 1) outer(sum_0[1], nothing);
+          if (ch == 0) outer(sum_0[0], 0, nothing);
+          else if (ch == 1) outer(sum_0[1], -1, nothing);
           else {
             float* slot = a.slots + (int64_t(blockIdx.x) + e) * a.slot;
             f4 acc[kOwn];
 #pragma unroll
             for (int j = 0; j < kOwn; ++j) acc[j] = first ? f4{0.f, 0.f, 0.f, 0.f} : *place(slot, ch, j);
-            outer(acc, nothing);
+            outer(acc, -1, nothing);
 #pragma unroll
             for (int j = 0; j < kOwn; ++j) *place(slot, ch, j) = acc[j];
           }
