@@ -162,6 +162,15 @@ __device__ __forceinline__ void column(const float* base, f4 v[4]) {
 #pragma unroll
   for (int t = 0; t < 4; ++t) v[t] = vec4(base, bytes + 64 * t);
 }
+// The kernel's arguments read again: held in scalar registers across the loop
+// over tiles, they do not fit beside the rest, and come and go through vector
+// registers.
+__device__ __forceinline__ const HeadsArgs& again() {
+  typedef const __attribute__((address_space(4))) HeadsArgs* Args;
+  Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const HeadsArgs*)p;
+}
 // A value that all lanes hold, for the scalar registers.
 __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -501,7 +510,8 @@ __host__ __device__ __forceinline__ int64_t slot_values(int D, int H) {
 
 // Energies, gradients in the descriptors and (TRAIN) in the weights.
 template <int H, int NW, bool TRAIN, bool BF>
-__global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(HeadsArgs a) {
+__global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(HeadsArgs args) {
+  const HeadsArgs& a = again();
   constexpr int kRows = 16 * NW;
   constexpr int kOwn = 16 / NW;          // result tiles of a wavefront in a 64x64 block
   constexpr int kPlane = kRows * kRowBytes;   // a limb of the tile's rows
@@ -648,7 +658,6 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       for (; tile < stop; ++tile) empty_tile<NW, BF>(a, begin + (tile - t0) * kRows, end);
       break;
     }
-    const float* wt = a.weights + e * a.values;
     const unsigned char* split = a.split + e * int64_t(blocks) * a.split_block;
     if (TRAIN) clear();
     // blocks of weights in LDS: one in use, the next on its way into the other
@@ -669,6 +678,8 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
     load_x<BF>(a, r, 0, in);
     turn();
     for (bool first = true; tile < stop; ++tile, first = false) {
+      const HeadsArgs& a = again();
+      const float* const wt = a.weights + e * a.values;
       // forward: z_t of every layer and the last y stay
       Limbs x;
       f4 y[4] = {}, z[H][4];
