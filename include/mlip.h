@@ -422,8 +422,9 @@ void mlip_learn_destroy(mlip_learn* ctx);
  * A NaN (or +infinity) among the logits a row may use makes its gates NaN.
  * mlip_route_backward writes the logits' gradient (their type, [n][n_experts]
  * contiguous) of sum(dgates gates) + dloss loss: the choice of experts and the
- * shares f_e are constants of it.  dgates_dev [n][top_k] (not looked at where
- * experts is -1) or NULL, dloss_dev [1] or NULL: none.
+ * shares f_e are constants of it.  experts_dev and counts_dev are what
+ * mlip_route wrote for the same logits; dgates_dev [n][top_k] (not looked at
+ * where experts is -1) or NULL, dloss_dev [1] or NULL: none.
  * n in [0, 2^31 / top_k), n_experts 1..256, top_k 1..16 and <= n_experts.
  * Errors: MLIP_E_ARG, MLIP_E_OOM, MLIP_E_HIP.
  */

@@ -18,39 +18,78 @@ namespace {
 constexpr int kRouteThreads = 256;
 constexpr int kV = 16;              // logits a lane holds
 
-// Row i's logits of this lane: expert 4 (c L + l) + q at z[4 c + q]; what the
-// row may not use is -inf, whatever stands there.  True if anything is left in
-// this lane.
+typedef uint32_t U4 __attribute__((aligned(1)));   // four bytes from anywhere
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// The value of another lane: CTRL names it.
+template <int CTRL, typename T>
+__device__ __forceinline__ T from_lane(T v) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// f over the L lanes of a row, in all of them: with lane c ^ 1, c ^ 2, and by
+// mirrored halves of 8 and of 16 lanes.
+template <int L, typename T, typename F>
+__device__ __forceinline__ T over_row(T v, F f) {
+  if (L > 1) v = f(v, from_lane<0xb1>(v));
+  if (L > 2) v = f(v, from_lane<0x4e>(v));
+  if (L > 4) v = f(v, from_lane<0x141>(v));
+  if (L > 8) v = f(v, from_lane<0x140>(v));
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float row_sum(float v) {
+  return over_row<L>(v, [](float x, float y) { return x + y; });
+}
+template <int L>
+__device__ __forceinline__ float row_max(float v) {
+  return over_row<L>(v, [](float x, float y) { return fmaxf(x, y); });
+}
+
+// The expert whose logit a lane l of a row holds as its j-th.
+template <int L>
+__device__ __forceinline__ int expert_of(int j, int l) { return 4 * ((j >> 2) * L + l) + (j & 3); }
+
+// Row i's logits of this lane, what the row may not use as -inf, whatever
+// stands there.
 template <int L, bool BF>
-__device__ __forceinline__ bool load_row(const RouteArgs& a, int64_t i, int l, float z[kV]) {
-  const uint8_t* ok = nullptr;
+__device__ __forceinline__ void load_row(const RouteArgs& a, int64_t i, int l, float z[kV]) {
   bool live = i < a.n;
+  const uint8_t* ok = nullptr;
   if (live && a.kinds) {
     const int kind = a.kinds[i];
     live = kind >= 0 && kind < a.n_kinds;
     ok = a.allowed + int64_t(live ? kind : 0) * a.E;
   }
-  bool any = false;
 #pragma unroll
   for (int c = 0; c < kV / 4; ++c) {
     const int e = 4 * (c * L + l);
     float t[4];
     load4(a.logits, BF, i * a.stride + e, live ? a.E - e : 0, t);
+    uint32_t use = 0x01010101u;
+    if (ok) {
+      if (e + 4 <= a.E) {
+        use = *reinterpret_cast<const U4*>(ok + e);
+      } else {
+        use = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const bool use = live && e + q < a.E && (!ok || ok[e + q]);
-      z[4 * c + q] = use ? t[q] : -INFINITY;
-      any |= use && t[q] != -INFINITY;
+        for (int q = 0; q < 3; ++q)
+          if (e + q < a.E) use |= uint32_t(ok[e + q]) << (8 * q);
+      }
     }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) z[4 * c + q] = live && e + q < a.E && (use >> (8 * q) & 255u) ? t[q] : -INFINITY;
   }
-  return any;
 }
 
-template <int L>
-__device__ __forceinline__ float row_sum(float v) {
+// The loss from a wavefront's sums over experts (lane by lane) and the routed rows.
+__device__ __forceinline__ void write_loss(const RouteArgs& a, double entries, double cross, int rows) {
 #pragma unroll
-  for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  for (int o = 32; o > 0; o >>= 1) {
+    entries += __shfl_xor(entries, o, 64);
+    cross += __shfl_xor(cross, o, 64);
+  }
+  if ((threadIdx.x & 63) == 0) a.loss[0] = rows > 0 ? float(a.E * cross / (entries * double(rows))) : 0.f;
 }
 
 // Forward: L lanes per row, every lane with up to 16 of its logits, rows taken
@@ -59,6 +98,7 @@ __device__ __forceinline__ float row_sum(float v) {
 // order of work-groups.
 template <int L, bool BF>
 __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, bool only) {
+  constexpr int kKept = (kMaxTopK + L - 1) / L;   // choices a lane keeps: lane s % L the s-th
   __shared__ int32_t s_count[kMaxExperts + 1];
   __shared__ float s_p[kRouteThreads / 64][L * kV];
   const int tid = threadIdx.x, l = tid % L, lane = tid & 63, w = tid >> 6;
@@ -69,112 +109,111 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, bool only)
   for (int j = 0; j < kV; ++j) psum[j] = 0.f;
   constexpr int kRows = kRouteThreads / L;
   const int64_t step = int64_t(gridDim.x) * kRows;
+  int rows = 0;
   for (int64_t i0 = int64_t(blockIdx.x) * kRows; i0 < a.n; i0 += step) {
     const int64_t i = i0 + tid / L;
-    float z[kV];
-    bool any = load_row<L, BF>(a, i, l, z);
+    float z[kV], key[kV];
+    load_row<L, BF>(a, i, l, z);
+    // a NaN counts as the largest
+    float top = -INFINITY;
 #pragma unroll
-    for (int o = 1; o < L; o <<= 1) any |= bool(__shfl_xor(int(any), o, 64));
-    unsigned used = 0;
-    float top = 0.f, sum = 1.f, chosen_sum = 0.f;
-    float pick_v = 0.f;       // of the choice this lane keeps: lane s % L keeps s
-    int my_id[(kMaxTopK + L - 1) / L];
-    float my_w[(kMaxTopK + L - 1) / L];
+    for (int j = 0; j < kV; ++j) {
+      key[j] = z[j] != z[j] ? INFINITY : z[j];
+      top = fmaxf(top, key[j]);
+    }
+    top = row_max<L>(top);
+    const bool any = top != -INFINITY;
+    const float base = any ? top : 0.f;
+    float sum = 0.f;
 #pragma unroll
-    for (int r = 0; r < (kMaxTopK + L - 1) / L; ++r) my_id[r] = -1, my_w[r] = 0.f;
+    for (int j = 0; j < kV; ++j) {
+      z[j] = __builtin_amdgcn_exp2f((z[j] - base) * kLog2e);
+      sum += z[j];
+    }
+    sum = row_sum<L>(sum);
+    const float inv = any ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int j = 0; j < kV; ++j) psum[j] += z[j] * inv;
+    rows += any && l == 0;
+    float chosen = 0.f;
+    int my_id[kKept];
+    float my_w[kKept];
+#pragma unroll
+    for (int r = 0; r < kKept; ++r) my_id[r] = -1, my_w[r] = 0.f;
 #pragma unroll 1
     for (int s = 0; s < a.K; ++s) {
-      // largest of the lane's unused logits (a NaN counts as the largest)
-      float best = -INFINITY;
-      int id = 0x7fffffff, at = -1;
+      float best = top;
+      if (s > 0) {
+        best = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < kV; ++j) {
-        const float key = z[j] != z[j] ? INFINITY : z[j];
-        const bool take = !((used >> j) & 1u) && key > best;
-        best = take ? key : best;
-        at = take ? j : at;
+        for (int j = 0; j < kV; ++j) best = fmaxf(best, key[j]);
+        best = row_max<L>(best);
       }
-      if (at >= 0) id = 4 * ((at >> 2) * L + l) + (at & 3);
-      const int own = id;
+      // the lowest expert that has it
+      int at = 0;
+      bool has = false;
 #pragma unroll
-      for (int o = 1; o < L; o <<= 1) {
-        const float v = __shfl_xor(best, o, 64);
-        const int d = __shfl_xor(id, o, 64);
-        if (v > best || (v == best && d < id)) best = v, id = d;
+      for (int j = kV - 1; j >= 0; --j) {
+        const bool eq = key[j] == best;
+        at = eq ? j : at;
+        has |= eq;
       }
-      const bool there = id != 0x7fffffff;
-      if (there && own == id) used |= 1u << at;
-      if (s == 0) {
-        // the first choice is the row's largest logit
-        top = any ? best : 0.f;
-        float t = 0.f;
+      const int own = has ? expert_of<L>(at, l) : 0x7fffffff;
+      const int id = over_row<L>(own, [](int x, int y) { return x < y ? x : y; });
+      const bool there = best != -INFINITY;
+      at = own == id ? at : -1;
 #pragma unroll
-        for (int j = 0; j < kV; ++j) t += expf(z[j] - top);
-        sum = row_sum<L>(t);
-        sum = any ? sum : 1.f;
-      }
-      pick_v = there ? expf(best - top) : 0.f;
-      chosen_sum += pick_v;
+      for (int j = 0; j < kV; ++j) key[j] = at == j ? -INFINITY : key[j];
+      const float e = there ? __builtin_amdgcn_exp2f((best - base) * kLog2e) : 0.f;
+      chosen += e;
 #pragma unroll
-      for (int r = 0; r < (kMaxTopK + L - 1) / L; ++r)
-        if (s == r * L + l) my_id[r] = there ? id : -1, my_w[r] = pick_v;
+      for (int r = 0; r < kKept; ++r)
+        if (s == r * L + l) my_id[r] = there ? id : -1, my_w[r] = e;
       if (there && l == 0) atomicAdd(&s_count[id], 1);
     }
-    const float inv = 1.f / sum;
-    const float norm = any ? (a.all ? inv : 1.f / chosen_sum) : 0.f;
     if (i < a.n) {
+      const float norm = any ? (a.all ? inv : 1.f / chosen) : 0.f;
 #pragma unroll
-      for (int r = 0; r < (kMaxTopK + L - 1) / L; ++r) {
+      for (int r = 0; r < kKept; ++r) {
         const int s = r * L + l;
         if (s < a.K) {
           a.experts[i * a.K + s] = my_id[r];
-          a.gates[i * a.K + s] = my_id[r] >= 0 ? my_w[r] * norm : 0.f;
+          a.gates[i * a.K + s] = my_w[r] * norm;
         }
       }
     }
-    if (any) {
-#pragma unroll
-      for (int j = 0; j < kV; ++j) psum[j] += expf(z[j] - top) * inv;
-      if (l == 0) atomicAdd(&s_count[a.E], 1);
-    }
   }
+  if (rows) atomicAdd(&s_count[a.E], rows);
   // lanes with the same experts, then the wavefronts, in a fixed order
 #pragma unroll
   for (int j = 0; j < kV; ++j) {
     float v = psum[j];
 #pragma unroll
     for (int o = L; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-    if (lane < L) s_p[w][4 * ((j >> 2) * L + l) + (j & 3)] = v;
+    if (lane < L) s_p[w][expert_of<L>(j, l)] = v;
   }
   __syncthreads();
   if (!only) {
     for (int e = tid; e <= a.E; e += kRouteThreads) {
-      a.part_c[int64_t(blockIdx.x) * (a.E + 1) + e] = s_count[e];
-      if (e < a.E) a.part_p[int64_t(blockIdx.x) * a.E + e] = (s_p[0][e] + s_p[1][e]) + (s_p[2][e] + s_p[3][e]);
+      a.part_c[int64_t(e) * gridDim.x + blockIdx.x] = s_count[e];
+      if (e < a.E) a.part_p[int64_t(e) * gridDim.x + blockIdx.x] = (s_p[0][e] + s_p[1][e]) + (s_p[2][e] + s_p[3][e]);
     }
     return;
   }
   // one work-group has everything: the loss at once
-  __shared__ double s_sum[2];
-  if (tid == 0) {
+  for (int e = tid; e <= a.E; e += kRouteThreads) a.counts[e] = s_count[e];
+  if (w == 0) {
     double entries = 0.0, cross = 0.0;
-    for (int e = 0; e < a.E; ++e) {
+    for (int e = lane; e < a.E; e += 64) {
       entries += s_count[e];
       cross += double(s_count[e]) * double((s_p[0][e] + s_p[1][e]) + (s_p[2][e] + s_p[3][e]));
     }
-    s_sum[0] = entries;
-    s_sum[1] = cross;
-  }
-  __syncthreads();
-  for (int e = tid; e <= a.E; e += kRouteThreads) a.counts[e] = s_count[e];
-  if (tid == 0) {
-    const double rows = s_count[a.E];
-    a.loss[0] = rows > 0 ? float(a.E * s_sum[1] / (s_sum[0] * rows)) : 0.f;
+    write_loss(a, entries, cross, s_count[a.E]);
   }
 }
 
-// The work-groups' counts and sums added up in order, and the loss: one
-// wavefront per expert (and one for the routed rows), then one work-group.
+// The work-groups' counts and sums added up in order, and the loss: a
+// wavefront for every 16th expert (and the routed rows), then one for all.
 __global__ __launch_bounds__(1024) void k_route_total(RouteArgs a, int blocks) {
   __shared__ double s_p[kMaxExperts + 1];
   __shared__ int32_t s_c[kMaxExperts + 1];
@@ -182,9 +221,10 @@ __global__ __launch_bounds__(1024) void k_route_total(RouteArgs a, int blocks) {
   for (int e = w; e <= a.E; e += 16) {
     double p = 0.0;
     int c = 0;
+#pragma unroll 8
     for (int b = lane; b < blocks; b += 64) {
-      c += a.part_c[int64_t(b) * (a.E + 1) + e];
-      if (e < a.E) p += a.part_p[int64_t(b) * a.E + e];
+      c += a.part_c[int64_t(e) * blocks + b];
+      if (e < a.E) p += a.part_p[int64_t(e) * blocks + b];
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -194,107 +234,121 @@ __global__ __launch_bounds__(1024) void k_route_total(RouteArgs a, int blocks) {
     if (lane == 0) s_p[e] = p, s_c[e] = c, a.counts[e] = c;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (w == 0) {
     double entries = 0.0, cross = 0.0;
-    for (int e = 0; e < a.E; ++e) entries += s_c[e], cross += double(s_c[e]) * s_p[e];
-    const double rows = s_c[a.E];
-    a.loss[0] = rows > 0 ? float(a.E * cross / (entries * rows)) : 0.f;
+    for (int e = lane; e < a.E; e += 64) entries += s_c[e], cross += double(s_c[e]) * s_p[e];
+    write_loss(a, entries, cross, s_c[a.E]);
   }
 }
 
 // Backward: the probabilities again from the logits (they are read once in any
-// case, and keeping them would write and read as much again).
+// case, and keeping them would write and read as much again).  The lanes of a
+// row take its choices in turn; every lane writes the gradient without the
+// row's gates, then the lane that holds a chosen expert's logit writes that one
+// again with them.
 template <int L, bool BF>
 __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
-  const int tid = threadIdx.x, l = tid % L;
+  __shared__ float s_h[L * kV];
   __shared__ double s_entries;
-  if (tid == 0) {
+  const int tid = threadIdx.x, l = tid % L, lane = tid & 63;
+  if (tid < 64) {
     double t = 0.0;
-    for (int e = 0; e < a.E; ++e) t += a.counts[e];
-    s_entries = t;
+    for (int e = lane; e < a.E; e += 64) t += a.counts[e];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
+    if (lane == 0) s_entries = t;
   }
   __syncthreads();
-  float h0[kV];
   {
     const double rows = a.counts[a.E];
     const double f = a.dloss && rows > 0 && s_entries > 0 ? double(a.dloss[0]) * a.E / (rows * s_entries) : 0.0;
-#pragma unroll
-    for (int j = 0; j < kV; ++j) {
-      const int e = 4 * ((j >> 2) * L + l) + (j & 3);
-      h0[j] = e < a.E ? float(f * a.counts[e]) : 0.f;
-    }
+    for (int e = tid; e < L * kV; e += kRouteThreads) s_h[e] = e < a.E ? float(f * a.counts[e]) : 0.f;
   }
-  constexpr int kRows = kRouteThreads / L;
+  __syncthreads();
+  float h[kV];
+#pragma unroll
+  for (int j = 0; j < kV; ++j) h[j] = s_h[expert_of<L>(j, l)];
+  constexpr int kRows = kRouteThreads / L, kKept = (kMaxTopK + L - 1) / L;
   const int64_t step = int64_t(gridDim.x) * kRows;
   for (int64_t i0 = int64_t(blockIdx.x) * kRows; i0 < a.n; i0 += step) {
     const int64_t i = i0 + tid / L;
-    float z[kV], h[kV], d[kV];
-    bool any = load_row<L, BF>(a, i, l, z);
+    float z[kV];
+    load_row<L, BF>(a, i, l, z);
     float top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kV; ++j) top = fmaxf(top, z[j] != z[j] ? INFINITY : z[j]);
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) {
-      any |= bool(__shfl_xor(int(any), o, 64));
-      top = fmaxf(top, __shfl_xor(top, o, 64));
-    }
-    top = any ? top : 0.f;
-    float sum = 0.f;
+    top = row_max<L>(top);
+    const bool any = top != -INFINITY;
+    const float base = any ? top : 0.f;
+    float sum = 0.f, mean = 0.f;
 #pragma unroll
     for (int j = 0; j < kV; ++j) {
-      z[j] = expf(z[j] - top);
+      z[j] = __builtin_amdgcn_exp2f((z[j] - base) * kLog2e);
       sum += z[j];
-      h[j] = h0[j];
-      d[j] = 0.f;
-    }
-    sum = row_sum<L>(sum);
-    const float inv = any ? 1.f / sum : 0.f;
-    if (a.dgates && any) {
-      // the chosen experts' gradients, at the lanes that hold them
-      float wsum = 0.f, cross = 0.f;
-      if (!a.all) {
-#pragma unroll 1
-        for (int s = 0; s < a.K; ++s) {
-          const int id = a.experts[i * a.K + s];
-          if (id < 0 || id >= a.E) continue;
-          float e = 0.f;
-#pragma unroll
-          for (int j = 0; j < kV; ++j) e += 4 * ((j >> 2) * L + l) + (j & 3) == id ? z[j] : 0.f;
-          e = row_sum<L>(e);
-          wsum += e;
-          cross += e * a.dgates[i * a.K + s];
-        }
-      }
-      const float winv = wsum > 0.f || wsum != wsum ? 1.f / wsum : 0.f;
-      cross *= winv;
-#pragma unroll 1
-      for (int s = 0; s < a.K; ++s) {
-        const int id = a.experts[i * a.K + s];
-        if (id < 0 || id >= a.E) continue;
-        const float g = a.dgates[i * a.K + s];
-#pragma unroll
-        for (int j = 0; j < kV; ++j) {
-          const bool mine = 4 * ((j >> 2) * L + l) + (j & 3) == id;
-          if (a.all) h[j] += mine ? g : 0.f;
-          else d[j] += mine ? z[j] * winv * (g - cross) : 0.f;
-        }
-      }
-    }
-    float mean = 0.f;
-#pragma unroll
-    for (int j = 0; j < kV; ++j) {
-      z[j] *= inv;
       mean += z[j] * h[j];
     }
+    sum = row_sum<L>(sum);
     mean = row_sum<L>(mean);
+    const float inv = any ? 1.f / sum : 0.f;
+    mean *= inv;
+    // over the chosen: their exponentials, and the gates' gradients times those
+    const bool gates = a.dgates && any;
+    float chosen = 0.f, cross = 0.f;
+    int my_id[kKept];
+    float my_e[kKept], my_g[kKept];
+#pragma unroll
+    for (int r = 0; r < kKept; ++r) {
+      const int s = r * L + l;
+      my_id[r] = -1;
+      my_e[r] = my_g[r] = 0.f;
+      if (gates && s < a.K) {
+        const int id = a.experts[i * a.K + s];
+        if (id >= 0 && id < a.E) {
+          const int64_t at = i * a.stride + id;
+          const float x = BF ? from_bf16(static_cast<const uint16_t*>(a.logits)[at]) : static_cast<const float*>(a.logits)[at];
+          my_id[r] = id;
+          my_e[r] = __builtin_amdgcn_exp2f((x - base) * kLog2e);
+          my_g[r] = a.dgates[i * a.K + s];
+        }
+      }
+      if (r * L >= a.K) break;
+      chosen += my_e[r];
+      cross += my_e[r] * my_g[r];
+    }
+    chosen = row_sum<L>(chosen);
+    cross = row_sum<L>(cross);
+    if (a.all) mean += cross * inv;
     if (i < a.n) {
 #pragma unroll
       for (int c = 0; c < kV / 4; ++c) {
         const int e = 4 * (c * L + l);
         float t[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) t[q] = any ? z[4 * c + q] * (h[4 * c + q] - mean) + d[4 * c + q] : 0.f;
+        for (int q = 0; q < 4; ++q) t[q] = any ? z[4 * c + q] * inv * (h[4 * c + q] - mean) : 0.f;
         store4(a.dlogits, BF, i * a.E + e, a.E - e, t);
+      }
+    }
+    if (a.dgates) {
+      const float per = chosen != 0.f ? 1.f / chosen : 0.f;
+      cross *= per;
+#pragma unroll
+      for (int r = 0; r < kKept; ++r) {
+        if (r * L >= a.K) break;
+        const float p = my_e[r] * inv;
+        const float base_h = my_id[r] >= 0 ? s_h[my_id[r]] : 0.f;
+        const float d = a.all ? p * (base_h + my_g[r] - mean) : p * (base_h - mean) + my_e[r] * per * (my_g[r] - cross);
+        // each choice to the lane that has its logit
+#pragma unroll
+        for (int s = 0; s < L; ++s) {
+          const int from = (lane & ~(L - 1)) + s;
+          const int id = L > 1 ? __shfl(my_id[r], from, 64) : my_id[r];
+          const float v = L > 1 ? __shfl(d, from, 64) : d;
+          if (id >= 0 && (id >> 2) % L == l) {
+            const int64_t at = i * a.E + id;
+            if (BF) static_cast<uint16_t*>(a.dlogits)[at] = to_bf16(v);
+            else static_cast<float*>(a.dlogits)[at] = v;
+          }
+        }
       }
     }
   }
