@@ -15,10 +15,13 @@
 namespace mlip {
 namespace {
 
+constexpr int kForwardThreads = 1024;   // a work-group for each CU: few sums to add up afterwards
 constexpr int kRouteThreads = 256;
 constexpr int kV = 16;              // logits a lane holds
 
 typedef uint32_t U4 __attribute__((aligned(1)));   // four bytes from anywhere
+
+typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -66,19 +69,21 @@ __device__ __forceinline__ void load_row(const RouteArgs& a, int64_t i, int l, f
     const int e = 4 * (c * L + l);
     float t[4];
     load4(a.logits, BF, i * a.stride + e, live ? a.E - e : 0, t);
-    uint32_t use = 0x01010101u;
+    // a byte for each of the four that says whether the row may use it
+    const int left = live ? a.E - e : 0;
+    uint32_t use = left >= 4 ? 0x01010101u : (left > 0 ? 0x01010101u >> (8 * (4 - left)) : 0u);
     if (ok) {
-      if (e + 4 <= a.E) {
+      if (left >= 4) {
         use = *reinterpret_cast<const U4*>(ok + e);
       } else {
         use = 0;
 #pragma unroll
         for (int q = 0; q < 3; ++q)
-          if (e + q < a.E) use |= uint32_t(ok[e + q]) << (8 * q);
+          if (q < left) use |= uint32_t(ok[e + q]) << (8 * q);
       }
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) z[4 * c + q] = live && e + q < a.E && (use >> (8 * q) & 255u) ? t[q] : -INFINITY;
+    for (int q = 0; q < 4; ++q) z[4 * c + q] = use & (255u << (8 * q)) ? t[q] : -INFINITY;
   }
 }
 
@@ -97,33 +102,32 @@ __device__ __forceinline__ void write_loss(const RouteArgs& a, double entries, d
 // place and are added up in order afterwards, so results do not depend on the
 // order of work-groups.
 template <int L, bool BF>
-__global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, bool only) {
+__global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool only) {
   constexpr int kKept = (kMaxTopK + L - 1) / L;   // choices a lane keeps: lane s % L the s-th
   __shared__ int32_t s_count[kMaxExperts + 1];
-  __shared__ float s_p[kRouteThreads / 64][L * kV];
+  __shared__ float s_p[kForwardThreads / 64][L * kV];
   const int tid = threadIdx.x, l = tid % L, lane = tid & 63, w = tid >> 6;
-  for (int e = tid; e <= a.E; e += kRouteThreads) s_count[e] = 0;
+  for (int e = tid; e <= a.E; e += kForwardThreads) s_count[e] = 0;
   __syncthreads();
   float psum[kV];
 #pragma unroll
   for (int j = 0; j < kV; ++j) psum[j] = 0.f;
-  constexpr int kRows = kRouteThreads / L;
+  constexpr int kRows = kForwardThreads / L;
   const int64_t step = int64_t(gridDim.x) * kRows;
   int rows = 0;
   for (int64_t i0 = int64_t(blockIdx.x) * kRows; i0 < a.n; i0 += step) {
     const int64_t i = i0 + tid / L;
     float z[kV], key[kV];
     load_row<L, BF>(a, i, l, z);
-    // a NaN counts as the largest
+    // (a NaN is not looked at here; it is in the sum)
     float top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kV; ++j) {
-      key[j] = z[j] != z[j] ? INFINITY : z[j];
+      key[j] = z[j];
       top = fmaxf(top, key[j]);
     }
     top = row_max<L>(top);
-    const bool any = top != -INFINITY;
-    const float base = any ? top : 0.f;
+    const float base = top != -INFINITY ? top : 0.f;
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < kV; ++j) {
@@ -131,6 +135,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, bool only)
       sum += z[j];
     }
     sum = row_sum<L>(sum);
+    const bool any = sum != 0.f;
     const float inv = any ? 1.f / sum : 0.f;
 #pragma unroll
     for (int j = 0; j < kV; ++j) psum[j] += z[j] * inv;
@@ -150,15 +155,10 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, bool only)
         best = row_max<L>(best);
       }
       // the lowest expert that has it
-      int at = 0;
-      bool has = false;
+      int at = -1;
 #pragma unroll
-      for (int j = kV - 1; j >= 0; --j) {
-        const bool eq = key[j] == best;
-        at = eq ? j : at;
-        has |= eq;
-      }
-      const int own = has ? expert_of<L>(at, l) : 0x7fffffff;
+      for (int j = kV - 1; j >= 0; --j) at = key[j] == best ? j : at;
+      const int own = at >= 0 ? expert_of<L>(at, l) : 0x7fffffff;
       const int id = over_row<L>(own, [](int x, int y) { return x < y ? x : y; });
       const bool there = best != -INFINITY;
       at = own == id ? at : -1;
@@ -172,7 +172,8 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, bool only)
       if (there && l == 0) atomicAdd(&s_count[id], 1);
     }
     if (i < a.n) {
-      const float norm = any ? (a.all ? inv : 1.f / chosen) : 0.f;
+      // a NaN is in every gate of its row
+      const float norm = !any ? 0.f : (a.all || sum != sum ? inv : 1.f / chosen);
 #pragma unroll
       for (int r = 0; r < kKept; ++r) {
         const int s = r * L + l;
@@ -193,20 +194,25 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, bool only)
     if (lane < L) s_p[w][expert_of<L>(j, l)] = v;
   }
   __syncthreads();
+  auto sum_of = [&](int e) {
+    float v = 0.f;
+    for (int u = 0; u < kForwardThreads / 64; ++u) v += s_p[u][e];
+    return v;
+  };
   if (!only) {
-    for (int e = tid; e <= a.E; e += kRouteThreads) {
+    for (int e = tid; e <= a.E; e += kForwardThreads) {
       a.part_c[int64_t(e) * gridDim.x + blockIdx.x] = s_count[e];
-      if (e < a.E) a.part_p[int64_t(e) * gridDim.x + blockIdx.x] = (s_p[0][e] + s_p[1][e]) + (s_p[2][e] + s_p[3][e]);
+      if (e < a.E) a.part_p[int64_t(e) * gridDim.x + blockIdx.x] = sum_of(e);
     }
     return;
   }
   // one work-group has everything: the loss at once
-  for (int e = tid; e <= a.E; e += kRouteThreads) a.counts[e] = s_count[e];
+  for (int e = tid; e <= a.E; e += kForwardThreads) a.counts[e] = s_count[e];
   if (w == 0) {
     double entries = 0.0, cross = 0.0;
     for (int e = lane; e < a.E; e += 64) {
       entries += s_count[e];
-      cross += double(s_count[e]) * double((s_p[0][e] + s_p[1][e]) + (s_p[2][e] + s_p[3][e]));
+      cross += double(s_count[e]) * double(sum_of(e));
     }
     write_loss(a, entries, cross, s_count[a.E]);
   }
@@ -243,12 +249,12 @@ __global__ __launch_bounds__(1024) void k_route_total(RouteArgs a, int blocks) {
 
 // Backward: the probabilities again from the logits (they are read once in any
 // case, and keeping them would write and read as much again).  The lanes of a
-// row take its choices in turn; every lane writes the gradient without the
-// row's gates, then the lane that holds a chosen expert's logit writes that one
-// again with them.
+// row take its choices in turn; what a choice adds to its logit's gradient
+// goes through LDS to the lane that holds the logit.
 template <int L, bool BF>
 __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
   __shared__ float s_h[L * kV];
+  __shared__ __attribute__((aligned(16))) float s_add[kRouteThreads * kV];
   __shared__ double s_entries;
   const int tid = threadIdx.x, l = tid % L, lane = tid & 63;
   if (tid < 64) {
@@ -268,6 +274,10 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
   float h[kV];
 #pragma unroll
   for (int j = 0; j < kV; ++j) h[j] = s_h[expert_of<L>(j, l)];
+  float* const mine = s_add + tid / L * (L * kV);   // the row's
+#pragma unroll
+  for (int c = 0; c < kV / 4; ++c) *reinterpret_cast<f4*>(mine + 4 * (c * L + l)) = f4{0.f, 0.f, 0.f, 0.f};
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   constexpr int kRows = kRouteThreads / L, kKept = (kMaxTopK + L - 1) / L;
   const int64_t step = int64_t(gridDim.x) * kRows;
   for (int64_t i0 = int64_t(blockIdx.x) * kRows; i0 < a.n; i0 += step) {
@@ -276,10 +286,9 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
     load_row<L, BF>(a, i, l, z);
     float top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kV; ++j) top = fmaxf(top, z[j] != z[j] ? INFINITY : z[j]);
+    for (int j = 0; j < kV; ++j) top = fmaxf(top, z[j]);
     top = row_max<L>(top);
-    const bool any = top != -INFINITY;
-    const float base = any ? top : 0.f;
+    const float base = top != -INFINITY ? top : 0.f;
     float sum = 0.f, mean = 0.f;
 #pragma unroll
     for (int j = 0; j < kV; ++j) {
@@ -289,6 +298,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
     }
     sum = row_sum<L>(sum);
     mean = row_sum<L>(mean);
+    const bool any = sum != 0.f;
     const float inv = any ? 1.f / sum : 0.f;
     mean *= inv;
     // over the chosen: their exponentials, and the gates' gradients times those
@@ -311,45 +321,37 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
           my_g[r] = a.dgates[i * a.K + s];
         }
       }
-      if (r * L >= a.K) break;
       chosen += my_e[r];
       cross += my_e[r] * my_g[r];
     }
     chosen = row_sum<L>(chosen);
     cross = row_sum<L>(cross);
     if (a.all) mean += cross * inv;
+    const float per = chosen != 0.f ? 1.f / chosen : 0.f;
+    cross *= per;
+    if (a.dgates) {
+#pragma unroll
+      for (int r = 0; r < kKept; ++r)
+        if (my_id[r] >= 0) mine[my_id[r]] = a.all ? my_e[r] * inv * my_g[r] : my_e[r] * per * (my_g[r] - cross);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
     if (i < a.n) {
 #pragma unroll
       for (int c = 0; c < kV / 4; ++c) {
         const int e = 4 * (c * L + l);
+        const f4 add = *reinterpret_cast<const f4*>(mine + e);
         float t[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) t[q] = any ? z[4 * c + q] * inv * (h[4 * c + q] - mean) : 0.f;
+        for (int q = 0; q < 4; ++q) t[q] = any ? z[4 * c + q] * inv * (h[4 * c + q] - mean) + add[q] : 0.f;
         store4(a.dlogits, BF, i * a.E + e, a.E - e, t);
       }
     }
     if (a.dgates) {
-      const float per = chosen != 0.f ? 1.f / chosen : 0.f;
-      cross *= per;
+      // zero again for the next row
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-      for (int r = 0; r < kKept; ++r) {
-        if (r * L >= a.K) break;
-        const float p = my_e[r] * inv;
-        const float base_h = my_id[r] >= 0 ? s_h[my_id[r]] : 0.f;
-        const float d = a.all ? p * (base_h + my_g[r] - mean) : p * (base_h - mean) + my_e[r] * per * (my_g[r] - cross);
-        // each choice to the lane that has its logit
-#pragma unroll
-        for (int s = 0; s < L; ++s) {
-          const int from = (lane & ~(L - 1)) + s;
-          const int id = L > 1 ? __shfl(my_id[r], from, 64) : my_id[r];
-          const float v = L > 1 ? __shfl(d, from, 64) : d;
-          if (id >= 0 && (id >> 2) % L == l) {
-            const int64_t at = i * a.E + id;
-            if (BF) static_cast<uint16_t*>(a.dlogits)[at] = to_bf16(v);
-            else static_cast<float*>(a.dlogits)[at] = v;
-          }
-        }
-      }
+      for (int r = 0; r < kKept; ++r)
+        if (my_id[r] >= 0) mine[my_id[r]] = 0.f;
     }
   }
 }
@@ -520,7 +522,7 @@ int64_t group_chunk(int64_t m) { return std::max<int64_t>(1024, (m + 4096 * 64 -
 
 template <bool BF>
 hipError_t route_of(const RouteArgs& a, int blocks, hipStream_t s) {
-  const dim3 g(blocks), b(kRouteThreads);
+  const dim3 g(blocks), b(kForwardThreads);
   const bool only = blocks == 1;
   switch (route_lanes(a.E)) {
     case 1: k_route<1, BF><<<g, b, 0, s>>>(a, only); break;
@@ -547,9 +549,12 @@ hipError_t route_backward_of(const RouteArgs& a, int blocks, hipStream_t s) {
 
 }  // namespace
 
+// One work-group for up to four rounds of rows: adding up several costs a
+// launch, some 8 us, a round 2.
 int route_blocks(int64_t n, int E, int n_cu) {
-  const int rows = kRouteThreads / route_lanes(E);
-  return int(std::max<int64_t>(1, std::min<int64_t>((n + rows - 1) / rows, 4 * n_cu)));
+  const int rows = kForwardThreads / route_lanes(E);
+  if (n <= 4 * rows) return 1;
+  return int(std::min<int64_t>((n + rows - 1) / rows, n_cu));
 }
 
 hipError_t launch_route(const RouteArgs& a, int blocks, hipStream_t s) {
