@@ -145,31 +145,37 @@ __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool onl
     float my_w[kKept];
 #pragma unroll
     for (int r = 0; r < kKept; ++r) my_id[r] = -1, my_w[r] = 0.f;
+    // choices r L .. r L + L - 1, each kept by a lane of the row
+#pragma unroll
+    for (int r = 0; r < kKept; ++r) {
 #pragma unroll 1
-    for (int s = 0; s < a.K; ++s) {
-      float best = top;
-      if (s > 0) {
-        best = -INFINITY;
+      for (int s = r * L; s < min(a.K, r * L + L); ++s) {
+        float best = top;
+        if (s > 0) {
+          best = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < kV; ++j) best = fmaxf(best, key[j]);
-        best = row_max<L>(best);
+          for (int j = 0; j < kV; ++j) best = fmaxf(best, key[j]);
+          best = row_max<L>(best);
+        }
+        // the lowest expert that has it
+        int at = -1;
+#pragma unroll
+        for (int j = kV - 1; j >= 0; --j) at = key[j] == best ? j : at;
+        const int own = at >= 0 ? expert_of<L>(at, l) : 0x7fffffff;
+        const int id = over_row<L>(own, [](int x, int y) { return x < y ? x : y; });
+        const bool there = best != -INFINITY;
+        if (s + 1 < a.K) {
+          at = own == id ? at : -1;
+#pragma unroll
+          for (int j = 0; j < kV; ++j) key[j] = at == j ? -INFINITY : key[j];
+        }
+        const float e = there ? __builtin_amdgcn_exp2f((best - base) * kLog2e) : 0.f;
+        chosen += e;
+        const bool mine = s == r * L + l;
+        my_id[r] = mine && there ? id : my_id[r];
+        my_w[r] = mine ? e : my_w[r];
+        if (there && l == 0) atomicAdd(&s_count[id], 1);
       }
-      // the lowest expert that has it
-      int at = -1;
-#pragma unroll
-      for (int j = kV - 1; j >= 0; --j) at = key[j] == best ? j : at;
-      const int own = at >= 0 ? expert_of<L>(at, l) : 0x7fffffff;
-      const int id = over_row<L>(own, [](int x, int y) { return x < y ? x : y; });
-      const bool there = best != -INFINITY;
-      at = own == id ? at : -1;
-#pragma unroll
-      for (int j = 0; j < kV; ++j) key[j] = at == j ? -INFINITY : key[j];
-      const float e = there ? __builtin_amdgcn_exp2f((best - base) * kLog2e) : 0.f;
-      chosen += e;
-#pragma unroll
-      for (int r = 0; r < kKept; ++r)
-        if (s == r * L + l) my_id[r] = there ? id : -1, my_w[r] = e;
-      if (there && l == 0) atomicAdd(&s_count[id], 1);
     }
     if (i < a.n) {
       // a NaN is in every gate of its row

@@ -6,7 +6,6 @@ arithmetic runs in the library's HIP kernels, and there is no fallback.
 """
 from __future__ import annotations
 
-from contextlib import contextmanager
 from typing import Optional
 
 from . import binding as b
@@ -35,18 +34,19 @@ class _OnStream:
         self.device = self.stream.device
         self._dtypes = {torch.float32: b.MLIP_F32, torch.bfloat16: b.MLIP_BF16}
 
-    @contextmanager
-    def _ordered(self):
+    def _run(self, call, *args) -> None:
         """The call's work after what the current stream has, and what it gets next after the call's."""
         current = self.torch.cuda.current_stream(self.device)
         if current == self.stream:
-            yield
+            call(*args)
             return
         self.stream.wait_stream(current)
-        yield
+        call(*args)
         current.wait_stream(self.stream)
 
     def _dense(self, t, name: str, dtype, *shape):
+        if t.dtype is dtype and t.shape == shape and t.device == self.device and t.is_contiguous():
+            return
         _need(t.device == self.device, f"{name} is on {t.device}, not {self.device}")
         _need(t.dtype == dtype, f"{name} is {t.dtype}, not {dtype}")
         _need(tuple(t.shape) == shape, f"{name} has shape {tuple(t.shape)}, not {shape}")
@@ -54,6 +54,8 @@ class _OnStream:
 
     def _rows(self, t, name: str) -> int:
         """The values between the rows of a 2-d f32 or bf16 tensor."""
+        if t.dim() == 2 and t.dtype in self._dtypes and t.device == self.device and t.is_contiguous():
+            return t.shape[1]
         _need(t.device == self.device, f"{name} is on {t.device}, not {self.device}")
         _need(t.dtype in self._dtypes, f"{name} is {t.dtype}, not float32 or bfloat16")
         _need(t.dim() == 2, f"{name} has {t.dim()} dimensions, not 2")
@@ -72,6 +74,7 @@ class Learner(_OnStream):
 
     def __init__(self, stream=None):
         self.ctx = None
+        self._kept = {}
         self._bind(stream)
         with self.torch.cuda.device(self.device):
             self.ctx = b.mlip_learn_create(self.stream.cuda_stream)
@@ -102,8 +105,17 @@ class Learner(_OnStream):
             self._dense(kinds, "kinds", t.int32, n)
             _need(allowed.dim() == 2, "allowed is not 2-d")
             self._dense(allowed, "allowed", t.uint8, allowed.shape[0], n_experts)
-        return b.mlip_route_params(n_experts, top_k, 0 if kinds is None else allowed.shape[0], _GATES[gates_of],
-                                   self._dtypes[logits.dtype], max(stride, n_experts))
+        return self._params(b.mlip_route_params, n_experts, top_k, 0 if kinds is None else allowed.shape[0],
+                            _GATES[gates_of], self._dtypes[logits.dtype], max(stride, n_experts))
+
+    def _params(self, kind, *values):
+        """A parameter structure, kept: the same few come again in every step."""
+        p = self._kept.get((kind, values))
+        if p is None:
+            if len(self._kept) >= 64:
+                self._kept.clear()
+            p = self._kept[(kind, values)] = kind(*values)
+        return p
 
     def route(self, logits, experts, gates, counts, loss, *, kinds=None, allowed=None, gates_of: str = "chosen") -> None:
         """Route the rows of `logits` (f32 or bf16 [n, E], rows may be apart) to
@@ -118,9 +130,8 @@ class Learner(_OnStream):
         self._dense(gates, "gates", t.float32, n, p.top_k)
         self._dense(counts, "counts", t.int32, n_experts + 1)
         self._dense(loss, "loss", t.float32, 1)
-        with self._ordered():
-            b.mlip_route(self.ctx, p, n, _ptr(logits), _ptr(kinds), _ptr(allowed), _ptr(experts), _ptr(gates),
-                         _ptr(counts), _ptr(loss))
+        self._run(b.mlip_route, self.ctx, p, n, _ptr(logits), _ptr(kinds), _ptr(allowed), _ptr(experts), _ptr(gates),
+                  _ptr(counts), _ptr(loss))
 
     def route_backward(self, logits, experts, counts, dlogits, *, dgates=None, dloss=None, kinds=None, allowed=None,
                        gates_of: str = "chosen") -> None:
@@ -137,9 +148,8 @@ class Learner(_OnStream):
             self._dense(dgates, "dgates", t.float32, n, p.top_k)
         if dloss is not None:
             self._dense(dloss, "dloss", t.float32, 1)
-        with self._ordered():
-            b.mlip_route_backward(self.ctx, p, n, _ptr(logits), _ptr(kinds), _ptr(allowed), _ptr(experts), _ptr(counts),
-                                  _ptr(dgates), _ptr(dloss), _ptr(dlogits))
+        self._run(b.mlip_route_backward, self.ctx, p, n, _ptr(logits), _ptr(kinds), _ptr(allowed), _ptr(experts), _ptr(counts),
+                  _ptr(dgates), _ptr(dloss), _ptr(dlogits))
 
     def group(self, experts, offsets, order) -> None:
         """The entries of `experts` (int32, any shape: [n, k] or one species per
@@ -150,8 +160,7 @@ class Learner(_OnStream):
         self._dense(experts, "experts", t.int32, *experts.shape)
         self._dense(offsets, "offsets", t.int32, offsets.shape[0])
         self._dense(order, "order", t.int32, m)
-        with self._ordered():
-            b.mlip_group(self.ctx, m, offsets.shape[0] - 1, _ptr(experts), _ptr(offsets), _ptr(order))
+        self._run(b.mlip_group, self.ctx, m, offsets.shape[0] - 1, _ptr(experts), _ptr(offsets), _ptr(order))
 
     # -- energy heads ------------------------------------------------------------
 
@@ -167,7 +176,7 @@ class Learner(_OnStream):
         n, width = x.shape
         _need(weights.dim() == 2, "weights is not 2-d")
         n_experts, values = weights.shape
-        p = b.mlip_heads_params(n_experts, width, hidden, top_k, self._dtypes[x.dtype], max(stride, width))
+        p = self._params(b.mlip_heads_params, n_experts, width, hidden, top_k, self._dtypes[x.dtype], max(stride, width))
         count = b.mlip_heads_weight_count(p)
         _need(count == 0 or values * n_experts == count,
               f"weights has {values} values a head, {width} inputs and {hidden} layers need {count // max(n_experts, 1)}")
@@ -180,9 +189,8 @@ class Learner(_OnStream):
                                       (dgates, "dgates", t.float32, (n, top_k))):
             if v is not None:
                 self._dense(v, name, dtype, *shape)
-        with self._ordered():
-            b.mlip_heads(self.ctx, p, n, _ptr(x), _ptr(weights), _ptr(offsets), _ptr(order), _ptr(gates), _ptr(denergy),
-                         _ptr(energy), _ptr(dx), _ptr(dweights), _ptr(dgates))
+        self._run(b.mlip_heads, self.ctx, p, n, _ptr(x), _ptr(weights), _ptr(offsets), _ptr(order), _ptr(gates), _ptr(denergy),
+                  _ptr(energy), _ptr(dx), _ptr(dweights), _ptr(dgates))
 
 
 class AdamW(_OnStream):
@@ -259,8 +267,7 @@ class AdamW(_OnStream):
              weight_decay: float = 0.0, grad_scale: float = 1.0, seed: int = 0) -> None:
         """Step number `step` (from 1).  seed: of the rounding of 8-bit moments, another one each step."""
         p = b.mlip_adamw_params(step, lr, beta1, beta2, eps, weight_decay, grad_scale, seed & 0xFFFFFFFF)
-        with self._ordered():
-            b.mlip_adamw_step(self.plan, p, self._from, self._into, self._reverse)
+        self._run(b.mlip_adamw_step, self.plan, p, self._from, self._into, self._reverse)
 
     def accept(self) -> None:
         """With `into`: the next step starts from what the last one wrote."""
@@ -274,5 +281,4 @@ class AdamW(_OnStream):
         """The values that 8-bit moments as the last step wrote them stand for, f32 [elements] each."""
         self._dense(m, "m", self.torch.float32, self.m.shape[0])
         self._dense(v, "v", self.torch.float32, self.m.shape[0])
-        with self._ordered():
-            b.mlip_adamw_moments(self.plan, self._into, _ptr(m), _ptr(v))
+        self._run(b.mlip_adamw_moments, self.plan, self._into, _ptr(m), _ptr(v))
