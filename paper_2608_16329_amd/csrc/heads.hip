@@ -146,21 +146,17 @@ __device__ __forceinline__ int share(int64_t tiles, int64_t b, int blocks) { ret
 __device__ __forceinline__ f4 vec4(const float* p) {
   return *reinterpret_cast<const F4*>(p);
 }
-// The same from a place that all lanes share, and the lane's own bytes from there.
-__device__ __forceinline__ f4 vec4(const float* base, uint32_t bytes) {
-  return vec4(reinterpret_cast<const float*>(reinterpret_cast<const char*>(base) + bytes));
-}
 // The same value, not known to be: what is computed from it is computed where
 // it is used and not kept in registers around the loop over tiles.
 __device__ __forceinline__ int here(int v) {
   asm volatile("" : "+v"(v));
   return v;
 }
-// 64 values as the lanes hold a column: 16 t + 4 g + i in v[t][i].
+// 64 values in LDS as the lanes hold a column: 16 t + 4 g + i in v[t][i].
 __device__ __forceinline__ void column(const float* base, f4 v[4]) {
-  const uint32_t bytes = here(threadIdx.x & 48);
+  const float* p = base + here((threadIdx.x & 48) / 4);
 #pragma unroll
-  for (int t = 0; t < 4; ++t) v[t] = vec4(base, bytes + 64 * t);
+  for (int t = 0; t < 4; ++t) v[t] = *reinterpret_cast<const f4*>(p + 16 * t);
 }
 // The kernel's arguments read again: held in scalar registers across the loop
 // over tiles, they do not fit beside the rest, and come and go through vector
@@ -295,23 +291,28 @@ struct Row {
   int32_t entry;   // -1: none
   int32_t i;
   float gate, up;  // gate and denergy
+  const char* x;   // its inputs; of row 0 where there is none
+  char* dx;        // where their gradient goes
 };
 __device__ __forceinline__ int32_t entry_of(const HeadsArgs& a, int64_t at, int64_t end) {
   return at < end ? a.order[at] : -1;
 }
+template <bool BF>
 __device__ __forceinline__ Row row_of(const HeadsArgs& a, int32_t ent) {
-  Row r{-1, 0, 0.f, 0.f};
+  Row r{-1, 0, 0.f, 0.f, static_cast<const char*>(a.x), nullptr};
   if (ent >= 0 && ent < a.m) {
     r.entry = ent;
     r.i = a.K == 1 ? ent : ent / a.K;
     r.gate = a.gates ? a.gates[ent] : 1.f;
     r.up = a.denergy ? a.denergy[r.i] : 1.f;
+    r.x += (BF ? 2 : 4) * (int64_t(r.i) * a.stride);
+    r.dx = a.K == 1 ? static_cast<char*>(a.dx) + (BF ? 2 : 4) * (int64_t(r.i) * a.D)
+                    : reinterpret_cast<char*>(a.entry_dx) + 4 * (int64_t(ent) * a.D);
   }
   return r;
 }
-
 template <bool BF>
-__device__ __forceinline__ f4 x4(const void* p, int64_t at) {
+__device__ __forceinline__ f4 x4(const void* p, int at) {
   f4 f;
   if (BF) {
     const H4 h = *reinterpret_cast<const H4*>(static_cast<const uint16_t*>(p) + at);
@@ -323,47 +324,37 @@ __device__ __forceinline__ f4 x4(const void* p, int64_t at) {
   return f;
 }
 
-// Inputs 64 ch .. 64 ch + 63 of the lane's row: 16 T + 4 g + i in in[T][i],
-// zero from the last on.  Every lane loads four values that are there; where
-// they are the row's last four and not the ones asked for, they are shifted.
+// Inputs 64 ch .. 64 ch + 63 of the lane's row on their way: 16 T + 4 g + i in
+// in[T][i].  Every lane loads four values that are there; ready() takes out those
+// beyond the row's end and those of lanes without a row when they are used, so
+// that loading does not wait.
 template <bool BF>
-__device__ __forceinline__ void load_x(const HeadsArgs& a, const Row& r, int ch, f4 in[4]) {
-  const int g = (threadIdx.x >> 4) & 3;
-  const int64_t row = int64_t(r.i) * a.stride;
+__device__ __forceinline__ void load_x(const Row& r, int D, int ch, f4 in[4]) {
+  const int g = (threadIdx.x >> 4) & 3, last = max(D, 4) - 4;   // rows of fewer than four are copied to four (k_pad)
 #pragma unroll
-  for (int T = 0; T < 4; ++T) {
-    const int c = 64 * ch + 16 * T + 4 * g;
-    f4 f;
-    int shift = 0;
-    if (a.D >= 4) {
-      const int from = min(c, a.D - 4);
-      f = x4<BF>(a.x, row + from);
-      shift = c - from;
-    } else {
+  for (int T = 0; T < 4; ++T) in[T] = x4<BF>(r.x, min(64 * ch + 16 * T + 4 * g, last));
+}
+__device__ __forceinline__ f4 ready(const Row& r, int D, int ch, int T, f4 f) {
+  const int c = 64 * ch + 16 * T + 4 * ((threadIdx.x >> 4) & 3);
+  const int left = r.entry >= 0 ? D - c : 0;
+  if (D & 3) {
+    // the row's last four values where fewer are left
+    const int shift = D < 4 ? 0 : (left < 4 ? 4 - left : 0);
+    if (shift & 1) f = f4{f[1], f[2], f[3], 0.f};
+    if (shift & 2) f = f4{f[2], f[3], 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t at = row + min(i, a.D - 1);
-        f[i] = BF ? from_bf16(static_cast<const uint16_t*>(a.x)[at]) : static_cast<const float*>(a.x)[at];
-      }
-      if (a.D < 4) f[3] = 0.f;
-      if (a.D < 3) f[2] = 0.f;
-      if (a.D < 2) f[1] = 0.f;
-      shift = c;
-    }
-    if (a.D & 3) {
-      if (shift & 1) f = f4{f[1], f[2], f[3], 0.f};
-      if (shift & 2) f = f4{f[2], f[3], 0.f, 0.f};
-    }
-    const bool there = shift < 4 && r.entry >= 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) in[T][i] = there ? f[i] : 0.f;
+    for (int i = 0; i < 4; ++i) f[i] = i < left ? f[i] : 0.f;
+    return f;
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = left > 0 ? f[i] : 0.f;
+  return f;
 }
 
-// d[T][i] to the row of `to` at inputs 64 ch + 16 T + 4 g + i, those below `D`.
-template <bool BF>
-__device__ __forceinline__ void store_row(void* to, int64_t row, int D, int ch, const f4 d[4]) {
+// d[T][i] to the gradient of the lane's row at inputs 64 ch + 16 T + 4 g + i.
+__device__ __forceinline__ void store_dx(const Row& r, bool bf16, int D, int ch, const f4 d[4]) {
   const int g = (threadIdx.x >> 4) & 3;
+  if (r.entry < 0) return;
 #pragma unroll
   for (int T = 0; T < 4; ++T) {
     const int c = 64 * ch + 16 * T + 4 * g;
@@ -371,15 +362,8 @@ __device__ __forceinline__ void store_row(void* to, int64_t row, int D, int ch, 
     float v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = d[T][i];
-    store4(to, BF, row + c, D - c, v);
+    store4(r.dx, bf16, c, D - c, v);
   }
-}
-
-template <bool BF>
-__device__ __forceinline__ void store_dx(const HeadsArgs& a, const Row& r, int ch, const f4 d[4]) {
-  if (r.entry < 0) return;
-  if (a.K == 1) store_row<BF>(a.dx, int64_t(r.i) * a.D, a.D, ch, d);
-  else store_row<false>(a.entry_dx, int64_t(r.entry) * a.D, a.D, ch, d);
 }
 
 // Value v of the lane's row: energy and the gate's gradient.
@@ -394,17 +378,28 @@ template <int NW, bool BF>
 __device__ void empty_tile(const HeadsArgs& a, int64_t at0, int64_t end) {
   const int lane = threadIdx.x & 63;
   const int64_t at = at0 + 16 * (threadIdx.x >> 6) + (lane & 15);
-  Row r = row_of(a, entry_of(a, at, end));
+  Row r = row_of<BF>(a, entry_of(a, at, end));
   r.gate = r.up = 0.f;   // the gate of such an entry may be anything
   store_value(a, r, 0.f);
   if (a.dx) {
     const f4 zero[4] = {};
-    for (int ch = 0; 64 * ch < a.D; ++ch) store_dx<BF>(a, r, ch, zero);
+    for (int ch = 0; 64 * ch < a.D; ++ch) store_dx(r, BF && a.K == 1, a.D, ch, zero);
   }
 }
 
 __device__ __forceinline__ const float* layer(const float* w, int D, int t) {
   return w + (kR * D + kR + (t - 1) * (kR * kR + kR));
+}
+
+// A head's vectors to LDS: c_0 .. c_{H-1}, a, c.  (Loaded where they are used they
+// would wait for whatever loads and stores are under way.)
+constexpr int vectors(int H) { return (H + 1) * kR + 4; }
+__device__ __forceinline__ void load_vectors(const float* wt, int D, int H, float* to) {
+  for (int at = threadIdx.x; at <= (H + 1) * kR; at += blockDim.x) {
+    const int l = at / kR;
+    const float* from = l == 0 ? wt + kR * D : (l < H ? layer(wt, D, l) + kR * kR : layer(wt, D, H));
+    to[at] = from[l < H ? at % kR : at - H * kR];
+  }
 }
 
 // Energies alone.
@@ -413,6 +408,7 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
   constexpr int kRows = 16 * NW;
   __shared__ int32_t s_first[kMaxExperts + 2], s_entry[kMaxExperts + 2];
   __shared__ __attribute__((aligned(16))) unsigned char s_w[2 * kBlockBytes];
+  __shared__ __attribute__((aligned(16))) float s_vec[vectors(kMaxHeadLayers)];
   tile_table(a, kRows, s_first, s_entry);
   const int lane = threadIdx.x & 63, w = uni(threadIdx.x >> 6);
   const int tiles = uni(s_first[a.E + 1]);
@@ -431,10 +427,11 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
     const unsigned char* split = a.split + e * int64_t(blocks) * a.split_block;
     int cur = 0;
     __syncthreads();
+    load_vectors(wt, a.D, a.H, s_vec);
     stage<NW>(split, s_w);
-    Row r = row_of(a, entry_of(a, begin + (tile - t0) * kRows + 16 * w + (lane & 15), end));
+    Row r = row_of<BF>(a, entry_of(a, begin + (tile - t0) * kRows + 16 * w + (lane & 15), end));
     f4 in[4];
-    load_x<BF>(a, r, 0, in);
+    load_x<BF>(r, a.D, 0, in);
     landed();
     __syncthreads();
     // block b is in use: the next one, or the next tile's first, on its way
@@ -456,26 +453,28 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
         for (int i = 0; i < 4; ++i) y[t][i] += z[t][i] * sigmoid(z[t][i]);
         if (t & 1) next.step(t >> 1, y[t - 1], y[t]);
       };
-      column(wt + kR * a.D, z);
+      column(s_vec, z);
       // the next tile's rows, in time for their inputs
       const int32_t entry = tile + 1 < stop ? entry_of(a, begin + (tile + 1 - t0) * kRows + 16 * w + (lane & 15), end) : -1;
       for (int ch = 0; ch < chunks; ++ch) {
         ahead(ch);
+#pragma unroll
+        for (int T = 0; T < 4; ++T) in[T] = ready(r, a.D, ch, T, in[T]);
         x.of(in);
-        if (ch + 1 < chunks) load_x<BF>(a, r, ch + 1, in);
+        if (ch + 1 < chunks) load_x<BF>(r, a.D, ch + 1, in);
         product(s_w + cur * kBlockBytes, x, z);
         turn();
       }
-      Row next{-1, 0, 0.f, 0.f};
+      Row next = r;
       if (tile + 1 < stop) {
-        next = row_of(a, entry);
-        load_x<BF>(a, next, 0, in);
+        next = row_of<BF>(a, entry);
+        load_x<BF>(next, a.D, 0, in);
       }
 #pragma unroll
       for (int t = 0; t < 4; ++t) activate(t, x);
       for (int l = 1; l < a.H; ++l) {
         ahead(chunks + l - 1);
-        column(layer(wt, a.D, l) + kR * kR, z);
+        column(s_vec + l * kR, z);
         Limbs after;
         product(s_w + cur * kBlockBytes, x, z, [&](int t) {
           if (t > 0) activate(t - 1, after);
@@ -484,17 +483,16 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
         x = after;
         turn();
       }
-      const float* out = layer(wt, a.D, a.H);
       float v = 0.f;
       f4 o[4];
-      column(out, o);
+      column(s_vec + a.H * kR, o);
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) v += o[t][i] * y[t][i];
       v += __shfl_xor(v, 16, 64);
       v += __shfl_xor(v, 32, 64);
-      store_value(a, r, v + out[kR]);
+      store_value(a, r, v + s_vec[(a.H + 1) * kR]);
       r = next;
     }
   }
@@ -511,6 +509,8 @@ __host__ __device__ __forceinline__ int64_t slot_values(int D, int H) {
 // Energies, gradients in the descriptors and (TRAIN) in the weights.
 template <int H, int NW, bool TRAIN, bool BF>
 __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(HeadsArgs args) {
+  // (what the loop over tiles uses all the time; the rest is read again where it
+  // is used, away from LDS: scalar loads wait for what LDS has to do)
   const HeadsArgs& a = again();
   constexpr int kRows = 16 * NW;
   constexpr int kOwn = 16 / NW;          // result tiles of a wavefront in a 64x64 block
@@ -520,12 +520,14 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
   unsigned char* const s_g = s_mem + 2 * kBlockBytes;  // limbs of g, then of y
   unsigned char* const s_y = s_g + 3 * kPlane;
   __shared__ int32_t s_first[kMaxExperts + 2], s_entry[kMaxExperts + 2];
+  __shared__ __attribute__((aligned(16))) float s_vec[vectors(H)];
   tile_table(a, kRows, s_first, s_entry);
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = uni(tid >> 6);
   const int tiles = uni(s_first[a.E + 1]);
   const int t_begin = share(tiles, blockIdx.x, a.blocks), t_end = share(tiles, blockIdx.x + 1, a.blocks);
-  const int chunks = (a.D + 63) / 64, blocks = chunks + H - 1;
+  const int D = a.D, chunks = (D + 63) / 64, blocks = chunks + H - 1;
+  const bool one = a.K == 1, with_dx = a.dx != nullptr;
   // the wavefront's tiles of a block: outputs 16 ta .., inputs 16 (tb + k) ..
   const int ta = NW == 8 ? w >> 1 : w, tb = NW == 8 ? 2 * (w & 1) : 0;
 
@@ -612,7 +614,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
     sum_c = 0.f;
   };
   auto place = [&](float* slot, int b, int k) {
-    return reinterpret_cast<f4*>(reinterpret_cast<char*>(slot + slot_block(a.D, b) + (4 * ta + tb + k) * 256) + uint32_t(16 * lane));
+    return reinterpret_cast<f4*>(reinterpret_cast<char*>(slot + slot_block(D, b) + (4 * ta + tb + k) * 256) + uint32_t(16 * lane));
   };
   // the sums of head e to this work-group's slot for it; all threads call
   auto flush = [&](int e) {
@@ -625,7 +627,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
 #pragma unroll
       for (int t = 1; t < H; ++t) *place(slot, chunks + t - 1, k) = sum_h[t - 1][k];
     }
-    float* tail = slot + slot_block(a.D, blocks);
+    float* tail = slot + slot_block(D, blocks);
     // dc_t over the two wavefronts that have its value, da and dc over all
     float* const s_sum = reinterpret_cast<float*>(s_g);
     float* const s_all = s_sum + 2 * H * kR;
@@ -658,12 +660,12 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       for (; tile < stop; ++tile) empty_tile<NW, BF>(a, begin + (tile - t0) * kRows, end);
       break;
     }
-    const unsigned char* split = a.split + e * int64_t(blocks) * a.split_block;
+    const unsigned char* split = a.split + e * int64_t(blocks) * (2 * kBlockBytes);
     if (TRAIN) clear();
     // blocks of weights in LDS: one in use, the next on its way into the other
     int cur = 0;
     auto ahead = [&](int b, bool transposed) {
-      stage<NW>(split + b * a.split_block + (transposed ? kBlockBytes : 0), s_w + (cur ^ 1) * kBlockBytes);
+      stage<NW>(split + b * (2 * kBlockBytes) + (transposed ? kBlockBytes : 0), s_w + (cur ^ 1) * kBlockBytes);
     };
     auto turn = [&]() {
       landed();
@@ -671,29 +673,30 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       cur ^= 1;
     };
     __syncthreads();
+    load_vectors(a.weights + e * a.values, a.D, H, s_vec);
     cur = 1;
     ahead(0, false);
-    Row r = row_of(a, entry_of(a, begin + (tile - t0) * kRows + 16 * w + c, end));
+    Row r = row_of<BF>(a, entry_of(a, begin + (tile - t0) * kRows + 16 * w + c, end));
     f4 in[4];
-    load_x<BF>(a, r, 0, in);
+    load_x<BF>(r, D, 0, in);
     turn();
     for (bool first = true; tile < stop; ++tile, first = false) {
-      const HeadsArgs& a = again();
-      const float* const wt = a.weights + e * a.values;
       // forward: z_t of every layer and the last y stay
       Limbs x;
       f4 y[4] = {}, z[H][4];
-      column(wt + kR * a.D, z[0]);
+      column(s_vec, z[0]);
       // the next tile's rows, in time for their inputs
       const bool follows = tile + 1 < stop;
-      const int32_t entry = follows ? entry_of(a, begin + (tile + 1 - t0) * kRows + 16 * w + c, end) : -1;
+      const int32_t entry = follows ? entry_of(again(), begin + (tile + 1 - t0) * kRows + 16 * w + c, end) : -1;
       for (int ch = 0; ch < chunks; ++ch) {
         const bool more = ch + 1 < chunks;
         if (more) ahead(ch + 1, false);
         else if (H > 1) ahead(chunks, false);
         else ahead(0, true);
+#pragma unroll
+        for (int T = 0; T < 4; ++T) in[T] = ready(r, D, ch, T, in[T]);
         x.of(in);
-        if (more) load_x<BF>(a, r, ch + 1, in);
+        if (more) load_x<BF>(r, D, ch + 1, in);
         product(s_w + cur * kBlockBytes, x, z[0]);
         turn();
       }
@@ -707,7 +710,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       for (int t = 0; t < 4; ++t) activate(0, t, x);
 #pragma unroll
       for (int l = 1; l < H; ++l) {
-        column(layer(wt, a.D, l) + kR * kR, z[l]);
+        column(s_vec + l * kR, z[l]);
         ahead(chunks + (l + 1 < H ? l : l - 1), l + 1 == H);
         Limbs after;
         product(s_w + cur * kBlockBytes, x, z[l], [&](int t) {
@@ -717,12 +720,11 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         if (l + 1 < H) x = after;
         turn();
       }
-      const float* out = layer(wt, a.D, H);
       f4 u[4];
       const float d = r.entry >= 0 ? r.up * r.gate : 0.f;
       {
         float v = 0.f;
-        column(out, u);
+        column(s_vec + H * kR, u);
         f4 dy[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -738,7 +740,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         }
         v += __shfl_xor(v, 16, 64);
         v += __shfl_xor(v, 32, 64);
-        store_value(a, r, v + out[kR]);
+        store_value(again(), r, v + s_vec[(H + 1) * kR]);
       }
       // g_l = u silu'(z_l) of one tile, its limbs from two, and y_{l-1} from y_l
       // (the sigmoid again: keeping y or silu' of every layer takes 16 registers
@@ -761,7 +763,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
 #pragma unroll
       for (int l = H - 1; l > 0; --l) {
         ahead(l > 1 ? chunks + l - 2 : 0, true);
-        if (TRAIN && l == 1) load_x<BF>(a, r, 0, in);   // for the chunks below
+        if (TRAIN && l == 1) load_x<BF>(r, D, 0, in);   // for the chunks below
         if (TRAIN) put_limbs(s_g, x);
         product(s_w + cur * kBlockBytes, x, u, [&](int t) {
           if (TRAIN) put_value(s_y, t, y[t]);
@@ -777,25 +779,25 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       }
       if (TRAIN) {
         put_limbs(s_g, x);
-        if (H == 1) load_x<BF>(a, r, 0, in);
+        if (H == 1) load_x<BF>(r, D, 0, in);
       }
       const Row now = r;
-      r = row_of(a, entry);
+      r = row_of<BF>(again(), entry);
       for (int ch = 0; ch < chunks; ++ch) {
         const bool more = ch + 1 < chunks;
         if (more) ahead(ch + 1, true);
         else if (follows) ahead(0, false);
         if (TRAIN) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t) put_value(s_y, t, in[t]);
+          for (int t = 0; t < 4; ++t) put_value(s_y, t, ready(now, D, ch, t, in[t]));
         }
         // the next chunk, or the next tile's first
-        if (TRAIN && more) load_x<BF>(a, now, ch + 1, in);
-        else if (!more && follows) load_x<BF>(a, r, 0, in);
-        if (a.dx) {
+        if (TRAIN && more) load_x<BF>(now, D, ch + 1, in);
+        else if (!more && follows) load_x<BF>(r, D, 0, in);
+        if (with_dx) {
           f4 dx[4] = {};
           product(s_w + cur * kBlockBytes, x, dx);
-          store_dx<BF>(a, now, ch, dx);
+          store_dx(now, BF && one, D, ch, dx);
         }
         if (TRAIN) {
           __syncthreads();
@@ -865,6 +867,15 @@ __global__ __launch_bounds__(256) void k_sum_slots(HeadsArgs a) {
   a.dweights[e * a.values + dst] = v;
 }
 
+// Rows of fewer than four values to rows of four, so that every load of four
+// values is one that may be made.
+template <typename T>
+__global__ __launch_bounds__(256) void k_pad(const T* x, int64_t n, int64_t stride, int D, T* to) {
+  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const int c = int(at & 3);
+  if (at < 4 * n) to[at] = c < D ? x[(at >> 2) * stride + c] : T(0);
+}
+
 // Rows with several entries: their energies and gradients added up in order.
 __global__ __launch_bounds__(256) void k_sum_entries(HeadsArgs a) {
   const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
@@ -930,6 +941,7 @@ size_t heads_plan(HeadsArgs* a, int n_cu) {
   if (a->dweights) b += size_t(a->blocks + a->E) * size_t(a->slot) * sizeof(float);
   if (a->K > 1 && a->energy) b += size_t(a->m) * sizeof(float);
   if (a->K > 1 && a->dx) b += size_t(a->m) * size_t(a->D) * sizeof(float);
+  if (a->D < 4) b += size_t(a->n) * 4 * sizeof(float);
   return b;
 }
 
@@ -939,12 +951,22 @@ void heads_workspace(HeadsArgs* a, unsigned char* ws) {
   float* at = reinterpret_cast<float*>(ws);
   if (a->dweights) a->slots = at, at += int64_t(a->blocks + a->E) * a->slot;
   if (a->K > 1 && a->dx) a->entry_dx = at, at += a->m * a->D;
-  if (a->K > 1 && a->energy) a->entry_energy = at;
+  if (a->K > 1 && a->energy) a->entry_energy = at, at += a->m;
+  if (a->D < 4) a->padded = at;
 }
 
-hipError_t launch_heads(const HeadsArgs& a, hipStream_t s) {
+hipError_t launch_heads(const HeadsArgs& given, hipStream_t s) {
   hipError_t e = hipSuccess;
+  HeadsArgs a = given;
   if (a.m > 0) {
+    if (a.D < 4) {
+      const unsigned blocks = unsigned((4 * a.n + 255) / 256);
+      if (a.bf16) k_pad<<<blocks, 256, 0, s>>>(static_cast<const uint16_t*>(a.x), a.n, a.stride, a.D, static_cast<uint16_t*>(a.padded));
+      else k_pad<<<blocks, 256, 0, s>>>(static_cast<const float*>(a.x), a.n, a.stride, a.D, static_cast<float*>(a.padded));
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      a.x = a.padded;
+      a.stride = 4;
+    }
     k_split<<<dim3((a.D + 63) / 64 + a.H - 1, a.E), 256, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (!a.dx && !a.dweights) {

@@ -103,6 +103,7 @@ struct HeadsArgs {
   float* dgates;              // [m] or null
   float* entry_energy;        // [m], with several entries a row
   float* entry_dx;            // [m][D], with several entries a row and dx
+  void* padded;               // [n][4], x with fewer than four inputs
   unsigned char* split;       // the heads' matrices in limbs, split_block bytes a block
   int64_t split_block;
   float* slots;               // [blocks + E][slot] sums of a work-group for a head
