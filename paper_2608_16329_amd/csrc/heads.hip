@@ -235,9 +235,17 @@ __global__ __launch_bounds__(256) void k_split(HeadsArgs a) {
   const float* w = a.weights + e * a.values;
   const float* src = b < chunks ? w + 64 * b : w + (kR * a.D + kR + (b - chunks) * (kR * kR + kR));
   const int ld = b < chunks ? a.D : kR, cols = b < chunks ? a.D - 64 * b : kR;
-  for (int at = threadIdx.x; at < kR * kR; at += 256) {
-    const int r = at / kR, c = at % kR;
-    m[r][c] = c < cols ? src[r * ld + c] : 0.f;
+  // (the loads first, then what is stored of them)
+  float v[kR * kR / 256];
+#pragma unroll
+  for (int k = 0; k < kR * kR / 256; ++k) {
+    const int r = (256 * k + threadIdx.x) / kR, c = threadIdx.x % kR;
+    v[k] = src[r * ld + (c < cols ? c : 0)];
+  }
+#pragma unroll
+  for (int k = 0; k < kR * kR / 256; ++k) {
+    const int r = (256 * k + threadIdx.x) / kR, c = threadIdx.x % kR;
+    m[r][c] = c < cols ? v[k] : 0.f;
   }
   __syncthreads();
   unsigned char* dst = a.split + (e * int64_t(chunks + a.H - 1) + b) * a.split_block;
@@ -861,8 +869,16 @@ __global__ __launch_bounds__(256) void k_sum_slots(HeadsArgs a) {
       return b;
     };
     const int b0 = group_of(lo), b1 = group_of(hi - 1);
-    for (int b = b0; b <= b1; ++b)
-      if (share(tiles, b, a.blocks) < share(tiles, b + 1, a.blocks)) v += a.slots[(int64_t(b) + e) * a.slot + at];
+    const float* slot = a.slots + (int64_t(b0) + e) * a.slot + at;
+    // (all of them have tiles of the head where there are no more work-groups
+    // than tiles)
+    if (a.blocks <= tiles) {
+#pragma unroll 8
+      for (int b = b0; b <= b1; ++b, slot += a.slot) v += *slot;
+    } else {
+      for (int b = b0; b <= b1; ++b, slot += a.slot)
+        if (share(tiles, b, a.blocks) < share(tiles, b + 1, a.blocks)) v += *slot;
+    }
   }
   a.dweights[e * a.values + dst] = v;
 }
@@ -899,10 +915,6 @@ __global__ __launch_bounds__(256) void k_sum_entries(HeadsArgs a) {
   }
 }
 
-// Wavefronts of a work-group: eight, two a SIMD; four where y and silu' of more
-// than four layers and the sums of their gradients need all of a SIMD's registers.
-int heads_waves(const HeadsArgs& a) { return a.dweights && a.H <= 4 ? 8 : 4; }
-
 template <int H, int NW, bool TRAIN, bool BF>
 hipError_t gradient_of(const HeadsArgs& a, hipStream_t s) {
   constexpr size_t lds = 2 * kBlockBytes + (TRAIN ? 2 * 3 * 16 * NW * kRowBytes : 0);
@@ -915,12 +927,19 @@ hipError_t gradient_of(const HeadsArgs& a, hipStream_t s) {
 
 template <bool TRAIN, bool BF>
 hipError_t gradient_by_layers(const HeadsArgs& a, hipStream_t s) {
-  constexpr int kShallow = TRAIN ? 8 : 4;
+  if (TRAIN && a.waves == 8) {
+    switch (a.H) {
+      case 1: return gradient_of<1, 8, true, BF>(a, s);
+      case 2: return gradient_of<2, 8, true, BF>(a, s);
+      case 3: return gradient_of<3, 8, true, BF>(a, s);
+      default: return gradient_of<4, 8, true, BF>(a, s);
+    }
+  }
   switch (a.H) {
-    case 1: return gradient_of<1, kShallow, TRAIN, BF>(a, s);
-    case 2: return gradient_of<2, kShallow, TRAIN, BF>(a, s);
-    case 3: return gradient_of<3, kShallow, TRAIN, BF>(a, s);
-    case 4: return gradient_of<4, kShallow, TRAIN, BF>(a, s);
+    case 1: return gradient_of<1, 4, TRAIN, BF>(a, s);
+    case 2: return gradient_of<2, 4, TRAIN, BF>(a, s);
+    case 3: return gradient_of<3, 4, TRAIN, BF>(a, s);
+    case 4: return gradient_of<4, 4, TRAIN, BF>(a, s);
     case 5: return gradient_of<5, 4, TRAIN, BF>(a, s);
     case 6: return gradient_of<6, 4, TRAIN, BF>(a, s);
     case 7: return gradient_of<7, 4, TRAIN, BF>(a, s);
@@ -930,8 +949,14 @@ hipError_t gradient_by_layers(const HeadsArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// Wavefronts of a work-group, 16 rows each.  For weight gradients eight, two a
+// SIMD, where there are tiles of 128 rows for all CUs; four where there are
+// not, or where z of more than four layers and the sums of their gradients need
+// all of a SIMD's registers.  Without weight gradients four, and two work-groups
+// a CU that need not wait for each other.
 size_t heads_plan(HeadsArgs* a, int n_cu) {
-  const int rows = 16 * heads_waves(*a);
+  a->waves = a->dweights && a->H <= 4 && a->m / 128 + a->E > n_cu ? 8 : 4;
+  const int rows = 16 * a->waves;
   // at most one more tile than full ones for each head and for entries without
   const int64_t tiles = a->m / rows + a->E + 1;
   a->blocks = int(std::min<int64_t>(tiles, a->dweights ? n_cu : 2 * n_cu));
@@ -982,7 +1007,7 @@ hipError_t launch_heads(const HeadsArgs& given, hipStream_t s) {
   }
   if (a.dweights) {
     const dim3 g((unsigned)((a.slot + 255) / 256), (unsigned)a.E);
-    if (heads_waves(a) == 8) k_sum_slots<8><<<g, 256, 0, s>>>(a);
+    if (a.waves == 8) k_sum_slots<8><<<g, 256, 0, s>>>(a);
     else k_sum_slots<4><<<g, 256, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }

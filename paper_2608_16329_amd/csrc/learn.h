@@ -90,6 +90,7 @@ struct HeadsArgs {
   int E, D, H, K;
   bool bf16;                  // x and dx
   int blocks;                 // work-groups that share the tiles
+  int waves;                  // wavefronts of one, 16 rows of a tile each
   int64_t values;             // of one head
   const void* x;
   const float* weights;       // [E][values]
@@ -109,7 +110,7 @@ struct HeadsArgs {
   float* slots;               // [blocks + E][slot] sums of a work-group for a head
   int64_t slot;
 };
-// Sets blocks, split_block and slot; the workspace in bytes, which
+// Sets waves, blocks, split_block and slot; the workspace in bytes, which
 // heads_workspace divides.
 size_t heads_plan(HeadsArgs* a, int n_cu);
 void heads_workspace(HeadsArgs* a, unsigned char* ws);

@@ -374,6 +374,7 @@ int route_lanes(int E) {
 constexpr int kGroupWaves = 4;
 constexpr int64_t kGroupOne = 8192;      // entries one work-group sorts by itself
 constexpr int kGroupOneWaves = 16;
+constexpr int kScanThreads = 1024;
 
 __device__ __forceinline__ int group_key(int32_t id, int E) { return id >= 0 && id < E ? id : E; }
 
@@ -387,21 +388,58 @@ __device__ __forceinline__ uint64_t peers_of(int key, int bits, bool on) {
   return p;
 }
 
+constexpr int kAhead = 8;                // rounds of 64 entries loaded before the first is used
+
+__device__ __forceinline__ void load_ids(const int32_t* __restrict__ experts, int64_t i0, int64_t hi, int32_t id[kAhead]) {
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int64_t i = i0 + 64 * k + (threadIdx.x & 63);
+    id[k] = experts[i < hi ? i : hi - 1];
+  }
+}
+
 // Entries [lo, hi) placed in order by one wavefront from the running places in
 // pos[key].
 __device__ __forceinline__ void place(const int32_t* __restrict__ experts, int64_t lo, int64_t hi, int E, int bits,
                                       volatile int32_t* pos, int32_t* __restrict__ order) {
   const int lane = threadIdx.x & 63;
-  for (int64_t i = lo; i < hi; i += 64) {
-    const bool on = i + lane < hi;
-    const int key = on ? group_key(experts[i + lane], E) : 0;
-    const uint64_t peers = peers_of(key, bits, on);
-    const int rank = __popcll(peers & ((uint64_t(1) << lane) - 1));
-    const int at = on ? pos[key] : 0;
-    __builtin_amdgcn_wave_barrier();
-    if (on && rank == 0) pos[key] = at + __popcll(peers);
-    __builtin_amdgcn_wave_barrier();
-    if (on) order[at + rank] = int32_t(i + lane);
+  for (int64_t i0 = lo; i0 < hi; i0 += 64 * kAhead) {
+    int32_t id[kAhead];
+    load_ids(experts, i0, hi, id);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i0 + 64 * k >= hi) break;
+      const int64_t i = i0 + 64 * k + lane;
+      const bool on = i < hi;
+      const int key = on ? group_key(id[k], E) : 0;
+      const uint64_t peers = peers_of(key, bits, on);
+      const int rank = __popcll(peers & ((uint64_t(1) << lane) - 1));
+      const int at = on ? pos[key] : 0;
+      __builtin_amdgcn_wave_barrier();
+      if (on && rank == 0) pos[key] = at + __popcll(peers);
+      __builtin_amdgcn_wave_barrier();
+      if (on) order[at + rank] = int32_t(i);
+    }
+  }
+}
+
+// Entries [lo, hi) counted into cnt[key] by one wavefront: a key's lanes by
+// the one that is first among them.
+__device__ __forceinline__ void count(const int32_t* __restrict__ experts, int64_t lo, int64_t hi, int E, int bits,
+                                      volatile int32_t* cnt) {
+  const int lane = threadIdx.x & 63;
+  for (int64_t i0 = lo; i0 < hi; i0 += 64 * kAhead) {
+    int32_t id[kAhead];
+    load_ids(experts, i0, hi, id);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i0 + 64 * k >= hi) break;
+      const bool on = i0 + 64 * k + lane < hi;
+      const int key = on ? group_key(id[k], E) : 0;
+      const uint64_t peers = peers_of(key, bits, on);
+      if (on && (peers & ((uint64_t(1) << lane) - 1)) == 0) cnt[key] = cnt[key] + __popcll(peers);
+      __builtin_amdgcn_wave_barrier();
+    }
   }
 }
 
@@ -415,7 +453,7 @@ __global__ __launch_bounds__(kGroupOneWaves * 64) void k_group_one(const int32_t
   __syncthreads();
   const int64_t chunk = (m + kGroupOneWaves * 64 - 1) / (kGroupOneWaves * 64) * 64;
   const int64_t lo = w * chunk < m ? w * chunk : m, hi = lo + chunk < m ? lo + chunk : m;
-  for (int64_t i = lo + lane; i < hi; i += 64) atomicAdd(&pos[w][group_key(experts[i], E)], 1);
+  count(experts, lo, hi, E, bits, pos[w]);
   __syncthreads();
   if (tid <= E) {
     int t = 0;
@@ -449,7 +487,7 @@ __global__ __launch_bounds__(kGroupOneWaves * 64) void k_group_one(const int32_t
 }
 
 // Many: counts of each wavefront's chunk, hist[key][chunk].
-__global__ __launch_bounds__(kGroupWaves * 64) void k_group_count(const int32_t* experts, int64_t m, int E,
+__global__ __launch_bounds__(kGroupWaves * 64) void k_group_count(const int32_t* experts, int64_t m, int E, int bits,
                                                                   int64_t chunk, int chunks, int32_t* hist) {
   __shared__ int32_t cnt[kGroupWaves][kMaxExperts + 1];
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -457,19 +495,19 @@ __global__ __launch_bounds__(kGroupWaves * 64) void k_group_count(const int32_t*
   for (int e = lane; e <= E; e += 64) cnt[w][e] = 0;
   __syncthreads();
   const int64_t lo = c * chunk < m ? c * chunk : m, hi = lo + chunk < m ? lo + chunk : m;
-  for (int64_t i = lo + lane; i < hi; i += 64) atomicAdd(&cnt[w][group_key(experts[i], E)], 1);
+  count(experts, lo, hi, E, bits, cnt[w]);
   __syncthreads();
   if (c < chunks)
     for (int e = lane; e <= E; e += 64) hist[int64_t(e) * chunks + c] = cnt[w][e];
 }
 
 // One work-group per key: its chunks' counts to places within the key.
-__global__ __launch_bounds__(256) void k_group_scan(int32_t* hist, int chunks, int32_t* total) {
-  __shared__ int32_t part[4];
+__global__ __launch_bounds__(kScanThreads) void k_group_scan(int32_t* hist, int chunks, int32_t* total) {
+  __shared__ int32_t part[kScanThreads / 64];
   int32_t* row = hist + int64_t(blockIdx.x) * chunks;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   int run = 0;
-  for (int c0 = 0; c0 < chunks; c0 += 256) {
+  for (int c0 = 0; c0 < chunks; c0 += kScanThreads) {
     const int c = c0 + threadIdx.x;
     const int n = c < chunks ? row[c] : 0;
     int v = n;
@@ -480,10 +518,14 @@ __global__ __launch_bounds__(256) void k_group_scan(int32_t* hist, int chunks, i
     }
     if (lane == 63) part[w] = v;
     __syncthreads();
-    int before = run;
-    for (int u = 0; u < w; ++u) before += part[u];
+    int before = run, all = 0;
+#pragma unroll
+    for (int u = 0; u < kScanThreads / 64; ++u) {
+      before += u < w ? part[u] : 0;
+      all += part[u];
+    }
     if (c < chunks) row[c] = before + v - n;
-    run += part[0] + part[1] + part[2] + part[3];
+    run += all;
     __syncthreads();
   }
   if (threadIdx.x == 0) total[blockIdx.x] = run;
@@ -523,8 +565,9 @@ __global__ __launch_bounds__(kGroupWaves * 64) void k_group_place(const int32_t*
   if (c < chunks) place(experts, lo, hi, E, bits, pos[w], order);
 }
 
-// A wavefront's chunk: 1,024 entries, more where there would be over 4,096 chunks.
-int64_t group_chunk(int64_t m) { return std::max<int64_t>(1024, (m + 4096 * 64 - 1) / (4096 * 64) * 64); }
+// A wavefront's chunk: 256 entries, more where there would be over 2,048 chunks
+// (1,048,576 entries: 22 us with 2,048 chunks, 24 with 1,024).
+int64_t group_chunk(int64_t m) { return std::max<int64_t>(256, (m + 2048 * 64 - 1) / (2048 * 64) * 64); }
 
 template <bool BF>
 hipError_t route_of(const RouteArgs& a, int blocks, hipStream_t s) {
@@ -595,8 +638,8 @@ hipError_t launch_group(const int32_t* experts, int64_t m, int E, int32_t* offse
   const int blocks = (chunks + kGroupWaves - 1) / kGroupWaves;
   int32_t* hist = static_cast<int32_t*>(ws);
   int32_t* total = hist + size_t(E + 1) * size_t(chunks);
-  k_group_count<<<blocks, kGroupWaves * 64, 0, s>>>(experts, m, E, chunk, chunks, hist);
-  k_group_scan<<<E + 1, 256, 0, s>>>(hist, chunks, total);
+  k_group_count<<<blocks, kGroupWaves * 64, 0, s>>>(experts, m, E, bits, chunk, chunks, hist);
+  k_group_scan<<<E + 1, kScanThreads, 0, s>>>(hist, chunks, total);
   k_group_place<<<blocks, kGroupWaves * 64, 0, s>>>(experts, m, E, bits, chunk, chunks, hist, total, offsets, order);
   return hipGetLastError();
 }
