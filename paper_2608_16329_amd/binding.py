@@ -75,6 +75,12 @@ class mlip_adamw_tensor(ctypes.Structure):
                 ("decay", ctypes.c_int32)]
 
 
+# the same as a NumPy type: thousands of tensors are filled in by columns
+ADAMW_TENSOR = np.dtype([("param_dev", np.uint64), ("into_dev", np.uint64), ("grad_dev", np.uint64), ("n", np.int64),
+                         ("param_dtype", np.int32), ("grad_dtype", np.int32), ("decay", np.int32)], align=True)
+assert ADAMW_TENSOR.itemsize == ctypes.sizeof(mlip_adamw_tensor)
+
+
 class mlip_adamw_params(ctypes.Structure):
     _fields_ = [("step", ctypes.c_int64), ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
                 ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
@@ -341,10 +347,11 @@ def _check_adamw(plan, status: int):
 
 
 def mlip_adamw_create(tensors, state_bits: int, hip_stream: int = 0) -> int:
-    """tensors: list of mlip_adamw_tensor."""
+    """tensors: NumPy array of ADAMW_TENSOR."""
     plan = ctypes.c_void_p()
-    array = (mlip_adamw_tensor * max(len(tensors), 1))(*tensors)
-    _check_adamw(None, _lib.mlip_adamw_create(array, len(tensors), state_bits, hip_stream or None, ctypes.byref(plan)))
+    t = np.ascontiguousarray(tensors, dtype=ADAMW_TENSOR)
+    _check_adamw(None, _lib.mlip_adamw_create(t.ctypes.data_as(ctypes.POINTER(mlip_adamw_tensor)), len(t), state_bits,
+                                              hip_stream or None, ctypes.byref(plan)))
     return plan.value
 
 

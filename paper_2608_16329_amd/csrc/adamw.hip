@@ -89,20 +89,18 @@ __device__ __forceinline__ float update(const Step& s, float keep, float p, floa
   return p * keep - s.lr1 * (m / (sqrtf(v) * s.bc2 + s.eps));
 }
 
-// A piece is up to kAdamPiece elements of a tensor; a wavefront takes 256 of
-// them at a time, four a lane: a block of 8-bit moments.
+// A work-group takes a piece, a wavefront 256 elements of it, four a lane: a
+// block of 8-bit moments.
 template <bool B8>
 __global__ __launch_bounds__(kThreads) void k_adamw(AdamArgs a, Step s) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = 256 * w + 4 * lane;
   for (int64_t piece = blockIdx.x; piece < a.pieces; piece += gridDim.x) {
-    const AdamPiece pc = a.piece[piece];
-    const AdamTensor t = a.tensor[pc.tensor];
+    const AdamPiece t = a.piece[piece];
     const float keep = t.decay ? s.keep : 1.f;
     const void* const from = a.reverse ? t.into : t.param;
     void* const to = a.reverse ? t.param : t.into;
-    for (int64_t i0 = pc.from + 256 * w; i0 < pc.to; i0 += 256 * (kThreads / 64)) {
-      const int64_t i = i0 + 4 * lane;
-      const int left = int(pc.to - i < 4 ? pc.to - i : 4);
+    if (256 * w < t.n) {
+      const int left = min(t.n - i, 4);
       float p[4], g[4], m[4], v[4];
       load4(from, t.param_bf16, i, left, p);
       load4(t.grad, t.grad_bf16, i, left, g);
@@ -114,7 +112,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw(AdamArgs a, Step s) {
         store4(a.new_m, false, t.at + i, left, m);
         store4(a.new_v, false, t.at + i, left, v);
       } else {
-        const int64_t block = t.block + i0 / 256;
+        const int64_t block = t.block + w;
         const uint8_t* mc = static_cast<const uint8_t*>(a.m) + t.at + i;
         const uint8_t* vc = static_cast<const uint8_t*>(a.v) + t.at + i;
         B4 cm{}, cv{};
@@ -163,13 +161,12 @@ __global__ __launch_bounds__(kThreads) void k_adamw(AdamArgs a, Step s) {
 
 // The values that 8-bit moments stand for.
 __global__ __launch_bounds__(kThreads) void k_moments(AdamArgs a, float* m_out, float* v_out) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = 256 * w + 4 * lane;
   for (int64_t piece = blockIdx.x; piece < a.pieces; piece += gridDim.x) {
-    const AdamPiece pc = a.piece[piece];
-    const AdamTensor t = a.tensor[pc.tensor];
-    for (int64_t i0 = pc.from + 256 * w; i0 < pc.to; i0 += 256 * (kThreads / 64)) {
-      const int64_t i = i0 + 4 * lane, block = t.block + i0 / 256;
-      const int left = int(pc.to - i < 4 ? pc.to - i : 4);
+    const AdamPiece t = a.piece[piece];
+    if (256 * w < t.n) {
+      const int left = min(t.n - i, 4);
+      const int64_t block = t.block + w;
       const int em = int(a.m_exp[block]) - 127, ev = int(a.v_exp[block]) - 127;
       const uint8_t* mc = static_cast<const uint8_t*>(a.m) + t.at + i;
       const uint8_t* vc = static_cast<const uint8_t*>(a.v) + t.at + i;

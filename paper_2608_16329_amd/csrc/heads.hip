@@ -140,8 +140,8 @@ __device__ void tile_table(const HeadsArgs& a, int rows, int32_t* first, int32_t
   __syncthreads();
 }
 
-// First tile of work-group b of `blocks` that share `tiles`.
-__device__ __forceinline__ int share(int64_t tiles, int64_t b, int blocks) { return int(tiles * b / blocks); }
+// First tile of work-group b of `groups` that share `tiles`, groups <= tiles.
+__device__ __forceinline__ int share(int64_t tiles, int64_t b, int groups) { return int(tiles * b / groups); }
 
 __device__ __forceinline__ f4 vec4(const float* p) {
   return *reinterpret_cast<const F4*>(p);
@@ -419,11 +419,12 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) float s_vec[vectors(kMaxHeadLayers)];
   tile_table(a, kRows, s_first, s_entry);
   const int lane = threadIdx.x & 63, w = uni(threadIdx.x >> 6);
-  const int tiles = uni(s_first[a.E + 1]);
-  const int t_end = share(tiles, blockIdx.x + 1, a.blocks);
+  const int tiles = uni(s_first[a.E + 1]), groups = min(a.blocks, tiles);
+  if (int(blockIdx.x) >= groups) return;
+  const int t_end = share(tiles, blockIdx.x + 1, groups);
   const int chunks = (a.D + 63) / 64, blocks = chunks + a.H - 1;
   int e = 0;
-  for (int tile = share(tiles, blockIdx.x, a.blocks); tile < t_end;) {
+  for (int tile = share(tiles, blockIdx.x, groups); tile < t_end;) {
     while (tile >= uni(s_first[e + 1])) ++e;
     const int stop = min(t_end, uni(s_first[e + 1]));
     const int64_t begin = uni(s_entry[e]), end = uni(s_entry[e + 1]), t0 = uni(s_first[e]);
@@ -532,8 +533,9 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
   tile_table(a, kRows, s_first, s_entry);
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = uni(tid >> 6);
-  const int tiles = uni(s_first[a.E + 1]);
-  const int t_begin = share(tiles, blockIdx.x, a.blocks), t_end = share(tiles, blockIdx.x + 1, a.blocks);
+  const int tiles = uni(s_first[a.E + 1]), groups = min(a.blocks, tiles);
+  if (int(blockIdx.x) >= groups) return;
+  const int t_begin = share(tiles, blockIdx.x, groups), t_end = share(tiles, blockIdx.x + 1, groups);
   const int D = a.D, chunks = (D + 63) / 64, blocks = chunks + H - 1;
   const bool one = a.K == 1, with_dx = a.dx != nullptr;
   // the wavefront's tiles of a block: outputs 16 ta .., inputs 16 (tb + k) ..
@@ -862,23 +864,17 @@ __global__ __launch_bounds__(256) void k_sum_slots(HeadsArgs a) {
   float v = 0.f;
   if (lo < hi) {
     // work-group of a tile: the last whose share starts at or before it
+    const int groups = min(a.blocks, tiles);
     auto group_of = [&](int tile) {
-      int b = int(int64_t(tile) * a.blocks / tiles);
-      while (b + 1 < a.blocks && share(tiles, b + 1, a.blocks) <= tile) ++b;
-      while (share(tiles, b, a.blocks) > tile) --b;
+      int b = int(int64_t(tile) * groups / tiles);
+      while (b + 1 < groups && share(tiles, b + 1, groups) <= tile) ++b;
+      while (share(tiles, b, groups) > tile) --b;
       return b;
     };
     const int b0 = group_of(lo), b1 = group_of(hi - 1);
     const float* slot = a.slots + (int64_t(b0) + e) * a.slot + at;
-    // (all of them have tiles of the head where there are no more work-groups
-    // than tiles)
-    if (a.blocks <= tiles) {
 #pragma unroll 8
-      for (int b = b0; b <= b1; ++b, slot += a.slot) v += *slot;
-    } else {
-      for (int b = b0; b <= b1; ++b, slot += a.slot)
-        if (share(tiles, b, a.blocks) < share(tiles, b + 1, a.blocks)) v += *slot;
-    }
+    for (int b = b0; b <= b1; ++b, slot += a.slot) v += *slot;
   }
   a.dweights[e * a.values + dst] = v;
 }

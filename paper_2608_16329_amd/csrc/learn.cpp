@@ -106,8 +106,7 @@ bool state_given(const mlip_adamw* h, const mlip_adamw_state* s) {
 
 AdamArgs adam_args(const mlip_adamw* h, const mlip_adamw_state* from, const mlip_adamw_state* into) {
   AdamArgs a{};
-  a.tensor = reinterpret_cast<const AdamTensor*>(h->d_tables);
-  a.piece = reinterpret_cast<const AdamPiece*>(h->d_tables + h->tensors * sizeof(AdamTensor));
+  a.piece = h->d_pieces;
   a.pieces = h->pieces;
   a.bits = h->bits;
   a.m = from->m_dev;
@@ -272,7 +271,6 @@ mlip_status mlip_adamw_create(const mlip_adamw_tensor* tensors, int64_t n_tensor
   if (state_bits != 32 && state_bits != 8) return fail(none, MLIP_E_ARG, "state_bits must be 32 or 8");
   mlip_adamw* h = nullptr;
   try {
-    std::vector<AdamTensor> tt;
     std::vector<AdamPiece> pp;
     int64_t at = 0, block = 0, into = 0, filled = 0;
     for (int64_t k = 0; k < n_tensors; ++k) {
@@ -283,17 +281,20 @@ mlip_status mlip_adamw_create(const mlip_adamw_tensor* tensors, int64_t n_tensor
         return fail(none, MLIP_E_ARG, "unknown dtype");
       filled += t.n > 0 ? 1 : 0;   // an empty tensor may be nowhere
       into += t.n > 0 && t.into_dev ? 1 : 0;
-      AdamTensor d{};
-      d.param = t.param_dev;
-      d.into = t.into_dev ? t.into_dev : t.param_dev;
-      d.grad = t.grad_dev;
-      d.at = at;
-      d.block = block;
-      d.param_bf16 = t.param_dtype == MLIP_BF16;
-      d.grad_bf16 = t.grad_dtype == MLIP_BF16;
-      d.decay = t.decay != 0;
-      tt.push_back(d);
-      for (int64_t i = 0; i < t.n; i += kAdamPiece) pp.push_back({k, i, std::min<int64_t>(t.n, i + kAdamPiece)});
+      const int64_t size = t.param_dtype == MLIP_BF16 ? 2 : 4, grad_size = t.grad_dtype == MLIP_BF16 ? 2 : 4;
+      for (int64_t i = 0; i < t.n; i += kAdamPiece) {
+        AdamPiece p{};
+        p.param = static_cast<char*>(t.param_dev) + size * i;
+        p.into = static_cast<char*>(t.into_dev ? t.into_dev : t.param_dev) + size * i;
+        p.grad = static_cast<const char*>(t.grad_dev) + grad_size * i;
+        p.at = at + i;
+        p.block = block + i / 256;
+        p.n = int32_t(std::min<int64_t>(t.n - i, kAdamPiece));
+        p.param_bf16 = t.param_dtype == MLIP_BF16;
+        p.grad_bf16 = t.grad_dtype == MLIP_BF16;
+        p.decay = t.decay != 0;
+        pp.push_back(p);
+      }
       at += t.n;
       block += (t.n + 255) / 256;
     }
@@ -305,8 +306,6 @@ mlip_status mlip_adamw_create(const mlip_adamw_tensor* tensors, int64_t n_tensor
     h->elements = at;
     h->blocks = block;
     h->pieces = int64_t(pp.size());
-    h->tensors = tt.size();
-    h->bytes = tt.size() * sizeof(AdamTensor) + pp.size() * sizeof(AdamPiece);
     int device = 0;
     if (hipGetDevice(&device) != hipSuccess ||
         hipDeviceGetAttribute(&h->n_cu, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) {
@@ -314,17 +313,16 @@ mlip_status mlip_adamw_create(const mlip_adamw_tensor* tensors, int64_t n_tensor
       delete h;
       return fail(none, MLIP_E_HIP, "no current HIP device");
     }
-    if (hipMalloc(reinterpret_cast<void**>(&h->d_tables), h->bytes) != hipSuccess) {
+    const size_t bytes = std::max<size_t>(1, pp.size()) * sizeof(AdamPiece);
+    if (hipMalloc(reinterpret_cast<void**>(&h->d_pieces), bytes) != hipSuccess) {
       (void)hipGetLastError();
       delete h;
-      return fail(none, MLIP_E_OOM, "device allocation failed: tables");
+      return fail(none, MLIP_E_OOM, "device allocation failed: table of pieces");
     }
-    hipError_t e = hipMemcpy(h->d_tables, tt.data(), tt.size() * sizeof(AdamTensor), hipMemcpyHostToDevice);
-    if (e == hipSuccess && !pp.empty())
-      e = hipMemcpy(h->d_tables + tt.size() * sizeof(AdamTensor), pp.data(), pp.size() * sizeof(AdamPiece),
-                    hipMemcpyHostToDevice);
+    const hipError_t e = pp.empty() ? hipSuccess
+                                    : hipMemcpy(h->d_pieces, pp.data(), pp.size() * sizeof(AdamPiece), hipMemcpyHostToDevice);
     if (e != hipSuccess) {
-      (void)hipFree(h->d_tables);
+      (void)hipFree(h->d_pieces);
       delete h;
       return fail_hip(none, e);
     }
@@ -348,7 +346,7 @@ mlip_status mlip_adamw_state_count(const mlip_adamw* plan, int64_t* elements, in
 void mlip_adamw_destroy(mlip_adamw* plan) {
   if (!plan) return;
   (void)hipStreamSynchronize(plan->stream);
-  if (plan->d_tables) (void)hipFree(plan->d_tables);
+  if (plan->d_pieces) (void)hipFree(plan->d_pieces);
   (void)hipGetLastError();
   delete plan;
 }

@@ -12,18 +12,17 @@
 
 namespace mlip {
 
-// A tensor of an AdamW plan and a piece of one, as the kernels read them.
-constexpr int kAdamPiece = 2048;   // a multiple of 256: pieces start where blocks of 8-bit moments do
-struct AdamTensor {
-  void* param;
+// A piece of a tensor of an AdamW plan, as the kernels read it: up to
+// kAdamPiece elements, 256 a wavefront, which are a block of 8-bit moments.
+constexpr int kAdamPiece = 1024;
+struct AdamPiece {
+  void* param;                // at the piece's first element
   void* into;
   const void* grad;
-  int64_t at;                 // first element among the moments
-  int64_t block;              // first block of 8-bit moments
-  int32_t param_bf16, grad_bf16, decay, pad;
-};
-struct AdamPiece {
-  int64_t tensor, from, to;
+  int64_t at;                 // its first element among the moments
+  int64_t block;              // its first block of 8-bit moments
+  int32_t n;
+  uint8_t param_bf16, grad_bf16, decay, pad;
 };
 
 }  // namespace mlip
@@ -44,8 +43,7 @@ struct mlip_adamw {
   bool into = false;          // the plan has a second set of parameters
   int64_t elements = 0, blocks = 0, pieces = 0;
   std::string err;
-  unsigned char* d_tables = nullptr;   // AdamTensor [tensors], then AdamPiece [pieces]
-  size_t tensors = 0, bytes = 0;
+  mlip::AdamPiece* d_pieces = nullptr;
 };
 
 namespace mlip {
@@ -118,7 +116,6 @@ hipError_t launch_heads(const HeadsArgs& a, hipStream_t s);
 
 // Arguments of the AdamW kernels.
 struct AdamArgs {
-  const AdamTensor* tensor;
   const AdamPiece* piece;
   int64_t pieces;
   int bits;

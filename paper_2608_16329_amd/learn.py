@@ -8,6 +8,8 @@ from __future__ import annotations
 
 from typing import Optional
 
+import numpy as np
+
 from . import binding as b
 
 _GATES = {"chosen": b.MLIP_GATES_CHOSEN, "all": b.MLIP_GATES_ALL}
@@ -213,22 +215,29 @@ class AdamW(_OnStream):
         self._bind(stream)
         t = self.torch
         params, grads = list(params), list(grads)
-        into = list(into) if into is not None else [None] * len(params)
+        into = None if into is None else list(into)
         decay = [p.dim() >= 2 for p in params] if decay is None else list(decay)
-        _need(len(params) == len(grads) == len(into) == len(decay), "params, grads, into and decay differ in length")
+        _need(len(params) == len(grads) == len(decay) and len(params) == len(into if into is not None else params),
+              "params, grads, into and decay differ in length")
         _need(bits in (8, 32), f"bits is {bits}, not 32 or 8")
-        table = []
-        for k, (p, g, q, d) in enumerate(zip(params, grads, into, decay)):
-            for v, name in ((p, "params"), (g, "grads")):
-                _need(v.dtype in self._dtypes, f"{name}[{k}] is {v.dtype}, not float32 or bfloat16")
-            self._dense(p, f"params[{k}]", p.dtype, *p.shape)
-            self._dense(g, f"grads[{k}]", g.dtype, *p.shape)
-            if q is not None:
-                self._dense(q, f"into[{k}]", p.dtype, *p.shape)
-            table.append(b.mlip_adamw_tensor(_ptr(p), _ptr(q), _ptr(g), p.numel(), self._dtypes[p.dtype],
-                                             self._dtypes[g.dtype], int(bool(d))))
+        for k, (p, g) in enumerate(zip(params, grads)):
+            if p.dtype not in self._dtypes or g.dtype not in self._dtypes:
+                _need(p.dtype in self._dtypes, f"params[{k}] is {p.dtype}, not float32 or bfloat16")
+                _need(False, f"grads[{k}] is {g.dtype}, not float32 or bfloat16")
+            self._dense(p, "a tensor of params", p.dtype, *p.shape)
+            self._dense(g, "a tensor of grads", g.dtype, *p.shape)
+        for p, q in zip(params, into or []):
+            self._dense(q, "a tensor of into", p.dtype, *p.shape)
+        table = np.zeros(len(params), b.ADAMW_TENSOR)
+        table["param_dev"] = [p.data_ptr() for p in params]
+        table["into_dev"] = [q.data_ptr() for q in into] if into is not None else 0
+        table["grad_dev"] = [g.data_ptr() for g in grads]
+        table["n"] = [p.numel() for p in params]
+        table["param_dtype"] = [self._dtypes[p.dtype] for p in params]
+        table["grad_dtype"] = [self._dtypes[g.dtype] for g in grads]
+        table["decay"] = [bool(d) for d in decay]
         self._hold = (params, grads, into)
-        self.bits, self._twice, self._reverse = bits, bool(into) and into[0] is not None, False
+        self.bits, self._twice, self._reverse = bits, into is not None, False
         with t.cuda.device(self.device):
             self.plan = b.mlip_adamw_create(table, bits, self.stream.cuda_stream)
             n, blocks = b.mlip_adamw_state_count(self.plan)
