@@ -18,7 +18,9 @@
 // 2^-24 of it, which 16x16x32 bfloat16 matrix instructions add up in float32.
 // That errs no more than float32 products, and six of them take 0.43 of the
 // time of the float32 matrix instructions (2,100 against 150 TFLOP/s in a loop
-// of nothing else).  A first kernel splits the heads' matrices, in the order in
+// of nothing else).  Inputs in bfloat16 are one limb, and theirs are three products (all
+// gradients of 131,072 such rows of 128 values, two heads each: 366 us, with
+// six 415).  A first kernel splits the heads' matrices, in the order in
 // which lanes take them, for products with the matrix and with its transpose;
 // the main kernel brings them to LDS one 64x64 block at a time, the next block
 // on its way while one is used.
@@ -29,6 +31,7 @@
 // tiles of a head, which are written once and added up in order by a third
 // kernel.
 #include <algorithm>
+#include <type_traits>
 
 #include "learn.h"
 #include "learn_math.h"
@@ -53,12 +56,18 @@ __device__ __forceinline__ f4 mfma(u4 a, u4 b, f4 c) {
 }
 
 // The sum of products of two numbers of three limbs, those above 2^-24 of it.
-__device__ __forceinline__ f4 mfma6(const u4 a[3], const u4 b[3], f4 c) {
+__device__ __forceinline__ f4 products(const u4 a[3], const u4 (&b)[3], f4 c) {
   c = mfma(a[2], b[0], c);
   c = mfma(a[0], b[2], c);
   c = mfma(a[1], b[1], c);
   c = mfma(a[1], b[0], c);
   c = mfma(a[0], b[1], c);
+  return mfma(a[0], b[0], c);
+}
+// The same where the second has one limb, a bfloat16, and the products are all there are.
+__device__ __forceinline__ f4 products(const u4 a[3], const u4 (&b)[1], f4 c) {
+  c = mfma(a[2], b[0], c);
+  c = mfma(a[1], b[0], c);
   return mfma(a[0], b[0], c);
 }
 
@@ -77,21 +86,33 @@ __device__ __forceinline__ void split4(const f4 v, u2 limb[3]) {
   }
 }
 
+// Four bfloat16 are one limb as they are.
+__device__ __forceinline__ void split4(const u2 v, u2 limb[1]) { limb[0] = v; }
+
 // 64 values of a column as a product's second operand: step s, limb k.
+template <int N>
 struct Limbs {
-  u4 v[2][3];
-  __device__ __forceinline__ void step(int s, const f4 a, const f4 b) {
-    u2 lo[3], hi[3];
+  u4 v[2][N];
+  template <typename T>
+  __device__ __forceinline__ void step(int s, const T a, const T b) {
+    u2 lo[N], hi[N];
     split4(a, lo);
     split4(b, hi);
 #pragma unroll
-    for (int k = 0; k < 3; ++k) v[s][k] = u4{lo[k][0], lo[k][1], hi[k][0], hi[k][1]};
+    for (int k = 0; k < N; ++k) v[s][k] = u4{lo[k][0], lo[k][1], hi[k][0], hi[k][1]};
   }
-  __device__ __forceinline__ void of(const f4 in[4]) {
+  template <typename T>
+  __device__ __forceinline__ void of(const T in[4]) {
     step(0, in[0], in[1]);
     step(1, in[2], in[3]);
   }
 };
+// Four inputs of a row, and how many limbs they have.
+template <bool BF>
+using Input = std::conditional_t<BF, u2, f4>;
+template <bool BF>
+constexpr int kInputLimbs = BF ? 1 : 3;
+
 // Which of a block's 64 inputs value j of lane group g is in step s.
 __device__ __forceinline__ int input_of(int s, int g, int j) { return 32 * s + 16 * (j >> 2) + 4 * g + (j & 3); }
 
@@ -199,8 +220,8 @@ __device__ __forceinline__ void mixed() {
 // out += block in, one tile of 16 results after another, the next tile's
 // operands loaded before this one's products; beside(t) is work that goes with
 // the products of tile t, such as what becomes of the results of the tiles before.
-template <typename F>
-__device__ __forceinline__ void product(const unsigned char* block, const Limbs& in, f4 out[4], F beside) {
+template <int N, typename F>
+__device__ __forceinline__ void product(const unsigned char* block, const Limbs<N>& in, f4 out[4], F beside) {
   const unsigned char* p = block + here(16 * (threadIdx.x & 63));
   u4 a[2][3];   // of step 0, step 1
   auto fetch = [&](int t, int s) {
@@ -212,16 +233,17 @@ __device__ __forceinline__ void product(const unsigned char* block, const Limbs&
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     __builtin_amdgcn_sched_barrier(0);
-    f4 sum = mfma6(a[0], in.v[0], out[t]);
+    f4 sum = products(a[0], in.v[0], out[t]);
     if (t < 3) fetch(t + 1, 0);
-    out[t] = mfma6(a[1], in.v[1], sum);
+    out[t] = products(a[1], in.v[1], sum);
     if (t < 3) fetch(t + 1, 1);
     beside(t);
-    mixed<12>();
+    mixed<N == 3 ? 12 : 6>();
   }
   __builtin_amdgcn_sched_barrier(0);
 }
-__device__ __forceinline__ void product(const unsigned char* block, const Limbs& in, f4 out[4]) {
+template <int N>
+__device__ __forceinline__ void product(const unsigned char* block, const Limbs<N>& in, f4 out[4]) {
   product(block, in, out, [](int) {});
 }
 
@@ -319,34 +341,27 @@ __device__ __forceinline__ Row row_of(const HeadsArgs& a, int32_t ent) {
   }
   return r;
 }
-template <bool BF>
-__device__ __forceinline__ f4 x4(const void* p, int at) {
-  f4 f;
-  if (BF) {
-    const H4 h = *reinterpret_cast<const H4*>(static_cast<const uint16_t*>(p) + at);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = from_bf16(h[i]);
-  } else {
-    f = vec4(static_cast<const float*>(p) + at);
-  }
-  return f;
-}
-
 // Inputs 64 ch .. 64 ch + 63 of the lane's row on their way: 16 T + 4 g + i in
 // in[T][i].  Every lane loads four values that are there; ready() takes out those
 // beyond the row's end and those of lanes without a row when they are used, so
 // that loading does not wait.
 template <bool BF>
-__device__ __forceinline__ void load_x(const Row& r, int D, int ch, f4 in[4]) {
+__device__ __forceinline__ void load_x(const Row& r, int D, int ch, Input<BF> in[4]) {
   const int g = (threadIdx.x >> 4) & 3, last = max(D, 4) - 4;   // rows of fewer than four are copied to four (k_pad)
 #pragma unroll
-  for (int T = 0; T < 4; ++T) in[T] = x4<BF>(r.x, min(64 * ch + 16 * T + 4 * g, last));
+  for (int T = 0; T < 4; ++T) {
+    const int at = min(64 * ch + 16 * T + 4 * g, last);
+    if constexpr (BF) in[T] = __builtin_bit_cast(u2, *reinterpret_cast<const H4*>(reinterpret_cast<const uint16_t*>(r.x) + at));
+    else in[T] = vec4(reinterpret_cast<const float*>(r.x) + at);
+  }
+}
+// (where fewer than four are left, what was loaded are the row's last four values)
+__device__ __forceinline__ int inputs_left(const Row& r, int D, int ch, int T) {
+  return r.entry >= 0 ? D - (64 * ch + 16 * T + 4 * int((threadIdx.x >> 4) & 3)) : 0;
 }
 __device__ __forceinline__ f4 ready(const Row& r, int D, int ch, int T, f4 f) {
-  const int c = 64 * ch + 16 * T + 4 * ((threadIdx.x >> 4) & 3);
-  const int left = r.entry >= 0 ? D - c : 0;
+  const int left = inputs_left(r, D, ch, T);
   if (D & 3) {
-    // the row's last four values where fewer are left
     const int shift = D < 4 ? 0 : (left < 4 ? 4 - left : 0);
     if (shift & 1) f = f4{f[1], f[2], f[3], 0.f};
     if (shift & 2) f = f4{f[2], f[3], 0.f, 0.f};
@@ -357,6 +372,15 @@ __device__ __forceinline__ f4 ready(const Row& r, int D, int ch, int T, f4 f) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) f[i] = left > 0 ? f[i] : 0.f;
   return f;
+}
+__device__ __forceinline__ u2 ready(const Row& r, int D, int ch, int T, u2 h) {
+  const int left = inputs_left(r, D, ch, T);
+  if (D & 3) {
+    // (four values at D < 4: those beyond the row's end are zero)
+    const int shift = D < 4 || left >= 4 || left <= 0 ? 0 : 4 - left;
+    h = __builtin_bit_cast(u2, __builtin_bit_cast(uint64_t, h) >> (16 * shift));
+  }
+  return u2{left > 0 ? h[0] : 0u, left > 0 ? h[1] : 0u};
 }
 
 // d[T][i] to the gradient of the lane's row at inputs 64 ch + 16 T + 4 g + i.
@@ -439,7 +463,7 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
     load_vectors(wt, a.D, a.H, s_vec);
     stage<NW>(split, s_w);
     Row r = row_of<BF>(a, entry_of(a, begin + (tile - t0) * kRows + 16 * w + (lane & 15), end));
-    f4 in[4];
+    Input<BF> in[4];
     load_x<BF>(r, a.D, 0, in);
     landed();
     __syncthreads();
@@ -454,10 +478,11 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
       cur ^= 1;
     };
     for (; tile < stop; ++tile) {
-      Limbs x;
+      Limbs<kInputLimbs<BF>> x0;
+      Limbs<3> x;
       f4 z[4], y[4] = {};
       // y += silu(z) of one tile, and the next product's operand from two
-      auto activate = [&](int t, Limbs& next) {
+      auto activate = [&](int t, Limbs<3>& next) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[t][i] += z[t][i] * sigmoid(z[t][i]);
         if (t & 1) next.step(t >> 1, y[t - 1], y[t]);
@@ -469,9 +494,9 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
         ahead(ch);
 #pragma unroll
         for (int T = 0; T < 4; ++T) in[T] = ready(r, a.D, ch, T, in[T]);
-        x.of(in);
+        x0.of(in);
         if (ch + 1 < chunks) load_x<BF>(r, a.D, ch + 1, in);
-        product(s_w + cur * kBlockBytes, x, z);
+        product(s_w + cur * kBlockBytes, x0, z);
         turn();
       }
       Row next = r;
@@ -484,7 +509,7 @@ __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
       for (int l = 1; l < a.H; ++l) {
         ahead(chunks + l - 1);
         column(s_vec + l * kR, z);
-        Limbs after;
+        Limbs<3> after;
         product(s_w + cur * kBlockBytes, x, z, [&](int t) {
           if (t > 0) activate(t - 1, after);
         });
@@ -551,17 +576,17 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
   // and reading.
   const int put_at = (16 * w + c) * kRowBytes + 8 * (g ^ (c >> 3 << 1)) + ((c << 4) & 96);
   const int get_at = (4 * g + (c >> 2)) * kRowBytes + 8 * ((c & 3) ^ (g & 2)) + (((4 * g + (c >> 2)) << 4) & 96);
-  auto put = [&](unsigned char* to, int t, const u2 limb[3]) {
+  auto put = [&](unsigned char* to, int t, const auto& limb) {
     const int at = here(put_at) ^ (32 * t);
 #pragma unroll
-    for (int k = 0; k < 3; ++k) *reinterpret_cast<u2*>(to + k * kPlane + at) = limb[k];
+    for (int k = 0; k < int(sizeof(limb) / sizeof(u2)); ++k) *reinterpret_cast<u2*>(to + k * kPlane + at) = limb[k];
   };
   // group t of 16 values of rows 32 s .. 32 s + 31 as an operand: lane (g, c)
   // gets value c at rows 4 g + j and 16 + 4 g + j, j < 4
-  auto get = [&](const unsigned char* from, int t, int s, u4 limb[3]) {
+  auto get = [&](const unsigned char* from, int t, int s, auto& limb) {
     const int at = here(get_at) ^ (32 * t);
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < int(sizeof(limb) / sizeof(u4)); ++k) {
       u2 half[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -570,15 +595,15 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       limb[k] = u4{half[0][0], half[0][1], half[1][0], half[1][1]};
     }
   };
-  // sums of g y^T over the tile's rows into the wavefront's tiles, and (bias >=
+  // sums of g y^T (y of `limbs` limbs) over the tile's rows into the wavefront's tiles, and (bias >=
   // 0) of g into column `bias` of sum_b, for which two wavefronts with the same
-  // outputs take turns; beside(s) is
-  // work that goes with the products of the s-th quarter of the rows (half, with
-  // four wavefronts: then it is called for two quarters)
-  auto outer = [&](f4 acc[kOwn], int bias, auto beside) {
+  // outputs take turns; beside(s) is work that goes with the products of the
+  // s-th quarter of the rows (half, with four wavefronts: then it is called for
+  // two quarters)
+  auto outer = [&](auto limbs, f4 acc[kOwn], int bias, auto beside) {
 #pragma unroll
     for (int s = 0; s < NW / 2; ++s) {
-      u4 ga[3], yb[kOwn][3];
+      u4 ga[3], yb[kOwn][limbs.value];
       __builtin_amdgcn_sched_barrier(0);
       get(s_g, ta, s, ga);
 #pragma unroll
@@ -586,7 +611,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
 #pragma unroll
       for (int q = 0; q < 8 / NW; ++q) beside(8 / NW * s + q);
 #pragma unroll
-      for (int k = 0; k < kOwn; ++k) acc[k] = mfma6(ga, yb[k], acc[k]);
+      for (int k = 0; k < kOwn; ++k) acc[k] = products(ga, yb[k], acc[k]);
       if (bias >= 0 && (NW == 4 || (w & 1) == (s & 1))) {
         const uint32_t one = c == bias ? 0x3f803f80u : 0u;
         const u4 ones = {one, one, one, one};
@@ -597,7 +622,9 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
     __builtin_amdgcn_sched_barrier(0);
   };
   auto nothing = [](int) {};
-  auto put_limbs = [&](unsigned char* to, const Limbs& l) {
+  constexpr std::integral_constant<int, 3> limbs_y{};
+  constexpr std::integral_constant<int, kInputLimbs<BF>> limbs_x{};
+  auto put_limbs = [&](unsigned char* to, const Limbs<3>& l) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       u2 limb[3];
@@ -606,8 +633,8 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       put(to, t, limb);
     }
   };
-  auto put_value = [&](unsigned char* to, int t, const f4 v) {
-    u2 limb[3];
+  auto put_value = [&](unsigned char* to, int t, const auto v) {
+    u2 limb[sizeof(v) == sizeof(f4) ? 3 : 1];
     split4(v, limb);
     put(to, t, limb);
   };
@@ -687,12 +714,13 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
     cur = 1;
     ahead(0, false);
     Row r = row_of<BF>(a, entry_of(a, begin + (tile - t0) * kRows + 16 * w + c, end));
-    f4 in[4];
+    Input<BF> in[4];
     load_x<BF>(r, D, 0, in);
     turn();
     for (bool first = true; tile < stop; ++tile, first = false) {
       // forward: z_t of every layer and the last y stay
-      Limbs x;
+      Limbs<kInputLimbs<BF>> x0;
+      Limbs<3> x;
       f4 y[4] = {}, z[H][4];
       column(s_vec, z[0]);
       // the next tile's rows, in time for their inputs
@@ -705,13 +733,13 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         else ahead(0, true);
 #pragma unroll
         for (int T = 0; T < 4; ++T) in[T] = ready(r, D, ch, T, in[T]);
-        x.of(in);
+        x0.of(in);
         if (more) load_x<BF>(r, D, ch + 1, in);
-        product(s_w + cur * kBlockBytes, x, z[0]);
+        product(s_w + cur * kBlockBytes, x0, z[0]);
         turn();
       }
       // y += silu(z_l) of one tile, and the next product's operand from two
-      auto activate = [&](int l, int t, Limbs& next) {
+      auto activate = [&](int l, int t, Limbs<3>& next) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[t][i] += z[l][t][i] * sigmoid(z[l][t][i]);
         if (l + 1 < H && (t & 1)) next.step(t >> 1, y[t - 1], y[t]);
@@ -722,7 +750,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       for (int l = 1; l < H; ++l) {
         column(s_vec + l * kR, z[l]);
         ahead(chunks + (l + 1 < H ? l : l - 1), l + 1 == H);
-        Limbs after;
+        Limbs<3> after;
         product(s_w + cur * kBlockBytes, x, z[l], [&](int t) {
           if (t > 0) activate(l, t - 1, after);
         });
@@ -780,7 +808,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         });
         if (TRAIN) {
           __syncthreads();
-          outer(sum_h[l - 1], l, [&](int t) { back(l - 1, t); });
+          outer(limbs_y, sum_h[l - 1], l, [&](int t) { back(l - 1, t); });
         } else {
 #pragma unroll
           for (int t = 0; t < 4; ++t) back(l - 1, t);
@@ -811,14 +839,14 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         }
         if (TRAIN) {
           __syncthreads();
-          if (ch == 0) outer(sum_0[0], 0, nothing);
-          else if (ch == 1) outer(sum_0[1], -1, nothing);
+          if (ch == 0) outer(limbs_x, sum_0[0], 0, nothing);
+          else if (ch == 1) outer(limbs_x, sum_0[1], -1, nothing);
           else {
             float* slot = a.slots + (int64_t(blockIdx.x) + e) * a.slot;
             f4 acc[kOwn];
 #pragma unroll
             for (int j = 0; j < kOwn; ++j) acc[j] = first ? f4{0.f, 0.f, 0.f, 0.f} : *place(slot, ch, j);
-            outer(acc, -1, nothing);
+            outer(limbs_x, acc, -1, nothing);
 #pragma unroll
             for (int j = 0; j < kOwn; ++j) *place(slot, ch, j) = acc[j];
           }
