@@ -8,6 +8,7 @@
 //   dz_ie = p_ie (h_e - sum_j p_ij h_j) + w_ie (dw_ie - sum_s w_is dw_is),
 //   h_e = dloss E f_e / rows (the shares f are constants of the gradient).
 #include <algorithm>
+#include <type_traits>
 
 #include "learn.h"
 #include "learn_math.h"
@@ -53,35 +54,67 @@ __device__ __forceinline__ float row_max(float v) {
 template <int L>
 __device__ __forceinline__ int expert_of(int j, int l) { return 4 * ((j >> 2) * L + l) + (j & 3); }
 
-// Row i's logits of this lane, what the row may not use as -inf, whatever
-// stands there.
-template <int L, bool BF>
-__device__ __forceinline__ void load_row(const RouteArgs& a, int64_t i, int l, float z[kV]) {
-  bool live = i < a.n;
-  const uint8_t* ok = nullptr;
-  if (live && a.kinds) {
-    const int kind = a.kinds[i];
-    live = kind >= 0 && kind < a.n_kinds;
-    ok = a.allowed + int64_t(live ? kind : 0) * a.E;
+// What a lane has of a row, as loaded: up to 16 logits and a byte for each that
+// says whether the row may use it.  Every load is one that may be made, whatever
+// the row, so that none stands in a branch and the next row's are under way while
+// one is worked on: rows beyond the last are the last again, quads beyond a row's
+// end its last four.  unpack() puts this right.
+template <bool BF>
+struct Raw {
+  std::conditional_t<BF, H4, f4> v[kV / 4];
+  uint32_t ok[kV / 4];
+  bool live;
+};
+template <int L, bool BF, bool KINDS>
+__device__ __forceinline__ int kind_of(const RouteArgs& a, int64_t i) {
+  return KINDS ? a.kinds[i < a.n ? i : a.n - 1] : 0;
+}
+template <int L, bool BF, bool KINDS>
+__device__ __forceinline__ void load_row(const RouteArgs& a, int64_t i, int kind, int l, Raw<BF>& r) {
+  typedef std::conditional_t<BF, uint16_t, float> T;
+  typedef std::conditional_t<BF, H4, F4> Quad;
+  const bool real = !KINDS || (kind >= 0 && kind < a.n_kinds);
+  r.live = i < a.n && real;
+  const T* row = static_cast<const T*>(a.logits) + (i < a.n ? i : a.n - 1) * a.stride;
+  const uint8_t* ok = KINDS ? a.allowed + (real ? int64_t(kind) : 0) * a.E : nullptr;
+  if (L == 1 && a.E < 4) {
+    const int e1 = a.E > 1 ? 1 : 0, e2 = a.E > 2 ? 2 : 0;
+    r.v[0][0] = row[0], r.v[0][1] = row[e1], r.v[0][2] = row[e2], r.v[0][3] = T(0);
+    if (KINDS) r.ok[0] = ok[0] | uint32_t(ok[e1]) << 8 | uint32_t(ok[e2]) << 16;
+    for (int c = 1; c < kV / 4; ++c) r.v[c] = r.v[0], r.ok[c] = 0;
+    return;
   }
 #pragma unroll
   for (int c = 0; c < kV / 4; ++c) {
-    const int e = 4 * (c * L + l);
-    float t[4];
-    load4(a.logits, BF, i * a.stride + e, live ? a.E - e : 0, t);
-    // a byte for each of the four that says whether the row may use it
-    const int left = live ? a.E - e : 0;
-    uint32_t use = left >= 4 ? 0x01010101u : (left > 0 ? 0x01010101u >> (8 * (4 - left)) : 0u);
-    if (ok) {
-      if (left >= 4) {
-        use = *reinterpret_cast<const U4*>(ok + e);
-      } else {
-        use = 0;
+    const int e = 4 * (c * L + l), at = e < a.E - 4 ? e : a.E - 4;
+    r.v[c] = *reinterpret_cast<const Quad*>(row + at);
+    if (KINDS) r.ok[c] = *reinterpret_cast<const U4*>(ok + at);
+  }
+}
+// Its logits, what the row may not use as -inf, whatever stands there.
+template <int L, bool BF, bool KINDS>
+__device__ __forceinline__ void unpack(const RouteArgs& a, const Raw<BF>& r, int l, float z[kV]) {
 #pragma unroll
-        for (int q = 0; q < 3; ++q)
-          if (q < left) use |= uint32_t(ok[e + q]) << (8 * q);
-      }
+  for (int c = 0; c < kV / 4; ++c) {
+    const int left = r.live ? a.E - 4 * (c * L + l) : 0;
+    float t[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (BF) t[q] = from_bf16(r.v[c][q]);
+      else t[q] = r.v[c][q];
     }
+    uint32_t use = KINDS ? r.ok[c] : 0x01010101u;
+    if (a.E & 3) {
+      const int part = left > 0 && left < 4 ? 4 - left : 0, shift = a.E < 4 ? 0 : part;
+      if (shift & 1) t[0] = t[1], t[1] = t[2], t[2] = t[3];
+      if (shift & 2) t[0] = t[2], t[1] = t[3];
+      use = KINDS ? use >> (8 * shift) & 0xffffffffu >> (8 * part) : use >> (8 * part);
+    } else if (!KINDS) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) z[4 * c + q] = left > 0 ? t[q] : -INFINITY;
+      continue;
+    }
+    use = left > 0 ? use : 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) z[4 * c + q] = use & (255u << (8 * q)) ? t[q] : -INFINITY;
   }
@@ -101,7 +134,7 @@ __device__ __forceinline__ void write_loss(const RouteArgs& a, double entries, d
 // in turn by the grid.  Each work-group's counts and sums of p go to its own
 // place and are added up in order afterwards, so results do not depend on the
 // order of work-groups.
-template <int L, bool BF>
+template <int L, bool BF, bool KINDS>
 __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool only) {
   constexpr int kKept = (kMaxTopK + L - 1) / L;   // choices a lane keeps: lane s % L the s-th
   __shared__ int32_t s_count[kMaxExperts + 1];
@@ -115,10 +148,21 @@ __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool onl
   constexpr int kRows = kForwardThreads / L;
   const int64_t step = int64_t(gridDim.x) * kRows;
   int rows = 0;
-  for (int64_t i0 = int64_t(blockIdx.x) * kRows; i0 < a.n; i0 += step) {
+  const int64_t first = int64_t(blockIdx.x) * kRows;
+  Raw<BF> raw;
+  int kind = 0;
+  if (first < a.n) {
+    load_row<L, BF, KINDS>(a, first + tid / L, kind_of<L, BF, KINDS>(a, first + tid / L), l, raw);
+    kind = kind_of<L, BF, KINDS>(a, first + step + tid / L);
+  }
+  for (int64_t i0 = first; i0 < a.n; i0 += step) {
     const int64_t i = i0 + tid / L;
     float z[kV], key[kV];
-    load_row<L, BF>(a, i, l, z);
+    unpack<L, BF, KINDS>(a, raw, l, z);
+    if (i0 + step < a.n) {
+      load_row<L, BF, KINDS>(a, i + step, kind, l, raw);
+      kind = kind_of<L, BF, KINDS>(a, i + 2 * step);
+    }
     // (a NaN is not looked at here; it is in the sum)
     float top = -INFINITY;
 #pragma unroll
@@ -257,7 +301,7 @@ __global__ __launch_bounds__(1024) void k_route_total(RouteArgs a, int blocks) {
 // case, and keeping them would write and read as much again).  The lanes of a
 // row take its choices in turn; what a choice adds to its logit's gradient
 // goes through LDS to the lane that holds the logit.
-template <int L, bool BF>
+template <int L, bool BF, bool KINDS>
 __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
   __shared__ float s_h[L * kV];
   __shared__ __attribute__((aligned(16))) float s_add[kRouteThreads * kV];
@@ -286,10 +330,21 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   constexpr int kRows = kRouteThreads / L, kKept = (kMaxTopK + L - 1) / L;
   const int64_t step = int64_t(gridDim.x) * kRows;
-  for (int64_t i0 = int64_t(blockIdx.x) * kRows; i0 < a.n; i0 += step) {
+  const int64_t first = int64_t(blockIdx.x) * kRows;
+  Raw<BF> raw;
+  int kind = 0;
+  if (first < a.n) {
+    load_row<L, BF, KINDS>(a, first + tid / L, kind_of<L, BF, KINDS>(a, first + tid / L), l, raw);
+    kind = kind_of<L, BF, KINDS>(a, first + step + tid / L);
+  }
+  for (int64_t i0 = first; i0 < a.n; i0 += step) {
     const int64_t i = i0 + tid / L;
     float z[kV];
-    load_row<L, BF>(a, i, l, z);
+    unpack<L, BF, KINDS>(a, raw, l, z);
+    if (i0 + step < a.n) {
+      load_row<L, BF, KINDS>(a, i + step, kind, l, raw);
+      kind = kind_of<L, BF, KINDS>(a, i + 2 * step);
+    }
     float top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kV; ++j) top = fmaxf(top, z[j]);
@@ -569,29 +624,37 @@ __global__ __launch_bounds__(kGroupWaves * 64) void k_group_place(const int32_t*
 // (1,048,576 entries: 22 us with 2,048 chunks, 24 with 1,024).
 int64_t group_chunk(int64_t m) { return std::max<int64_t>(256, (m + 2048 * 64 - 1) / (2048 * 64) * 64); }
 
-template <bool BF>
+template <typename F>
+hipError_t by_type(const RouteArgs& a, F f) {
+  const std::true_type yes;
+  const std::false_type no;
+  if (a.bf16) return a.kinds ? f(yes, yes) : f(yes, no);
+  return a.kinds ? f(no, yes) : f(no, no);
+}
+
+template <bool BF, bool KINDS>
 hipError_t route_of(const RouteArgs& a, int blocks, hipStream_t s) {
   const dim3 g(blocks), b(kForwardThreads);
   const bool only = blocks == 1;
   switch (route_lanes(a.E)) {
-    case 1: k_route<1, BF><<<g, b, 0, s>>>(a, only); break;
-    case 2: k_route<2, BF><<<g, b, 0, s>>>(a, only); break;
-    case 4: k_route<4, BF><<<g, b, 0, s>>>(a, only); break;
-    case 8: k_route<8, BF><<<g, b, 0, s>>>(a, only); break;
-    default: k_route<16, BF><<<g, b, 0, s>>>(a, only); break;
+    case 1: k_route<1, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
+    case 2: k_route<2, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
+    case 4: k_route<4, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
+    case 8: k_route<8, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
+    default: k_route<16, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
   }
   return hipGetLastError();
 }
 
-template <bool BF>
+template <bool BF, bool KINDS>
 hipError_t route_backward_of(const RouteArgs& a, int blocks, hipStream_t s) {
   const dim3 g(blocks), b(kRouteThreads);
   switch (route_lanes(a.E)) {
-    case 1: k_route_backward<1, BF><<<g, b, 0, s>>>(a); break;
-    case 2: k_route_backward<2, BF><<<g, b, 0, s>>>(a); break;
-    case 4: k_route_backward<4, BF><<<g, b, 0, s>>>(a); break;
-    case 8: k_route_backward<8, BF><<<g, b, 0, s>>>(a); break;
-    default: k_route_backward<16, BF><<<g, b, 0, s>>>(a); break;
+    case 1: k_route_backward<1, BF, KINDS><<<g, b, 0, s>>>(a); break;
+    case 2: k_route_backward<2, BF, KINDS><<<g, b, 0, s>>>(a); break;
+    case 4: k_route_backward<4, BF, KINDS><<<g, b, 0, s>>>(a); break;
+    case 8: k_route_backward<8, BF, KINDS><<<g, b, 0, s>>>(a); break;
+    default: k_route_backward<16, BF, KINDS><<<g, b, 0, s>>>(a); break;
   }
   return hipGetLastError();
 }
@@ -607,7 +670,7 @@ int route_blocks(int64_t n, int E, int n_cu) {
 }
 
 hipError_t launch_route(const RouteArgs& a, int blocks, hipStream_t s) {
-  const hipError_t e = a.bf16 ? route_of<true>(a, blocks, s) : route_of<false>(a, blocks, s);
+  const hipError_t e = by_type(a, [&](auto bf, auto kinds) { return route_of<bf.value, kinds.value>(a, blocks, s); });
   if (e != hipSuccess || blocks == 1) return e;
   k_route_total<<<1, 1024, 0, s>>>(a, blocks);
   return hipGetLastError();
@@ -616,7 +679,7 @@ hipError_t launch_route(const RouteArgs& a, int blocks, hipStream_t s) {
 hipError_t launch_route_backward(const RouteArgs& a, int n_cu, hipStream_t s) {
   const int rows = kRouteThreads / route_lanes(a.E);
   const int blocks = int(std::max<int64_t>(1, std::min<int64_t>((a.n + rows - 1) / rows, 8 * n_cu)));
-  return a.bf16 ? route_backward_of<true>(a, blocks, s) : route_backward_of<false>(a, blocks, s);
+  return by_type(a, [&](auto bf, auto kinds) { return route_backward_of<bf.value, kinds.value>(a, blocks, s); });
 }
 
 size_t group_ws_bytes(int64_t m, int E) {
