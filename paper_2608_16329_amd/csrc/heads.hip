@@ -974,12 +974,15 @@ hipError_t gradient_by_layers(const HeadsArgs& a, hipStream_t s) {
 }  // namespace
 
 // Wavefronts of a work-group, 16 rows each.  For weight gradients eight, two a
-// SIMD, where there are tiles of 128 rows for all CUs; four where there are
-// not, or where z of more than four layers and the sums of their gradients need
-// all of a SIMD's registers.  Without weight gradients four, and two work-groups
-// a CU that need not wait for each other.
+// SIMD; four where each CU has at most one tile of 64 rows, which is sooner done
+// than one of 128 (6 heads of 128 inputs and 3 layers, all gradients, with the
+// grouping: 5,000 rows 47 us with four, 54 with eight, 10,000 rows 52 and 59;
+// 20,000 rows 72 and 60, 100,000 rows 167 and 145), or where z of more than four
+// layers and the sums of their gradients need all of a SIMD's registers.  Without
+// weight gradients four, and two work-groups a CU that need not wait for each
+// other.
 size_t heads_plan(HeadsArgs* a, int n_cu) {
-  a->waves = a->dweights && a->H <= 4 && a->m / 128 + a->E > n_cu ? 8 : 4;
+  a->waves = a->dweights && a->H <= 4 && a->m / 64 + a->E > n_cu ? 8 : 4;
   const int rows = 16 * a->waves;
   // at most one more tile than full ones for each head and for entries without
   const int64_t tiles = a->m / rows + a->E + 1;

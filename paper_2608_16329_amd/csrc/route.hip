@@ -427,7 +427,9 @@ int route_lanes(int E) {
 // ---- grouping ------------------------------------------------------------------
 
 constexpr int kGroupWaves = 4;
-constexpr int64_t kGroupOne = 8192;      // entries one work-group sorts by itself
+// Entries one work-group sorts by itself (4,096, 8 experts: 7.6 us, by three
+// kernels 10.6; 8,192: 11.0 and 10.7; 16,384: 18.8 and 10.7).
+constexpr int64_t kGroupOne = 8192;
 constexpr int kGroupOneWaves = 16;
 constexpr int kScanThreads = 1024;
 
@@ -621,7 +623,8 @@ __global__ __launch_bounds__(kGroupWaves * 64) void k_group_place(const int32_t*
 }
 
 // A wavefront's chunk: 256 entries, more where there would be over 2,048 chunks
-// (1,048,576 entries: 22 us with 2,048 chunks, 24 with 1,024).
+// (1,048,576 entries, 8 experts: 15.6 us with 2,048 chunks, 20.6 with 1,024, 16.1
+// with 4,096; 8,388,608 entries, 64 experts: 84, 145 and 100).
 int64_t group_chunk(int64_t m) { return std::max<int64_t>(256, (m + 2048 * 64 - 1) / (2048 * 64) * 64); }
 
 template <typename F>
@@ -661,11 +664,13 @@ hipError_t route_backward_of(const RouteArgs& a, int blocks, hipStream_t s) {
 
 }  // namespace
 
-// One work-group for up to four rounds of rows: adding up several costs a
-// launch, some 8 us, a round 2.
+// One work-group for up to two rounds of rows: several cost a launch that adds
+// them up (two rounds, 512 rows of 64 experts, 4 chosen: 13.4 us by one, 15.5 by
+// two; 2,048 rows of 4 experts 13.7 and 13.8; four rounds, 1,024 rows of 64
+// experts: 21.2 by one, 15.4 by four).
 int route_blocks(int64_t n, int E, int n_cu) {
   const int rows = kForwardThreads / route_lanes(E);
-  if (n <= 4 * rows) return 1;
+  if (n <= 2 * rows) return 1;
   return int(std::min<int64_t>((n + rows - 1) / rows, n_cu));
 }
 
