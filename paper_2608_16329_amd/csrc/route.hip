@@ -18,7 +18,6 @@ namespace {
 
 constexpr int kForwardThreads = 1024;   // a work-group for each CU: few sums to add up afterwards
 constexpr int kRouteThreads = 256;
-constexpr int kV = 16;              // logits a lane holds
 
 typedef uint32_t U4 __attribute__((aligned(1)));   // four bytes from anywhere
 
@@ -54,23 +53,23 @@ __device__ __forceinline__ float row_max(float v) {
 template <int L>
 __device__ __forceinline__ int expert_of(int j, int l) { return 4 * ((j >> 2) * L + l) + (j & 3); }
 
-// What a lane has of a row, as loaded: up to 16 logits and a byte for each that
+// What a lane has of a row, as loaded: V logits and a byte for each that
 // says whether the row may use it.  Every load is one that may be made, whatever
 // the row, so that none stands in a branch and the next row's are under way while
 // one is worked on: rows beyond the last are the last again, quads beyond a row's
 // end its last four.  unpack() puts this right.
-template <bool BF>
+template <int V, bool BF>
 struct Raw {
-  std::conditional_t<BF, H4, f4> v[kV / 4];
-  uint32_t ok[kV / 4];
+  std::conditional_t<BF, H4, f4> v[V / 4];
+  uint32_t ok[V / 4];
   bool live;
 };
-template <int L, bool BF, bool KINDS>
+template <bool KINDS>
 __device__ __forceinline__ int kind_of(const RouteArgs& a, int64_t i) {
   return KINDS ? a.kinds[i < a.n ? i : a.n - 1] : 0;
 }
-template <int L, bool BF, bool KINDS>
-__device__ __forceinline__ void load_row(const RouteArgs& a, int64_t i, int kind, int l, Raw<BF>& r) {
+template <int L, int V, bool BF, bool KINDS>
+__device__ __forceinline__ void load_row(const RouteArgs& a, int64_t i, int kind, int l, Raw<V, BF>& r) {
   typedef std::conditional_t<BF, uint16_t, float> T;
   typedef std::conditional_t<BF, H4, F4> Quad;
   const bool real = !KINDS || (kind >= 0 && kind < a.n_kinds);
@@ -81,21 +80,21 @@ __device__ __forceinline__ void load_row(const RouteArgs& a, int64_t i, int kind
     const int e1 = a.E > 1 ? 1 : 0, e2 = a.E > 2 ? 2 : 0;
     r.v[0][0] = row[0], r.v[0][1] = row[e1], r.v[0][2] = row[e2], r.v[0][3] = T(0);
     if (KINDS) r.ok[0] = ok[0] | uint32_t(ok[e1]) << 8 | uint32_t(ok[e2]) << 16;
-    for (int c = 1; c < kV / 4; ++c) r.v[c] = r.v[0], r.ok[c] = 0;
+    for (int c = 1; c < V / 4; ++c) r.v[c] = r.v[0], r.ok[c] = 0;
     return;
   }
 #pragma unroll
-  for (int c = 0; c < kV / 4; ++c) {
+  for (int c = 0; c < V / 4; ++c) {
     const int e = 4 * (c * L + l), at = e < a.E - 4 ? e : a.E - 4;
     r.v[c] = *reinterpret_cast<const Quad*>(row + at);
     if (KINDS) r.ok[c] = *reinterpret_cast<const U4*>(ok + at);
   }
 }
 // Its logits, what the row may not use as -inf, whatever stands there.
-template <int L, bool BF, bool KINDS>
-__device__ __forceinline__ void unpack(const RouteArgs& a, const Raw<BF>& r, int l, float z[kV]) {
+template <int L, int V, bool BF, bool KINDS>
+__device__ __forceinline__ void unpack(const RouteArgs& a, const Raw<V, BF>& r, int l, float z[V]) {
 #pragma unroll
-  for (int c = 0; c < kV / 4; ++c) {
+  for (int c = 0; c < V / 4; ++c) {
     const int left = r.live ? a.E - 4 * (c * L + l) : 0;
     float t[4];
 #pragma unroll
@@ -134,39 +133,39 @@ __device__ __forceinline__ void write_loss(const RouteArgs& a, double entries, d
 // in turn by the grid.  Each work-group's counts and sums of p go to its own
 // place and are added up in order afterwards, so results do not depend on the
 // order of work-groups.
-template <int L, bool BF, bool KINDS>
+template <int L, int V, bool BF, bool KINDS>
 __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool only) {
   constexpr int kKept = (kMaxTopK + L - 1) / L;   // choices a lane keeps: lane s % L the s-th
   __shared__ int32_t s_count[kMaxExperts + 1];
-  __shared__ float s_p[kForwardThreads / 64][L * kV];
+  __shared__ float s_p[kForwardThreads / 64][L * V];
   const int tid = threadIdx.x, l = tid % L, lane = tid & 63, w = tid >> 6;
   for (int e = tid; e <= a.E; e += kForwardThreads) s_count[e] = 0;
   __syncthreads();
-  float psum[kV];
+  float psum[V];
 #pragma unroll
-  for (int j = 0; j < kV; ++j) psum[j] = 0.f;
+  for (int j = 0; j < V; ++j) psum[j] = 0.f;
   constexpr int kRows = kForwardThreads / L;
   const int64_t step = int64_t(gridDim.x) * kRows;
   int rows = 0;
   const int64_t first = int64_t(blockIdx.x) * kRows;
-  Raw<BF> raw;
+  Raw<V, BF> raw;
   int kind = 0;
   if (first < a.n) {
-    load_row<L, BF, KINDS>(a, first + tid / L, kind_of<L, BF, KINDS>(a, first + tid / L), l, raw);
-    kind = kind_of<L, BF, KINDS>(a, first + step + tid / L);
+    load_row<L, V, BF, KINDS>(a, first + tid / L, kind_of<KINDS>(a, first + tid / L), l, raw);
+    kind = kind_of<KINDS>(a, first + step + tid / L);
   }
   for (int64_t i0 = first; i0 < a.n; i0 += step) {
     const int64_t i = i0 + tid / L;
-    float z[kV], key[kV];
-    unpack<L, BF, KINDS>(a, raw, l, z);
+    float z[V], key[V];
+    unpack<L, V, BF, KINDS>(a, raw, l, z);
     if (i0 + step < a.n) {
-      load_row<L, BF, KINDS>(a, i + step, kind, l, raw);
-      kind = kind_of<L, BF, KINDS>(a, i + 2 * step);
+      load_row<L, V, BF, KINDS>(a, i + step, kind, l, raw);
+      kind = kind_of<KINDS>(a, i + 2 * step);
     }
     // (a NaN is not looked at here; it is in the sum)
     float top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kV; ++j) {
+    for (int j = 0; j < V; ++j) {
       key[j] = z[j];
       top = fmaxf(top, key[j]);
     }
@@ -174,7 +173,7 @@ __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool onl
     const float base = top != -INFINITY ? top : 0.f;
     float sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < kV; ++j) {
+    for (int j = 0; j < V; ++j) {
       z[j] = __builtin_amdgcn_exp2f((z[j] - base) * kLog2e);
       sum += z[j];
     }
@@ -182,7 +181,7 @@ __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool onl
     const bool any = sum != 0.f;
     const float inv = any ? 1.f / sum : 0.f;
 #pragma unroll
-    for (int j = 0; j < kV; ++j) psum[j] += z[j] * inv;
+    for (int j = 0; j < V; ++j) psum[j] += z[j] * inv;
     rows += any && l == 0;
     float chosen = 0.f;
     int my_id[kKept];
@@ -198,20 +197,20 @@ __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool onl
         if (s > 0) {
           best = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < kV; ++j) best = fmaxf(best, key[j]);
+          for (int j = 0; j < V; ++j) best = fmaxf(best, key[j]);
           best = row_max<L>(best);
         }
         // the lowest expert that has it
         int at = -1;
 #pragma unroll
-        for (int j = kV - 1; j >= 0; --j) at = key[j] == best ? j : at;
+        for (int j = V - 1; j >= 0; --j) at = key[j] == best ? j : at;
         const int own = at >= 0 ? expert_of<L>(at, l) : 0x7fffffff;
         const int id = over_row<L>(own, [](int x, int y) { return x < y ? x : y; });
         const bool there = best != -INFINITY;
         if (s + 1 < a.K) {
           at = own == id ? at : -1;
 #pragma unroll
-          for (int j = 0; j < kV; ++j) key[j] = at == j ? -INFINITY : key[j];
+          for (int j = 0; j < V; ++j) key[j] = at == j ? -INFINITY : key[j];
         }
         const float e = there ? __builtin_amdgcn_exp2f((best - base) * kLog2e) : 0.f;
         chosen += e;
@@ -237,7 +236,7 @@ __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool onl
   if (rows) atomicAdd(&s_count[a.E], rows);
   // lanes with the same experts, then the wavefronts, in a fixed order
 #pragma unroll
-  for (int j = 0; j < kV; ++j) {
+  for (int j = 0; j < V; ++j) {
     float v = psum[j];
 #pragma unroll
     for (int o = L; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
@@ -301,10 +300,10 @@ __global__ __launch_bounds__(1024) void k_route_total(RouteArgs a, int blocks) {
 // case, and keeping them would write and read as much again).  The lanes of a
 // row take its choices in turn; what a choice adds to its logit's gradient
 // goes through LDS to the lane that holds the logit.
-template <int L, bool BF, bool KINDS>
+template <int L, int V, bool BF, bool KINDS>
 __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
-  __shared__ float s_h[L * kV];
-  __shared__ __attribute__((aligned(16))) float s_add[kRouteThreads * kV];
+  __shared__ float s_h[L * V];
+  __shared__ __attribute__((aligned(16))) float s_add[kRouteThreads * V];
   __shared__ double s_entries;
   const int tid = threadIdx.x, l = tid % L, lane = tid & 63;
   if (tid < 64) {
@@ -318,41 +317,41 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
   {
     const double rows = a.counts[a.E];
     const double f = a.dloss && rows > 0 && s_entries > 0 ? double(a.dloss[0]) * a.E / (rows * s_entries) : 0.0;
-    for (int e = tid; e < L * kV; e += kRouteThreads) s_h[e] = e < a.E ? float(f * a.counts[e]) : 0.f;
+    for (int e = tid; e < L * V; e += kRouteThreads) s_h[e] = e < a.E ? float(f * a.counts[e]) : 0.f;
   }
   __syncthreads();
-  float h[kV];
+  float h[V];
 #pragma unroll
-  for (int j = 0; j < kV; ++j) h[j] = s_h[expert_of<L>(j, l)];
-  float* const mine = s_add + tid / L * (L * kV);   // the row's
+  for (int j = 0; j < V; ++j) h[j] = s_h[expert_of<L>(j, l)];
+  float* const mine = s_add + tid / L * (L * V);   // the row's
 #pragma unroll
-  for (int c = 0; c < kV / 4; ++c) *reinterpret_cast<f4*>(mine + 4 * (c * L + l)) = f4{0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < V / 4; ++c) *reinterpret_cast<f4*>(mine + 4 * (c * L + l)) = f4{0.f, 0.f, 0.f, 0.f};
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   constexpr int kRows = kRouteThreads / L, kKept = (kMaxTopK + L - 1) / L;
   const int64_t step = int64_t(gridDim.x) * kRows;
   const int64_t first = int64_t(blockIdx.x) * kRows;
-  Raw<BF> raw;
+  Raw<V, BF> raw;
   int kind = 0;
   if (first < a.n) {
-    load_row<L, BF, KINDS>(a, first + tid / L, kind_of<L, BF, KINDS>(a, first + tid / L), l, raw);
-    kind = kind_of<L, BF, KINDS>(a, first + step + tid / L);
+    load_row<L, V, BF, KINDS>(a, first + tid / L, kind_of<KINDS>(a, first + tid / L), l, raw);
+    kind = kind_of<KINDS>(a, first + step + tid / L);
   }
   for (int64_t i0 = first; i0 < a.n; i0 += step) {
     const int64_t i = i0 + tid / L;
-    float z[kV];
-    unpack<L, BF, KINDS>(a, raw, l, z);
+    float z[V];
+    unpack<L, V, BF, KINDS>(a, raw, l, z);
     if (i0 + step < a.n) {
-      load_row<L, BF, KINDS>(a, i + step, kind, l, raw);
-      kind = kind_of<L, BF, KINDS>(a, i + 2 * step);
+      load_row<L, V, BF, KINDS>(a, i + step, kind, l, raw);
+      kind = kind_of<KINDS>(a, i + 2 * step);
     }
     float top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kV; ++j) top = fmaxf(top, z[j]);
+    for (int j = 0; j < V; ++j) top = fmaxf(top, z[j]);
     top = row_max<L>(top);
     const float base = top != -INFINITY ? top : 0.f;
     float sum = 0.f, mean = 0.f;
 #pragma unroll
-    for (int j = 0; j < kV; ++j) {
+    for (int j = 0; j < V; ++j) {
       z[j] = __builtin_amdgcn_exp2f((z[j] - base) * kLog2e);
       sum += z[j];
       mean += z[j] * h[j];
@@ -398,7 +397,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
     }
     if (i < a.n) {
 #pragma unroll
-      for (int c = 0; c < kV / 4; ++c) {
+      for (int c = 0; c < V / 4; ++c) {
         const int e = 4 * (c * L + l);
         const f4 add = *reinterpret_cast<const f4*>(mine + e);
         float t[4];
@@ -417,10 +416,12 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
   }
 }
 
-// Lanes per row: as few as hold E logits, 16 a lane.
+// Lanes per row: as few as hold E logits, 16 a lane.  (Up to 8 or 4 experts a
+// lane holds only so many.)
+constexpr int kMost = 16;
 int route_lanes(int E) {
   int L = 1;
-  while (L * kV < E) L *= 2;
+  while (L * kMost < E) L *= 2;
   return L;
 }
 
@@ -640,11 +641,15 @@ hipError_t route_of(const RouteArgs& a, int blocks, hipStream_t s) {
   const dim3 g(blocks), b(kForwardThreads);
   const bool only = blocks == 1;
   switch (route_lanes(a.E)) {
-    case 1: k_route<1, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
-    case 2: k_route<2, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
-    case 4: k_route<4, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
-    case 8: k_route<8, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
-    default: k_route<16, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
+    case 1:
+      if (a.E <= 4) k_route<1, 4, BF, KINDS><<<g, b, 0, s>>>(a, only);
+      else if (a.E <= 8) k_route<1, 8, BF, KINDS><<<g, b, 0, s>>>(a, only);
+      else k_route<1, 16, BF, KINDS><<<g, b, 0, s>>>(a, only);
+      break;
+    case 2: k_route<2, 16, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
+    case 4: k_route<4, 16, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
+    case 8: k_route<8, 16, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
+    default: k_route<16, 16, BF, KINDS><<<g, b, 0, s>>>(a, only); break;
   }
   return hipGetLastError();
 }
@@ -653,11 +658,15 @@ template <bool BF, bool KINDS>
 hipError_t route_backward_of(const RouteArgs& a, int blocks, hipStream_t s) {
   const dim3 g(blocks), b(kRouteThreads);
   switch (route_lanes(a.E)) {
-    case 1: k_route_backward<1, BF, KINDS><<<g, b, 0, s>>>(a); break;
-    case 2: k_route_backward<2, BF, KINDS><<<g, b, 0, s>>>(a); break;
-    case 4: k_route_backward<4, BF, KINDS><<<g, b, 0, s>>>(a); break;
-    case 8: k_route_backward<8, BF, KINDS><<<g, b, 0, s>>>(a); break;
-    default: k_route_backward<16, BF, KINDS><<<g, b, 0, s>>>(a); break;
+    case 1:
+      if (a.E <= 4) k_route_backward<1, 4, BF, KINDS><<<g, b, 0, s>>>(a);
+      else if (a.E <= 8) k_route_backward<1, 8, BF, KINDS><<<g, b, 0, s>>>(a);
+      else k_route_backward<1, 16, BF, KINDS><<<g, b, 0, s>>>(a);
+      break;
+    case 2: k_route_backward<2, 16, BF, KINDS><<<g, b, 0, s>>>(a); break;
+    case 4: k_route_backward<4, 16, BF, KINDS><<<g, b, 0, s>>>(a); break;
+    case 8: k_route_backward<8, 16, BF, KINDS><<<g, b, 0, s>>>(a); break;
+    default: k_route_backward<16, 16, BF, KINDS><<<g, b, 0, s>>>(a); break;
   }
   return hipGetLastError();
 }
