@@ -34,14 +34,17 @@ class _OnStream:
         self.torch = torch
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         self.device = self.stream.device
+        self._raw = self.stream.cuda_stream
+        # (the current stream's handle alone: a stream object for every call takes longer than the call's checks)
+        self._current = torch._C._cuda_getCurrentRawStream
         self._dtypes = {torch.float32: b.MLIP_F32, torch.bfloat16: b.MLIP_BF16}
 
     def _run(self, call, *args) -> None:
         """The call's work after what the current stream has, and what it gets next after the call's."""
-        current = self.torch.cuda.current_stream(self.device)
-        if current == self.stream:
+        if self._current(self.device.index) == self._raw:
             call(*args)
             return
+        current = self.torch.cuda.current_stream(self.device)
         self.stream.wait_stream(current)
         call(*args)
         current.wait_stream(self.stream)
@@ -117,6 +120,8 @@ class Learner(_OnStream):
             if len(self._kept) >= 64:
                 self._kept.clear()
             p = self._kept[(kind, values)] = kind(*values)
+            if kind is b.mlip_heads_params:
+                p.count = b.mlip_heads_weight_count(p)
         return p
 
     def route(self, logits, experts, gates, counts, loss, *, kinds=None, allowed=None, gates_of: str = "chosen") -> None:
@@ -179,9 +184,8 @@ class Learner(_OnStream):
         _need(weights.dim() == 2, "weights is not 2-d")
         n_experts, values = weights.shape
         p = self._params(b.mlip_heads_params, n_experts, width, hidden, top_k, self._dtypes[x.dtype], max(stride, width))
-        count = b.mlip_heads_weight_count(p)
-        _need(count == 0 or values * n_experts == count,
-              f"weights has {values} values a head, {width} inputs and {hidden} layers need {count // max(n_experts, 1)}")
+        if p.count and values * n_experts != p.count:
+            raise ValueError(f"weights has {values} values a head, {width} inputs and {hidden} layers need {p.count // n_experts}")
         self._dense(weights, "weights", t.float32, n_experts, values)
         self._dense(offsets, "offsets", t.int32, n_experts + 1)
         self._dense(order, "order", t.int32, n * top_k)
