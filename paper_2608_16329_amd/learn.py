@@ -224,10 +224,13 @@ class AdamW(_OnStream):
         _need(len(params) == len(grads) == len(decay) and len(params) == len(into if into is not None else params),
               "params, grads, into and decay differ in length")
         _need(bits in (8, 32), f"bits is {bits}, not 32 or 8")
+        kinds, here = self._dtypes, self.device.index
         for k, (p, g) in enumerate(zip(params, grads)):
-            if p.dtype not in self._dtypes or g.dtype not in self._dtypes:
-                _need(p.dtype in self._dtypes, f"params[{k}] is {p.dtype}, not float32 or bfloat16")
-                _need(False, f"grads[{k}] is {g.dtype}, not float32 or bfloat16")
+            if (p.dtype in kinds and g.dtype in kinds and p.get_device() == here == g.get_device() and p.shape == g.shape
+                    and p.is_contiguous() and g.is_contiguous()):
+                continue
+            _need(p.dtype in kinds, f"params[{k}] is {p.dtype}, not float32 or bfloat16")
+            _need(g.dtype in kinds, f"grads[{k}] is {g.dtype}, not float32 or bfloat16")
             self._dense(p, "a tensor of params", p.dtype, *p.shape)
             self._dense(g, "a tensor of grads", g.dtype, *p.shape)
         for p, q in zip(params, into or []):
