@@ -1,7 +1,10 @@
 // The descriptor buffer of the three-kernel configuration (by sorted slot, in
 // the network's type) and the caller's rows (by atom, float32): what goes to
 // heads outside the fused kernel and comes back from them.  Bound by memory:
-// a wavefront copies neighbouring values of a row, four a lane.
+// a wavefront copies neighbouring values of a row, four a lane.  131,072 atoms of
+// 128 values, float64 network: 30 us out, 37 back (201 MB, 6.7 and 5.4 TB/s, part
+// of it from the last-level cache).  Float32 rows: the heads' arithmetic is
+// float32, so a wider row would only be rounded later.
 #include "learn_math.h"
 #include "mlip_internal.h"
 
