@@ -146,7 +146,7 @@ __device__ void tile_table(const HeadsArgs& a, int rows, int32_t* first, int32_t
         hi = e + 1 <= a.E ? a.offsets[e + 1] : int(a.m);
         hi = hi < lo ? lo : (hi > a.m ? int(a.m) : hi);
       }
-      const int tiles = e <= a.E ? (hi - lo + rows - 1) / rows : 0;
+      const int tiles = e <= a.E ? int((uint32_t(hi - lo) + uint32_t(rows - 1)) / uint32_t(rows)) : 0;
       int v = tiles;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -928,9 +928,9 @@ __global__ __launch_bounds__(256) void k_sum_slots(HeadsArgs a) {
 // values is one that may be made.  Bound by memory: 1,048,576 rows of 3, 9 us.
 template <typename T>
 __global__ __launch_bounds__(256) void k_pad(const T* x, int64_t n, int64_t stride, int D, T* to) {
-  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  const int c = int(at & 3);
-  if (at < 4 * n) to[at] = c < D ? x[(at >> 2) * stride + c] : T(0);
+  const int c = threadIdx.x & 3;
+  for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < 4 * n; at += int64_t(gridDim.x) * 256)
+    to[at] = c < D ? x[(at >> 2) * stride + c] : T(0);
 }
 
 // Rows with several entries: their energies and gradients added up in order,
@@ -938,14 +938,17 @@ __global__ __launch_bounds__(256) void k_pad(const T* x, int64_t n, int64_t stri
 // 131,071 rows of 192, two entries each, 40 us (252 MB, 6.3 TB/s, part of it from
 // the last-level cache).
 __global__ __launch_bounds__(256) void k_sum_entries(HeadsArgs a) {
-  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (a.energy && at < a.n) {
-    float v = 0.f;
-    for (int s = 0; s < a.K; ++s) v += a.entry_energy[at * a.K + s];
-    a.energy[at] = v;
+  const int64_t first = int64_t(blockIdx.x) * 256 + threadIdx.x, step = int64_t(gridDim.x) * 256;
+  if (a.energy) {
+    for (int64_t at = first; at < a.n; at += step) {
+      float v = 0.f;
+      for (int s = 0; s < a.K; ++s) v += a.entry_energy[at * a.K + s];
+      a.energy[at] = v;
+    }
   }
+  if (!a.dx) return;
   const int groups = (a.D + 3) / 4;
-  if (a.dx && at < a.n * groups) {
+  for (int64_t at = first; at < a.n * groups; at += step) {
     const int64_t i = at / groups;
     const int c = 4 * int(at % groups);
     float v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -958,6 +961,9 @@ __global__ __launch_bounds__(256) void k_sum_entries(HeadsArgs a) {
     store4(a.dx, a.bf16, i * a.D + c, a.D - c, v);
   }
 }
+
+// Work-groups of 256 for that many values, fewer than 2^32 threads a launch.
+unsigned blocks_for(int64_t values) { return unsigned(std::min<int64_t>((values + 255) / 256, 1 << 22)); }
 
 template <int H, int NW, bool TRAIN, bool BF>
 hipError_t gradient_of(const HeadsArgs& a, hipStream_t s) {
@@ -1032,7 +1038,7 @@ hipError_t launch_heads(const HeadsArgs& given, hipStream_t s) {
   HeadsArgs a = given;
   if (a.m > 0) {
     if (a.D < 4) {
-      const unsigned blocks = unsigned((4 * a.n + 255) / 256);
+      const unsigned blocks = blocks_for(4 * a.n);
       if (a.bf16) k_pad<<<blocks, 256, 0, s>>>(static_cast<const uint16_t*>(a.x), a.n, a.stride, a.D, static_cast<uint16_t*>(a.padded));
       else k_pad<<<blocks, 256, 0, s>>>(static_cast<const float*>(a.x), a.n, a.stride, a.D, static_cast<float*>(a.padded));
       if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -1060,7 +1066,7 @@ hipError_t launch_heads(const HeadsArgs& given, hipStream_t s) {
   }
   if (a.K > 1 && a.m > 0 && (a.energy || a.dx)) {
     const int64_t work = std::max<int64_t>(a.n, a.dx ? a.n * ((a.D + 3) / 4) : 0);
-    k_sum_entries<<<unsigned((work + 255) / 256), 256, 0, s>>>(a);
+    k_sum_entries<<<blocks_for(work), 256, 0, s>>>(a);
     e = hipGetLastError();
   }
   return e;

@@ -230,3 +230,49 @@ def test_refusals():
         L.heads(x, w.double(), offsets, order, hidden=2, top_k=2, energy=e)
     with pytest.raises(ValueError, match="next to each other"):
         L.heads(torch.empty((32, 20), device="cuda:0").t(), w, offsets, order, hidden=2, top_k=2, energy=e)
+
+
+@pytest.mark.parametrize("rows,width,heads,dtype", [((1 << 31) - 1, 1, 1, "bfloat16"), ((1 << 30) + 5, 2, 2, "float32")])
+def test_as_many_rows_as_there_may_be(rows, width, heads, dtype):
+    """Row numbers up to 2^31 - 2, more than 2^32 values that are copied to rows
+    of four, and memory beyond 2^32 bytes from its start."""
+    import torch
+    from paper_2608_16329_amd import Learner
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("100 GiB of free memory")
+    dev = torch.device("cuda:0")
+    g = torch.Generator(device=dev).manual_seed(3)
+    _, w, _, _, _ = inputs(1, width, 1, heads, 1, dtype, 0, 8)
+    x = torch.empty((rows, width), dtype=getattr(torch, dtype), device=dev)
+    ids = torch.zeros((rows, 1), dtype=torch.int32, device=dev)
+    for at in range(0, rows, 1 << 27):
+        x[at:at + (1 << 27)].copy_(torch.rand(x[at:at + (1 << 27)].shape, generator=g, device=dev))
+        if heads > 1:
+            ids[at:at + (1 << 27)].copy_(torch.randint(0, heads, ids[at:at + (1 << 27)].shape, generator=g, device=dev))
+    L = Learner()
+    offsets, order = torch.empty(heads + 1, dtype=torch.int32, device=dev), torch.empty(rows, dtype=torch.int32, device=dev)
+    L.group(ids, offsets, order)
+    energy = torch.full((rows,), float("nan"), device=dev)
+    L.heads(x, w, offsets, order, hidden=1, energy=energy)
+    torch.cuda.synchronize()
+    assert int(offsets[heads]) == rows
+    some = torch.cat([torch.arange(0, 500), torch.arange((1 << 30) - 250, (1 << 30) + 5), torch.arange(rows - 500, rows)]).to(dev)
+    ref = definition(x[some], w, ids[some], torch.ones((len(some), 1), device=dev), None, 1)[0]
+    close(energy[some], ref, "energy")
+    del energy, order, ids, x
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_far_apart(dtype):
+    """Rows 2^26 values apart, memory beyond 2^32 values from its start: the same bits as rows side by side."""
+    import torch
+    from paper_2608_16329_amd import Learner
+    n, D, H, E = 70, 36, 2, 3
+    x, w, ids, gates, up = inputs(n, D, H, E, 1, dtype, 0, 6)
+    far = torch.empty((n, 1 << 26), dtype=x.dtype, device=x.device)[:, 7:7 + D]
+    far.copy_(x)
+    L = Learner()
+    a, b = run(L, x, w, ids, gates, up, H), run(L, far, w, ids, gates, up, H)
+    for k in a:
+        assert torch.equal(a[k], b[k]), k

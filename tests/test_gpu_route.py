@@ -249,3 +249,26 @@ def test_refusals():
         L.group(a[1], torch.zeros(300, dtype=torch.int32, device=dev), torch.zeros(8, dtype=torch.int32, device=dev))
     with pytest.raises(ValueError, match="order"):
         L.group(a[1], torch.zeros(9, dtype=torch.int32, device=dev), torch.zeros(7, dtype=torch.int32, device=dev))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("experts", [3, 8, 29])
+def test_rows_far_apart(dtype, experts):
+    """Rows 2^26 values apart, memory beyond 2^32 values from its start: the same bits as rows side by side."""
+    import torch
+    from paper_2608_16329_amd import Learner
+    n, K, dev = 70, 2, torch.device("cuda:0")
+    z = torch.randn((n, experts), generator=torch.Generator(device=dev).manual_seed(experts), device=dev).to(getattr(torch, dtype))
+    far = torch.empty((n, 1 << 26), dtype=z.dtype, device=dev)[:, 5:5 + experts]
+    far.copy_(z)
+    dgates, one = torch.ones((n, K), device=dev).cumsum(0), torch.ones(1, device=dev)
+    L, out = Learner(), []
+    for logits in (z, far):
+        ids, gates = torch.empty((n, K), dtype=torch.int32, device=dev), torch.empty((n, K), device=dev)
+        counts, loss = torch.empty(experts + 1, dtype=torch.int32, device=dev), torch.empty(1, device=dev)
+        dlogits = torch.empty((n, experts), dtype=z.dtype, device=dev)
+        L.route(logits, ids, gates, counts, loss)
+        L.route_backward(logits, ids, counts, dlogits, dgates=dgates, dloss=one)
+        out.append((ids, gates, counts, loss, dlogits))
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
