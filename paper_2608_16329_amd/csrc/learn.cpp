@@ -37,6 +37,15 @@ mlip_status fail_hip(Ctx* ctx, hipError_t e) {
     if (e_ != hipSuccess) return fail_hip((ctx), e_); \
   } while (0)
 
+// A call on another device's stream would take memory and sizes of the wrong one.
+template <typename Ctx>
+bool elsewhere(Ctx* ctx) {
+  int device = -1;
+  if (hipGetDevice(&device) != hipSuccess) (void)hipGetLastError();
+  return device != ctx->device;
+}
+constexpr const char* kElsewhere = "the device of the context is not current";
+
 // The workspace holds at least `need` bytes; it is freed and allocated anew
 // where it is smaller, after the stream's work that may still use it.
 mlip_status workspace(mlip_learn* ctx, size_t need) {
@@ -162,6 +171,7 @@ mlip_status mlip_route(mlip_learn* ctx, const mlip_route_params* p, int64_t n, c
                        int32_t* counts_dev, float* loss_dev) {
   if (!ctx) return MLIP_E_ARG;
   ctx->err.clear();
+  if (elsewhere(ctx)) return fail(ctx, MLIP_E_ARG, kElsewhere);
   const mlip_status st = check_route(ctx, p, n, logits_dev, kinds_dev, allowed_dev);
   if (st != MLIP_OK) return st;
   if (!counts_dev || !loss_dev || (n > 0 && (!experts_dev || !gates_dev))) return fail(ctx, MLIP_E_ARG, "NULL output");
@@ -187,6 +197,7 @@ mlip_status mlip_route_backward(mlip_learn* ctx, const mlip_route_params* p, int
                                 void* dlogits_dev) {
   if (!ctx) return MLIP_E_ARG;
   ctx->err.clear();
+  if (elsewhere(ctx)) return fail(ctx, MLIP_E_ARG, kElsewhere);
   const mlip_status st = check_route(ctx, p, n, logits_dev, kinds_dev, allowed_dev);
   if (st != MLIP_OK) return st;
   if (n == 0) return MLIP_OK;
@@ -205,6 +216,7 @@ mlip_status mlip_group(mlip_learn* ctx, int64_t n_entries, int32_t n_experts, co
                        int32_t* offsets_dev, int32_t* order_dev) {
   if (!ctx) return MLIP_E_ARG;
   ctx->err.clear();
+  if (elsewhere(ctx)) return fail(ctx, MLIP_E_ARG, kElsewhere);
   if (n_experts < 1 || n_experts > kMaxExperts) return fail(ctx, MLIP_E_ARG, "n_experts must be in 1..256");
   if (n_entries < 0 || n_entries >= (int64_t(1) << 31)) return fail(ctx, MLIP_E_ARG, "n_entries outside [0, 2^31)");
   if (!offsets_dev || (n_entries > 0 && (!experts_dev || !order_dev))) return fail(ctx, MLIP_E_ARG, "NULL argument");
@@ -224,6 +236,7 @@ mlip_status mlip_heads(mlip_learn* ctx, const mlip_heads_params* p, int64_t n, c
                        float* dweights_dev, float* dgates_dev) {
   if (!ctx) return MLIP_E_ARG;
   ctx->err.clear();
+  if (elsewhere(ctx)) return fail(ctx, MLIP_E_ARG, kElsewhere);
   if (!p) return fail(ctx, MLIP_E_ARG, "NULL parameters");
   if (!heads_valid(p)) return fail(ctx, MLIP_E_ARG, "n_experts must be in 1..256, width in 1..1024, hidden in 1..8");
   if (p->top_k < 1 || p->top_k > kMaxTopK) return fail(ctx, MLIP_E_ARG, "top_k must be in 1..16");
@@ -306,9 +319,8 @@ mlip_status mlip_adamw_create(const mlip_adamw_tensor* tensors, int64_t n_tensor
     h->elements = at;
     h->blocks = block;
     h->pieces = int64_t(pp.size());
-    int device = 0;
-    if (hipGetDevice(&device) != hipSuccess ||
-        hipDeviceGetAttribute(&h->n_cu, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) {
+    if (hipGetDevice(&h->device) != hipSuccess ||
+        hipDeviceGetAttribute(&h->n_cu, hipDeviceAttributeMultiprocessorCount, h->device) != hipSuccess) {
       (void)hipGetLastError();
       delete h;
       return fail(none, MLIP_E_HIP, "no current HIP device");
@@ -355,6 +367,7 @@ mlip_status mlip_adamw_step(mlip_adamw* plan, const mlip_adamw_params* p, const 
                             const mlip_adamw_state* into, int32_t reverse) {
   if (!plan) return MLIP_E_ARG;
   plan->err.clear();
+  if (elsewhere(plan)) return fail(plan, MLIP_E_ARG, kElsewhere);
   if (!p) return fail(plan, MLIP_E_ARG, "NULL parameters");
   if (p->step < 1) return fail(plan, MLIP_E_ARG, "step must be 1 or more");
   if (!(p->beta1 >= 0.0 && p->beta1 < 1.0) || !(p->beta2 >= 0.0 && p->beta2 < 1.0))
@@ -384,6 +397,7 @@ mlip_status mlip_adamw_step(mlip_adamw* plan, const mlip_adamw_params* p, const 
 mlip_status mlip_adamw_moments(mlip_adamw* plan, const mlip_adamw_state* state, float* m_out_dev, float* v_out_dev) {
   if (!plan) return MLIP_E_ARG;
   plan->err.clear();
+  if (elsewhere(plan)) return fail(plan, MLIP_E_ARG, kElsewhere);
   if (plan->bits != 8) return fail(plan, MLIP_E_ARG, "the moments are values already");
   if (!state_given(plan, state)) return fail(plan, MLIP_E_ARG, "NULL state");
   if (plan->pieces == 0) return MLIP_OK;

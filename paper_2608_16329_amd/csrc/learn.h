@@ -38,6 +38,7 @@ struct mlip_learn {
 
 struct mlip_adamw {
   hipStream_t stream = nullptr;
+  int device = 0;
   int n_cu = 0;
   int bits = 32;
   bool into = false;          // the plan has a second set of parameters

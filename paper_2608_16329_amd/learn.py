@@ -36,11 +36,14 @@ class _OnStream:
         self.device = self.stream.device
         self._raw = self.stream.cuda_stream
         # (the current stream's handle alone: a stream object for every call takes longer than the call's checks)
-        self._current = torch._C._cuda_getCurrentRawStream
+        self._current, self._device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         self._dtypes = {torch.float32: b.MLIP_F32, torch.bfloat16: b.MLIP_BF16}
 
     def _run(self, call, *args) -> None:
         """The call's work after what the current stream has, and what it gets next after the call's."""
+        if self._device() != self.device.index:
+            with self.torch.cuda.device(self.device):
+                return self._run(call, *args)
         if self._current(self.device.index) == self._raw:
             call(*args)
             return
