@@ -383,7 +383,8 @@ mlip_status mlip_md_kinetic(mlip_ctx* ctx, const double* vel_dev, double* ke_hos
  * the calls made with it.  Work is enqueued on its stream; buffers are the
  * caller's, as above.  The context's device must be current (MLIP_E_ARG).  A call may enlarge the workspace (hipMalloc, and a
  * wait for the stream where an older one is freed) the first time it meets a
- * size; later calls of that size or smaller allocate nothing.  All results
+ * size; later calls of that size or smaller allocate nothing, and may be
+ * recorded in a HIP graph.  All results
  * are the same from run to run: nothing is summed in an order that depends on
  * the scheduling of work-groups.
  */

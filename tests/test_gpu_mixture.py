@@ -107,3 +107,60 @@ def test_mixture_learns_and_runs():
         assert abs(slope - along) <= 2e-2 * float(forces.norm())
     totals = mixture_heads.run(potential, w, pos, steps=30, say=log)
     assert max(totals) - min(totals) < 0.02 * np.mean(np.abs(totals))
+
+
+def test_captured_training_step_replays():
+    """Routing, grouping, heads, their gradients and AdamW recorded in a graph: every replay, with the program's own
+    work between, gives the bits of the calls one by one."""
+    import torch
+    from paper_2608_16329_amd import AdamW, Learner
+    n, D, H, E, K = 3000, 64, 3, 5, 2
+    dev = torch.device("cuda:0")
+    g = torch.Generator(device=dev).manual_seed(2)
+    x, logits = (torch.randn(s, generator=g, device=dev) for s in ((n, D), (n, E)))
+    w0 = torch.randn((E, values_of(D, H)), generator=g, device=dev) * 0.1
+    up = torch.randn(n, generator=g, device=dev)
+    one = torch.ones(1, device=dev)
+
+    def build(stream):
+        L = Learner(stream=stream)
+        t = dict(w=w0.clone(), dw=torch.zeros_like(w0), ids=torch.empty((n, K), dtype=torch.int32, device=dev),
+                 gates=torch.empty((n, K), device=dev), counts=torch.empty(E + 1, dtype=torch.int32, device=dev),
+                 loss=torch.empty(1, device=dev), offsets=torch.empty(E + 1, dtype=torch.int32, device=dev),
+                 order=torch.empty(n * K, dtype=torch.int32, device=dev), energy=torch.empty(n, device=dev),
+                 dx=torch.empty((n, D), device=dev), dgates=torch.empty((n, K), device=dev), dz=torch.empty((n, E), device=dev))
+        opt = AdamW([t["w"]], [t["dw"]], bits=8, stream=stream)
+
+        def step():
+            L.route(logits, t["ids"], t["gates"], t["counts"], t["loss"])
+            L.group(t["ids"], t["offsets"], t["order"])
+            L.heads(x, t["w"], t["offsets"], t["order"], hidden=H, top_k=K, gates=t["gates"], denergy=up, energy=t["energy"],
+                    dx=t["dx"], dweights=t["dw"], dgates=t["dgates"])
+            L.route_backward(logits, t["ids"], t["counts"], t["dz"], dgates=t["dgates"], dloss=one)
+            opt.step(1, lr=1e-3, seed=7)
+        return t, opt, step, L
+
+    eager, opt_e, step_e, keep_e = build(torch.cuda.current_stream())
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    t, opt, step, keep = build(s)
+    with torch.cuda.stream(s):
+        step()                                       # the workspace is laid out here
+        t["w"].copy_(w0)
+        for m in (opt.m, opt.v, opt.m_exp, opt.v_exp):
+            m.zero_()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for _ in range(4):
+        step_e()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in t:
+            assert torch.equal(t[k], eager[k]), k
+        assert torch.equal(opt.m, opt_e.m) and torch.equal(opt.v, opt_e.v)
+        up.mul_(0.5).add_(0.1)                       # other inputs the next time
+        x.add_(0.01)
+        torch.cuda.synchronize()
+    keep.close(), keep_e.close(), opt.close(), opt_e.close()
