@@ -119,6 +119,24 @@ __device__ __forceinline__ void unpack(const RouteArgs& a, const Raw<V, BF>& r, 
   }
 }
 
+// Sums of v[0] .. v[N - 1] over the lanes that differ in bits O, O / 2 .. L: each
+// step adds two lanes' halves of what is left, so that 16 values take 17
+// exchanges over 64 lanes, not 96.  What a lane has then begins at value `first`.
+template <int N, int O, int L>
+__device__ __forceinline__ void fold(float* v, int& first) {
+  if constexpr (O >= L) {
+    constexpr int kLeft = N > 1 ? N / 2 : 1;
+    const bool upper = threadIdx.x & O;
+#pragma unroll
+    for (int k = 0; k < kLeft; ++k) {
+      const float send = N > 1 && !upper ? v[k + N - kLeft] : v[k], keep = N > 1 && upper ? v[k + N - kLeft] : v[k];
+      v[k] = keep + __shfl_xor(send, O, 64);
+    }
+    if (N > 1) first += upper ? kLeft : 0;
+    fold<kLeft, O / 2, L>(v, first);
+  }
+}
+
 // The loss from a wavefront's sums over experts (lane by lane) and the routed rows.
 __device__ __forceinline__ void write_loss(const RouteArgs& a, double entries, double cross, int rows) {
 #pragma unroll
@@ -241,13 +259,11 @@ __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool onl
   }
   if (rows) atomicAdd(&s_count[a.E], rows);
   // lanes with the same experts, then the wavefronts, in a fixed order
+  int at = 0;
+  fold<V, 32, L>(psum, at);
+  constexpr int kLeft = V * L > 64 ? V * L / 64 : 1;
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    float v = psum[j];
-#pragma unroll
-    for (int o = L; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-    if (lane < L) s_p[w][expert_of<L>(j, l)] = v;
-  }
+  for (int k = 0; k < kLeft; ++k) s_p[w][expert_of<L>(at + k, l)] = psum[k];
   __syncthreads();
   auto sum_of = [&](int e) {
     float v = 0.f;
