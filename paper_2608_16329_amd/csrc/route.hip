@@ -289,28 +289,44 @@ __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool onl
   }
 }
 
-// The work-groups' counts and sums added up in order, and the loss: a
-// wavefront for every 16th expert (and the routed rows), then one for all.  In 64
-// bits: the loss is a quotient of sums over all rows.  Latency: 5 us at 16 experts
-// of 256 work-groups, 12 at 64.
+// The work-groups' counts and sums added up in order, and the loss: 16 lanes for
+// an expert (and for the routed rows), each with every 16th work-group, 16 loads
+// of either under way at once; then a wavefront for all.  In 64 bits: the loss is a
+// quotient of sums over all rows.  Latency: 4 us up to 63 experts of 256
+// work-groups, 7 at 64 to 127.
 __global__ __launch_bounds__(1024) void k_route_total(RouteArgs a, int blocks) {
   __shared__ double s_p[kMaxExperts + 1];
   __shared__ int32_t s_c[kMaxExperts + 1];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  for (int e = w; e <= a.E; e += 16) {
+  for (int e0 = 0; e0 <= a.E; e0 += 64) {
+    const int e = e0 + (threadIdx.x >> 4);
+    // (places that there are none of: the last expert's)
+    const int32_t* pc = a.part_c + int64_t(e < a.E ? e : a.E) * blocks;
+    const float* pp = a.part_p + int64_t(e < a.E ? e : a.E - 1) * blocks;
     double p = 0.0;
     int c = 0;
-#pragma unroll 8
-    for (int b = lane; b < blocks; b += 64) {
-      c += a.part_c[int64_t(e) * blocks + b];
-      if (e < a.E) p += a.part_p[int64_t(e) * blocks + b];
+    for (int b0 = lane & 15; b0 < blocks; b0 += 256) {
+      int32_t vc[16];
+      float vp[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const int b = b0 + 16 * k < blocks ? b0 + 16 * k : blocks - 1;
+        vc[k] = pc[b];
+        vp[k] = pp[b];
+      }
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const bool there = b0 + 16 * k < blocks;
+        c += there ? vc[k] : 0;
+        p += there ? double(vp[k]) : 0.0;
+      }
     }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
+    for (int o = 8; o > 0; o >>= 1) {
       p += __shfl_xor(p, o, 64);
       c += __shfl_xor(c, o, 64);
     }
-    if (lane == 0) s_p[e] = p, s_c[e] = c, a.counts[e] = c;
+    if ((lane & 15) == 0 && e <= a.E) s_p[e] = p, s_c[e] = c, a.counts[e] = c;
   }
   __syncthreads();
   if (w == 0) {
