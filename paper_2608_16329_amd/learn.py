@@ -266,6 +266,7 @@ class AdamW(_OnStream):
         # the moments' zeros are written by the current stream
         self.stream.wait_stream(t.cuda.current_stream(self.device))
         self._states()
+        self._written = self._from
 
     def _states(self) -> None:
         self._from = b.mlip_adamw_state(_ptr(self.m), _ptr(self.v), _ptr(self.m_exp), _ptr(self.v_exp))
@@ -287,6 +288,7 @@ class AdamW(_OnStream):
         """Step number `step` (from 1).  seed: of the rounding of 8-bit moments, another one each step."""
         p = b.mlip_adamw_params(step, lr, beta1, beta2, eps, weight_decay, grad_scale, seed & 0xFFFFFFFF)
         self._run(b.mlip_adamw_step, self.plan, p, self._from, self._into, self._reverse)
+        self._written = self._into
 
     def accept(self) -> None:
         """With `into`: the next step starts from what the last one wrote."""
@@ -297,7 +299,8 @@ class AdamW(_OnStream):
         self._states()
 
     def moments(self, m, v) -> None:
-        """The values that 8-bit moments as the last step wrote them stand for, f32 [elements] each."""
+        """The values that 8-bit moments as the last step wrote them stand for,
+        accepted or not (before the first step: the start's), f32 [elements] each."""
         self._dense(m, "m", self.torch.float32, self.m.shape[0])
         self._dense(v, "v", self.torch.float32, self.m.shape[0])
-        self._run(b.mlip_adamw_moments, self.plan, self._into, _ptr(m), _ptr(v))
+        self._run(b.mlip_adamw_moments, self.plan, self._written, _ptr(m), _ptr(v))

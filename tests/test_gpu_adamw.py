@@ -206,6 +206,35 @@ def test_into_leaves_the_start_alone():
         assert torch.equal(opt.m, ref.m) and torch.equal(opt.v, ref.v)
 
 
+def test_moments_are_the_last_step_s():
+    """What the last step wrote, before and after it is accepted: the moments of
+    a plan that updates in place."""
+    import torch
+    from paper_2608_16329_amd import AdamW
+    sizes = SETS["odd"]
+    n = sum(sizes)
+    param, grad = make(sizes, "float32", "float32", 9)
+    twin, new = param.clone(), torch.empty_like(param)
+    opt = AdamW(param.split(sizes), grad.split(sizes), bits=8, into=new.split(sizes))
+    ref = AdamW(twin.split(sizes), grad.split(sizes), bits=8)
+
+    def values(o):
+        m, v = torch.empty(n, device="cuda:0"), torch.empty(n, device="cuda:0")
+        o.moments(m, v)
+        return m, v
+
+    assert not any(bool(x.any()) for x in values(opt))
+    for step in (1, 2, 3):
+        opt.step(step, lr=1e-3, seed=step)
+        ref.step(step, lr=1e-3, seed=step)
+        want = values(ref)
+        assert bool(want[0].any() and want[1].any())
+        before = values(opt)
+        opt.accept()
+        for got in (before, values(opt)):
+            assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
 def test_other_stream():
     import torch
     from paper_2608_16329_amd import AdamW
