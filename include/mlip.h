@@ -381,10 +381,13 @@ mlip_status mlip_md_kinetic(mlip_ctx* ctx, const double* vel_dev, double* ke_hos
  *
  * A mlip_learn context holds the stream, the workspace and the error text of
  * the calls made with it.  Work is enqueued on its stream; buffers are the
- * caller's, as above.  The context's device must be current (MLIP_E_ARG).  A call may enlarge the workspace (hipMalloc, and a
- * wait for the stream where an older one is freed) the first time it meets a
- * size; later calls of that size or smaller allocate nothing, and may be
- * recorded in a HIP graph.  All results
+ * caller's, as above.  The context's device must be current (MLIP_E_ARG).  A
+ * call may enlarge the workspace (hipMalloc, and a wait for the stream where an
+ * older one is freed) the first time it meets a size; later calls of that size
+ * or smaller allocate nothing, and may be recorded in a HIP graph (a call that
+ * would have to enlarge it while its stream is recorded is refused,
+ * MLIP_E_STATE).  A graph keeps to the workspace it was recorded with: record it
+ * anew after a call that enlarged it (mlip_learn_memory_bytes grew).  All results
  * are the same from run to run: nothing is summed in an order that depends on
  * the scheduling of work-groups.
  */
@@ -427,7 +430,7 @@ void mlip_learn_destroy(mlip_learn* ctx);
  * mlip_route wrote for the same logits; dgates_dev [n][top_k] (not looked at
  * where experts is -1) or NULL, dloss_dev [1] or NULL: none.
  * n in [0, 2^31 / top_k), n_experts 1..256, top_k 1..16 and <= n_experts.
- * Errors: MLIP_E_ARG, MLIP_E_OOM, MLIP_E_HIP.
+ * Errors: MLIP_E_ARG, MLIP_E_STATE, MLIP_E_OOM, MLIP_E_HIP.
  */
 typedef enum { MLIP_GATES_CHOSEN = 0, MLIP_GATES_ALL = 1 } mlip_gates;
 typedef struct {
@@ -453,7 +456,8 @@ mlip_status mlip_route_backward(mlip_learn* ctx, const mlip_route_params* p, int
  * indices, those of expert e at offsets_dev[e] .. offsets_dev[e + 1] - 1 in
  * rising order, and after offsets_dev[n_experts] those whose id is outside
  * [0, n_experts).  offsets_dev int32 [n_experts + 1].
- * n_entries in [0, 2^31), n_experts 1..256.  Errors: MLIP_E_ARG, MLIP_E_OOM, MLIP_E_HIP.
+ * n_entries in [0, 2^31), n_experts 1..256.  Errors: MLIP_E_ARG, MLIP_E_STATE,
+ * MLIP_E_OOM, MLIP_E_HIP.
  */
 mlip_status mlip_group(mlip_learn* ctx, int64_t n_entries, int32_t n_experts, const int32_t* experts_dev,
                        int32_t* offsets_dev, int32_t* order_dev);
@@ -477,7 +481,7 @@ mlip_status mlip_group(mlip_learn* ctx, int64_t n_entries, int32_t n_experts, co
  * Products, activations and sums are float32 whatever x's type; values of bf16
  * are rounded to nearest once, at the end.
  * n in [0, 2^31 / top_k), n_experts 1..256, width 1..1024, hidden 1..8, top_k
- * 1..16.  Errors: MLIP_E_ARG, MLIP_E_OOM, MLIP_E_HIP.
+ * 1..16.  Errors: MLIP_E_ARG, MLIP_E_STATE, MLIP_E_OOM, MLIP_E_HIP.
  */
 typedef struct {
   int32_t n_experts;

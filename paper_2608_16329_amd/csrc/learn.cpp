@@ -47,9 +47,14 @@ bool elsewhere(Ctx* ctx) {
 constexpr const char* kElsewhere = "the device of the context is not current";
 
 // The workspace holds at least `need` bytes; it is freed and allocated anew
-// where it is smaller, after the stream's work that may still use it.
+// where it is smaller, after the stream's work that may still use it.  Not while
+// the stream is recorded: the recording would end with an error at the wait.
 mlip_status workspace(mlip_learn* ctx, size_t need) {
   if (need <= ctx->cap_ws) return MLIP_OK;
+  hipStreamCaptureStatus recorded = hipStreamCaptureStatusNone;
+  LEARN_HIP(ctx, hipStreamIsCapturing(ctx->stream, &recorded));
+  if (recorded != hipStreamCaptureStatusNone)
+    return fail(ctx, MLIP_E_STATE, "the workspace is too small and the stream is being recorded: make the call once before");
   if (ctx->d_ws) {
     LEARN_HIP(ctx, hipStreamSynchronize(ctx->stream));
     (void)hipFree(ctx->d_ws);

@@ -164,3 +164,40 @@ def test_captured_training_step_replays():
         x.add_(0.01)
         torch.cuda.synchronize()
     keep.close(), keep_e.close(), opt.close(), opt_e.close()
+
+
+def test_a_recorded_call_does_not_enlarge_the_workspace():
+    """A first call of its size is refused while its stream is recorded; what else is recorded stays, and the call
+    works once it was made before."""
+    import torch
+    from paper_2608_16329_amd import Learner, MlipError
+    m, E = 20000, 7
+    ids = (torch.arange(m, device="cuda:0") * 5 % (E + 1)).to(torch.int32)
+    offsets, order = torch.zeros(E + 1, dtype=torch.int32, device="cuda:0"), torch.zeros(m, dtype=torch.int32, device="cuda:0")
+    few = torch.zeros(100, dtype=torch.int32, device="cuda:0")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    L = Learner(stream=s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        L.group(ids[:100], offsets, few)             # needs no workspace
+        with pytest.raises(MlipError, match="recorded"):
+            L.group(ids, offsets, order)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert L.memory_bytes() == 0 and few.long().bincount().tolist() == [1] * 100 and not bool(order.any())
+    with torch.cuda.stream(s):
+        L.group(ids, offsets, order)
+    torch.cuda.synchronize()
+    want = torch.sort(ids.cpu(), stable=True).indices.to(torch.int32)
+    assert torch.equal(order.cpu(), want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        L.group(ids, offsets, order)
+    for turn in range(3):
+        ids.copy_(ids.roll(turn + 1))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(order.cpu(), torch.sort(ids.cpu(), stable=True).indices.to(torch.int32))
+    L.close()
