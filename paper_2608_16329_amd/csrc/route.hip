@@ -154,8 +154,8 @@ __device__ __forceinline__ void write_loss(const RouteArgs& a, double entries, d
 // to its own place and are added up in order afterwards, so results do not depend
 // on the order of work-groups.
 // Bound by vector instructions, some 25 a logit and 5 more for each choice but
-// the first: 2,097,152 rows of 64 float32 logits, 4 chosen, 192 us (612 MB, 3.2
-// TB/s); 1,048,576 rows of 16 bfloat16, 2 chosen, 23 us (50 MB, 2.2 TB/s); 108 rows
+// the first: 2,097,152 rows of 64 float32 logits, 4 chosen, 193 us (612 MB, 3.2
+// TB/s); 1,048,576 rows of 16 bfloat16, 2 chosen, 21 us (50 MB, 2.4 TB/s); 108 rows
 // of 4, 6 us, most of it the launch and the loads' latency.
 template <int L, int V, bool BF, bool KINDS>
 __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool only) {
