@@ -549,6 +549,16 @@ __host__ __device__ __forceinline__ int64_t slot_values(int D, int H) {
   return int64_t((D + 63) / 64 + H - 1) * kR * kR + int64_t(H + 1) * kR + 64;
 }
 
+// The gradient of A_l needs y_{l-1} again (y_l - silu(z_l) would lose of it what
+// silu(z_l) is larger by).  That of the last layer waits in LDS from the forward
+// pass on; y_0 .. y_{kAgain - 1} are added up again from z; those between
+// are left in memory, layers_kept() of them: registers for 16 values a layer there
+// are none.  All gradients, 4 layers, 1,048,576 rows: 1,023 us so, 1,037 with y_0
+// and y_1 in memory too; 8 layers, 131,072 rows: 354 us, with all of them added up
+// again 388.
+constexpr int kAgain = 2;
+constexpr int layers_kept(int H) { return H > kAgain + 2 ? H - kAgain - 2 : 0; }
+
 // Energies, gradients in the descriptors and (TRAIN) in the weights.
 // 128 inputs, 4 layers: without weight gradients 262,144 rows 186 us (116 TFLOP/s
 // of float32 products as the formulas count them), with them 1,048,576 rows 1,080
@@ -581,6 +591,14 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
   const bool one = a.K == 1, with_dx = a.dx != nullptr;
   // the wavefront's tiles of a block: outputs 16 ta .., inputs 16 (tb + k) ..
   const int ta = NW == 8 ? w >> 1 : w, tb = NW == 8 ? 2 * (w & 1) : 0;
+
+  // values 16 t .. of y_l of the wavefront's rows in memory
+  constexpr int kKept = layers_kept(H);
+  float* const kept_here = a.kept + (int64_t(blockIdx.x) * kKept * NW + w) * (16 * kR);
+  auto kept = [&](int l, int t) {
+    float* from = kept_here + (l - kAgain) * (NW * 16 * kR);
+    return reinterpret_cast<f4*>(reinterpret_cast<char*>(from) + uint32_t(kFragBytes * t + here(16 * lane)));
+  };
 
   f4 sum_h[H > 1 ? H - 1 : 1][kOwn], sum_0[kChunksHeld][kOwn];
   f4 sum_b;                                   // of dc_t, column t: the sums of g_t are products with ones there
@@ -758,6 +776,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       auto activate = [&](int l, int t, Limbs<3>& next) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[t][i] += z[l][t][i] * sigmoid(z[l][t][i]);
+        if (TRAIN && l >= kAgain && l < kAgain + kKept) *kept(l, t) = y[t];
         if (l + 1 < H && (t & 1)) next.step(t >> 1, y[t - 1], y[t]);
       };
 #pragma unroll
@@ -766,6 +785,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
       for (int l = 1; l < H; ++l) {
         column(s_vec + l * kR, z[l]);
         ahead(chunks + (l + 1 < H ? l : l - 1), l + 1 == H);
+        if (TRAIN && l + 1 == H) put_limbs(s_y, x);   // for the first product over rows
         Limbs<3> after;
         product(s_w + cur * kBlockBytes, x, z[l], [&](int t) {
           if (t > 0) activate(l, t - 1, after);
@@ -796,19 +816,23 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         v += __shfl_xor(v, 32, 64);
         store_value(again(), r, v + s_vec[(H + 1) * kR]);
       }
-      // g_l = u silu'(z_l) of one tile, its limbs from two, and y_{l-1} from y_l
-      // (the sigmoid again: keeping y or silu' of every layer takes 16 registers
-      // a layer that there are not)
+      // (so that the compiler does not keep the forward pass's sigmoids)
+      auto again_z = [](float v) {
+        asm volatile("" : "+v"(v));
+        return v;
+      };
+      auto silu_again = [&](float v) {
+        v = again_z(v);
+        return v * sigmoid(v);
+      };
+      // g_l = u silu'(z_l) of one tile, its limbs from two (the sigmoid again: for
+      // silu' of every layer there are no registers either)
       f4 gz[4];
       auto back = [&](int l, int t) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          // (so that the compiler does not keep the forward pass's sigmoids)
-          float zl = z[l][t][i];
-          asm volatile("" : "+v"(zl));
-          const float s = sigmoid(zl);
+          const float zl = again_z(z[l][t][i]), s = sigmoid(zl);
           gz[t][i] = u[t][i] * (s * (1.f + zl * (1.f - s)));
-          if (TRAIN && l > 0) y[t][i] -= zl * s;
         }
         if (t & 1) x.step(t >> 1, gz[t - 1], gz[t]);
       };
@@ -820,9 +844,19 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
         if (TRAIN && l == 1) load_x<BF>(r, D, 0, in);   // for the chunks below
         if (TRAIN) put_limbs(s_g, x);
         product(s_w + cur * kBlockBytes, x, u, [&](int t) {
-          if (TRAIN) put_value(s_y, t, y[t]);
+          if (TRAIN && l <= kAgain && l + 1 < H) {
+            y[t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int b = 0; b < l; ++b)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) y[t][i] += silu_again(z[b][t][i]);
+          }
+          if (TRAIN && l + 1 < H) put_value(s_y, t, y[t]);
         });
         if (TRAIN) {
+          if (l - 2 >= kAgain)   // for the next layer down
+#pragma unroll
+            for (int t = 0; t < 4; ++t) y[t] = *kept(l - 2, t);
           __syncthreads();
           outer(limbs_y, sum_h[l - 1], l, [&](int t) { back(l - 1, t); });
         } else {
@@ -962,6 +996,9 @@ __global__ __launch_bounds__(256) void k_sum_entries(HeadsArgs a) {
   }
 }
 
+// What the work-groups keep of a tile's layers.
+size_t kept_values(const HeadsArgs& a) { return size_t(a.blocks) * size_t(layers_kept(a.H)) * size_t(16 * a.waves * kR); }
+
 // Work-groups of 256 for that many values, fewer than 2^32 threads a launch.
 unsigned blocks_for(int64_t values) { return unsigned(std::min<int64_t>((values + 255) / 256, 1 << 22)); }
 
@@ -1016,7 +1053,7 @@ size_t heads_plan(HeadsArgs* a, int n_cu) {
   a->slot = slot_values(a->D, a->H);
   a->split_block = (a->dx || a->dweights ? 2 : 1) * kBlockBytes;
   size_t b = size_t(a->E) * size_t((a->D + 63) / 64 + a->H - 1) * size_t(a->split_block);
-  if (a->dweights) b += size_t(a->blocks + a->E) * size_t(a->slot) * sizeof(float);
+  if (a->dweights) b += (size_t(a->blocks + a->E) * size_t(a->slot) + kept_values(*a)) * sizeof(float);
   if (a->K > 1 && a->energy) b += size_t(a->m) * sizeof(float);
   if (a->K > 1 && a->dx) b += size_t(a->m) * size_t(a->D) * sizeof(float);
   if (a->D < 4) b += size_t(a->n) * 4 * sizeof(float);
@@ -1027,7 +1064,10 @@ void heads_workspace(HeadsArgs* a, unsigned char* ws) {
   a->split = ws;
   ws += size_t(a->E) * size_t((a->D + 63) / 64 + a->H - 1) * size_t(a->split_block);
   float* at = reinterpret_cast<float*>(ws);
-  if (a->dweights) a->slots = at, at += int64_t(a->blocks + a->E) * a->slot;
+  if (a->dweights) {
+    a->slots = at, at += int64_t(a->blocks + a->E) * a->slot;
+    a->kept = at, at += kept_values(*a);
+  }
   if (a->K > 1 && a->dx) a->entry_dx = at, at += a->m * a->D;
   if (a->K > 1 && a->energy) a->entry_energy = at, at += a->m;
   if (a->D < 4) a->padded = at;

@@ -108,6 +108,7 @@ struct HeadsArgs {
   int64_t split_block;
   float* slots;               // [blocks + E][slot] sums of a work-group for a head
   int64_t slot;
+  float* kept;                // y of a tile's layers in the middle, 16 waves x 64 values each
 };
 // Sets waves, blocks, split_block and slot; the workspace in bytes, which
 // heads_workspace divides.
