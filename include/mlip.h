@@ -479,7 +479,8 @@ mlip_status mlip_group(mlip_learn* ctx, int64_t n_entries, int32_t n_experts, co
  *   dweights_dev f32 [n_experts][values of a head], 0 for heads without rows
  *   dgates_dev  f32 [n][top_k], denergy_i v_is, 0 at entries without a head
  * Products, activations and sums are float32 whatever x's type; values of bf16
- * are rounded to nearest once, at the end.
+ * are rounded to nearest once, at the end.  An infinity, or a value of 2^128 (1 -
+ * 2^-9) or more in size, makes what depends on it NaN.
  * n in [0, 2^31 / top_k), n_experts 1..256, width 1..1024, hidden 1..8, top_k
  * 1..16.  Errors: MLIP_E_ARG, MLIP_E_STATE, MLIP_E_OOM, MLIP_E_HIP.
  */

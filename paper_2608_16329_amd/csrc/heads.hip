@@ -14,11 +14,14 @@
 // the order in which the lane groups hold them).
 //
 // Products: a float32 is three bfloat16 limbs, exactly (24 bits in 8 + 8 + 8,
-// cut off, not rounded), and the product of two the six limb products above
-// 2^-24 of it, which 16x16x32 bfloat16 matrix instructions add up in float32.
-// That errs no more than float32 products, and six of them take 0.43 of the
-// time of the float32 matrix instructions (2,100 against 150 TFLOP/s in a loop
-// of nothing else).  Inputs in bfloat16 are one limb, and theirs are three products (all
+// each the rest rounded to nearest, so up to 2^-8 and 2^-17 of the value and of either
+// sign), and the product of two the six limb products but for those of a second
+// and a third, 2^-24 of it at most, which 16x16x32 bfloat16 matrix instructions
+// add up in float32.  (Limbs cut off would leave out 2^-22 each, of the product's sign.)
+// The instruction rounds to nearest where its addend is not the smaller part, and
+// otherwise down, by up to one unit in the last place, 0.17 on average.  Six
+// products take 0.43 of the time of the float32 matrix instructions (2,100 against
+// 150 TFLOP/s in a loop of nothing else).  Inputs in bfloat16 are one limb, and theirs are three products (all
 // gradients of 131,072 such rows of 128 values, two heads each: 366 us, with
 // six 415).  A first kernel splits the heads' matrices, in the order in
 // which lanes take them, for products with the matrix and with its transpose;
@@ -31,8 +34,9 @@
 // tiles of a head, which are written once and added up in order by a third
 // kernel.
 //
-// An infinity has no limbs: in a row it gives NaN, in that row and in the weights'
-// gradients, as a NaN does.  (The bias sums are products with ones and zeros, so a
+// An infinity has no limbs, nor has a value that rounds to one (2^128 (1 - 2^-9) and
+// more): in a row it gives NaN, in that row and in the weights' gradients, as a
+// NaN does.  (The bias sums are products with ones and zeros, so a
 // NaN in one layer's g is in the dc of all layers.)
 #include <algorithm>
 #include <type_traits>
@@ -47,6 +51,8 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 
 constexpr int kR = 64;                 // hidden width
@@ -59,7 +65,8 @@ __device__ __forceinline__ f4 mfma(u4 a, u4 b, f4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
 }
 
-// The sum of products of two numbers of three limbs, those above 2^-24 of it.
+// The sum of products of two numbers of three limbs, but for those of a second
+// and a third.
 __device__ __forceinline__ f4 products(const u4 a[3], const u4 (&b)[3], f4 c) {
   c = mfma(a[2], b[0], c);
   c = mfma(a[0], b[2], c);
@@ -77,17 +84,16 @@ __device__ __forceinline__ f4 products(const u4 a[3], const u4 (&b)[1], f4 c) {
 
 // Limb k of four values, two to a register.
 __device__ __forceinline__ void split4(const f4 v, u2 limb[3]) {
-  float r[4] = {v[0], v[1], v[2], v[3]};
+  f2 r[2] = {{v[0], v[1]}, {v[2], v[3]}};
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    uint32_t u[4];
+  for (int k = 0; k < 3; ++k)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(r[i]);
-    limb[k][0] = __builtin_amdgcn_perm(u[1], u[0], 0x07060302u);
-    limb[k][1] = __builtin_amdgcn_perm(u[3], u[2], 0x07060302u);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] -= __uint_as_float(u[i] & 0xffff0000u);
-  }
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t u = __builtin_bit_cast(uint32_t, __builtin_convertvector(r[i], bf2));
+      limb[k][i] = u;
+      r[i][0] -= __uint_as_float(u << 16);
+      r[i][1] -= __uint_as_float(u & 0xffff0000u);
+    }
 }
 
 // Four bfloat16 are one limb as they are.
