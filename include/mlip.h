@@ -386,10 +386,12 @@ mlip_status mlip_md_kinetic(mlip_ctx* ctx, const double* vel_dev, double* ke_hos
  * older one is freed) the first time it meets a size; later calls of that size
  * or smaller allocate nothing, and may be recorded in a HIP graph (a call that
  * would have to enlarge it while its stream is recorded is refused,
- * MLIP_E_STATE).  A graph keeps to the workspace it was recorded with: record it
- * anew after a call that enlarged it (mlip_learn_memory_bytes grew).  All results
- * are the same from run to run: nothing is summed in an order that depends on
- * the scheduling of work-groups.
+ * MLIP_E_STATE).  A graph keeps to the workspace it was recorded with, which
+ * stays allocated until the context is released, also where a later call needs
+ * a larger one (mlip_learn_memory_bytes counts both).  Replay it in order with
+ * the context's calls, and not after the context, or a plan whose step it has,
+ * is released.  All results are the same from run to run: nothing is summed in
+ * an order that depends on the scheduling of work-groups.
  */
 typedef struct mlip_learn mlip_learn;
 typedef enum { MLIP_F32 = 0, MLIP_BF16 = 1 } mlip_dtype;

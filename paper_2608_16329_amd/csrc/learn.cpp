@@ -46,20 +46,42 @@ bool elsewhere(Ctx* ctx) {
 }
 constexpr const char* kElsewhere = "the device of the context is not current";
 
-// The workspace holds at least `need` bytes; it is freed and allocated anew
-// where it is smaller, after the stream's work that may still use it.  Not while
-// the stream is recorded: the recording would end with an error at the wait.
+// The workspace holds at least `need` bytes; it is allocated anew where it is
+// smaller, and freed after the stream's work that may still use it, or, where a
+// recorded call has it, with the context: the graph may be replayed at any time.
+// Not while the stream is recorded: the recording would end with an error at the
+// wait.
 mlip_status workspace(mlip_learn* ctx, size_t need) {
-  if (need <= ctx->cap_ws) return MLIP_OK;
+  if (need == 0) return MLIP_OK;
+  if (need <= ctx->cap_ws) {
+    // (the null stream cannot be recorded; without an answer it may be)
+    if (ctx->stream && !ctx->recorded_ws) {
+      hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+      const bool known = hipStreamIsCapturing(ctx->stream, &status) == hipSuccess;
+      if (!known) (void)hipGetLastError();
+      ctx->recorded_ws = !known || status != hipStreamCaptureStatusNone;
+    }
+    return MLIP_OK;
+  }
   hipStreamCaptureStatus recorded = hipStreamCaptureStatusNone;
   LEARN_HIP(ctx, hipStreamIsCapturing(ctx->stream, &recorded));
   if (recorded != hipStreamCaptureStatusNone)
     return fail(ctx, MLIP_E_STATE, "the workspace is too small and the stream is being recorded: make the call once before");
   if (ctx->d_ws) {
-    LEARN_HIP(ctx, hipStreamSynchronize(ctx->stream));
-    (void)hipFree(ctx->d_ws);
+    if (ctx->recorded_ws) {
+      try {
+        ctx->kept.push_back(ctx->d_ws);
+      } catch (...) {
+        return fail(ctx, MLIP_E_OOM, "host allocation failed");
+      }
+      ctx->kept_bytes += ctx->cap_ws;
+    } else {
+      LEARN_HIP(ctx, hipStreamSynchronize(ctx->stream));
+      (void)hipFree(ctx->d_ws);
+    }
     ctx->d_ws = nullptr;
     ctx->cap_ws = 0;
+    ctx->recorded_ws = false;
   }
   const size_t size = (need + need / 4 + 255) / 256 * 256;
   if (hipMalloc(reinterpret_cast<void**>(&ctx->d_ws), size) != hipSuccess) {
@@ -159,7 +181,7 @@ const char* mlip_learn_last_error(const mlip_learn* ctx) { return ctx ? ctx->err
 
 mlip_status mlip_learn_memory_bytes(const mlip_learn* ctx, size_t* bytes) {
   if (!ctx || !bytes) return MLIP_E_ARG;
-  *bytes = ctx->cap_ws;
+  *bytes = ctx->cap_ws + ctx->kept_bytes;
   return MLIP_OK;
 }
 
@@ -167,6 +189,7 @@ void mlip_learn_destroy(mlip_learn* ctx) {
   if (!ctx) return;
   (void)hipStreamSynchronize(ctx->stream);
   if (ctx->d_ws) (void)hipFree(ctx->d_ws);
+  for (unsigned char* ws : ctx->kept) (void)hipFree(ws);
   (void)hipGetLastError();
   delete ctx;
 }

@@ -7,6 +7,7 @@
 #include <cstddef>
 #include <cstdint>
 #include <string>
+#include <vector>
 
 #include "../../include/mlip.h"
 
@@ -34,6 +35,9 @@ struct mlip_learn {
   std::string err;
   unsigned char* d_ws = nullptr;  // workspace of the calls, in the order of the stream
   size_t cap_ws = 0;
+  bool recorded_ws = false;       // a recorded call uses it
+  std::vector<unsigned char*> kept;   // earlier workspaces that recorded calls use
+  size_t kept_bytes = 0;
 };
 
 struct mlip_adamw {
