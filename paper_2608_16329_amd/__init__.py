@@ -81,18 +81,24 @@ class Potential:
     def descriptors(self, pos, rows) -> None:
         """Descriptors of `pos` into `rows`, float32 [n, (lmax + 1) k], for heads
         outside the fused evaluation (mlip_descriptors; needs MLIP_FUSION_PARTIAL)."""
-        assert pos.is_cuda and pos.dtype == self.torch.float64 and pos.is_contiguous()
+        self._check_atoms(pos, "positions", 3)
         self._check_rows(rows)
         binding.mlip_descriptors(self.ctx, pos.data_ptr(), rows.data_ptr())
 
     def forces_from_descriptors(self, pos, drows, forces, virial=None) -> None:
         """Forces (and virials) of energies whose gradient in the descriptors is
         `drows` (mlip_forces_from_descriptors; needs MLIP_FUSION_PARTIAL)."""
-        assert pos.is_cuda and pos.dtype == self.torch.float64 and pos.is_contiguous()
-        assert forces.is_cuda and forces.dtype == self.torch.float64 and forces.is_contiguous()
+        self._check_atoms(pos, "positions", 3)
+        self._check_atoms(forces, "forces", 3)
+        if virial is not None:
+            self._check_atoms(virial, "virials", 9)
         self._check_rows(drows)
         binding.mlip_forces_from_descriptors(self.ctx, pos.data_ptr(), drows.data_ptr(), forces.data_ptr(),
                                              virial.data_ptr() if virial is not None else None)
+
+    def _check_atoms(self, t, name: str, values: int) -> None:
+        assert t.is_cuda and t.dtype == self.torch.float64 and t.is_contiguous()
+        assert t.numel() == self.n * values, f"{name} have {t.numel()} values, not {self.n} x {values}"
 
     def _check_rows(self, rows) -> None:
         assert rows.is_cuda and rows.dtype == self.torch.float32 and rows.is_contiguous()
