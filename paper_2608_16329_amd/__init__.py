@@ -80,10 +80,12 @@ class Potential:
 
     def descriptors(self, pos, rows) -> None:
         """Descriptors of `pos` into `rows`, float32 [n, (lmax + 1) k], for heads
-        outside the fused evaluation (mlip_descriptors; needs MLIP_FUSION_PARTIAL)."""
+        outside the fused evaluation (mlip_descriptors; needs MLIP_FUSION_PARTIAL).
+        Put in order with the current stream where that is not the potential's own,
+        as a Learner's calls are, and forces_from_descriptors too."""
         self._check_atoms(pos, "positions", 3)
         self._check_rows(rows)
-        binding.mlip_descriptors(self.ctx, pos.data_ptr(), rows.data_ptr())
+        self._ordered(binding.mlip_descriptors, self.ctx, pos.data_ptr(), rows.data_ptr())
 
     def forces_from_descriptors(self, pos, drows, forces, virial=None) -> None:
         """Forces (and virials) of energies whose gradient in the descriptors is
@@ -93,8 +95,18 @@ class Potential:
         if virial is not None:
             self._check_atoms(virial, "virials", 9)
         self._check_rows(drows)
-        binding.mlip_forces_from_descriptors(self.ctx, pos.data_ptr(), drows.data_ptr(), forces.data_ptr(),
-                                             virial.data_ptr() if virial is not None else None)
+        self._ordered(binding.mlip_forces_from_descriptors, self.ctx, pos.data_ptr(), drows.data_ptr(), forces.data_ptr(),
+                      virial.data_ptr() if virial is not None else None)
+
+    def _ordered(self, call, *args) -> None:
+        """The call's work after what the current stream has, and what it gets next after the call's."""
+        current = self.torch.cuda.current_stream(self.stream.device)
+        if current == self.stream:
+            call(*args)
+            return
+        self.stream.wait_stream(current)
+        call(*args)
+        current.wait_stream(self.stream)
 
     def _check_atoms(self, t, name: str, values: int) -> None:
         assert t.is_cuda and t.dtype == self.torch.float64 and t.is_contiguous()
