@@ -210,12 +210,17 @@ class AdamW(_OnStream):
     the same tensors.  decay: one truth value a tensor, whether weight_decay
     applies (default: to those with two dimensions or more).  The moments are `m`
     and `v`, flat over the tensors back to back, with 8 bits codes beside
-    `m_exp` and `v_exp`; they start as zeros and may be read and overwritten.
+    `m_exp` and `v_exp`; they start as zeros, may be read, and are overwritten
+    in place (opt.m.copy_(saved)): the plan holds their places.
 
     into: tensors that new parameters go to, like `params`; `new_m`, `new_v`
     (`new_m_exp`, `new_v_exp`) receive the new moments.  A step then changes
     nothing that it reads; `accept` makes what it wrote the next step's start
     and the old values the place to write to."""
+
+    m, v, m_exp, v_exp, new_m, new_v, new_m_exp, new_v_exp = (
+        property(lambda self, name=name: self._moments[name]) for name in
+        ("m", "v", "m_exp", "v_exp", "new_m", "new_v", "new_m_exp", "new_v_exp"))
 
     def __init__(self, params, grads, *, bits: int = 32, decay=None, into=None, stream=None):
         self.plan = None
@@ -254,15 +259,14 @@ class AdamW(_OnStream):
 
             def zeros(m, dtype):
                 return t.zeros(m, dtype=dtype, device=self.device)
-            self.m_exp = self.v_exp = self.new_m_exp = self.new_v_exp = None
             kind = t.float32 if bits == 32 else t.uint8
-            self.m, self.v = zeros(n, kind), zeros(n, kind)
+            held = {"m": (n, kind), "v": (n, kind)}
             if bits == 8:
-                self.m_exp, self.v_exp = zeros(blocks, t.uint8), zeros(blocks, t.uint8)
-            self.new_m, self.new_v = (zeros(n, kind), zeros(n, kind)) if self._twice else (self.m, self.v)
-            if bits == 8:
-                self.new_m_exp, self.new_v_exp = (zeros(blocks, t.uint8), zeros(blocks, t.uint8)) if self._twice \
-                    else (self.m_exp, self.v_exp)
+                held.update(m_exp=(blocks, t.uint8), v_exp=(blocks, t.uint8))
+            self._moments = dict.fromkeys(("m_exp", "v_exp", "new_m_exp", "new_v_exp"))
+            for name, of in held.items():
+                self._moments[name] = zeros(*of)
+                self._moments["new_" + name] = zeros(*of) if self._twice else self._moments[name]
         # the moments' zeros are written by the current stream
         self.stream.wait_stream(t.cuda.current_stream(self.device))
         self._states()
@@ -294,8 +298,9 @@ class AdamW(_OnStream):
         """With `into`: the next step starts from what the last one wrote."""
         _need(self._twice, "accept() is for a plan with into")
         self._reverse = not self._reverse
-        self.m, self.new_m, self.v, self.new_v = self.new_m, self.m, self.new_v, self.v
-        self.m_exp, self.new_m_exp, self.v_exp, self.new_v_exp = self.new_m_exp, self.m_exp, self.new_v_exp, self.v_exp
+        k = self._moments
+        for name in ("m", "v", "m_exp", "v_exp"):
+            k[name], k["new_" + name] = k["new_" + name], k[name]
         self._states()
 
     def moments(self, m, v) -> None:
