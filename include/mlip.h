@@ -425,7 +425,8 @@ void mlip_learn_destroy(mlip_learn* ctx);
  *               counts_e / sum counts and P_e the mean of p_ie over the rows
  *               that have any expert: 1 where all experts are used alike, up to
  *               n_experts where one is; 0 without such rows
- * A NaN (or +infinity) among the logits a row may use makes its gates NaN.
+ * A NaN (or +infinity) among the logits a row may use makes all its gates NaN,
+ * those at -1 too (a NaN is never chosen).
  * mlip_route_backward writes the logits' gradient (their type, [n][n_experts]
  * contiguous) of sum(dgates gates) + dloss loss: the choice of experts and the
  * shares f_e are constants of it.  experts_dev and counts_dev are what
