@@ -527,8 +527,14 @@ mlip_status mlip_heads(mlip_learn* ctx, const mlip_heads_params* p, int64_t n, c
  * part that is cut off (to nearest, v would never change: a step moves it by
  * less than half of what its codes are apart); the random bits are mixed from
  * `seed` (another one each step) and the element's place, so a step can be
- * repeated bit for bit.  A v that is not 0 is not rounded to 0.  An element
- * whose moment is not finite keeps NaN and leaves its block's others alone.
+ * repeated bit for bit.  An element whose moment is not finite keeps NaN and
+ * leaves its block's others alone; a size of 2^127 and more is held as the
+ * largest code.
+ * A v that is not 0 is not rounded to 0: less than 2^-18 2^e is held as that.
+ * So where an element's gradients stay below 1/512 to 1/362 of the largest of
+ * its block (the root of v's share of 2^e), its v is too large and its steps are
+ * shorter than with 32 bits, by the root of v / (2^-18 2^e).  Tensors whose
+ * gradients spread wider than that within 256 neighbours want 32 bits.
  *
  * mlip_adamw_create  tensors: host array, copied; into_dev, for all tensors or
  *                    for none: where new parameters go (NULL: param_dev), equal

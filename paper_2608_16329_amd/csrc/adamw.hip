@@ -13,8 +13,10 @@
 // v 2^-e; exponent field E > 0 stands for 2^(E - 15) (1 + f), 0 for subnormal
 // 2^-14 f.  v changes by a part of 1 - b2 a step, less than half the distance
 // of its codes, so rounding to nearest would hold it where it is: both are
-// rounded up or down at random, up with the probability of the part cut off,
-// by bits mixed from the caller's seed and the element's place.
+// rounded up or down at random, up with the probability of the part cut off (to
+// 2^-16), by bits mixed from the caller's seed and the element's place.  On average
+// that is the value, but for a v below the smallest code, 2^-18 2^e, which is
+// raised to it.
 #include <algorithm>
 
 #include "learn.h"
@@ -60,7 +62,8 @@ __device__ __forceinline__ uint32_t encode(float x, int e, float up) {
   const int ey = max(int(__float_as_uint(y) >> 23) - 127, -14);
   uint32_t code = ((uint32_t(ey + 14)) << M) + uint32_t(floorf(y * pow2(M - ey) + up));
   code = min(code, M == 3 ? 126u : 254u);
-  // a v that is not zero stays so: m / sqrt(v) would run away
+  // a v that is not zero stays so: m / sqrt(v) would run away; a v that is too
+  // large only shortens steps
   if (M == 4 && size > 0.f && code == 0) code = 1;
   return M == 3 && x < 0.f ? code | 128u : code;
 }
