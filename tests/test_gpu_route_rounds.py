@@ -23,3 +23,87 @@ def test_all_gates_of_a_row_with_nan_are_nan():
             assert torch.isnan(gates).all(1).tolist() == [True, True, False, False]
             assert gates[2:, 2].tolist() == [0.0, 0.0] and bool((gates[2:, :2] > 0).all())
             assert counts[:4].tolist() == [1, 3, 1, 0] and int(counts[E]) == 4 and bool(torch.isnan(loss))
+
+
+def reference(z, usable, k, gates_of):
+    """Experts, gates, counts, loss and p from logits in float64 and what rows may use."""
+    import torch
+    n, E = z.shape
+    open_ = usable & (z != -float("inf"))
+    z = torch.where(open_, z, -float("inf"))
+    live = open_.any(1)
+    p = torch.where(live[:, None], torch.softmax(torch.where(live[:, None], z, 0.0), 1), 0.0)
+    ids = torch.sort(z, dim=1, descending=True, stable=True).indices[:, :k]
+    there = open_.gather(1, ids)
+    gates = torch.where(there, p.gather(1, ids), 0.0)
+    if gates_of == "chosen":
+        gates = gates / torch.where(live, gates.sum(1), 1.0)[:, None]
+    counts = torch.stack([(there & (ids == e)).sum() for e in range(E)] + [live.sum()])
+    share = counts[:E].double() / counts[:E].sum().clamp(min=1)
+    loss = E * (share * p.sum(0)).sum() / live.sum().clamp(min=1)
+    return torch.where(there, ids, -1), gates, counts, loss, p, share
+
+
+def gradient(p, ids, gates, share, rows, gates_of, dgates, dloss):
+    import torch
+    E = p.shape[1]
+    there, at = ids >= 0, ids.clamp(min=0)
+    g = torch.where(there, dgates, 0.0)
+    h = (dloss * E * share / rows)[None, :].expand_as(p)
+    if gates_of == "all":
+        h = h.scatter_add(1, at, g)
+    d = p * (h - (p * h).sum(1, keepdim=True))
+    if gates_of == "chosen":
+        d = d.scatter_add(1, at, gates * (g - (gates * g).sum(1, keepdim=True)))
+    return d
+
+
+@pytest.mark.parametrize("rows,experts,top_k,n_kinds,spare", [(150000, 250, 5, 6, 3), (1200000, 5, 2, 4, 0), (600001, 16, 3, 3, 0),
+                                                              (400000, 61, 4, 0, 1)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("gates_of", ["chosen", "all"])
+def test_many_rounds_a_work_group(rows, experts, top_k, n_kinds, spare, dtype, gates_of):
+    """Rows, their kinds and their choices' gradients from one round to the next.  Tolerances as in test_gpu_route.py."""
+    import torch
+    from paper_2608_16329_amd import Learner
+    dev, dt = torch.device("cuda:0"), getattr(torch, dtype)
+    g = torch.Generator(device=dev).manual_seed(rows)
+    z = torch.full((rows, experts + spare), float("nan"), dtype=dt, device=dev)[:, :experts]
+    z.copy_(torch.randn((rows, experts), generator=g, device=dev) * 2)
+    z[torch.rand(rows, generator=g, device=dev) < 0.01] = -float("inf")
+    usable = torch.ones((rows, experts), dtype=torch.bool, device=dev)
+    how = dict(gates_of=gates_of)
+    z64 = z.double()
+    if n_kinds:
+        kinds = torch.randint(-1, n_kinds + 1, (rows,), generator=g, device=dev, dtype=torch.int32)
+        allowed = (torch.rand((n_kinds, experts), generator=g, device=dev) < 0.6).to(torch.uint8)
+        allowed[0] = 0
+        real = (kinds >= 0) & (kinds < n_kinds)
+        usable = real[:, None] & (allowed[kinds.long().clamp(0, n_kinds - 1)] != 0)
+        z[~usable] = float("nan")
+        z64 = torch.where(usable, z64, 0.0)
+        how.update(kinds=kinds, allowed=allowed)
+    ids, gates, counts, loss, p, share = reference(z64, usable, top_k, gates_of)
+    dg = torch.randn((rows, top_k), generator=g, device=dev)
+    dg[ids < 0] = float("nan")                       # not looked at
+    want = gradient(p, ids, gates, share, counts[experts].clamp(min=1), gates_of, dg.double(), 0.3 * rows)
+    L = Learner()
+    out = []
+    for _ in range(2):
+        got = dict(experts=torch.full((rows, top_k), 7, dtype=torch.int32, device=dev), gates=torch.full((rows, top_k), 9.0, device=dev),
+                   counts=torch.zeros(experts + 1, dtype=torch.int32, device=dev), loss=torch.zeros(1, device=dev),
+                   dlogits=torch.full((rows, experts), 9.0, dtype=dt, device=dev))
+        L.route(z, got["experts"], got["gates"], got["counts"], got["loss"], **how)
+        L.route_backward(z, got["experts"], got["counts"], got["dlogits"], dgates=dg,
+                         dloss=torch.full((1,), 0.3 * rows, device=dev), **how)
+        out.append(got)
+    got = out[0]
+    for name in got:
+        assert torch.equal(got[name], out[1][name]), name
+    assert torch.equal(got["experts"].long(), ids) and torch.equal(got["counts"].long(), counts)
+    assert float((got["gates"].double() - gates).abs().max()) <= 1e-5
+    assert abs(float(got["loss"]) - float(loss)) <= 1e-5 * float(loss)
+    err = (got["dlogits"].double() - want).abs()
+    # (dloss is the number of rows, so that the balance loss's part is of the gates' size)
+    assert bool((err <= 2e-5 + (2.0 ** -8 * want.abs() if dtype == "bfloat16" else 0.0)).all()), float(err.max())
+    L.close()
