@@ -2,6 +2,7 @@
 of more pieces than work-groups."""
 import math
 
+import numpy as np
 import pytest
 
 from tests.gpu_helpers import log
@@ -62,3 +63,59 @@ def test_the_largest_sizes():
     opt.moments(m, v)
     assert opt.v_exp.tolist() == [126 + 127]
     assert v.tolist() == [1.875 * 2.0 ** 126] * 256
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("gtype", ["float32", "bfloat16"])
+def test_more_pieces_than_work_groups(bits, gtype):
+    """7,900 pieces for at most 2,048 work-groups: long tensors, thousands of one element, and odd ones.  Moments and codes
+    exactly as float32 operations one by one give them; parameters as in test_gpu_adamw.py."""
+    import torch
+    from paper_2608_16329_amd import AdamW
+    from tests.test_gpu_adamw import dice, f32, make, pow2
+    sizes = [5000003] + [1] * 3000 + [257, 1025, 0, 255] + [1024] * 3
+    n = sum(sizes)
+    param, grad = make(sizes, "float32", gtype, 5)
+    opt = AdamW(param.split(sizes), grad.split(sizes), bits=bits, decay=[k % 2 == 0 for k in range(len(sizes))])
+    starts = np.cumsum([0] + sizes[:-1])
+    first = np.concatenate([a + np.arange(0, z, 256) for a, z in zip(starts, sizes) if z])       # of every block
+    block = np.repeat(np.arange(len(first)), np.diff(np.append(first, n)))
+    lr, b1, b2, eps, wd = 1e-3, 0.9, 0.99, 1e-8, 0.05
+    keep = np.repeat(np.where(np.arange(len(sizes)) % 2 == 0, f32(1 - lr * wd), f32(1)), sizes).astype(f32)
+    m = v = np.zeros(n, f32)
+
+    def held(x, mant, up):
+        size = np.abs(x)
+        e = np.clip((np.maximum.reduceat(size, first).view(np.int32) >> 23) - 126, -126, 126)
+        y = size * pow2(-e)[block]
+        ey = np.maximum((y.view(np.int32) >> 23) - 127, -14)
+        code = ((ey + 14) << mant) + np.floor((y * pow2(mant - ey)) + up).astype(np.int32)
+        code = np.minimum(code, 126 if mant == 3 else 254)
+        if mant == 4:
+            code = np.where((size > 0) & (code == 0), 1, code)
+        ec = code >> mant
+        near = ((code & (2 ** mant - 1)) + np.where(ec > 0, 2 ** mant, 0)).astype(f32) * pow2(np.maximum(ec, 1) - 15 - mant) * pow2(e)[block]
+        return e + 127, np.where(x < 0, code | 128, code) if mant == 3 else code, np.where(x < 0, -near, near).astype(f32)
+
+    for step in (1, 2, 3):
+        p = param.cpu().numpy().astype(np.float64)
+        opt.step(step, lr=lr, beta1=b1, beta2=b2, eps=eps, weight_decay=wd, seed=step)
+        torch.cuda.synchronize()
+        gr = grad.float().cpu().numpy()
+        m = m * f32(b1) + gr * f32(1 - b1)
+        v = v * f32(b2) + (gr * gr) * f32(1 - b2)
+        up = lr / (1 - b1 ** step) * m.astype(np.float64) / (np.sqrt(v.astype(np.float64)) / math.sqrt(1 - b2 ** step) + eps)
+        got = param.cpu().numpy()
+        assert (np.abs(got - (p * keep - up)) <= 1e-6 * np.abs(up) + 2.0 ** -23 * np.abs(p)).all()
+        if bits == 32:
+            assert np.array_equal(opt.m.cpu().numpy(), m) and np.array_equal(opt.v.cpu().numpy(), v)
+            continue
+        r = dice(step, np.arange(n))
+        for x, mant, bitsof, codes, exps in ((m, 3, r & 0xFFFF, opt.m, opt.m_exp), (v, 4, r >> 16, opt.v, opt.v_exp)):
+            e, code, near = held(x, mant, bitsof.astype(f32) * f32(2.0 ** -16))
+            assert np.array_equal(exps.cpu().numpy(), e) and np.array_equal(codes.cpu().numpy(), code)
+            x[:] = near
+        vals = [torch.empty(n, device="cuda:0") for _ in range(2)]
+        opt.moments(*vals)
+        assert np.array_equal(vals[0].cpu().numpy(), m) and np.array_equal(vals[1].cpu().numpy(), v)
+    opt.close()
