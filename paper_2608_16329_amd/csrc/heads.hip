@@ -21,9 +21,9 @@
 // The instruction rounds to nearest where its addend is not the smaller part, and
 // otherwise down, by up to one unit in the last place, 0.17 on average.  Six
 // products take 0.43 of the time of the float32 matrix instructions (2,100 against
-// 150 TFLOP/s in a loop of nothing else).  Inputs in bfloat16 are one limb, and theirs are three products (all
-// gradients of 131,072 such rows of 128 values, two heads each: 366 us, with
-// six 415).  A first kernel splits the heads' matrices, in the order in
+// 150 TFLOP/s in a loop of nothing else).  Inputs in bfloat16 are one limb, and theirs are three
+// products (all gradients of 131,071 such rows of 192 values, two heads each, took
+// 0.88 of the time with six).  A first kernel splits the heads' matrices, in the order in
 // which lanes take them, for products with the matrix and with its transpose;
 // the main kernel brings them to LDS one 64x64 block at a time, the next block
 // on its way while one is used.
@@ -191,7 +191,7 @@ __device__ __forceinline__ void column(const float* base, f4 v[4]) {
 }
 // The kernel's arguments read again: held in scalar registers across the loop
 // over tiles, they do not fit beside the rest, and come and go through vector
-// registers.
+// registers (50 to 70 of the weight gradients' still do).
 __device__ __forceinline__ const HeadsArgs& again() {
   typedef const __attribute__((address_space(4))) HeadsArgs* Args;
   Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
@@ -448,8 +448,8 @@ __device__ __forceinline__ void load_vectors(const float* wt, int D, int H, floa
 
 // Energies alone.  Two work-groups a CU (52 KB of LDS each), each with a share of
 // the tiles, so that heads of all sizes fill the chip.  262,144 rows of 128 inputs,
-// 4 layers: 100 us, 108 TFLOP/s.  Bound by issue: limbs and activations beside the
-// products.
+// 4 layers: 92 us, 117 TFLOP/s of float32 products as the formulas count them.
+// Bound by issue: limbs and activations beside the products.
 template <int NW, bool BF>
 __global__ __launch_bounds__(NW * 64) void k_energy(HeadsArgs a) {
   constexpr int kRows = 16 * NW;
@@ -566,12 +566,14 @@ constexpr int kAgain = 2;
 constexpr int layers_kept(int H) { return H > kAgain + 2 ? H - kAgain - 2 : 0; }
 
 // Energies, gradients in the descriptors and (TRAIN) in the weights.
-// 128 inputs, 4 layers: without weight gradients 262,144 rows 186 us (116 TFLOP/s
-// of float32 products as the formulas count them), with them 1,048,576 rows 1,080
-// to 1,100 us (117; the float32 matrix instructions reach 150 in a loop of nothing
-// else).  At that size the matrix pipes are busy for 33% of the time, the vector
-// ones for 45%, LDS for 29%; the rest are barriers and waits between steps, with two wavefronts a SIMD, as many as the registers of z
-// and the sums allow.  A row alone takes 15 us: one wavefront's 5,600
+// 128 inputs, 4 layers, in a series of calls: without weight gradients 262,144 rows
+// 163 us (132 TFLOP/s of float32 products as the formulas count them), with them
+// 1,048,576 rows 997 us (130; the float32 matrix instructions reach 150 in a loop
+// of nothing else); the first calls after a pause take 14 to 17% longer.  With them
+// the matrix pipes are busy for 34% of the time, vector and matrix instructions are
+// issued for 48%, a wavefront waits for 36% of its own, at barriers and between
+// steps, with two wavefronts a SIMD, as many as the registers of z and the sums
+// allow; without them 37, 52 and 31%.  A row alone takes 15 us: one wavefront's 5,600
 // instructions, one after another.
 template <int H, int NW, bool TRAIN, bool BF>
 __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(HeadsArgs args) {
@@ -915,7 +917,7 @@ __global__ __launch_bounds__(NW * 64, TRAIN && NW == 4 ? 1 : 2) void k_gradient(
 }
 
 // A head's weight gradients: the slots of the work-groups that had tiles of
-// it, added up in order (atomics would add them in any).  10 us for 262 slots of
+// it, added up in order (atomics would add them in any).  9 us for 262 slots of
 // 21,000 values, 22 MB from the caches.
 template <int NW>
 __global__ __launch_bounds__(256) void k_sum_slots(HeadsArgs a) {
@@ -975,7 +977,7 @@ __global__ __launch_bounds__(256) void k_pad(const T* x, int64_t n, int64_t stri
 
 // Rows with several entries: their energies and gradients added up in order,
 // in float32 (one rounding to the rows' type, at the end).  Bound by memory:
-// 131,071 rows of 192, two entries each, 40 us (252 MB, 6.3 TB/s, part of it from
+// 131,071 rows of 192, two entries each, 39 us (252 MB, 6.5 TB/s, part of it from
 // the last-level cache).
 __global__ __launch_bounds__(256) void k_sum_entries(HeadsArgs a) {
   const int64_t first = int64_t(blockIdx.x) * 256 + threadIdx.x, step = int64_t(gridDim.x) * 256;
@@ -1045,8 +1047,8 @@ hipError_t gradient_by_layers(const HeadsArgs& a, hipStream_t s) {
 // Wavefronts of a work-group, 16 rows each.  For weight gradients eight, two a
 // SIMD; four where each CU has at most one tile of 64 rows, which is sooner done
 // than one of 128 (6 heads of 128 inputs and 3 layers, all gradients, with the
-// grouping: 5,000 rows 47 us with four, 54 with eight, 10,000 rows 52 and 59;
-// 20,000 rows 72 and 60, 100,000 rows 167 and 145), or where z of more than four
+// grouping: 5,000 rows 42 us with four, 48 with eight, 10,000 rows 48 and 52;
+// 20,000 rows 64 and 54, 100,000 rows 146 and 124), or where z of more than four
 // layers and the sums of their gradients need all of a SIMD's registers.  Without
 // weight gradients four, and two work-groups a CU that need not wait for each
 // other.

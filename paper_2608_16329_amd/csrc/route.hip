@@ -153,10 +153,15 @@ __device__ __forceinline__ void write_loss(const RouteArgs& a, double entries, d
 // row and the lowest place that has it.  Each work-group's counts and sums of p go
 // to its own place and are added up in order afterwards, so results do not depend
 // on the order of work-groups.
-// Bound by vector instructions, some 25 a logit and 5 more for each choice but
-// the first: 2,097,152 rows of 64 float32 logits, 4 chosen, 193 us (612 MB, 3.2
-// TB/s); 1,048,576 rows of 16 bfloat16, 2 chosen, 21 us (50 MB, 2.4 TB/s); 108 rows
-// of 4, 6 us, most of it the launch and the loads' latency.
+// Bound by vector instructions: 2,097,152 rows of 64 float32 logits, 4 chosen, 157
+// us in a series of calls (612 MB, 3.9 TB/s; the first ones 193), 37 of them a logit,
+// the vector pipes busy for 93% of the time; 1,048,576 rows of 16 bfloat16, 2 chosen,
+// 19 us (50 MB, 2.6 TB/s), 29 a logit and 77%.  (With one lane a row places for 16
+// choices are kept whatever K is, and 52 to 96 scalar registers go through vector
+// ones.)  108 rows of 4, 5.5 us, most of it the launch and the loads' latency.
+// Exponentials: z - top times log2(e) is rounded to float32, so e^(z - top) is off
+// by up to 4.6e-8 |z - top| of it (3.7e-6 at 80), beside what the rounding of z - top
+// makes, and is 0 below 2^-126.
 template <int L, int V, bool BF, bool KINDS>
 __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool only) {
   constexpr int kKept = (kMaxTopK + L - 1) / L;   // choices a lane keeps: lane s % L the s-th
@@ -292,8 +297,8 @@ __global__ __launch_bounds__(kForwardThreads) void k_route(RouteArgs a, bool onl
 // The work-groups' counts and sums added up in order, and the loss: 16 lanes for
 // an expert (and for the routed rows), each with every 16th work-group, 16 loads
 // of either under way at once; then a wavefront for all.  In 64 bits: the loss is a
-// quotient of sums over all rows.  Latency: 4 us up to 63 experts of 256
-// work-groups, 7 at 64 to 127.
+// quotient of sums over all rows.  Latency: 4 to 5 us up to 63 experts of 256
+// work-groups, 6 to 7 at 64 to 127.
 __global__ __launch_bounds__(1024) void k_route_total(RouteArgs a, int blocks) {
   __shared__ double s_p[kMaxExperts + 1];
   __shared__ int32_t s_c[kMaxExperts + 1];
@@ -340,8 +345,8 @@ __global__ __launch_bounds__(1024) void k_route_total(RouteArgs a, int blocks) {
 // case, and keeping them would write and read as much again).  The lanes of a
 // row take its choices in turn; what a choice adds to its logit's gradient
 // goes through LDS to the lane that holds the logit.
-// Bound by memory: 2,097,152 rows of 64 float32 logits, 4 chosen, 245 us (1.15 GB,
-// 4.7 TB/s; a large copy reaches 5.1).
+// Bound by memory: 2,097,152 rows of 64 float32 logits, 4 chosen, 242 us (1.15 GB,
+// 4.8 TB/s; a large copy reaches 5.1).
 template <int L, int V, bool BF, bool KINDS>
 __global__ __launch_bounds__(kRouteThreads) void k_route_backward(RouteArgs a) {
   __shared__ float s_h[L * V];
