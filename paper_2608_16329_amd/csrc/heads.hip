@@ -9,24 +9,25 @@
 //
 // One kernel takes a row through all of it.  A work-group has a tile of rows
 // of one head, each wavefront 16 of them as the columns of its matrix products;
-// y, z and u never leave registers: a layer's result is, register by register,
-// the second operand of the next layer's product (which sums over the inputs in
-// the order in which the lane groups hold them).
+// z and u never leave registers, y only for the weights' gradients: a layer's
+// result is, register by register, the second operand of the next layer's product
+// (which sums over the inputs in the order in which the lane groups hold them).
 //
 // Products: a float32 is three bfloat16 limbs, exactly (24 bits in 8 + 8 + 8,
-// each the rest rounded to nearest, so up to 2^-8 and 2^-17 of the value and of either
-// sign), and the product of two the six limb products but for those of a second
-// and a third, 2^-24 of it at most, which 16x16x32 bfloat16 matrix instructions
-// add up in float32.  (Limbs cut off would leave out 2^-22 each, of the product's sign.)
-// The instruction rounds to nearest where its addend is not the smaller part, and
-// otherwise down, by up to one unit in the last place, 0.17 on average.  Six
-// products take 0.43 of the time of the float32 matrix instructions (2,100 against
-// 150 TFLOP/s in a loop of nothing else).  Inputs in bfloat16 are one limb, and theirs are three
-// products (all gradients of 131,071 such rows of 192 values, two heads each, took
-// 0.88 of the time with six).  A first kernel splits the heads' matrices, in the order in
-// which lanes take them, for products with the matrix and with its transpose;
-// the main kernel brings them to LDS one 64x64 block at a time, the next block
-// on its way while one is used.
+// each the rest rounded to nearest, so the second and third are up to 2^-8 and
+// 2^-17 of the value and of either sign), and the product of two is the six limb
+// products without those of a second and a third, 2^-24 of it at most, which
+// 16x16x32 bfloat16 matrix instructions add up in float32.  (Limbs cut off would
+// leave out 2^-22 each, of the product's sign.)  The instruction rounds to nearest
+// where its addend is not the smaller part, and otherwise down, by up to one unit
+// in the last place, 0.17 on average.  Six products take 0.43 of the time of the
+// float32 matrix instructions (2,100 against 150 TFLOP/s in a loop of nothing
+// else).  Inputs in bfloat16 are one limb, and theirs are three products (all
+// gradients of 131,071 such rows of 192 values, two heads each, took 0.88 of the
+// time with six).  A first kernel splits the heads' matrices, in the order in which
+// lanes take them, for products with the matrix and with its transpose; the main
+// kernel brings them to LDS one 64x64 block at a time, the next block on its way
+// while one is used.
 //
 // The weights' gradients are products over rows: the limbs of g and y change
 // places through LDS, read transposed, each wavefront owns some of the 16
@@ -36,8 +37,8 @@
 //
 // An infinity has no limbs, nor has a value that rounds to one (2^128 (1 - 2^-9) and
 // more): in a row it gives NaN, in that row and in the weights' gradients, as a
-// NaN does.  (The bias sums are products with ones and zeros, so a
-// NaN in one layer's g is in the dc of all layers.)
+// NaN does.  (The bias sums are products with ones and zeros, so a NaN in one
+// layer's g is in the dc of all layers.)
 #include <algorithm>
 #include <type_traits>
 
