@@ -505,6 +505,137 @@ mlip_status mlip_heads(mlip_learn* ctx, const mlip_heads_params* p, int64_t n, c
                        float* dweights_dev, float* dgates_dev);
 
 /*
+ * Layers of experts wider than the energy heads (hidden width 64): rows are
+ * brought into the experts' order, go through matrix products and activations,
+ * and come back with weights.  Between the products rows are held in 8 bits.
+ *
+ * mlip_sort: entry i top_k + s (row i, its s-th expert) stands at place p with
+ * order[p] = i top_k + s (offsets_dev, order_dev as mlip_group writes them):
+ *   sorted_dev  [n top_k][width] contiguous: sorted[p] = x[order[p] / top_k] for
+ *               p < offsets[n_experts]; rows from there on (entries without an
+ *               expert) are left as they are
+ *   places_dev  int32 [n][top_k]: p, or -1 for an entry without an expert
+ * mlip_combine: out_i = sum_s gates_is y[places_is] in float32, in the order of s,
+ * out_dev [n][width] contiguous; entries without an expert add nothing and their
+ * gates are not looked at.  gates_dev f32 [n][top_k] or NULL: 1.  Without gates,
+ * and given the gradient in sorted_dev, it is mlip_sort's gradient in x.
+ * mlip_combine_backward: of sum dout . out, dy_dev [n top_k][width] contiguous,
+ * dy[places_is] = gates_is dout_i (other rows are left as they are), and, unless
+ * NULL, dgates_dev f32 [n][top_k], dout_i . y[places_is], 0 for an entry without
+ * an expert (y_dev is needed for it alone).
+ * x, y and dout are f32 or bf16 (dtype), rows *_stride values apart; their
+ * results have their type.  No output may overlap an input.
+ * n in [0, 2^31 / top_k), n_experts 1..256, top_k 1..16, width 1..65536.
+ * Errors: MLIP_E_ARG, MLIP_E_HIP.
+ */
+typedef struct {
+  int32_t n_experts;   /* of offsets_dev, where there is one */
+  int32_t top_k;
+  int32_t width;
+  int32_t dtype;       /* mlip_dtype of the rows */
+} mlip_rows_params;
+
+mlip_status mlip_sort(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, const void* x_dev, int64_t x_stride,
+                      const int32_t* offsets_dev, const int32_t* order_dev, void* sorted_dev, int32_t* places_dev);
+mlip_status mlip_combine(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, const void* y_dev, int64_t y_stride,
+                         const int32_t* places_dev, const float* gates_dev, void* out_dev);
+mlip_status mlip_combine_backward(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, const void* dout_dev,
+                                  int64_t dout_stride, const void* y_dev, int64_t y_stride, const int32_t* places_dev,
+                                  const float* gates_dev, void* dy_dev, float* dgates_dev);
+
+/*
+ * Rows in 8 bits: for every 128 values of a row (the last block of a row may be
+ * shorter) a power of two 2^e and a code each of 4 exponent and 3 mantissa bits
+ * beside the sign, s (1 + f/8) 2^(E - 7) 2^e, for E = 0 s f/8 2^-6 2^e; 0x7f and
+ * 0xff are NaN.  With a the largest finite size of the block, a = f 2^q, 1 <= f < 2:
+ * e = q - 8 if f <= 1.75, else q - 7, kept within -100..120; codes are the values
+ * times 2^-e rounded to nearest, ties to even, and to 15/16 2^128 instead of 2^128,
+ * which float32 has not.  An infinity or a NaN is held as NaN and leaves its
+ * block's others alone.
+ *   codes uint8 [rows][mlip_row8_codes(width)], width rounded up to a multiple of
+ *         128, zeros behind the row's end; aligned to 16 bytes
+ *   exps  uint8 [rows][mlip_row8_exps(width)], e + 127 of each block, rounded up
+ *         to a multiple of four, zeros behind the last; aligned to 4 bytes
+ * mlip_pack8 packs n rows, or, with offsets_dev and order_dev (both or neither),
+ * their entries in the experts' order as mlip_sort would write them: n top_k rows,
+ * those from offsets[n_experts] on left as they are.  mlip_unpack8 writes the
+ * values of n packed rows, x_dev [n][width] contiguous in dtype; both types hold
+ * them without rounding.
+ * mlip_pack8_weights packs matrices w_dev f32 or bf16 [n_experts][outputs][inputs]
+ * with one power of two for 128 x 128 values (the same rule):
+ *   codes  [n_experts][outputs][mlip_row8_codes(inputs)]
+ *   exps   [n_experts][ceil(outputs / 128)][mlip_row8_exps(inputs)]
+ * and their transposes, with the same values:
+ *   t_codes [n_experts][inputs][mlip_row8_codes(outputs)]
+ *   t_exps  [n_experts][ceil(inputs / 128)][mlip_row8_exps(outputs)]
+ * either pair may be NULL.
+ * Errors: MLIP_E_ARG, MLIP_E_HIP.
+ */
+int64_t mlip_row8_codes(int32_t width);
+int64_t mlip_row8_exps(int32_t width);
+mlip_status mlip_pack8(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, const void* x_dev, int64_t x_stride,
+                       const int32_t* offsets_dev, const int32_t* order_dev, uint8_t* codes_dev, uint8_t* exps_dev);
+mlip_status mlip_unpack8(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, const uint8_t* codes_dev,
+                         const uint8_t* exps_dev, void* x_dev);
+
+/*
+ * Products of packed rows and matrices.  m rows stand in the experts' order:
+ * expert e has rows offsets[e] .. offsets[e + 1] - 1 (offsets_dev int32
+ * [n_experts + 1], rising; NULL with n_experts 1: all rows), and rows from
+ * offsets[n_experts] on are neither read nor written.
+ * mlip_product8: y_p = W_e x_p + c_e, y_dev [m][outputs] contiguous in dtype,
+ * aligned to 16 bytes, bias_dev f32 [n_experts][outputs] or NULL.  With the
+ * transposes and dy for x (inputs and outputs exchanged) it is the gradient in x.
+ * Sums from block to block are float32.  In float32 y has the accuracy of float32
+ * products of the packed values; for bf16 the 128 products of a block are added
+ * up in about 16 bits below the largest of them, y being rounded to 8 bits.
+ * mlip_product8_weights: dweights_dev f32 [n_experts][outputs][inputs] (aligned to
+ * 16 bytes), sum_p dy_p x_p^T over the expert's rows, and, unless NULL, dbias_dev f32
+ * [n_experts][outputs], sum_p dy_p; 0 for experts without rows.  Float32 sums of
+ * the packed values' products; dtype is not looked at beyond its range.  A NaN in
+ * a row gives NaN wherever it is a factor.
+ * m in [0, 2^31), n_experts 1..256, inputs and outputs 1..65536, and (m / 128 +
+ * n_experts) outputs / 128, and n_experts inputs outputs / 2^14 (times the slices of
+ * rows that are added up), below 2^24.
+ * Errors: MLIP_E_ARG, and of mlip_product8_weights MLIP_E_STATE, MLIP_E_OOM; MLIP_E_HIP.
+ */
+typedef struct {
+  int32_t n_experts;
+  int32_t inputs;
+  int32_t outputs;
+  int32_t dtype;       /* mlip_dtype of w and of y */
+} mlip_product8_params;
+
+mlip_status mlip_pack8_weights(mlip_learn* ctx, const mlip_product8_params* p, const void* w_dev, uint8_t* codes_dev,
+                               uint8_t* exps_dev, uint8_t* t_codes_dev, uint8_t* t_exps_dev);
+mlip_status mlip_product8(mlip_learn* ctx, const mlip_product8_params* p, int64_t m, const uint8_t* x_codes_dev,
+                          const uint8_t* x_exps_dev, const uint8_t* w_codes_dev, const uint8_t* w_exps_dev,
+                          const int32_t* offsets_dev, const float* bias_dev, void* y_dev);
+mlip_status mlip_product8_weights(mlip_learn* ctx, const mlip_product8_params* p, int64_t m, const uint8_t* dy_codes_dev,
+                                  const uint8_t* dy_exps_dev, const uint8_t* x_codes_dev, const uint8_t* x_exps_dev,
+                                  const int32_t* offsets_dev, float* dweights_dev, float* dbias_dev);
+
+/*
+ * An activation that keeps its argument in 8 bits for the backward pass:
+ *   h = r + silu(z), silu(z) = z / (1 + exp(-z));  r = residual_dev or NULL: 0
+ *   dz = dh silu'(z^), silu'(z) = s (1 + z (1 - s)), s = 1 / (1 + exp(-z)), with z^
+ *   the kept z's values (the residual's gradient is dh)
+ * in float32.  z, r, dh: n rows of `width` values in dtype, *_stride values apart;
+ * h_dev, dz_dev [n][width] contiguous in dtype.  h_codes_dev, h_exps_dev and
+ * dz_codes_dev, dz_exps_dev are what mlip_pack8 gives for h and dz as they are
+ * written, for the next product; kept_codes_dev, kept_exps_dev what it gives for z.
+ * Outputs that are not wanted are NULL (kept: nothing will be differentiated).
+ * silu(-infinity) is NaN.  p->n_experts and top_k are not used beyond their range.
+ * Errors: MLIP_E_ARG, MLIP_E_HIP.
+ */
+mlip_status mlip_activate8(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, const void* z_dev, int64_t z_stride,
+                           const void* residual_dev, int64_t residual_stride, void* h_dev, uint8_t* h_codes_dev,
+                           uint8_t* h_exps_dev, uint8_t* kept_codes_dev, uint8_t* kept_exps_dev);
+mlip_status mlip_activate8_backward(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, const uint8_t* kept_codes_dev,
+                                    const uint8_t* kept_exps_dev, const void* dh_dev, int64_t dh_stride, void* dz_dev,
+                                    uint8_t* dz_codes_dev, uint8_t* dz_exps_dev);
+
+/*
  * AdamW over many tensors at once (the tables of a potential are hundreds to
  * thousands: eight tensors for every pair of species and ten for every
  * species), in one launch:

@@ -12,9 +12,9 @@ import numpy as np
 
 from . import binding
 from .binding import MlipError, mlip_hparams
-from .learn import AdamW, Learner
+from .learn import AdamW, Learner, Rows8, Weights8
 
-__all__ = ["binding", "MlipError", "mlip_hparams", "Potential", "Learner", "AdamW"]
+__all__ = ["binding", "MlipError", "mlip_hparams", "Potential", "Learner", "AdamW", "Rows8", "Weights8"]
 
 
 class Potential:

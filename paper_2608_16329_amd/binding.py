@@ -29,7 +29,10 @@ EXPORTED = ["mlip_weight_count", "mlip_create", "mlip_build_neighbors", "mlip_co
             "mlip_descriptors", "mlip_forces_from_descriptors", "mlip_learn_create", "mlip_learn_last_error", "mlip_learn_memory_bytes", "mlip_learn_destroy",
             "mlip_route", "mlip_route_backward", "mlip_group", "mlip_heads_weight_count", "mlip_heads",
             "mlip_adamw_create", "mlip_adamw_last_error", "mlip_adamw_state_count", "mlip_adamw_destroy",
-            "mlip_adamw_step", "mlip_adamw_moments"]
+            "mlip_adamw_step", "mlip_adamw_moments",
+            "mlip_sort", "mlip_combine", "mlip_combine_backward", "mlip_row8_codes", "mlip_row8_exps", "mlip_pack8",
+            "mlip_unpack8", "mlip_pack8_weights", "mlip_product8", "mlip_product8_weights", "mlip_activate8",
+            "mlip_activate8_backward"]
 
 MLIP_STATIC_SCRATCH_BYTES = 256 * 1024 * 1024
 
@@ -69,6 +72,15 @@ class mlip_heads_params(ctypes.Structure):
                 ("top_k", ctypes.c_int32), ("dtype", ctypes.c_int32), ("row_stride", ctypes.c_int64)]
 
 
+class mlip_rows_params(ctypes.Structure):
+    _fields_ = [("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("width", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class mlip_product8_params(ctypes.Structure):
+    _fields_ = [("n_experts", ctypes.c_int32), ("inputs", ctypes.c_int32), ("outputs", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
 class mlip_adamw_tensor(ctypes.Structure):
     _fields_ = [("param_dev", ctypes.c_void_p), ("into_dev", ctypes.c_void_p), ("grad_dev", ctypes.c_void_p),
                 ("n", ctypes.c_int64), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
@@ -105,7 +117,8 @@ def _load() -> ctypes.CDLL:
     lib = ctypes.CDLL(LIB_PATH)
     vp, dp, ip32, ip64 = ctypes.c_void_p, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32), \
         ctypes.POINTER(ctypes.c_int64)
-    st = ctypes.c_int
+    st, i64 = ctypes.c_int, ctypes.c_int64
+    rows, product = ctypes.POINTER(mlip_rows_params), ctypes.POINTER(mlip_product8_params)
     sig = {
         "mlip_weight_count": (ctypes.c_size_t, [ctypes.POINTER(mlip_hparams)]),
         "mlip_create": (st, [ctypes.POINTER(mlip_hparams), dp, ctypes.c_size_t, vp, ctypes.POINTER(vp)]),
@@ -135,6 +148,18 @@ def _load() -> ctypes.CDLL:
         "mlip_route_backward": (st, [vp, ctypes.POINTER(mlip_route_params), ctypes.c_int64] + [vp] * 8),
         "mlip_heads_weight_count": (ctypes.c_size_t, [ctypes.POINTER(mlip_heads_params)]),
         "mlip_heads": (st, [vp, ctypes.POINTER(mlip_heads_params), ctypes.c_int64] + [vp] * 10),
+        "mlip_sort": (st, [vp, rows, i64, vp, i64, vp, vp, vp, vp]),
+        "mlip_combine": (st, [vp, rows, i64, vp, i64, vp, vp, vp]),
+        "mlip_combine_backward": (st, [vp, rows, i64, vp, i64, vp, i64, vp, vp, vp, vp]),
+        "mlip_row8_codes": (i64, [ctypes.c_int32]),
+        "mlip_row8_exps": (i64, [ctypes.c_int32]),
+        "mlip_pack8": (st, [vp, rows, i64, vp, i64, vp, vp, vp, vp]),
+        "mlip_unpack8": (st, [vp, rows, i64, vp, vp, vp]),
+        "mlip_pack8_weights": (st, [vp, product] + [vp] * 5),
+        "mlip_product8": (st, [vp, product, i64] + [vp] * 7),
+        "mlip_product8_weights": (st, [vp, product, i64] + [vp] * 7),
+        "mlip_activate8": (st, [vp, rows, i64, vp, i64, vp, i64] + [vp] * 5),
+        "mlip_activate8_backward": (st, [vp, rows, i64, vp, vp, vp, i64, vp, vp, vp]),
         "mlip_adamw_create": (st, [ctypes.POINTER(mlip_adamw_tensor), ctypes.c_int64, ctypes.c_int32, vp, ctypes.POINTER(vp)]),
         "mlip_adamw_last_error": (ctypes.c_char_p, [vp]),
         "mlip_adamw_state_count": (st, [vp, ip64, ip64]),
@@ -339,6 +364,68 @@ def mlip_heads(ctx: int, params: mlip_heads_params, n: int, x_ptr, weights_ptr, 
                denergy_ptr, energy_ptr, dx_ptr, dweights_ptr, dgates_ptr) -> None:
     _check_learn(ctx, _lib.mlip_heads(ctx, ctypes.byref(params), n, x_ptr, weights_ptr, offsets_ptr, order_ptr,
                                       gates_ptr, denergy_ptr, energy_ptr, dx_ptr, dweights_ptr, dgates_ptr))
+
+
+def mlip_sort(ctx: int, params: mlip_rows_params, n: int, x_ptr, x_stride: int, offsets_ptr, order_ptr, sorted_ptr,
+              places_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_sort(ctx, ctypes.byref(params), n, x_ptr, x_stride, offsets_ptr, order_ptr, sorted_ptr,
+                                     places_ptr))
+
+
+def mlip_combine(ctx: int, params: mlip_rows_params, n: int, y_ptr, y_stride: int, places_ptr, gates_ptr, out_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_combine(ctx, ctypes.byref(params), n, y_ptr, y_stride, places_ptr, gates_ptr, out_ptr))
+
+
+def mlip_combine_backward(ctx: int, params: mlip_rows_params, n: int, dout_ptr, dout_stride: int, y_ptr, y_stride: int,
+                          places_ptr, gates_ptr, dy_ptr, dgates_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_combine_backward(ctx, ctypes.byref(params), n, dout_ptr, dout_stride, y_ptr, y_stride,
+                                                 places_ptr, gates_ptr, dy_ptr, dgates_ptr))
+
+
+def mlip_row8_codes(width: int) -> int:
+    return int(_lib.mlip_row8_codes(width))
+
+
+def mlip_row8_exps(width: int) -> int:
+    return int(_lib.mlip_row8_exps(width))
+
+
+def mlip_pack8(ctx: int, params: mlip_rows_params, n: int, x_ptr, x_stride: int, offsets_ptr, order_ptr, codes_ptr,
+               exps_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_pack8(ctx, ctypes.byref(params), n, x_ptr, x_stride, offsets_ptr, order_ptr, codes_ptr,
+                                      exps_ptr))
+
+
+def mlip_unpack8(ctx: int, params: mlip_rows_params, n: int, codes_ptr, exps_ptr, x_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_unpack8(ctx, ctypes.byref(params), n, codes_ptr, exps_ptr, x_ptr))
+
+
+def mlip_pack8_weights(ctx: int, params: mlip_product8_params, w_ptr, codes_ptr, exps_ptr, t_codes_ptr, t_exps_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_pack8_weights(ctx, ctypes.byref(params), w_ptr, codes_ptr, exps_ptr, t_codes_ptr, t_exps_ptr))
+
+
+def mlip_product8(ctx: int, params: mlip_product8_params, m: int, x_codes_ptr, x_exps_ptr, w_codes_ptr, w_exps_ptr,
+                  offsets_ptr, bias_ptr, y_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_product8(ctx, ctypes.byref(params), m, x_codes_ptr, x_exps_ptr, w_codes_ptr, w_exps_ptr,
+                                         offsets_ptr, bias_ptr, y_ptr))
+
+
+def mlip_product8_weights(ctx: int, params: mlip_product8_params, m: int, dy_codes_ptr, dy_exps_ptr, x_codes_ptr,
+                          x_exps_ptr, offsets_ptr, dweights_ptr, dbias_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_product8_weights(ctx, ctypes.byref(params), m, dy_codes_ptr, dy_exps_ptr, x_codes_ptr,
+                                                 x_exps_ptr, offsets_ptr, dweights_ptr, dbias_ptr))
+
+
+def mlip_activate8(ctx: int, params: mlip_rows_params, n: int, z_ptr, z_stride: int, residual_ptr, residual_stride: int,
+                   h_ptr, h_codes_ptr, h_exps_ptr, kept_codes_ptr, kept_exps_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_activate8(ctx, ctypes.byref(params), n, z_ptr, z_stride, residual_ptr, residual_stride,
+                                          h_ptr, h_codes_ptr, h_exps_ptr, kept_codes_ptr, kept_exps_ptr))
+
+
+def mlip_activate8_backward(ctx: int, params: mlip_rows_params, n: int, kept_codes_ptr, kept_exps_ptr, dh_ptr,
+                            dh_stride: int, dz_ptr, dz_codes_ptr, dz_exps_ptr) -> None:
+    _check_learn(ctx, _lib.mlip_activate8_backward(ctx, ctypes.byref(params), n, kept_codes_ptr, kept_exps_ptr, dh_ptr,
+                                                   dh_stride, dz_ptr, dz_codes_ptr, dz_exps_ptr))
 
 
 def _check_adamw(plan, status: int):

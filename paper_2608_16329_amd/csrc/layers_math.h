@@ -1,0 +1,134 @@
+// Device helpers of the layers' kernels: chunks of values in either type, 8-bit
+// codes, sums and maxima over groups of lanes.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "layers.h"
+#include "learn_math.h"
+
+namespace mlip {
+
+// 16 and 8 neighbouring bytes at the alignment of one value or byte (rows start
+// anywhere; the hardware takes them in one access all the same).
+typedef uint32_t U4 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t U2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+
+// Values at .. at + 7 of an array of either type, those from `left` on as zero
+// (left <= 0: none is read).
+template <bool BF>
+__device__ __forceinline__ void load8(const void* p, int64_t at, int left, float v[8]) {
+  if (left >= 8) {
+    if (BF) {
+      const u4v h = *reinterpret_cast<const U4*>(static_cast<const uint16_t*>(p) + at);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v[2 * q] = __uint_as_float(h[q] << 16);
+        v[2 * q + 1] = __uint_as_float(h[q] & 0xffff0000u);
+      }
+    } else {
+      const u4v a = *reinterpret_cast<const U4*>(static_cast<const float*>(p) + at);
+      const u4v b = *reinterpret_cast<const U4*>(static_cast<const float*>(p) + at + 4);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v[q] = __uint_as_float(a[q]);
+        v[4 + q] = __uint_as_float(b[q]);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    v[q] = 0.f;
+    if (q < left) v[q] = BF ? from_bf16(static_cast<const uint16_t*>(p)[at + q]) : static_cast<const float*>(p)[at + q];
+  }
+}
+
+template <bool BF>
+__device__ __forceinline__ void store8(void* p, int64_t at, int left, const float v[8]) {
+  if (left >= 8) {
+    if (BF) {
+      u4v h;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) h[q] = uint32_t(to_bf16(v[2 * q])) | uint32_t(to_bf16(v[2 * q + 1])) << 16;
+      *reinterpret_cast<U4*>(static_cast<uint16_t*>(p) + at) = h;
+    } else {
+      u4v a, b;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        a[q] = __float_as_uint(v[q]);
+        b[q] = __float_as_uint(v[4 + q]);
+      }
+      *reinterpret_cast<U4*>(static_cast<float*>(p) + at) = a;
+      *reinterpret_cast<U4*>(static_cast<float*>(p) + at + 4) = b;
+    }
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    if (q < left) {
+      if (BF) static_cast<uint16_t*>(p)[at + q] = to_bf16(v[q]);
+      else static_cast<float*>(p)[at + q] = v[q];
+    }
+}
+
+// The largest of 16 neighbouring lanes' values, in each of them: rotations
+// within the row of 16, by 8, 4, 2 and 1.
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+  v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x128, 0xf, 0xf, true)));
+  v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x124, 0xf, 0xf, true)));
+  v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x122, 0xf, 0xf, true)));
+  return max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x121, 0xf, 0xf, true)));
+}
+
+// The exponent e of a block whose largest finite size has these bits: the least
+// with all of it within codes up to 448, kept within -100 .. 120 so that codes'
+// values and the scales are normal float32 and bfloat16 numbers.
+__device__ __forceinline__ int exponent8(uint32_t bits) {
+  return min(120, max(-100, int(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0)));
+}
+// 2^e, -126 <= e <= 127
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float(uint32_t(e + 127) << 23); }
+// The bits of a finite value's size; 0 for an infinity or a NaN.
+__device__ __forceinline__ uint32_t finite_size(float v) {
+  const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
+  return u < 0x7f800000u ? u : 0u;
+}
+// Codes of eight values times 2^-e, to nearest even (the conversion gives the
+// NaN code for infinities and NaN; nothing finite is over 448).
+__device__ __forceinline__ u2v encode8(const float v[8], int e) {
+  const float unit = pow2(-e);
+  float t[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) t[q] = v[q] * unit;
+  // 256 2^120 would be an infinity in float32: 240 is the largest code there
+  if (e == 120) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (finite_size(v[q]) && fabsf(t[q]) > 240.f) t[q] = copysignf(240.f, t[q]);
+  }
+  u2v c;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(t[4 * q], t[4 * q + 1], 0, false);
+    c[q] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(t[4 * q + 2], t[4 * q + 3], w, true));
+  }
+  return c;
+}
+__device__ __forceinline__ void decode8(u2v c, float unit, float v[8]) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const f2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(c[q]), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(c[q]), true);
+    v[4 * q] = lo[0] * unit;
+    v[4 * q + 1] = lo[1] * unit;
+    v[4 * q + 2] = hi[0] * unit;
+    v[4 * q + 3] = hi[1] * unit;
+  }
+}
+
+}  // namespace mlip

@@ -1,0 +1,241 @@
+// Rows and matrices in 8 bits, and activations that keep them.
+//
+// A block of 128 values has a power of two 2^e and codes of 4 exponent and 3
+// mantissa bits beside the sign (values up to 448, NaN, no infinity): with a =
+// f 2^q its largest finite size, 1 <= f < 2, e = q - 8 if f <= 1.75 and q - 7
+// otherwise, and a code is the value times 2^-e, rounded to nearest even, off
+// by at most 2^-4 of the value (and by 2^(e - 10) where the value is below
+// 2^(e - 6)).  A matrix shares e over 128 x 128 values, so that its transpose
+// has the same values.
+//
+// Bound by memory.  16 lanes have a block, 8 values each; a wavefront has four
+// blocks, whose exponents are one 32-bit word: four of a row, or one or two each
+// of four or two rows that have no more.
+#include <algorithm>
+
+#include "layers_math.h"
+
+namespace mlip {
+namespace {
+
+// What a lane works on: row and block, the first of its eight values and how
+// many there are from there on.
+struct Spot {
+  int64_t row;
+  int block, at, left;
+  bool there;                   // the row and the block exist
+};
+template <int G>
+__device__ __forceinline__ Spot spot(int64_t row0, int quad, int64_t n, int width) {
+  const int group = (threadIdx.x & 63) >> 4;
+  Spot s;
+  s.row = row0 + group / G;
+  s.block = 4 * quad + group % G;
+  s.at = s.block * kBlock8 + 8 * (threadIdx.x & 15);
+  s.left = width - s.at;
+  s.there = s.row < n && s.block * kBlock8 < width;
+  return s;
+}
+
+// Writes a block's codes and exponent: all lanes of the wavefront call.
+template <int G>
+__device__ __forceinline__ void put(const Spot& s, const float v[8], uint8_t* codes, uint8_t* exps, int quad, int width, int64_t n) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) top = max(top, finite_size(v[q]));
+  const int e = exponent8(max16(top));
+  if (s.there) *reinterpret_cast<u2v*>(codes + s.row * codes8(width) + s.at) = encode8(v, e);
+  uint32_t word = s.there ? uint32_t(e + 127) << (8 * (s.block & 3)) : 0u;
+  if (G >= 2) word |= __shfl_xor(word, 16);
+  if (G == 4) word |= __shfl_xor(word, 32);
+  if ((threadIdx.x & 15) == 0 && s.block % 4 == 0 && s.row < n)
+    *reinterpret_cast<uint32_t*>(exps + s.row * exps8(width) + 4 * quad) = word;
+}
+// Values of a block that was written.
+__device__ __forceinline__ void get(const Spot& s, const uint8_t* codes, const uint8_t* exps, int width, float v[8]) {
+  if (s.there) {
+    const u2v c = *reinterpret_cast<const u2v*>(codes + s.row * codes8(width) + s.at);
+    const uint32_t e = exps[s.row * exps8(width) + s.block];
+    decode8(c, __uint_as_float(e << 23), v);
+  }
+}
+
+// The row of x that packed row p is, or -1.
+__device__ __forceinline__ int64_t source(const Pack8Args& a, int64_t p, int64_t end) {
+  if (!a.order) return p;
+  if (p >= end) return -1;
+  const uint32_t entry = uint32_t(a.order[p]);
+  return int64_t(entry) < a.n ? int64_t(entry / uint32_t(a.K)) : -1;
+}
+
+template <bool BF, int G>
+__global__ __launch_bounds__(256) void k_pack8(Pack8Args a) {
+  const int64_t end = a.order ? min(a.n, max(int64_t(0), int64_t(a.offsets[a.E]))) : a.n;
+  const int quads = int(exps8(a.width) / 4);
+  for (int64_t row0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (4 / G); row0 < end; row0 += int64_t(gridDim.x) * 4 * (4 / G))
+    for (int quad = blockIdx.y; quad < quads; quad += gridDim.y) {
+      Spot s = spot<G>(row0, quad, end, a.width);
+      const int64_t from = s.there ? source(a, s.row, end) : -1;
+      s.there = s.there && from >= 0;
+      float v[8] = {};
+      if (s.there) load8<BF>(a.x, from * a.x_stride + s.at, s.left, v);
+      put<G>(s, v, a.codes, a.exps, quad, a.width, end);
+    }
+}
+
+template <bool BF, int G>
+__global__ __launch_bounds__(256) void k_unpack8(Pack8Args a) {
+  const int quads = int(exps8(a.width) / 4);
+  for (int64_t row0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (4 / G); row0 < a.n; row0 += int64_t(gridDim.x) * 4 * (4 / G))
+    for (int quad = blockIdx.y; quad < quads; quad += gridDim.y) {
+      const Spot s = spot<G>(row0, quad, a.n, a.width);
+      float v[8];
+      get(s, a.kept, a.kept_exps, a.width, v);
+      if (s.there && s.left > 0) store8<BF>(a.out, s.row * a.width + s.at, s.left, v);
+    }
+}
+
+// 1 / (1 + exp(-z)) from exp(-|z|), which does not overflow where the quotient is
+// still a number.
+__device__ __forceinline__ float sigmoid(float z) {
+  const float t = expf(-fabsf(z));
+  return (z < 0.f ? t : 1.f) / (1.f + t);
+}
+
+// h = r + silu(z), and z in 8 bits for the backward pass
+template <bool BF, int G>
+__global__ __launch_bounds__(256) void k_activate8(Pack8Args a) {
+  const int quads = int(exps8(a.width) / 4);
+  for (int64_t row0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (4 / G); row0 < a.n; row0 += int64_t(gridDim.x) * 4 * (4 / G))
+    for (int quad = blockIdx.y; quad < quads; quad += gridDim.y) {
+      const Spot s = spot<G>(row0, quad, a.n, a.width);
+      float z[8] = {}, h[8] = {};
+      if (s.there) {
+        load8<BF>(a.x, s.row * a.x_stride + s.at, s.left, z);
+        if (a.residual) load8<BF>(a.residual, s.row * a.residual_stride + s.at, s.left, h);
+      }
+      if (a.codes) put<G>(s, z, a.codes, a.exps, quad, a.width, a.n);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float t = z[q] * sigmoid(z[q]);
+        h[q] = a.residual ? h[q] + t : t;
+        if (BF) h[q] = from_bf16(to_bf16(h[q]));
+      }
+      if (a.out && s.there && s.left > 0) store8<BF>(a.out, s.row * a.width + s.at, s.left, h);
+      if (a.out_codes) put<G>(s, h, a.out_codes, a.out_exps, quad, a.width, a.n);
+    }
+}
+
+// dz = dh silu'(z) of the z that was kept
+template <bool BF, int G>
+__global__ __launch_bounds__(256) void k_activate8_backward(Pack8Args a) {
+  const int quads = int(exps8(a.width) / 4);
+  for (int64_t row0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (4 / G); row0 < a.n; row0 += int64_t(gridDim.x) * 4 * (4 / G))
+    for (int quad = blockIdx.y; quad < quads; quad += gridDim.y) {
+      const Spot s = spot<G>(row0, quad, a.n, a.width);
+      float z[8] = {}, d[8] = {};
+      if (s.there) load8<BF>(a.x, s.row * a.x_stride + s.at, s.left, d);
+      get(s, a.kept, a.kept_exps, a.width, z);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float t = sigmoid(z[q]);
+        d[q] *= t * (1.f + z[q] * (1.f - t));
+        if (BF) d[q] = from_bf16(to_bf16(d[q]));
+      }
+      if (a.out && s.there && s.left > 0) store8<BF>(a.out, s.row * a.width + s.at, s.left, d);
+      if (a.out_codes) put<G>(s, d, a.out_codes, a.out_exps, quad, a.width, a.n);
+    }
+}
+
+// One work-group for a block of 128 x 128 of a matrix: thread t has the 8 values
+// from 8 (t % 16) on of rows t / 16, t / 16 + 16 ..
+template <bool BF>
+__global__ __launch_bounds__(256) void k_pack8_weights(Weights8Args a) {
+  constexpr int kPitch = kBlock8 + 16;              // of a row of codes in LDS
+  __shared__ uint32_t tops[4];
+  __shared__ uint8_t tile[kBlock8 * kPitch];
+  const int kb = blockIdx.x, nb = blockIdx.y, t = threadIdx.x;
+  const int64_t e = blockIdx.z;
+  const int blocks_k = (a.K + kBlock8 - 1) / kBlock8, blocks_n = (a.N + kBlock8 - 1) / kBlock8;
+  const int k0 = kb * kBlock8 + 8 * (t & 15);
+  float v[8][8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int n = nb * kBlock8 + 16 * j + (t >> 4);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[j][q] = 0.f;
+    if (n < a.N) load8<BF>(a.w, (e * a.N + n) * a.K + k0, a.K - k0, v[j]);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) top = max(top, finite_size(v[j][q]));
+  }
+  top = max16(top);
+  top = max(top, uint32_t(__shfl_xor(top, 16)));
+  top = max(top, uint32_t(__shfl_xor(top, 32)));
+  if ((t & 63) == 0) tops[t >> 6] = top;
+  __syncthreads();
+  const int x = exponent8(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int r = 16 * j + (t >> 4), n = nb * kBlock8 + r;
+    const u2v c = encode8(v[j], x);
+    if (a.codes && n < a.N) *reinterpret_cast<u2v*>(a.codes + (e * a.N + n) * codes8(a.K) + k0) = c;
+    if (a.codes_t) *reinterpret_cast<u2v*>(tile + r * kPitch + 8 * (t & 15)) = c;
+  }
+  // the exponent, and zeros behind the last block
+  if (t < 4) {
+    if (a.codes && (t == 0 || (kb == blocks_k - 1 && kb + t < exps8(a.K))))
+      a.exps[(e * blocks_n + nb) * exps8(a.K) + kb + t] = t == 0 ? uint8_t(x + 127) : uint8_t(0);
+    if (a.codes_t && (t == 0 || (nb == blocks_n - 1 && nb + t < exps8(a.N))))
+      a.exps_t[(e * blocks_k + kb) * exps8(a.N) + nb + t] = t == 0 ? uint8_t(x + 127) : uint8_t(0);
+  }
+  if (!a.codes_t) return;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int r = 16 * j + (t >> 4), k = kb * kBlock8 + r, c0 = 8 * (t & 15);
+    if (k >= a.K) continue;
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      w[h] = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[h] |= uint32_t(tile[(c0 + 4 * h + q) * kPitch + r]) << (8 * q);
+    }
+    *reinterpret_cast<u2v*>(a.codes_t + (e * a.K + k) * codes8(a.N) + nb * kBlock8 + c0) = u2v{w[0], w[1]};
+  }
+}
+
+template <typename F>
+hipError_t with_group(const Pack8Args& a, int n_cu, F run) {
+  const int blocks = (a.width + kBlock8 - 1) / kBlock8, quads = (blocks + 3) / 4;
+  const int rows = blocks == 1 ? 16 : blocks == 2 ? 8 : 4;          // of a work-group
+  const int64_t x = std::max<int64_t>(1, std::min<int64_t>((a.n + rows - 1) / rows, int64_t(n_cu) * 64));
+  const dim3 g{unsigned(x), unsigned(std::min(quads, 1024)), 1};
+  if (blocks == 1) run(std::integral_constant<int, 1>(), g);
+  else if (blocks == 2) run(std::integral_constant<int, 2>(), g);
+  else run(std::integral_constant<int, 4>(), g);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+#define PACK8_LAUNCH(kernel)                                                \
+  return with_group(a, n_cu, [&](auto w, dim3 g) {                          \
+    if (a.bf16) kernel<true, w.value><<<g, 256, 0, s>>>(a);                 \
+    else kernel<false, w.value><<<g, 256, 0, s>>>(a);                       \
+  })
+
+hipError_t launch_pack8(const Pack8Args& a, int n_cu, hipStream_t s) { PACK8_LAUNCH(k_pack8); }
+hipError_t launch_unpack8(const Pack8Args& a, int n_cu, hipStream_t s) { PACK8_LAUNCH(k_unpack8); }
+hipError_t launch_activate8(const Pack8Args& a, int n_cu, hipStream_t s) { PACK8_LAUNCH(k_activate8); }
+hipError_t launch_activate8_backward(const Pack8Args& a, int n_cu, hipStream_t s) { PACK8_LAUNCH(k_activate8_backward); }
+
+hipError_t launch_pack8_weights(const Weights8Args& a, hipStream_t s) {
+  const dim3 g{unsigned((a.K + kBlock8 - 1) / kBlock8), unsigned((a.N + kBlock8 - 1) / kBlock8), unsigned(a.E)};
+  if (a.bf16) k_pack8_weights<true><<<g, 256, 0, s>>>(a);
+  else k_pack8_weights<false><<<g, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace mlip

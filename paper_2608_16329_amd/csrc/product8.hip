@@ -1,0 +1,487 @@
+// Products of rows and matrices in 8 bits over rows grouped by expert, and the
+// gradients of the matrices.
+//
+//   y_p = W_e x_p + c_e,  offsets[e] <= p < offsets[e + 1]
+//   dW_e = sum_p dy_p x_p^T,  dc_e = sum_p dy_p
+// (the gradient in x is the first with W packed transposed and dy for x).
+//
+// A block of 128 inputs is one 16x16x128 matrix instruction on the codes, whose
+// scale operands are the blocks' powers of two: values of x are columns, each
+// with its row's exponent, those of W rows with their block's.  That instruction
+// adds up its 128 products in about 16 bits below the largest (rms error 1.5e-5
+// of a sum of normally distributed values, at most 2^-12 of the sum of the
+// products' sizes where they spread over many powers of two); sums from block to
+// block are float32.  That is 2^-7 of the rounding of a bfloat16 result, so y in
+// bfloat16 is formed that way.  y in float32, and the gradients of W, are formed
+// on 16x16x32 bfloat16 instructions (8e-9 on the same values): a code and its
+// power of two make a bfloat16 without rounding, one conversion for two.
+#include <algorithm>
+
+#include "layers_math.h"
+
+namespace mlip {
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef int i8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// The rows of one expert that a work-group has: expert (-1: none), first, end.
+struct Part {
+  int expert;
+  int64_t first, end;
+  int64_t begin;                // the expert's first row
+};
+// Part t of the experts' rows in parts of `rows`, each expert's from its first
+// row on.  All lanes of a wavefront call with the same t.  `whole`: every expert
+// has one part at least, also one without rows.
+__device__ Part find_part(const int32_t* offsets, int E, int64_t m, int64_t rows, int64_t t, bool whole) {
+  if (!offsets) {
+    const int64_t first = t * rows;
+    if (first >= m && !(whole && t == 0)) return {-1, 0, 0, 0};
+    return {0, first, min(m, first + rows), 0};
+  }
+  const int lane = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int e0 = 0; e0 < E; e0 += 64) {
+    const int e = e0 + lane;
+    int64_t from = 0, to = 0;
+    if (e < E) {
+      from = min(m, max(int64_t(0), int64_t(offsets[e])));
+      to = min(m, max(from, int64_t(offsets[e + 1])));
+    }
+    // (fewer than 2^31 parts: their number is at most m + E)
+    int parts = int((to - from + rows - 1) / rows);
+    if (whole && e < E && parts == 0) parts = 1;
+    int sum = parts;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int up = __shfl_up(sum, o);
+      if (lane >= o) sum += up;
+    }
+    const int64_t upto = before + sum;
+    const uint64_t mine = __ballot(t < upto && t >= upto - parts);
+    if (mine) {
+      const int l = __ffsll(static_cast<unsigned long long>(mine)) - 1;
+      const int64_t k = t - (before + __shfl(sum, l) - __shfl(parts, l));
+      const int64_t f = __shfl(int(from), l), g = __shfl(int(to), l);
+      return {uni(e0 + l), f + k * rows, min(g, f + (k + 1) * rows), f};
+    }
+    before += __shfl(sum, 63);
+  }
+  return {-1, 0, 0, 0};
+}
+
+// A work-group's number such that neighbours in it run on the same XCD.
+__device__ __forceinline__ int64_t near(int64_t id, int64_t total) {
+  const int64_t each = (total + 7) / 8, k = (id & 7) * each + (id >> 3);
+  return k;
+}
+
+// One operand's 32 codes of a lane as four bfloat16 operands.
+__device__ __forceinline__ void widen(const i8 c, float unit, bf8 v[4]) {
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const bf2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * s], unit, false);
+    const bf2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * s], unit, true);
+    const bf2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * s + 1], unit, false);
+    const bf2 f = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * s + 1], unit, true);
+    v[s] = bf8{a[0], a[1], b[0], b[1], d[0], d[1], f[0], f[1]};
+  }
+}
+
+// Four neighbouring outputs of a row.
+template <bool F32>
+__device__ __forceinline__ void put4(void* y, int64_t at, int left, const f4 v, bool whole) {
+  if (F32) {
+    float* p = static_cast<float*>(y) + at;
+    if (whole && left >= 4) *reinterpret_cast<f4*>(p) = v;
+    else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < left) p[q] = v[q];
+    }
+  } else {
+    uint16_t* p = static_cast<uint16_t*>(y) + at;
+    if (whole && left >= 4) {
+      *reinterpret_cast<u2v*>(p) = u2v{uint32_t(to_bf16(v[0])) | uint32_t(to_bf16(v[1])) << 16,
+                                       uint32_t(to_bf16(v[2])) | uint32_t(to_bf16(v[3])) << 16};
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < left) p[q] = to_bf16(v[q]);
+    }
+  }
+}
+
+// ---- many rows: tiles of 128 rows and 128 outputs -------------------------------
+
+constexpr int kTile = 128;
+constexpr int kStage = 2 * kTile * kBlock8;     // bytes of both operands' block of inputs
+
+// Rows first .. first + 127 of `codes` (none behind `last`), one block of 128
+// codes each, to LDS: 16-byte pieces, piece c of row r at (c ^ r % 8).
+__device__ __forceinline__ void stage(const uint8_t* codes, int64_t pitch, int64_t first, int64_t last, unsigned char* lds) {
+  const int w = uni(threadIdx.x >> 6), lane = threadIdx.x & 63;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r0 = 8 * (4 * w + k);
+    const int64_t row = min(last, first + r0 + (lane >> 3));
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(codes + row * pitch + 16 * ((lane & 7) ^ (lane >> 3))),
+                                     (__attribute__((address_space(3))) void*)(lds + r0 * kBlock8), 16, 0, 0);
+  }
+}
+// A lane's 32 codes of row r of a block: pieces g and g + 4 of the eight, for both operands.
+__device__ __forceinline__ i8 take(const unsigned char* lds, int r, int g) {
+  const u4v a = *reinterpret_cast<const u4v*>(lds + r * kBlock8 + 16 * (g ^ (r & 7)));
+  const u4v b = *reinterpret_cast<const u4v*>(lds + r * kBlock8 + 16 * ((g + 4) ^ (r & 7)));
+  return i8{int(a[0]), int(a[1]), int(a[2]), int(a[3]), int(b[0]), int(b[1]), int(b[2]), int(b[3])};
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256) void k_product(Product8Args a, int64_t row_tiles, int col_tiles) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * kStage];
+  const int64_t id = near(blockIdx.x, row_tiles * col_tiles);
+  if (id >= row_tiles * col_tiles) return;
+  // eight tiles of rows beside each other for each tile of outputs
+  const int64_t band = id / (8 * col_tiles), in = id - band * 8 * col_tiles;
+  const int deep = int(min(int64_t(8), row_tiles - 8 * band));
+  const int nt = int(in / deep);
+  const Part part = find_part(a.offsets, a.E, a.m, kTile, 8 * band + in % deep, false);
+  if (part.expert < 0) return;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, w = uni(threadIdx.x >> 6);
+  const int rows0 = 64 * (w & 1), cols0 = 64 * (w >> 1);      // of the wavefront, within the tile
+  const int64_t kp = codes8(a.K), xp = exps8(a.K);
+  const int blocks = (a.K + kBlock8 - 1) / kBlock8, blocks_n = (a.N + kBlock8 - 1) / kBlock8;
+  const uint8_t* wcodes = a.w + int64_t(part.expert) * a.N * kp;
+  const uint8_t* wexps = a.w_exps + (int64_t(part.expert) * blocks_n + nt) * xp;
+  const uint8_t* xexps[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) xexps[j] = a.x_exps + min(part.end - 1, part.first + rows0 + 16 * j + r) * xp;
+
+  f4 sum[4][4];                                               // outputs, rows
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+  uint32_t xe[4] = {}, we = 0;
+  stage(a.x, kp, part.first, part.end - 1, lds);
+  stage(wcodes, kp, int64_t(nt) * kTile, a.N - 1, lds + kTile * kBlock8);
+  for (int b = 0; b < blocks; ++b) {
+    unsigned char* here = lds + (b & 1) * kStage;
+    if (b % 4 == 0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) xe[j] = *reinterpret_cast<const uint32_t*>(xexps[j] + b);
+      we = *reinterpret_cast<const uint32_t*>(wexps + b);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();                                          // this block is there, the other one is used up
+    if (b + 1 < blocks) {
+      unsigned char* next = lds + ((b + 1) & 1) * kStage;
+      stage(a.x + int64_t(b + 1) * kBlock8, kp, part.first, part.end - 1, next);
+      stage(wcodes + int64_t(b + 1) * kBlock8, kp, int64_t(nt) * kTile, a.N - 1, next + kTile * kBlock8);
+    }
+    i8 x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = take(here, rows0 + 16 * j + r, g);
+    if constexpr (F32) {
+      bf8 xv[4][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) widen(x[j], __uint_as_float((xe[j] & 255u) << 23), xv[j]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        bf8 wv[4];
+        widen(take(here + kTile * kBlock8, cols0 + 16 * i + r, g), __uint_as_float((we & 255u) << 23), wv);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int s = 0; s < 4; ++s) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[s], xv[j][s], sum[i][j], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const i8 c = take(here + kTile * kBlock8, cols0 + 16 * i + r, g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          sum[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(c, x[j], sum[i][j], 0, 0, 0, int(we), 0, int(xe[j]));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) xe[j] >>= 8;
+    we >>= 8;
+  }
+  // a lane has four neighbouring outputs of a row
+  const bool whole = a.N % 4 == 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int n = nt * kTile + cols0 + 16 * i + 4 * g;
+    f4 bias = {0.f, 0.f, 0.f, 0.f};
+    if (a.bias) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (n + q < a.N) bias[q] = a.bias[int64_t(part.expert) * a.N + n + q];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t p = part.first + rows0 + 16 * j + r;
+      if (p < part.end) put4<F32>(a.y, p * a.N + n, a.N - n, sum[i][j] + bias, whole);
+    }
+  }
+}
+
+// ---- few rows: 16 rows and 16 outputs, the blocks of inputs shared by wavefronts ----
+
+template <bool F32>
+__global__ __launch_bounds__(256) void k_product_few(Product8Args a, int64_t row_tiles, int col_tiles) {
+  __shared__ f4 part_sum[4][64];
+  const int64_t id = blockIdx.x;
+  const int64_t rt = id / col_tiles;
+  const int n0 = int(id - rt * col_tiles) * 16;
+  const Part part = find_part(a.offsets, a.E, a.m, 16, rt, false);
+  if (part.expert < 0) return;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, w = uni(threadIdx.x >> 6);
+  const int64_t kp = codes8(a.K), xp = exps8(a.K);
+  const int blocks = (a.K + kBlock8 - 1) / kBlock8, blocks_n = (a.N + kBlock8 - 1) / kBlock8;
+  const uint8_t* wc = a.w + (int64_t(part.expert) * a.N + min(a.N - 1, n0 + r)) * kp + 16 * g;
+  const uint8_t* we = a.w_exps + (int64_t(part.expert) * blocks_n + n0 / kBlock8) * xp;
+  const int64_t p = min(part.end - 1, part.first + r);
+  const uint8_t* xc = a.x + p * kp + 16 * g;
+  const uint8_t* xe = a.x_exps + p * xp;
+  f4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int b = w; b < blocks; b += 4) {
+    const u4v w0 = *reinterpret_cast<const u4v*>(wc + int64_t(b) * kBlock8), w1 = *reinterpret_cast<const u4v*>(wc + int64_t(b) * kBlock8 + 64);
+    const u4v x0 = *reinterpret_cast<const u4v*>(xc + int64_t(b) * kBlock8), x1 = *reinterpret_cast<const u4v*>(xc + int64_t(b) * kBlock8 + 64);
+    const uint32_t ew = we[b], ex = xe[b];
+    const i8 c = {int(w0[0]), int(w0[1]), int(w0[2]), int(w0[3]), int(w1[0]), int(w1[1]), int(w1[2]), int(w1[3])};
+    const i8 x = {int(x0[0]), int(x0[1]), int(x0[2]), int(x0[3]), int(x1[0]), int(x1[1]), int(x1[2]), int(x1[3])};
+    if constexpr (F32) {
+      bf8 cv[4], xv[4];
+      widen(c, __uint_as_float(ew << 23), cv);
+      widen(x, __uint_as_float(ex << 23), xv);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cv[s], xv[s], sum, 0, 0, 0);
+    } else {
+      sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(c, x, sum, 0, 0, 0, int(ew), 0, int(ex));
+    }
+  }
+  part_sum[w][lane] = sum;
+  __syncthreads();
+  if (w != 0) return;
+  sum = (sum + part_sum[1][lane]) + (part_sum[2][lane] + part_sum[3][lane]);
+  const int n = n0 + 4 * g;
+  if (a.bias) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (n + q < a.N) sum[q] += a.bias[int64_t(part.expert) * a.N + n + q];
+  }
+  if (part.first + r < part.end) put4<F32>(a.y, (part.first + r) * a.N + n, a.N - n, sum, a.N % 4 == 0);
+}
+
+// ---- gradients of the matrices ----------------------------------------------------
+
+constexpr int kRows = 32;                       // rows of a step
+constexpr int kWide = kRows * kTile * 2;        // bytes of a step of one operand in bfloat16
+
+// A step's rows of one operand: 16 codes of one row a thread, half a block of lanes
+// each ..., with the row's power of two; zeros behind the part's end.
+struct Codes {
+  u4v c;
+  float unit;
+};
+__device__ __forceinline__ Codes fetch(const uint8_t* codes, const uint8_t* exps, int64_t pitch, int64_t xp, int64_t p, int64_t end, int block) {
+  Codes v;
+  v.c = u4v{0, 0, 0, 0};
+  v.unit = 1.f;
+  if (p < end) {
+    v.c = *reinterpret_cast<const u4v*>(codes + p * pitch + int64_t(block) * kBlock8 + 16 * (threadIdx.x & 7));
+    v.unit = __uint_as_float(uint32_t(exps[p * xp + block]) << 23);
+  }
+  return v;
+}
+// To LDS in bfloat16: rows of 256 bytes, 16 values (32 bytes) c of row p at c ^ p % 8.
+__device__ __forceinline__ void lay(const Codes v, unsigned char* lds) {
+  const int p = threadIdx.x >> 3, c = threadIdx.x & 7;
+  bf2 h[8];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    h[2 * q] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(v.c[q]), v.unit, false);
+    h[2 * q + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(v.c[q]), v.unit, true);
+  }
+  u4v* to = reinterpret_cast<u4v*>(lds + p * 256 + 32 * (c ^ (p & 7)));
+  to[0] = u4v{__builtin_bit_cast(uint32_t, h[0]), __builtin_bit_cast(uint32_t, h[1]), __builtin_bit_cast(uint32_t, h[2]),
+              __builtin_bit_cast(uint32_t, h[3])};
+  to[1] = u4v{__builtin_bit_cast(uint32_t, h[4]), __builtin_bit_cast(uint32_t, h[5]), __builtin_bit_cast(uint32_t, h[6]),
+              __builtin_bit_cast(uint32_t, h[7])};
+}
+// Values of 16 columns (c: which 16 of the 128) and the step's 32 rows as an
+// operand: read transposed, 16 lanes have 4 rows of 16 values at a time.
+__device__ __forceinline__ bf8 columns(const unsigned char* lds, int c) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, j = (lane & 15) >> 2, q = lane & 3;
+  s4 h[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int p = 16 * s + 4 * g + j;
+    h[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s4*)(lds + p * 256 + 32 * (c ^ (p & 7)) + 8 * q));
+  }
+  typedef short s8 __attribute__((ext_vector_type(8)));
+  return __builtin_bit_cast(bf8, s8{h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]});
+}
+
+__global__ __launch_bounds__(256) void k_product_weights(Product8Args a, int tiles_n, int tiles_k) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kWide];
+  const int64_t id = blockIdx.x;
+  const int tiles = tiles_n * tiles_k;
+  const int64_t item = id / tiles;
+  const int t = int(id - item * tiles), nt = t / tiles_k, kt = t - nt * tiles_k;
+  const Part part = find_part(a.offsets, a.E, a.m, a.slice, item, true);
+  if (part.expert < 0) return;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, w = uni(threadIdx.x >> 6);
+  const int n0 = w & 1, k0 = w >> 1;                          // 64 of the tile's outputs and inputs
+  const int64_t wp = codes8(a.N), wx = exps8(a.N), kp = codes8(a.K), kx = exps8(a.K);
+  const bool bias = a.dbias && kt == 0 && k0 == 0;
+  f4 sum[4][4], bsum[4];                                      // inputs, outputs
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    bsum[i] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+  }
+  const __bf16 one = 1.f;
+  const bf8 ones = {one, one, one, one, one, one, one, one};
+  int64_t p = part.first;
+  Codes dy = fetch(a.w, a.w_exps, wp, wx, p + (threadIdx.x >> 3), part.end, nt);
+  Codes x = fetch(a.x, a.x_exps, kp, kx, p + (threadIdx.x >> 3), part.end, kt);
+  for (int turn = 0; p < part.end; p += kRows, turn ^= 1) {
+    unsigned char* here = lds + turn * 2 * kWide;
+    lay(dy, here);
+    lay(x, here + kWide);
+    dy = fetch(a.w, a.w_exps, wp, wx, p + kRows + (threadIdx.x >> 3), part.end, nt);
+    x = fetch(a.x, a.x_exps, kp, kx, p + kRows + (threadIdx.x >> 3), part.end, kt);
+    __syncthreads();                                          // two buffers: one barrier a step
+    bf8 dv[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dv[j] = columns(here, 4 * n0 + j);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bf8 xv = columns(here + kWide, 4 * k0 + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, dv[j], sum[i][j], 0, 0, 0);
+    }
+    if (bias)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) bsum[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, dv[j], bsum[j], 0, 0, 0);
+  }
+  const int64_t to = a.slots ? item : part.expert;
+  float* out = (a.slots ? a.slots : a.dweights) + to * a.N * a.K;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int n = nt * kTile + 64 * n0 + 16 * j + r;
+    if (n >= a.N) continue;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = kt * kTile + 64 * k0 + 16 * i + 4 * g;
+      put4<true>(out, int64_t(n) * a.K + k, a.K - k, sum[i][j], a.K % 4 == 0);
+    }
+    if (bias && g == 0) (a.slots ? a.bias_slots : a.dbias)[to * a.N + n] = bsum[j][0];
+  }
+}
+
+// The experts' sums of their slices, in order.
+__global__ __launch_bounds__(256) void k_add_slices(Product8Args a) {
+  const int e = blockIdx.y;
+  int64_t first = 0, slices = 0;
+  {
+    // slices of the experts before, and of this one
+    const int lane = threadIdx.x & 63;
+    int64_t before = 0, mine = 0;
+    for (int f = lane; f <= e; f += 64) {
+      int64_t from = 0, to = a.m;
+      if (a.offsets) {
+        from = min(a.m, max(int64_t(0), int64_t(a.offsets[f])));
+        to = min(a.m, max(from, int64_t(a.offsets[f + 1])));
+      }
+      const int64_t parts = max(int64_t(1), (to - from + a.slice - 1) / a.slice);
+      if (f < e) before += parts;
+      else mine = parts;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) {
+      before += __shfl_xor(static_cast<long long>(before), o);
+      mine += __shfl_xor(static_cast<long long>(mine), o);
+    }
+    first = before;
+    slices = mine;
+  }
+  const int64_t values = int64_t(a.N) * a.K, all = values + (a.dbias ? a.N : 0);
+  for (int64_t v = int64_t(blockIdx.x) * 256 + threadIdx.x; v < all; v += int64_t(gridDim.x) * 256) {
+    const bool w = v < values;
+    const int64_t stride = w ? values : a.N, at = w ? v : v - values;
+    const float* from = (w ? a.slots : a.bias_slots) + first * stride + at;
+    float sum = 0.f;
+    for (int64_t s = 0; s < slices; ++s) sum += from[s * stride];
+    (w ? a.dweights : a.dbias)[e * stride + at] = sum;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_product8(const Product8Args& a, int n_cu, hipStream_t s) {
+  (void)n_cu;
+  // no more parts of T rows than this, whatever the experts' shares
+  const auto parts = [&](int64_t t) { return a.offsets ? std::min(a.m, (a.m + int64_t(a.E) * (t - 1)) / t) : (a.m + t - 1) / t; };
+  const bool few = a.m <= int64_t(16) * a.E;
+  if (few) {
+    const int cols = (a.N + 15) / 16;
+    const int64_t rows = parts(16);
+    if (a.bf16) k_product_few<false><<<unsigned(rows * cols), 256, 0, s>>>(a, rows, cols);
+    else k_product_few<true><<<unsigned(rows * cols), 256, 0, s>>>(a, rows, cols);
+  } else {
+    const int cols = (a.N + kTile - 1) / kTile;
+    const int64_t rows = parts(kTile), blocks = (rows * cols + 7) / 8 * 8;
+    if (a.bf16) k_product<false><<<unsigned(blocks), 256, 0, s>>>(a, rows, cols);
+    else k_product<true><<<unsigned(blocks), 256, 0, s>>>(a, rows, cols);
+  }
+  return hipGetLastError();
+}
+
+namespace {
+int64_t items(const Product8Args& a) { return a.m / a.slice + a.E; }
+}  // namespace
+
+size_t product8_weights_plan(Product8Args* a, int n_cu) {
+  const int64_t tiles = int64_t((a->N + kTile - 1) / kTile) * ((a->K + kTile - 1) / kTile);
+  // slices so that there are work-groups for every CU, of 256 rows at least
+  const int64_t want = std::max<int64_t>(1, (4 * int64_t(n_cu) + tiles - 1) / tiles);
+  a->slice = a->m;
+  if (tiles * a->E < 2 * int64_t(n_cu) && want > a->E) a->slice = std::max<int64_t>(256, (a->m + want - 1) / want);
+  a->slice = std::max<int64_t>(1, (a->slice + kRows - 1) / kRows * kRows);
+  if (a->slice >= a->m) return 0;
+  return size_t(items(*a)) * size_t(int64_t(a->N) * a->K + a->N) * sizeof(float);
+}
+
+void product8_workspace(Product8Args* a, unsigned char* ws) {
+  a->slots = nullptr;
+  a->bias_slots = nullptr;
+  if (a->slice >= a->m) return;
+  a->slots = reinterpret_cast<float*>(ws);
+  a->bias_slots = a->slots + items(*a) * a->N * a->K;
+}
+
+hipError_t launch_product8_weights(const Product8Args& a, int n_cu, hipStream_t s) {
+  const int tiles_n = (a.N + kTile - 1) / kTile, tiles_k = (a.K + kTile - 1) / kTile;
+  const int64_t count = a.slots ? items(a) : a.E;
+  k_product_weights<<<unsigned(count * tiles_n * tiles_k), 256, 0, s>>>(a, tiles_n, tiles_k);
+  if (a.slots) {
+    const int64_t values = int64_t(a.N) * a.K + a.N;
+    const dim3 g{unsigned(std::min<int64_t>((values + 255) / 256, int64_t(n_cu) * 8)), unsigned(a.E), 1};
+    k_add_slices<<<g, 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace mlip

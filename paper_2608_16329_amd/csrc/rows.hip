@@ -1,0 +1,220 @@
+// Rows brought into the experts' order and back with weights, and the gradient.
+//
+//   xs[p] = x[order[p] / k], p < offsets[E]; places[order[p]] = p, -1 from there on
+//   out_i = sum_s g_is y[places_is]
+//   dy[places_is] = g_is dout_i,  dg_is = <dout_i, y[places_is]>
+// and the gradient of the first in x is the second without weights.
+//
+// Bound by memory: each row is read once and written once, whole, in pieces of 16
+// bytes a lane.  A row has a group of 8 to 64 lanes, as many as take about four
+// pieces each, whose loads are under way together.  Sums are float32, in the
+// order of s; nothing is added up by atomics.
+#include <algorithm>
+
+#include "layers_math.h"
+
+namespace mlip {
+namespace {
+
+constexpr int kPieces = 4;      // 16-byte pieces a lane has under way
+
+// A row's pieces: whole ones, and the values behind them.
+struct Shape {
+  int pieces, tail, size;       // size of a value in bytes
+};
+__device__ __forceinline__ Shape shape(const RowsArgs& a) {
+  const int size = a.bf16 ? 2 : 4, bytes = a.width * size;
+  return {bytes / 16, bytes % 16 / size, size};
+}
+
+// Where entry `e` stands: its place, or -1 for none (and for what is no place).
+__device__ __forceinline__ int64_t place_of(const RowsArgs& a, int64_t e) {
+  const int64_t p = a.places[e];
+  return p < a.m ? p : -1;
+}
+
+template <bool BF>
+__device__ __forceinline__ void add(float* sum, const u4v v, float g) {
+  if (BF) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      sum[2 * q] = fmaf(g, __uint_as_float(v[q] << 16), sum[2 * q]);
+      sum[2 * q + 1] = fmaf(g, __uint_as_float(v[q] & 0xffff0000u), sum[2 * q + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum[q] = fmaf(g, __uint_as_float(v[q]), sum[q]);
+  }
+}
+template <bool BF>
+__device__ __forceinline__ u4v rounded(const float* v) {
+  u4v u;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    u[q] = BF ? uint32_t(to_bf16(v[2 * q])) | uint32_t(to_bf16(v[2 * q + 1])) << 16 : __float_as_uint(v[q]);
+  return u;
+}
+template <bool BF>
+__device__ __forceinline__ float value(const void* p, int64_t at) {
+  return BF ? from_bf16(static_cast<const uint16_t*>(p)[at]) : static_cast<const float*>(p)[at];
+}
+template <bool BF>
+__device__ __forceinline__ void set(void* p, int64_t at, float v) {
+  if (BF) static_cast<uint16_t*>(p)[at] = to_bf16(v);
+  else static_cast<float*>(p)[at] = v;
+}
+
+// One group of lanes for each place in the experts' order.
+template <bool BF, int L>
+__global__ __launch_bounds__(256) void k_sort(RowsArgs a) {
+  const Shape f = shape(a);
+  const int lane = threadIdx.x % L;
+  const int64_t end = min(a.m, max(int64_t(0), int64_t(a.offsets[a.E])));
+  for (int64_t p = int64_t(blockIdx.x) * (256 / L) + threadIdx.x / L; p < a.m; p += int64_t(gridDim.x) * (256 / L)) {
+    const uint32_t entry = uint32_t(a.order[p]);
+    if (entry >= a.m) continue;
+    if (lane == 0) a.places[entry] = p < end ? int32_t(p) : -1;
+    if (p >= end) continue;
+    const char* from = static_cast<const char*>(a.x) + int64_t(entry / uint32_t(a.K)) * a.x_stride * f.size;
+    char* to = static_cast<char*>(a.out) + p * a.width * f.size;
+    for (int c = lane; c < f.pieces; c += L * kPieces) {
+      u4v v[kPieces];
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q)
+        if (c + q * L < f.pieces) v[q] = *reinterpret_cast<const U4*>(from + 16 * (c + q * L));
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q)
+        if (c + q * L < f.pieces) *reinterpret_cast<U4*>(to + 16 * (c + q * L)) = v[q];
+    }
+    if (lane < f.tail) {
+      if (BF) reinterpret_cast<uint16_t*>(to)[f.pieces * 8 + lane] = reinterpret_cast<const uint16_t*>(from)[f.pieces * 8 + lane];
+      else reinterpret_cast<uint32_t*>(to)[f.pieces * 4 + lane] = reinterpret_cast<const uint32_t*>(from)[f.pieces * 4 + lane];
+    }
+  }
+}
+
+// One group of lanes for each row.
+template <bool BF, int L>
+__global__ __launch_bounds__(256) void k_combine(RowsArgs a) {
+  constexpr int V = BF ? 8 : 4;
+  const Shape f = shape(a);
+  const int lane = threadIdx.x % L;
+  for (int64_t i = int64_t(blockIdx.x) * (256 / L) + threadIdx.x / L; i < a.n; i += int64_t(gridDim.x) * (256 / L)) {
+    char* to = static_cast<char*>(a.out) + i * a.width * f.size;
+    for (int c = lane; c < f.pieces; c += L * kPieces) {
+      float sum[kPieces][V] = {};
+      for (int s = 0; s < a.K; ++s) {
+        const int64_t p = place_of(a, i * a.K + s);
+        if (p < 0) continue;
+        const float g = a.gates ? a.gates[i * a.K + s] : 1.f;
+        const char* from = static_cast<const char*>(a.x) + p * a.x_stride * f.size;
+        u4v v[kPieces];
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q)
+          if (c + q * L < f.pieces) v[q] = *reinterpret_cast<const U4*>(from + 16 * (c + q * L));
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q)
+          if (c + q * L < f.pieces) add<BF>(sum[q], v[q], g);
+      }
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q)
+        if (c + q * L < f.pieces) *reinterpret_cast<U4*>(to + 16 * (c + q * L)) = rounded<BF>(sum[q]);
+    }
+    if (lane < f.tail) {
+      float sum = 0.f;
+      const int at = f.pieces * V + lane;
+      for (int s = 0; s < a.K; ++s) {
+        const int64_t p = place_of(a, i * a.K + s);
+        if (p >= 0) sum = fmaf(a.gates ? a.gates[i * a.K + s] : 1.f, value<BF>(a.x, p * a.x_stride + at), sum);
+      }
+      set<BF>(a.out, i * a.width + at, sum);
+    }
+  }
+}
+
+// One group of lanes for each row: its gradient goes to its entries' places, and
+// its products with the experts' outputs there are the gates' gradients.
+template <bool BF, int L>
+__global__ __launch_bounds__(256) void k_combine_backward(RowsArgs a) {
+  constexpr int V = BF ? 8 : 4;
+  const Shape f = shape(a);
+  const int lane = threadIdx.x % L;
+  for (int64_t i = int64_t(blockIdx.x) * (256 / L) + threadIdx.x / L; i < a.n; i += int64_t(gridDim.x) * (256 / L)) {
+    const char* from = static_cast<const char*>(a.x) + i * a.x_stride * f.size;
+    for (int s = 0; s < a.K; ++s) {
+      const int64_t p = place_of(a, i * a.K + s);
+      float dot = 0.f;
+      if (p >= 0) {
+        const float g = a.gates ? a.gates[i * a.K + s] : 1.f;
+        const char* y = static_cast<const char*>(a.y) + p * a.y_stride * f.size;
+        char* to = static_cast<char*>(a.out) + p * a.width * f.size;
+        for (int c = lane; c < f.pieces; c += L * kPieces) {
+          u4v d[kPieces], v[kPieces];
+#pragma unroll
+          for (int q = 0; q < kPieces; ++q)
+            if (c + q * L < f.pieces) {
+              d[q] = *reinterpret_cast<const U4*>(from + 16 * (c + q * L));
+              if (a.dgates) v[q] = *reinterpret_cast<const U4*>(y + 16 * (c + q * L));
+            }
+#pragma unroll
+          for (int q = 0; q < kPieces; ++q)
+            if (c + q * L < f.pieces) {
+              float dv[V] = {}, out[V];
+              add<BF>(dv, d[q], 1.f);
+              if (a.dgates) {
+                float yv[V] = {};
+                add<BF>(yv, v[q], 1.f);
+#pragma unroll
+                for (int j = 0; j < V; ++j) dot = fmaf(dv[j], yv[j], dot);
+              }
+#pragma unroll
+              for (int j = 0; j < V; ++j) out[j] = g * dv[j];
+              *reinterpret_cast<U4*>(to + 16 * (c + q * L)) = rounded<BF>(out);
+            }
+        }
+        if (lane < f.tail) {
+          const int at = f.pieces * V + lane;
+          const float d = value<BF>(a.x, i * a.x_stride + at);
+          if (a.dgates) dot = fmaf(d, value<BF>(a.y, p * a.y_stride + at), dot);
+          set<BF>(a.out, p * a.width + at, g * d);
+        }
+      }
+      if (a.dgates) {
+#pragma unroll
+        for (int o = L / 2; o > 0; o /= 2) dot += __shfl_xor(dot, o);
+        if (lane == 0) a.dgates[i * a.K + s] = dot;
+      }
+    }
+  }
+}
+
+// Lanes of a row: 8 to 64, about kPieces pieces each.
+int lanes(const RowsArgs& a) {
+  const int pieces = a.width * (a.bf16 ? 2 : 4) / 16;
+  int l = 8;
+  while (l < 64 && l * kPieces < pieces) l *= 2;
+  return l;
+}
+int grid(int64_t rows, int l, int n_cu) { return int(std::max<int64_t>(1, std::min<int64_t>((rows * l + 255) / 256, int64_t(n_cu) * 64))); }
+
+template <bool BF, typename F>
+void with_lanes(int l, F run) {
+  if (l == 8) run(std::integral_constant<int, 8>());
+  else if (l == 16) run(std::integral_constant<int, 16>());
+  else if (l == 32) run(std::integral_constant<int, 32>());
+  else run(std::integral_constant<int, 64>());
+}
+
+}  // namespace
+
+#define ROWS_LAUNCH(kernel, rows)                                                                       \
+  const int l = lanes(a), g = grid(rows, l, n_cu);                                                      \
+  if (a.bf16) with_lanes<true>(l, [&](auto w) { kernel<true, w.value><<<g, 256, 0, s>>>(a); });         \
+  else with_lanes<false>(l, [&](auto w) { kernel<false, w.value><<<g, 256, 0, s>>>(a); });              \
+  return hipGetLastError()
+
+hipError_t launch_sort(const RowsArgs& a, int n_cu, hipStream_t s) { ROWS_LAUNCH(k_sort, a.m); }
+hipError_t launch_combine(const RowsArgs& a, int n_cu, hipStream_t s) { ROWS_LAUNCH(k_combine, a.n); }
+hipError_t launch_combine_backward(const RowsArgs& a, int n_cu, hipStream_t s) { ROWS_LAUNCH(k_combine_backward, a.n); }
+
+}  // namespace mlip

@@ -74,6 +74,38 @@ class _OnStream:
         return stride
 
 
+class Rows8:
+    """Places for `rows` rows of `width` values in 8 bits (mlip_pack8): codes uint8
+    [rows, width rounded up to 128s], exps uint8 [rows, blocks of 128 rounded up to fours]."""
+
+    def __init__(self, rows: int, width: int, *, device=None):
+        import torch
+        _need(rows >= 0, f"rows is {rows}")
+        _need(1 <= width <= 65536, f"width is {width}, not in 1..65536")
+        device = torch.device("cuda") if device is None else device
+        self.rows, self.width = rows, width
+        self.codes = torch.empty((rows, b.mlip_row8_codes(width)), dtype=torch.uint8, device=device)
+        self.exps = torch.empty((rows, b.mlip_row8_exps(width)), dtype=torch.uint8, device=device)
+
+
+class Weights8:
+    """Places for `experts` matrices [outputs, inputs] in 8 bits (mlip_pack8_weights),
+    and, with `transposed`, for their transposes, which gradients in x need."""
+
+    def __init__(self, experts: int, outputs: int, inputs: int, *, transposed: bool = True, device=None):
+        import torch
+        _need(1 <= experts <= 256, f"experts is {experts}, not in 1..256")
+        _need(1 <= outputs <= 65536 and 1 <= inputs <= 65536, f"{outputs} outputs and {inputs} inputs are not in 1..65536")
+        device = torch.device("cuda") if device is None else device
+        self.experts, self.outputs, self.inputs, self.transposed = experts, outputs, inputs, transposed
+
+        def places(rows, width):
+            return (torch.empty((experts, rows, b.mlip_row8_codes(width)), dtype=torch.uint8, device=device),
+                    torch.empty((experts, (rows + 127) // 128, b.mlip_row8_exps(width)), dtype=torch.uint8, device=device))
+        self.codes, self.exps = places(outputs, inputs)
+        self.t_codes, self.t_exps = places(inputs, outputs) if transposed else (None, None)
+
+
 class Learner(_OnStream):
     """One mlip_learn context bound to a stream (default: the current one).
 
@@ -200,6 +232,190 @@ class Learner(_OnStream):
                 self._dense(v, name, dtype, *shape)
         self._run(b.mlip_heads, self.ctx, p, n, _ptr(x), _ptr(weights), _ptr(offsets), _ptr(order), _ptr(gates), _ptr(denergy),
                   _ptr(energy), _ptr(dx), _ptr(dweights), _ptr(dgates))
+
+
+    # -- wide layers of experts ----------------------------------------------------
+
+    def _packed(self, r: Rows8, name: str, rows: int, width: int) -> None:
+        _need(r.codes.device == self.device, f"{name} is on {r.codes.device}, not {self.device}")
+        _need(r.rows == rows and r.width == width, f"{name} has {r.rows} rows of {r.width} values, not {rows} of {width}")
+
+    def _expert_offsets(self, offsets, experts: int) -> None:
+        if offsets is None:
+            _need(experts == 1, f"{experts} experts need offsets")
+        else:
+            self._dense(offsets, "offsets", self.torch.int32, experts + 1)
+
+    def sort(self, x, offsets, order, xs, places) -> None:
+        """The rows of `x` (f32 or bf16 [n, width], rows may be apart) in the order
+        that `group` found: xs (x's type) [n k, width], rows of entries without an
+        expert left as they are; places int32 [n, k], where each entry stands or -1
+        (mlip_sort).  The gradient in x is `combine` of xs' gradient."""
+        t = self.torch
+        stride = self._rows(x, "x")
+        n, width = x.shape
+        _need(places.dim() == 2, "places is not 2-d")
+        _need(offsets.dim() == 1 and offsets.shape[0] >= 2, "offsets is not 1-d with at least 2 places")
+        top_k = places.shape[1]
+        self._dense(places, "places", t.int32, n, top_k)
+        self._dense(offsets, "offsets", t.int32, offsets.shape[0])
+        self._dense(order, "order", t.int32, n * top_k)
+        self._dense(xs, "xs", x.dtype, n * top_k, width)
+        p = self._params(b.mlip_rows_params, offsets.shape[0] - 1, top_k, width, self._dtypes[x.dtype])
+        self._run(b.mlip_sort, self.ctx, p, n, _ptr(x), stride, _ptr(offsets), _ptr(order), _ptr(xs), _ptr(places))
+
+    def combine(self, y, places, out, *, gates=None) -> None:
+        """out (y's type, [n, width]): each row's sum of the rows of `y` ([n k, width],
+        rows may be apart) at its `places`, times its gates f32 [n, k] (mlip_combine)."""
+        t = self.torch
+        stride = self._rows(y, "y")
+        _need(places.dim() == 2, "places is not 2-d")
+        n, top_k = places.shape
+        _need(y.shape[0] == n * top_k, f"y has {y.shape[0]} rows, not {n} x {top_k}")
+        width = y.shape[1]
+        self._dense(places, "places", t.int32, n, top_k)
+        self._dense(out, "out", y.dtype, n, width)
+        if gates is not None:
+            self._dense(gates, "gates", t.float32, n, top_k)
+        p = self._params(b.mlip_rows_params, 1, top_k, width, self._dtypes[y.dtype])
+        self._run(b.mlip_combine, self.ctx, p, n, _ptr(y), stride, _ptr(places), _ptr(gates), _ptr(out))
+
+    def combine_backward(self, dout, y, places, dy, *, gates=None, dgates=None) -> None:
+        """Of sum(dout out): dy (dout's type, [n k, width], rows that are no place left as
+        they are) and, where it is given, dgates f32 [n, k], which alone needs `y`
+        (otherwise None may stand there) (mlip_combine_backward)."""
+        t = self.torch
+        stride = self._rows(dout, "dout")
+        _need(places.dim() == 2, "places is not 2-d")
+        n, top_k = places.shape
+        _need(dout.shape[0] == n, f"dout has {dout.shape[0]} rows, not {n}")
+        width = dout.shape[1]
+        self._dense(places, "places", t.int32, n, top_k)
+        self._dense(dy, "dy", dout.dtype, n * top_k, width)
+        if gates is not None:
+            self._dense(gates, "gates", t.float32, n, top_k)
+        y_stride = width
+        if dgates is not None:
+            _need(y is not None, "dgates needs y")
+            self._dense(dgates, "dgates", t.float32, n, top_k)
+            y_stride = self._rows(y, "y")
+            _need(y.dtype == dout.dtype and tuple(y.shape) == (n * top_k, width),
+                  f"y is {y.dtype} {tuple(y.shape)}, not {dout.dtype} {(n * top_k, width)}")
+        p = self._params(b.mlip_rows_params, 1, top_k, width, self._dtypes[dout.dtype])
+        self._run(b.mlip_combine_backward, self.ctx, p, n, _ptr(dout), stride, _ptr(y) if dgates is not None else None,
+                  y_stride, _ptr(places), _ptr(gates), _ptr(dy), _ptr(dgates))
+
+    def pack8(self, x, rows8: Rows8, *, offsets=None, order=None, top_k: int = 1) -> None:
+        """The rows of `x` (f32 or bf16 [n, width], rows may be apart) in 8 bits, or,
+        with what `group` wrote, their n top_k entries in the experts' order, rows of
+        entries without an expert left as they are (mlip_pack8)."""
+        t = self.torch
+        stride = self._rows(x, "x")
+        n, width = x.shape
+        _need((offsets is None) == (order is None), "offsets and order go together")
+        _need(order is not None or top_k == 1, "top_k is 1 without an order")
+        experts = 1
+        if offsets is not None:
+            _need(offsets.dim() == 1 and offsets.shape[0] >= 2, "offsets is not 1-d with at least 2 places")
+            experts = offsets.shape[0] - 1
+            self._dense(offsets, "offsets", t.int32, experts + 1)
+            self._dense(order, "order", t.int32, n * top_k)
+        self._packed(rows8, "rows8", n * top_k, width)
+        p = self._params(b.mlip_rows_params, experts, top_k, width, self._dtypes[x.dtype])
+        self._run(b.mlip_pack8, self.ctx, p, n, _ptr(x), stride, _ptr(offsets), _ptr(order), _ptr(rows8.codes),
+                  _ptr(rows8.exps))
+
+    def unpack8(self, rows8: Rows8, x) -> None:
+        """The values of rows in 8 bits into x, f32 or bf16 [rows, width] (mlip_unpack8)."""
+        _need(x.dtype in self._dtypes, f"x is {x.dtype}, not float32 or bfloat16")
+        self._packed(rows8, "rows8", rows8.rows, rows8.width)
+        self._dense(x, "x", x.dtype, rows8.rows, rows8.width)
+        p = self._params(b.mlip_rows_params, 1, 1, rows8.width, self._dtypes[x.dtype])
+        self._run(b.mlip_unpack8, self.ctx, p, rows8.rows, _ptr(rows8.codes), _ptr(rows8.exps), _ptr(x))
+
+    def _matrices(self, w8: Weights8, name: str) -> None:
+        _need(w8.codes.device == self.device, f"{name} is on {w8.codes.device}, not {self.device}")
+
+    def pack8_weights(self, w, w8: Weights8) -> None:
+        """Matrices (f32 or bf16 [experts, outputs, inputs]) in 8 bits, and their
+        transposes where w8 has places for them (mlip_pack8_weights)."""
+        _need(w.dtype in self._dtypes, f"w is {w.dtype}, not float32 or bfloat16")
+        self._matrices(w8, "w8")
+        self._dense(w, "w", w.dtype, w8.experts, w8.outputs, w8.inputs)
+        p = self._params(b.mlip_product8_params, w8.experts, w8.inputs, w8.outputs, self._dtypes[w.dtype])
+        self._run(b.mlip_pack8_weights, self.ctx, p, _ptr(w), _ptr(w8.codes), _ptr(w8.exps), _ptr(w8.t_codes),
+                  _ptr(w8.t_exps))
+
+    def product8(self, x8: Rows8, w8: Weights8, y, *, offsets=None, bias=None, transposed: bool = False) -> None:
+        """y (f32 or bf16 [m, outputs]): each packed row's product with its expert's
+        matrix, plus bias f32 [experts, outputs]; offsets int32 [experts + 1] as `group`
+        writes them for rows in the experts' order (one expert needs none), rows from the
+        last one on left as they are.  transposed: with the transposes, [m, inputs] from
+        rows of `outputs` values, the gradient in x (mlip_product8)."""
+        t = self.torch
+        _need(y.dtype in self._dtypes, f"y is {y.dtype}, not float32 or bfloat16")
+        _need(not transposed or w8.transposed, "w8 has no transposes")
+        n_in, n_out = (w8.outputs, w8.inputs) if transposed else (w8.inputs, w8.outputs)
+        self._matrices(w8, "w8")
+        self._packed(x8, "x8", x8.rows, n_in)
+        self._dense(y, "y", y.dtype, x8.rows, n_out)
+        self._expert_offsets(offsets, w8.experts)
+        if bias is not None:
+            self._dense(bias, "bias", t.float32, w8.experts, n_out)
+        p = self._params(b.mlip_product8_params, w8.experts, n_in, n_out, self._dtypes[y.dtype])
+        codes, exps = (w8.t_codes, w8.t_exps) if transposed else (w8.codes, w8.exps)
+        self._run(b.mlip_product8, self.ctx, p, x8.rows, _ptr(x8.codes), _ptr(x8.exps), _ptr(codes), _ptr(exps),
+                  _ptr(offsets), _ptr(bias), _ptr(y))
+
+    def product8_weights(self, dy8: Rows8, x8: Rows8, dweights, *, offsets=None, dbias=None) -> None:
+        """The matrices' gradients, f32 [experts, outputs, inputs], and dbias f32
+        [experts, outputs], from packed rows (mlip_product8_weights)."""
+        t = self.torch
+        _need(dweights.dim() == 3, "dweights is not 3-d")
+        experts, n_out, n_in = dweights.shape
+        self._packed(x8, "x8", x8.rows, n_in)
+        self._packed(dy8, "dy8", x8.rows, n_out)
+        self._dense(dweights, "dweights", t.float32, experts, n_out, n_in)
+        self._expert_offsets(offsets, experts)
+        if dbias is not None:
+            self._dense(dbias, "dbias", t.float32, experts, n_out)
+        p = self._params(b.mlip_product8_params, experts, n_in, n_out, b.MLIP_F32)
+        self._run(b.mlip_product8_weights, self.ctx, p, x8.rows, _ptr(dy8.codes), _ptr(dy8.exps), _ptr(x8.codes),
+                  _ptr(x8.exps), _ptr(offsets), _ptr(dweights), _ptr(dbias))
+
+    def activate8(self, z, kept: Optional[Rows8] = None, h=None, *, h8: Optional[Rows8] = None, residual=None) -> None:
+        """h = residual + silu(z) of the rows of `z` (f32 or bf16 [n, width], rows may be
+        apart, residual too) into h (z's type) and, packed, h8; z itself, packed, into
+        `kept` for the backward pass (mlip_activate8)."""
+        stride = self._rows(z, "z")
+        n, width = z.shape
+        residual_stride = width
+        if residual is not None:
+            residual_stride = self._rows(residual, "residual")
+            _need(residual.dtype == z.dtype and residual.shape == z.shape,
+                  f"residual is {residual.dtype} {tuple(residual.shape)}, not {z.dtype} {tuple(z.shape)}")
+        if h is not None:
+            self._dense(h, "h", z.dtype, n, width)
+        for r, name in ((kept, "kept"), (h8, "h8")):
+            if r is not None:
+                self._packed(r, name, n, width)
+        p = self._params(b.mlip_rows_params, 1, 1, width, self._dtypes[z.dtype])
+        self._run(b.mlip_activate8, self.ctx, p, n, _ptr(z), stride, _ptr(residual), residual_stride, _ptr(h),
+                  _ptr(h8 and h8.codes), _ptr(h8 and h8.exps), _ptr(kept and kept.codes), _ptr(kept and kept.exps))
+
+    def activate8_backward(self, kept: Rows8, dh, dz=None, *, dz8: Optional[Rows8] = None) -> None:
+        """dz = dh silu'(z) with the z that was kept, into dz (dh's type, [n, width]) and,
+        packed, dz8; dh's rows may be apart (mlip_activate8_backward)."""
+        stride = self._rows(dh, "dh")
+        n, width = dh.shape
+        self._packed(kept, "kept", n, width)
+        if dz is not None:
+            self._dense(dz, "dz", dh.dtype, n, width)
+        if dz8 is not None:
+            self._packed(dz8, "dz8", n, width)
+        p = self._params(b.mlip_rows_params, 1, 1, width, self._dtypes[dh.dtype])
+        self._run(b.mlip_activate8_backward, self.ctx, p, n, _ptr(kept.codes), _ptr(kept.exps), _ptr(dh), stride, _ptr(dz),
+                  _ptr(dz8 and dz8.codes), _ptr(dz8 and dz8.exps))
 
 
 class AdamW(_OnStream):
