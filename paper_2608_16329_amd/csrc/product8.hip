@@ -16,8 +16,10 @@
 // on 16x16x32 bfloat16 instructions (8e-9 on the same values): a code and its
 // power of two make a bfloat16 without rounding, one conversion for two.
 #include <algorithm>
+#include <type_traits>
 
 #include "layers_math.h"
+#include "learn.h"
 
 namespace mlip {
 namespace {
@@ -29,6 +31,16 @@ typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uni64(int64_t v) {
+  return int64_t(uint64_t(uint32_t(uni(int(v >> 32)))) << 32 | uint32_t(uni(int(v))));
+}
+
+// The same value, of which the compiler does not know that an earlier one was: what
+// is worked out from it is worked out where it is used, not kept from the loop's start.
+__device__ __forceinline__ int anew(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
 
 // The rows of one expert that a work-group has: expert (-1: none), first, end.
 struct Part {
@@ -69,17 +81,11 @@ __device__ Part find_part(const int32_t* offsets, int E, int64_t m, int64_t rows
       const int l = __ffsll(static_cast<unsigned long long>(mine)) - 1;
       const int64_t k = t - (before + __shfl(sum, l) - __shfl(parts, l));
       const int64_t f = __shfl(int(from), l), g = __shfl(int(to), l);
-      return {uni(e0 + l), f + k * rows, min(g, f + (k + 1) * rows), f};
+      return {uni(e0 + l), uni64(f + k * rows), uni64(min(g, f + (k + 1) * rows)), uni64(f)};
     }
     before += __shfl(sum, 63);
   }
   return {-1, 0, 0, 0};
-}
-
-// A work-group's number such that neighbours in it run on the same XCD.
-__device__ __forceinline__ int64_t near(int64_t id, int64_t total) {
-  const int64_t each = (total + 7) / 8, k = (id & 7) * each + (id >> 3);
-  return k;
 }
 
 // One operand's 32 codes of a lane as four bfloat16 operands.
@@ -92,6 +98,14 @@ __device__ __forceinline__ void widen(const i8 c, float unit, bf8 v[4]) {
     const bf2 f = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 * s + 1], unit, true);
     v[s] = bf8{a[0], a[1], b[0], b[1], d[0], d[1], f[0], f[1]};
   }
+}
+
+typedef float f2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, bf2));
+}
+__device__ __forceinline__ u4v bf16x8(const f4 a, const f4 b) {
+  return u4v{bf16x2(a[0], a[1]), bf16x2(a[2], a[3]), bf16x2(b[0], b[1]), bf16x2(b[2], b[3])};
 }
 
 // Four neighbouring outputs of a row.
@@ -108,8 +122,7 @@ __device__ __forceinline__ void put4(void* y, int64_t at, int left, const f4 v, 
   } else {
     uint16_t* p = static_cast<uint16_t*>(y) + at;
     if (whole && left >= 4) {
-      *reinterpret_cast<u2v*>(p) = u2v{uint32_t(to_bf16(v[0])) | uint32_t(to_bf16(v[1])) << 16,
-                                       uint32_t(to_bf16(v[2])) | uint32_t(to_bf16(v[3])) << 16};
+      *reinterpret_cast<u2v*>(p) = u2v{bf16x2(v[0], v[1]), bf16x2(v[2], v[3])};
     } else {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
@@ -118,118 +131,345 @@ __device__ __forceinline__ void put4(void* y, int64_t at, int left, const f4 v, 
   }
 }
 
-// ---- many rows: tiles of 128 rows and 128 outputs -------------------------------
+// ---- many rows: tiles of 32 RF rows and 32 CF outputs ------------------------------
 
 constexpr int kTile = 128;
-constexpr int kStage = 2 * kTile * kBlock8;     // bytes of both operands' block of inputs
 
-// Rows first .. first + 127 of `codes` (none behind `last`), one block of 128
-// codes each, to LDS: 16-byte pieces, piece c of row r at (c ^ r % 8).
-__device__ __forceinline__ void stage(const uint8_t* codes, int64_t pitch, int64_t first, int64_t last, unsigned char* lds) {
-  const int w = uni(threadIdx.x >> 6), lane = threadIdx.x & 63;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int r0 = 8 * (4 * w + k);
-    const int64_t row = min(last, first + r0 + (lane >> 3));
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(codes + row * pitch + 16 * ((lane & 7) ^ (lane >> 3))),
-                                     (__attribute__((address_space(3))) void*)(lds + r0 * kBlock8), 16, 0, 0);
-  }
+// Which of a wavefront's outputs row r of its operand i of W is: the four that a
+// lane gets of each of two neighbouring operands (rows 4 g .. 4 g + 3) are eight
+// neighbouring outputs, so bfloat16 results are stored 16 bytes a lane; float32
+// results are that with one operand.
+template <bool F32>
+__device__ __forceinline__ int output_of(int i, int r) {
+  return F32 ? 16 * i + r : 32 * (i >> 1) + 8 * (r >> 2) + 4 * (i & 1) + (r & 3);
 }
-// A lane's 32 codes of row r of a block: pieces g and g + 4 of the eight, for both operands.
-__device__ __forceinline__ i8 take(const unsigned char* lds, int r, int g) {
-  const u4v a = *reinterpret_cast<const u4v*>(lds + r * kBlock8 + 16 * (g ^ (r & 7)));
-  const u4v b = *reinterpret_cast<const u4v*>(lds + r * kBlock8 + 16 * ((g + 4) ^ (r & 7)));
+// Where 16-byte piece c of row r of a block stands in LDS: at c ^ key, such that
+// the 16 rows that lanes read together spread over the banks.
+template <bool PAIRS>
+__device__ __forceinline__ int key(int r) {
+  return PAIRS ? (r & 3) | ((r >> 3) & 1) << 2 : r & 7;
+}
+
+// Brings one block of 128 codes of a tile's rows to LDS, 8 rows an instruction, N
+// instructions a wavefront; a row behind the last one is the last one again.
+template <int N, bool PAIRS>
+struct Stage {
+  const uint8_t* base;
+  uint32_t at[N];               // of a lane's piece, from the tile's first row on
+  __device__ __forceinline__ Stage(const uint8_t* first, int64_t pitch, int rows) : base(first) {
+    const int w = uni(int(threadIdx.x >> 6)), lane = anew(threadIdx.x & 63);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int r = 8 * (N * w + k) + (lane >> 3);
+      at[k] = uint32_t(min(r, rows - 1)) * uint32_t(pitch) + 16u * ((lane & 7) ^ key<PAIRS>(r));
+    }
+  }
+  __device__ __forceinline__ void bring(int k, int block, unsigned char* lds) const {
+    const uint8_t* from = base + int64_t(block) * kBlock8;
+    unsigned char* to = lds + (N * uni(int(threadIdx.x >> 6)) + k) * (8 * kBlock8);
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + at[k]),
+                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  }
+};
+// A lane's 32 codes of a row of a block: pieces g and g + 4 of the eight, for both
+// operands.  Where they are depends on the row's lowest bits alone, so other rows
+// that a lane takes are at a distance that the instruction has in it.
+struct Pieces {
+  int a, b;
+  template <bool PAIRS>
+  static __device__ __forceinline__ Pieces of(int r, int g) {
+    return {r * kBlock8 + 16 * (g ^ key<PAIRS>(r)), r * kBlock8 + 16 * ((g + 4) ^ key<PAIRS>(r))};
+  }
+};
+__device__ __forceinline__ i8 take(const unsigned char* lds, Pieces p, int rows_on) {
+  const u4v a = *reinterpret_cast<const u4v*>(lds + p.a + rows_on * kBlock8);
+  const u4v b = *reinterpret_cast<const u4v*>(lds + p.b + rows_on * kBlock8);
   return i8{int(a[0]), int(a[1]), int(a[2]), int(a[3]), int(b[0]), int(b[1]), int(b[2]), int(b[3])};
 }
 
-template <bool F32>
-__global__ __launch_bounds__(256) void k_product(Product8Args a, int64_t row_tiles, int col_tiles) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * kStage];
-  const int64_t id = near(blockIdx.x, row_tiles * col_tiles);
-  if (id >= row_tiles * col_tiles) return;
-  // eight tiles of rows beside each other for each tile of outputs
-  const int64_t band = id / (8 * col_tiles), in = id - band * 8 * col_tiles;
-  const int deep = int(min(int64_t(8), row_tiles - 8 * band));
-  const int nt = int(in / deep);
-  const Part part = find_part(a.offsets, a.E, a.m, kTile, 8 * band + in % deep, false);
-  if (part.expert < 0) return;
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, w = uni(threadIdx.x >> 6);
-  const int rows0 = 64 * (w & 1), cols0 = 64 * (w >> 1);      // of the wavefront, within the tile
-  const int64_t kp = codes8(a.K), xp = exps8(a.K);
-  const int blocks = (a.K + kBlock8 - 1) / kBlock8, blocks_n = (a.N + kBlock8 - 1) / kBlock8;
-  const uint8_t* wcodes = a.w + int64_t(part.expert) * a.N * kp;
-  const uint8_t* wexps = a.w_exps + (int64_t(part.expert) * blocks_n + nt) * xp;
-  const uint8_t* xexps[4];
+// Tiles of rows of all experts: which tile is each expert's first, and its rows.
+struct Tiles {
+  int first[kMaxExperts + 1], from[kMaxExperts], to[kMaxExperts];
+};
+// Filled in by the first wavefront; the work-group waits for it.  Returns the
+// number of tiles.
+__device__ __forceinline__ int count_tiles(Tiles& t, const Product8Args& a, int rows) {
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    int before = 0;
+    for (int e0 = 0; e0 < a.E; e0 += 64) {
+      const int e = e0 + lane;
+      int from = 0, to = 0;
+      if (e < a.E) {
+        from = a.offsets ? int(min(a.m, int64_t(max(0, a.offsets[e])))) : 0;
+        to = a.offsets ? int(min(a.m, int64_t(max(from, a.offsets[e + 1])))) : int(a.m);
+      }
+      int sum = (to - from) / rows + ((to - from) % rows ? 1 : 0);
+      const int mine = sum;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) xexps[j] = a.x_exps + min(part.end - 1, part.first + rows0 + 16 * j + r) * xp;
+      for (int o = 1; o < 64; o *= 2) {
+        const int up = __shfl_up(sum, o);
+        if (lane >= o) sum += up;
+      }
+      if (e < a.E) {
+        t.first[e] = before + sum - mine;
+        t.from[e] = from;
+        t.to[e] = to;
+      }
+      before += __shfl(sum, 63);
+    }
+    if (lane == 0) t.first[a.E] = before;
+  }
+  __syncthreads();
+  return uni(t.first[a.E]);
+}
+__device__ __forceinline__ int expert_of(const Tiles& t, int E, int tile) {
+  for (int e0 = 0;; e0 += 64) {
+    const int e = min(E - 1, e0 + int(threadIdx.x & 63));
+    const uint64_t mine = __ballot(t.first[e] <= tile && tile < t.first[e + 1]);
+    if (mine || e0 + 64 >= E) return min(E - 1, e0 + int(__ffsll(static_cast<unsigned long long>(mine))) - 1);
+  }
+}
 
-  f4 sum[4][4];                                               // outputs, rows
+// STREAM: y is larger than the last cache and goes past it.
+template <bool F32, int RF, int CF, int WR, int WC, bool STREAM = false>
+__global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
+  constexpr int kWaves = WR * WC, kRowTile = 16 * RF * WR, kColTile = 16 * CF * WC, kStage = (kRowTile + kColTile) * kBlock8;
+  constexpr int kBringX = kRowTile / 8 / kWaves, kBringW = kColTile / 8 / kWaves;
+  constexpr int kSide = F32 ? 1 : 2, kStores = RF * CF / kSide;
+  // (two variables, not one with two halves: what is read from the one does not wait
+  // for what is on its way to the other)
+  __shared__ __attribute__((aligned(16))) unsigned char lds0[kStage], lds1[kStage];
+  __shared__ __attribute__((aligned(16))) float col_bias[kColTile];
+  __shared__ uint32_t row_exps[2 * kRowTile];                 // of four blocks, and of the four behind them
+  __shared__ Tiles tiles;
+  const int row_tiles = count_tiles(tiles, a, kRowTile), col_tiles = (a.N + kColTile - 1) / kColTile;
+  // a work-group takes tiles of its XCD's share (work-groups go round the eight) in
+  // turn with the others there: neighbours in time share rows or outputs in its cache
+  const int64_t total = int64_t(row_tiles) * col_tiles;
+  const int xcd = blockIdx.x & 7, slots = gridDim.x >> 3;
+  const int last = uni(int(total * (xcd + 1) / 8));
+  int id = uni(int(total * xcd / 8)) + int(blockIdx.x >> 3);
+  if (id >= last) return;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, w = uni(int(threadIdx.x >> 6));
+  const int rows0 = 16 * RF * (w % WR), cols0 = 16 * CF * (w / WR);   // of the wavefront, within the tile
+  const int64_t kp = codes8(a.K);
+  const uint32_t xp = uint32_t(exps8(a.K));
+  const int blocks = (a.K + kBlock8 - 1) / kBlock8, blocks_n = (a.N + kBlock8 - 1) / kBlock8;
+  // a wavefront's outputs are within one block of W
+  static_assert(kBlock8 % (16 * CF) == 0);
+
+  struct Tile {
+    int expert, first, rows, n0;
+  };
+  const auto held = [](const Tile& t) { return Tile{uni(t.expert), uni(t.first), uni(t.rows), uni(t.n0)}; };
+  const auto tile_of = [&](int t) {
+    // eight tiles of rows beside each other for each tile of outputs
+    const int band = t / (8 * col_tiles), in = t - band * 8 * col_tiles, deep = min(8, row_tiles - 8 * band);
+    const int rt = 8 * band + in % deep;
+    Tile v;
+    v.expert = uni(expert_of(tiles, a.E, rt));
+    v.first = uni(tiles.from[v.expert] + (rt - tiles.first[v.expert]) * kRowTile);
+    v.rows = uni(min(kRowTile, tiles.to[v.expert] - v.first));
+    v.n0 = uni(in / deep) * kColTile;
+    return v;
+  };
+  const auto xstage_of = [&](const Tile& t) { return Stage<kBringX, false>(a.x + t.first * kp, kp, t.rows); };
+  const auto wstage_of = [&](const Tile& t) {
+    return Stage<kBringW, !F32>(a.w + (int64_t(t.expert) * a.N + t.n0) * kp, kp, min(kColTile, a.N - t.n0));
+  };
+  // On their way to LDS, for which a lane has one register: exponents of four blocks
+  // of a row (the first wavefronts), the bias of one of the tile's outputs (the
+  // others).  Those of the wavefront's outputs are in one block, and scalar.
+  constexpr int kRowWaves = kRowTile / 64;
+  static_assert(kRowWaves + kColTile / 64 == kWaves);
+  uint32_t we = 0, wnext, coming = 0;
+  const auto exponents = [&](const Tile& t, int b) {
+    wnext = *(const __attribute__((address_space(4))) uint32_t*)(a.w_exps + (int64_t(t.expert) * blocks_n + min(blocks_n - 1, (t.n0 + cols0) / kBlock8)) * xp + b);
+    if (w < kRowWaves)
+      coming = *reinterpret_cast<const uint32_t*>(a.x_exps + int64_t(t.first) * xp + b + uint32_t(min(t.rows - 1, 64 * w + anew(lane))) * xp);
+  };
+  const auto lay_exponents = [&](int half) {
+    if (w < kRowWaves) row_exps[half * kRowTile + 64 * w + anew(lane)] = coming;
+  };
+  const auto bias = [&](const Tile& t) {
+    if (a.bias && w >= kRowWaves)
+      coming = __float_as_uint(a.bias[int64_t(t.expert) * a.N + min(a.N - 1, t.n0 + 64 * (w - kRowWaves) + anew(lane))]);
+  };
+  const auto lay_bias = [&] {
+    if (a.bias && w >= kRowWaves) col_bias[64 * (w - kRowWaves) + anew(lane)] = __uint_as_float(coming);
+  };
+
+  Tile tile = tile_of(id);
+  Stage<kBringX, false> xstage = xstage_of(tile);
+  Stage<kBringW, !F32> wstage = wstage_of(tile);
+  exponents(tile, 0);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int k = 0; k < kBringX; ++k) xstage.bring(k, 0, lds0);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sum[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-  uint32_t xe[4] = {}, we = 0;
-  stage(a.x, kp, part.first, part.end - 1, lds);
-  stage(wcodes, kp, int64_t(nt) * kTile, a.N - 1, lds + kTile * kBlock8);
-  for (int b = 0; b < blocks; ++b) {
-    unsigned char* here = lds + (b & 1) * kStage;
+  for (int k = 0; k < kBringW; ++k) wstage.bring(k, 0, lds0 + kRowTile * kBlock8);
+  lay_exponents(0);
+  const Pieces xp0 = Pieces::of<false>(rows0 + r, g), wp0 = Pieces::of<!F32>(cols0 + output_of<F32>(0, r), g);
+  int half = 1;                                               // of row_exps that has the block's
+  bool more = id + slots < last;
+  Tile then = tile_of(more ? id + slots : id);
+  f4 sum[CF][RF];                                             // outputs, rows
+
+  // Products of block b of the tile, in LDS at xs, and before the first of them requests
+  // for block `after` of the tile that the stages are at (the last block once more,
+  // unused, where there is none).
+  const auto step = [&](int b, const unsigned char* xs, int after, unsigned char* next) {
+    const unsigned char* const ws = xs + kRowTile * kBlock8;
+    uint32_t xe[RF];
+    {
+      const uint8_t* const from = reinterpret_cast<const uint8_t*>(row_exps + half * kRowTile + rows0 + r) + (b & 3);
+#pragma unroll
+      for (int j = 0; j < RF; ++j) xe[j] = from[64 * j];
+    }
+    __builtin_amdgcn_sched_barrier(0);
     if (b % 4 == 0) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) xe[j] = *reinterpret_cast<const uint32_t*>(xexps[j] + b);
-      we = *reinterpret_cast<const uint32_t*>(wexps + b);
+      const bool on = b + 4 < blocks;
+      exponents(on ? tile : then, on ? b + 4 : 0);
+      if (b == 0) bias(tile);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();                                          // this block is there, the other one is used up
-    if (b + 1 < blocks) {
-      unsigned char* next = lds + ((b + 1) & 1) * kStage;
-      stage(a.x + int64_t(b + 1) * kBlock8, kp, part.first, part.end - 1, next);
-      stage(wcodes + int64_t(b + 1) * kBlock8, kp, int64_t(nt) * kTile, a.N - 1, next + kTile * kBlock8);
-    }
-    i8 x[4];
+    const auto bring = [&] {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = take(here, rows0 + 16 * j + r, g);
+      for (int k = 0; k < kBringX; ++k) xstage.bring(k, after, next);
+#pragma unroll
+      for (int k = 0; k < kBringW; ++k) wstage.bring(k, after, next + kRowTile * kBlock8);
+    };
+    const auto of_x = [&](int j) { return take(xs, xp0, 16 * j); };
+    const auto of_w = [&](int i) { return take(ws, wp0, output_of<F32>(i, 0)); };
     if constexpr (F32) {
-      bf8 xv[4][4];
+      bf8 wv[CF][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) widen(x[j], __uint_as_float((xe[j] & 255u) << 23), xv[j]);
+      for (int i = 0; i < CF; ++i) widen(of_w(i), __uint_as_float((we & 255u) << 23), wv[i]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bf8 wv[4];
-        widen(take(here + kTile * kBlock8, cols0 + 16 * i + r, g), __uint_as_float((we & 255u) << 23), wv);
+      for (int j = 0; j < RF; ++j) {
+        if (j == 0) bring();
+        bf8 xv[4];
+        widen(of_x(j), __uint_as_float(xe[j] << 23), xv);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int i = 0; i < CF; ++i)
 #pragma unroll
-          for (int s = 0; s < 4; ++s) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[s], xv[j][s], sum[i][j], 0, 0, 0);
+          for (int s = 0; s < 4; ++s) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i][s], xv[s], sum[i][j], 0, 0, 0);
       }
     } else {
+      i8 c[CF], x = of_x(0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const i8 c = take(here + kTile * kBlock8, cols0 + 16 * i + r, g);
+      for (int i = 0; i < CF; ++i) c[i] = of_w(i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          sum[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(c, x[j], sum[i][j], 0, 0, 0, int(we), 0, int(xe[j]));
+      for (int j = 0; j < RF; ++j) {
+        i8 ahead = x;
+        if (j + 1 < RF) ahead = of_x(j + 1);
+        if (j == 0) bring();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < CF; ++i)
+          sum[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(c[i], x, sum[i][j], 0, 0, 0, int(we), 0, int(xe[j]));
+        __builtin_amdgcn_sched_barrier(0);
+        x = ahead;
       }
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) xe[j] >>= 8;
     we >>= 8;
-  }
-  // a lane has four neighbouring outputs of a row
-  const bool whole = a.N % 4 == 0;
+  };
+  // What was asked for is there, and what was read is used up, in all wavefronts.
+  const auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+  meet();
+  for (;;) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int n = nt * kTile + cols0 + 16 * i + 4 * g;
-    f4 bias = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < CF; ++i)
+#pragma unroll
+      for (int j = 0; j < RF; ++j) sum[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < blocks; b += 2) {
+      if (b % 4 == 0) {
+        we = wnext;
+        half ^= 1;
+      }
+      step(b, lds0, min(b + 1, blocks - 1), lds1);
+      meet();
+      if (b % 4 == 0) lay_exponents(half ^ 1);
+      if (b == 0) lay_bias();
+      // behind the last block the next tile's first one
+      const bool on = b + 2 < blocks;
+      if (!on) {
+        xstage = xstage_of(then);
+        wstage = wstage_of(then);
+      }
+      if (b + 1 < blocks) {
+        step(b + 1, lds1, on ? b + 2 : 0, lds0);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kBringX; ++k) xstage.bring(k, 0, lds0);
+#pragma unroll
+        for (int k = 0; k < kBringW; ++k) wstage.bring(k, 0, lds0 + kRowTile * kBlock8);
+      }
+      if (on) meet();
+    }
+
+    // a lane has four neighbouring outputs of a row, with those of the next operand eight
+    const int lane1 = anew(lane), r1 = rows0 + (lane1 & 15), g1 = lane1 >> 4;
+    const bool whole = a.N % (4 * kSide) == 0;
+    using Out = std::conditional_t<F32, float, uint16_t>;
+    Out* const y = static_cast<Out*>(a.y) + int64_t(tile.first) * a.N;
     if (a.bias) {
+      if (blocks <= 2) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (n + q < a.N) bias[q] = a.bias[int64_t(part.expert) * a.N + n + q];
-    }
+      for (int i = 0; i < CF; ++i) {
+        const f4 c = *reinterpret_cast<const f4*>(col_bias + cols0 + output_of<F32>(i, 4 * g1));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t p = part.first + rows0 + 16 * j + r;
-      if (p < part.end) put4<F32>(a.y, p * a.N + n, a.N - n, sum[i][j] + bias, whole);
+        for (int j = 0; j < RF; ++j) sum[i][j] += c;
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
+    const auto store = [&](int i, int j, int p, int n) {
+      Out* const to = y + int64_t(p) * a.N + n;
+      if constexpr (F32) *reinterpret_cast<f4*>(to) = sum[i][j];
+      else if constexpr (STREAM) __builtin_nontemporal_store(bf16x8(sum[i][j], sum[i + 1][j]), reinterpret_cast<u4v*>(to));
+      else *reinterpret_cast<u4v*>(to) = bf16x8(sum[i][j], sum[i + 1][j]);
+    };
+    const bool full = whole && tile.rows == kRowTile && tile.n0 + kColTile <= a.N;
+    if (full) {
+#pragma unroll
+      for (int j = 0; j < RF; ++j) {
+#pragma unroll
+        for (int i = 0; i < CF; i += kSide) store(i, j, r1 + 16 * j, tile.n0 + cols0 + output_of<F32>(i, 4 * g1));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else if (whole) {
+#pragma unroll
+      for (int j = 0; j < RF; ++j)
+#pragma unroll
+        for (int i = 0; i < CF; i += kSide) {
+          const int p = r1 + 16 * j, n = tile.n0 + cols0 + output_of<F32>(i, 4 * g1);
+          if (p < tile.rows && n < a.N) store(i, j, p, n);
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < CF; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int n = tile.n0 + cols0 + output_of<F32>(i, 4 * g1) + q;
+          if (n < a.N)
+#pragma unroll
+            for (int j = 0; j < RF; ++j) {
+              const int p = r1 + 16 * j;
+              if (p >= tile.rows) continue;
+              if constexpr (F32) y[int64_t(p) * a.N + n] = sum[i][j][q];
+              else y[int64_t(p) * a.N + n] = to_bf16(sum[i][j][q]);
+            }
+        }
+    }
+    if (!more) break;
+    id += slots;
+    tile = held(then);
+    more = id + slots < last;
+    then = tile_of(more ? id + slots : id);
+    // the next tile's first block is there; a full tile's stores, which were issued
+    // after it and are counted in order, may be under way
+    if (full) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(kStores) : "memory");
+    else meet();
   }
 }
 
@@ -431,7 +671,6 @@ __global__ __launch_bounds__(256) void k_add_slices(Product8Args a) {
 }  // namespace
 
 hipError_t launch_product8(const Product8Args& a, int n_cu, hipStream_t s) {
-  (void)n_cu;
   // no more parts of T rows than this, whatever the experts' shares
   const auto parts = [&](int64_t t) { return a.offsets ? std::min(a.m, (a.m + int64_t(a.E) * (t - 1)) / t) : (a.m + t - 1) / t; };
   const bool few = a.m <= int64_t(16) * a.E;
@@ -441,10 +680,15 @@ hipError_t launch_product8(const Product8Args& a, int n_cu, hipStream_t s) {
     if (a.bf16) k_product_few<false><<<unsigned(rows * cols), 256, 0, s>>>(a, rows, cols);
     else k_product_few<true><<<unsigned(rows * cols), 256, 0, s>>>(a, rows, cols);
   } else {
-    const int cols = (a.N + kTile - 1) / kTile;
-    const int64_t rows = parts(kTile), blocks = (rows * cols + 7) / 8 * 8;
-    if (a.bf16) k_product<false><<<unsigned(blocks), 256, 0, s>>>(a, rows, cols);
-    else k_product<true><<<unsigned(blocks), 256, 0, s>>>(a, rows, cols);
+    // `each` work-groups a CU, as many as there is LDS for
+    const auto run = [&](auto kernel, int64_t row_tile, int col_tile, int threads, int each) {
+      const int64_t tiles = parts(row_tile) * ((a.N + col_tile - 1) / col_tile);
+      kernel<<<unsigned((std::min(tiles, int64_t(n_cu) * each) + 7) / 8 * 8), threads, 0, s>>>(a);
+    };
+    if (!a.bf16) run(k_product<true, 4, 4, 2, 2>, 128, 128, 256, 2);
+    else if (parts(256) * ((a.N + 255) / 256) >= n_cu / 2)
+      run(a.m * a.N > int64_t(1) << 27 ? k_product<false, 8, 4, 2, 4, true> : k_product<false, 8, 4, 2, 4>, 256, 256, 512, 1);
+    else run(k_product<false, 4, 4, 2, 2>, 128, 128, 256, 2);
   }
   return hipGetLastError();
 }
