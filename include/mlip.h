@@ -595,8 +595,7 @@ mlip_status mlip_unpack8(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, 
  * the packed values' products; dtype is not looked at beyond its range.  A NaN in
  * a row gives NaN wherever it is a factor.
  * m in [0, 2^31), n_experts 1..256, inputs and outputs 1..65536, and (m / 128 +
- * n_experts) outputs / 128, and n_experts inputs outputs / 2^14 (times the slices of
- * rows that are added up), below 2^24.
+ * n_experts) outputs / 128, and n_experts inputs outputs / 2^14, below 2^22.
  * Errors: MLIP_E_ARG, and of mlip_product8_weights MLIP_E_STATE, MLIP_E_OOM; MLIP_E_HIP.
  */
 typedef struct {

@@ -10,7 +10,7 @@ using namespace mlip;
 namespace {
 
 constexpr int64_t kMaxStride = int64_t(1) << 31;
-constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;      // work-groups of 256 in a launch
+constexpr int64_t kMaxBlocks = (int64_t(1) << 22) - 1;      // work-groups of up to 1024 in a launch
 
 mlip_status check_rows(mlip_learn* ctx, const mlip_rows_params* p, int64_t n) {
   if (!p) return fail(ctx, MLIP_E_ARG, "NULL parameters");
@@ -242,7 +242,7 @@ mlip_status mlip_product8(mlip_learn* ctx, const mlip_product8_params* p, int64_
                           const int32_t* offsets_dev, const float* bias_dev, void* y_dev) {
   LAYER_BEGIN(check_product(ctx, p, m));
   if (!offsets_dev && p->n_experts != 1) return fail(ctx, MLIP_E_ARG, "several experts need offsets");
-  if ((tiles_of(m) + p->n_experts) * tiles_of(p->outputs) > kMaxBlocks) return fail(ctx, MLIP_E_ARG, "m outputs exceeds 2^38");
+  if ((tiles_of(m) + p->n_experts) * tiles_of(p->outputs) > kMaxBlocks) return fail(ctx, MLIP_E_ARG, "m outputs exceeds 2^36");
   if (m == 0) return MLIP_OK;
   if (!x_codes_dev || !x_exps_dev || !w_codes_dev || !w_exps_dev || !y_dev) return fail(ctx, MLIP_E_ARG, "NULL argument");
   if (!placed(x_codes_dev, x_exps_dev) || !placed(w_codes_dev, w_exps_dev)) return fail(ctx, MLIP_E_ARG, kPlaced);
@@ -288,7 +288,7 @@ mlip_status mlip_product8_weights(mlip_learn* ctx, const mlip_product8_params* p
   a.dbias = dbias_dev;
   const size_t need = product8_weights_plan(&a, ctx->n_cu);
   if ((m / a.slice + p->n_experts) * tiles_of(p->outputs) * tiles_of(p->inputs) > kMaxBlocks)
-    return fail(ctx, MLIP_E_ARG, "n_experts inputs outputs exceeds 2^38");
+    return fail(ctx, MLIP_E_ARG, "n_experts inputs outputs exceeds 2^36");
   const mlip_status w = workspace(ctx, need);
   if (w != MLIP_OK) return w;
   product8_workspace(&a, ctx->d_ws);

@@ -88,6 +88,26 @@ __device__ Part find_part(const int32_t* offsets, int E, int64_t m, int64_t rows
   return {-1, 0, 0, 0};
 }
 
+// All rows of the expert that is the rank-th largest, for at most 64 experts: long
+// parts first leave the work-groups that come last short ones.
+__device__ Part sized_part(const int32_t* offsets, int E, int64_t m, int rank) {
+  const int lane = threadIdx.x & 63;
+  int from = 0, to = -1;
+  if (lane < E) {
+    from = int(min(m, int64_t(max(0, offsets[lane]))));
+    to = int(min(m, int64_t(max(from, offsets[lane + 1]))));
+  }
+  const int mine = to - from;
+  int larger = 0;
+  for (int f = 0; f < E; ++f) {
+    const int other = __builtin_amdgcn_readlane(mine, f);
+    larger += other > mine || (other == mine && f < lane) ? 1 : 0;
+  }
+  const int l = uni(int(__ffsll(static_cast<unsigned long long>(__ballot(lane < E && larger == rank))) - 1));
+  const int first = __builtin_amdgcn_readlane(from, l);
+  return {l, first, __builtin_amdgcn_readlane(to, l), first};
+}
+
 // One operand's 32 codes of a lane as four bfloat16 operands.
 __device__ __forceinline__ void widen(const i8 c, float unit, bf8 v[4]) {
 #pragma unroll
@@ -132,8 +152,6 @@ __device__ __forceinline__ void put4(void* y, int64_t at, int left, const f4 v, 
 }
 
 // ---- many rows: tiles of 32 RF rows and 32 CF outputs ------------------------------
-
-constexpr int kTile = 128;
 
 // Which of a wavefront's outputs row r of its operand i of W is: the four that a
 // lane gets of each of two neighbouring operands (rows 4 g .. 4 g + 3) are eight
@@ -282,7 +300,8 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
   // of a row (the first wavefronts), the bias of one of the tile's outputs (the
   // others).  Those of the wavefront's outputs are in one block, and scalar.
   constexpr int kRowWaves = kRowTile / 64;
-  static_assert(kRowWaves + kColTile / 64 == kWaves);
+  constexpr int kColWaves = kColTile / 64;
+  static_assert(kRowWaves + kColWaves <= kWaves);
   uint32_t we = 0, wnext, coming = 0;
   const auto exponents = [&](const Tile& t, int b) {
     wnext = *(const __attribute__((address_space(4))) uint32_t*)(a.w_exps + (int64_t(t.expert) * blocks_n + min(blocks_n - 1, (t.n0 + cols0) / kBlock8)) * xp + b);
@@ -293,11 +312,11 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
     if (w < kRowWaves) row_exps[half * kRowTile + 64 * w + anew(lane)] = coming;
   };
   const auto bias = [&](const Tile& t) {
-    if (a.bias && w >= kRowWaves)
+    if (a.bias && w >= kRowWaves && w < kRowWaves + kColWaves)
       coming = __float_as_uint(a.bias[int64_t(t.expert) * a.N + min(a.N - 1, t.n0 + 64 * (w - kRowWaves) + anew(lane))]);
   };
   const auto lay_bias = [&] {
-    if (a.bias && w >= kRowWaves) col_bias[64 * (w - kRowWaves) + anew(lane)] = __uint_as_float(coming);
+    if (a.bias && w >= kRowWaves && w < kRowWaves + kColWaves) col_bias[64 * (w - kRowWaves) + anew(lane)] = __uint_as_float(coming);
   };
 
   Tile tile = tile_of(id);
@@ -524,147 +543,250 @@ __global__ __launch_bounds__(256) void k_product_few(Product8Args a, int64_t row
 // ---- gradients of the matrices ----------------------------------------------------
 
 constexpr int kRows = 32;                       // rows of a step
-constexpr int kWide = kRows * kTile * 2;        // bytes of a step of one operand in bfloat16
 
-// A step's rows of one operand: 16 codes of one row a thread, half a block of lanes
-// each ..., with the row's power of two; zeros behind the part's end.
-struct Codes {
-  u4v c;
-  float unit;
-};
-__device__ __forceinline__ Codes fetch(const uint8_t* codes, const uint8_t* exps, int64_t pitch, int64_t xp, int64_t p, int64_t end, int block) {
-  Codes v;
-  v.c = u4v{0, 0, 0, 0};
-  v.unit = 1.f;
-  if (p < end) {
-    v.c = *reinterpret_cast<const u4v*>(codes + p * pitch + int64_t(block) * kBlock8 + 16 * (threadIdx.x & 7));
-    v.unit = __uint_as_float(uint32_t(exps[p * xp + block]) << 23);
-  }
-  return v;
-}
-// To LDS in bfloat16: rows of 256 bytes, 16 values (32 bytes) c of row p at c ^ p % 8.
-__device__ __forceinline__ void lay(const Codes v, unsigned char* lds) {
-  const int p = threadIdx.x >> 3, c = threadIdx.x & 7;
-  bf2 h[8];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    h[2 * q] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(v.c[q]), v.unit, false);
-    h[2 * q + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(v.c[q]), v.unit, true);
-  }
-  u4v* to = reinterpret_cast<u4v*>(lds + p * 256 + 32 * (c ^ (p & 7)));
-  to[0] = u4v{__builtin_bit_cast(uint32_t, h[0]), __builtin_bit_cast(uint32_t, h[1]), __builtin_bit_cast(uint32_t, h[2]),
-              __builtin_bit_cast(uint32_t, h[3])};
-  to[1] = u4v{__builtin_bit_cast(uint32_t, h[4]), __builtin_bit_cast(uint32_t, h[5]), __builtin_bit_cast(uint32_t, h[6]),
-              __builtin_bit_cast(uint32_t, h[7])};
-}
-// Values of 16 columns (c: which 16 of the 128) and the step's 32 rows as an
-// operand: read transposed, 16 lanes have 4 rows of 16 values at a time.
-__device__ __forceinline__ bf8 columns(const unsigned char* lds, int c) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, j = (lane & 15) >> 2, q = lane & 3;
-  s4 h[2];
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int p = 16 * s + 4 * g + j;
-    h[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s4*)(lds + p * 256 + 32 * (c ^ (p & 7)) + 8 * q));
-  }
-  typedef short s8 __attribute__((ext_vector_type(8)));
-  return __builtin_bit_cast(bf8, s8{h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]});
-}
+// One operand's rows of a step, on their way from memory to LDS: half of the
+// work-group's threads have P pieces of 16 codes each, with their rows' powers of two.
+template <int COLS, int THREADS>
+struct Rows {
+  static constexpr int kPieces = COLS / 16, P = kRows * kPieces / THREADS, kApart = THREADS / kPieces;
+  static_assert(P >= 1 && P * THREADS == kRows * kPieces && kApart % 8 == 0);
+  const uint8_t* codes;         // of the part's first row, the tile's first column
+  const uint8_t* exps;
+  uint32_t pitch, xpitch;
+  int col;
+  uint32_t at, xat;             // of a thread's first piece and its exponent
+  u4v c[2][P];
+  uint32_t e[2][P];
 
-__global__ __launch_bounds__(256) void k_product_weights(Product8Args a, int tiles_n, int tiles_k) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * kWide];
-  const int64_t id = blockIdx.x;
-  const int tiles = tiles_n * tiles_k;
-  const int64_t item = id / tiles;
-  const int t = int(id - item * tiles), nt = t / tiles_k, kt = t - nt * tiles_k;
-  const Part part = find_part(a.offsets, a.E, a.m, a.slice, item, true);
-  if (part.expert < 0) return;
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, w = uni(threadIdx.x >> 6);
-  const int n0 = w & 1, k0 = w >> 1;                          // 64 of the tile's outputs and inputs
-  const int64_t wp = codes8(a.N), wx = exps8(a.N), kp = codes8(a.K), kx = exps8(a.K);
-  const bool bias = a.dbias && kt == 0 && k0 == 0;
-  f4 sum[4][4], bsum[4];                                      // inputs, outputs
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    bsum[i] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ Rows(const uint8_t* all, const uint8_t* all_exps, int64_t width, int64_t first, int column) {
+    col = column;
+    pitch = uint32_t(codes8(width));
+    xpitch = uint32_t(exps8(width));
+    codes = all + first * pitch + col;
+    exps = all_exps + first * xpitch + col / kBlock8;
+    const int row = threadIdx.x % THREADS / kPieces, piece = threadIdx.x % kPieces;
+    // (a block behind the last one of the row is the tile's first, and not used)
+    const bool there = col + 16 * piece < int(pitch);
+    at = row * pitch + (there ? 16 * piece : 0);
+    xat = row * xpitch + (there ? piece / (kBlock8 / 16) : 0);
   }
-  const __bf16 one = 1.f;
-  const bf8 ones = {one, one, one, one, one, one, one, one};
-  int64_t p = part.first;
-  Codes dy = fetch(a.w, a.w_exps, wp, wx, p + (threadIdx.x >> 3), part.end, nt);
-  Codes x = fetch(a.x, a.x_exps, kp, kx, p + (threadIdx.x >> 3), part.end, kt);
-  for (int turn = 0; p < part.end; p += kRows, turn ^= 1) {
-    unsigned char* here = lds + turn * 2 * kWide;
-    lay(dy, here);
-    lay(x, here + kWide);
-    dy = fetch(a.w, a.w_exps, wp, wx, p + kRows + (threadIdx.x >> 3), part.end, nt);
-    x = fetch(a.x, a.x_exps, kp, kx, p + kRows + (threadIdx.x >> 3), part.end, kt);
-    __syncthreads();                                          // two buffers: one barrier a step
-    bf8 dv[4];
+  // Rows from step * kRows on into set s; zeros behind the part's `rows` (a buffer's
+  // loads give those behind its end).
+  __device__ __forceinline__ void fetch(int s, int64_t step, int64_t rows) {
+    const int64_t p0 = step * kRows;
+    const int left = int(max(int64_t(0), min(int64_t(kRows), rows - p0)));
+    const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(codes + p0 * pitch), 0, max(0, left * int(pitch) - col), 0x27000);
+    const auto efrom = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(exps + p0 * xpitch), 0, max(0, left * int(xpitch) - col / kBlock8), 0x27000);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) dv[j] = columns(here, 4 * n0 + j);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bf8 xv = columns(here + kWide, 4 * k0 + i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, dv[j], sum[i][j], 0, 0, 0);
+    for (int q = 0; q < P; ++q) {
+      c[s][q] = __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(from, int(at), q * kApart * int(pitch), 0));
+      e[s][q] = __builtin_amdgcn_raw_buffer_load_b8(efrom, int(xat), q * kApart * int(xpitch), 0);
     }
-    if (bias)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) bsum[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, dv[j], bsum[j], 0, 0, 0);
   }
+  // To LDS in bfloat16, without rounding: rows of 2 COLS bytes, 16 values (32 bytes) c of row p at c ^ p % 8.
+  __device__ __forceinline__ void lay(int s, int q, unsigned char* lds) const {
+    const int row = threadIdx.x % THREADS / kPieces, piece = threadIdx.x % kPieces;
+    const float unit = __uint_as_float(e[s][q] << 23);
+    bf2 h[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      h[2 * k] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(c[s][q][k]), unit, false);
+      h[2 * k + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(c[s][q][k]), unit, true);
+    }
+    u4v* to = reinterpret_cast<u4v*>(lds + row * (2 * COLS) + 32 * (piece ^ (row & 7)) + q * kApart * (2 * COLS));
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      to[k] = u4v{__builtin_bit_cast(uint32_t, h[4 * k]), __builtin_bit_cast(uint32_t, h[4 * k + 1]),
+                  __builtin_bit_cast(uint32_t, h[4 * k + 2]), __builtin_bit_cast(uint32_t, h[4 * k + 3])};
+  }
+};
+// Values of 16 columns (i: which 16, after the wavefront's first) and a step's rows
+// as an operand: read transposed, 16 lanes have 4 rows of 16 values at a time.
+template <int COLS>
+__device__ __forceinline__ bf8 columns(const unsigned char* lds, int lane_at, int i) {
+  typedef short s8 __attribute__((ext_vector_type(8)));
+  s4 v[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+    v[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s4*)(lds + (lane_at ^ (32 * i)) + 16 * s * (2 * COLS)));
+  return __builtin_bit_cast(bf8, s8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]});
+}
+// Where a lane's first four values of a wavefront's columns are (first a multiple of 64 columns).
+template <int COLS>
+__device__ __forceinline__ int columns_at(int first) {
+  const int lane = threadIdx.x & 63, p = 4 * (lane >> 4) + ((lane & 15) >> 2);
+  return p * (2 * COLS) + 32 * ((first / 16) ^ (p & 7)) + 8 * (lane & 3);
+}
+
+// A wavefront has 16 NF outputs by 16 KF inputs, a work-group WN x WK of those.
+// Three steps of rows are in LDS: one that is used, the next one, of which the first
+// operands are read before the barrier that ends this one, and one that is laid.
+// BIAS: the outputs' own sums too.
+template <int NF, int KF, int WN, int WK, bool BIAS>
+__device__ __forceinline__ void weights_tile(const Product8Args& a, const Part& part, int64_t item, int nt, int kt, unsigned char* lds) {
+  constexpr int kThreads = 64 * WN * WK, kN = 16 * NF * WN, kK = 16 * KF * WK, kOne = kRows * (kN + kK) * 2;
+  const int64_t first = uni64(part.first);
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, w = uni(int(threadIdx.x >> 6));
+  const int wn = 16 * NF * (w % WN), wk = 16 * KF * (w / WN);         // of the wavefront, within the tile
+  const int64_t rows = uni64(part.end - part.first), steps = (rows + kRows - 1) / kRows;
+  // the first half of the wavefronts brings dy's rows, the other one x's
+  static_assert(kN == kK);
+  const bool front = w < WN * WK / 2;
+  Rows<kN, kThreads / 2> mine(front ? a.w : a.x, front ? a.w_exps : a.x_exps, front ? a.N : a.K, first, front ? nt * kN : kt * kK);
+  const int nat = columns_at<kN>(wn), kat = columns_at<kK>(wk);
+  f4 sum[KF][NF];
+  float own[NF];                                                 // inputs, outputs; the outputs' own, of a lane's rows
+#pragma unroll
+  for (int j = 0; j < NF; ++j) {
+    own[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < KF; ++i) sum[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+  }
+  const auto lay = [&](int s, int q, unsigned char* to) { mine.lay(s, q, to + (front ? 0 : kRows * kN * 2)); };
+  const auto fetch = [&](int s, int64_t step) { mine.fetch(s, step, rows); };
+  bf8 dv[NF], xv;
+  const auto of_n = [&](const unsigned char* from, int j) { return columns<kN>(from, nat, j); };
+  const auto of_k = [&](const unsigned char* from, int i) { return columns<kK>(from + kRows * kN * 2, kat, i); };
+  // Products of the step at `here`; the rows in set s go to `then` beside them.
+  const auto step = [&](const unsigned char* here, const unsigned char* next, int s, unsigned char* then) {
+    bf8 dnext[NF];
+    if constexpr (BIAS) {
+      // products with ones, and sums, two rows an instruction
+#pragma unroll
+      for (int j = 0; j < NF; ++j)
+#pragma unroll
+        for (int q = 0; q < 8; q += 2)
+          own[j] = __builtin_amdgcn_fdot2_f32_bf16(bf2{dv[j][q], dv[j][q + 1]}, bf2{__bf16(1.f), __bf16(1.f)}, own[j], false);
+    }
+#pragma unroll
+    for (int i = 0; i < KF; ++i) {
+      // (the order as it stands here: loads any earlier would be held in registers)
+      __builtin_amdgcn_sched_barrier(0);
+      const bf8 ahead = i + 1 < KF ? of_k(here, i + 1) : of_k(next, 0);
+      if (i == KF - 2)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) dnext[j] = of_n(next, j);
+#pragma unroll
+      for (int j = 0; j < NF; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, dv[j], sum[i][j], 0, 0, 0);
+#pragma unroll
+      for (int q = 0; q < mine.P; ++q)
+        if (q % KF == i) lay(s, q, then);
+      xv = ahead;
+    }
+#pragma unroll
+    for (int j = 0; j < NF; ++j) dv[j] = dnext[j];
+  };
+  const auto meet = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  // rows of a step are asked for two steps before they go to LDS, two steps before their use
+  if (steps > 0) {
+    fetch(0, 0);
+    fetch(1, 1);
+#pragma unroll
+    for (int q = 0; q < mine.P; ++q) lay(0, q, lds);
+    fetch(0, 2);
+#pragma unroll
+    for (int q = 0; q < mine.P; ++q) lay(1, q, lds + kOne);
+    fetch(1, 3);
+    meet();
+#pragma unroll
+    for (int j = 0; j < NF; ++j) dv[j] = of_n(lds, j);
+    xv = of_k(lds, 0);
+    unsigned char *here = lds, *next = lds + kOne, *then = lds + 2 * kOne;
+    for (int64_t b = 0; b < steps; b += 2) {
+      step(here, next, 0, then);
+      fetch(0, b + 4);
+      meet();
+      step(next, then, 1, here);                              // (of zeros where there is none)
+      fetch(1, b + 5);
+      meet();
+      unsigned char* const t = here;
+      here = then;
+      then = next;
+      next = t;
+    }
+  }
+  if constexpr (BIAS)
+#pragma unroll
+    for (int j = 0; j < NF; ++j) {
+      own[j] += __shfl_xor(own[j], 16);
+      own[j] += __shfl_xor(own[j], 32);
+    }
   const int64_t to = a.slots ? item : part.expert;
   float* out = (a.slots ? a.slots : a.dweights) + to * a.N * a.K;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int n = nt * kTile + 64 * n0 + 16 * j + r;
+  for (int j = 0; j < NF; ++j) {
+    const int n = nt * kN + wn + 16 * j + r;
     if (n >= a.N) continue;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int k = kt * kTile + 64 * k0 + 16 * i + 4 * g;
+    for (int i = 0; i < KF; ++i) {
+      const int k = kt * kK + wk + 16 * i + 4 * g;
       put4<true>(out, int64_t(n) * a.K + k, a.K - k, sum[i][j], a.K % 4 == 0);
     }
-    if (bias && g == 0) (a.slots ? a.bias_slots : a.dbias)[to * a.N + n] = bsum[j][0];
+    if (BIAS && w / WN == 0 && g == 0) (a.slots ? a.bias_slots : a.dbias)[to * a.N + n] = own[j];
   }
 }
 
-// The experts' sums of their slices, in order.
+template <int NF, int KF, int WN, int WK>
+__global__ __launch_bounds__(64 * WN * WK) void k_product_weights(Product8Args a, int tiles_n, int tiles_k) {
+  __shared__ __attribute__((aligned(256))) unsigned char lds[3 * kRows * 2 * 16 * (NF * WN + KF * WK)];
+  const int64_t id = blockIdx.x;
+  const int tiles = tiles_n * tiles_k;
+  const int64_t item = id / tiles;
+  const int t = int(id - item * tiles), nt = uni(t / tiles_k), kt = uni(t - nt * tiles_k);
+  const Part part = !a.slots && a.offsets && a.E <= 64 ? sized_part(a.offsets, a.E, a.m, uni(int(item)))
+                                                        : find_part(a.offsets, a.E, a.m, a.slice, item, true);
+  if (part.expert < 0) return;
+  if (a.dbias && kt == 0) weights_tile<NF, KF, WN, WK, true>(a, part, item, nt, kt, lds);
+  else weights_tile<NF, KF, WN, WK, false>(a, part, item, nt, kt, lds);
+}
+
+// The experts' sums of their slices.  SPLIT: four wavefronts have every fourth slice
+// of 64 values, for matrices that would not fill the CUs with a thread a value.
+template <bool SPLIT>
 __global__ __launch_bounds__(256) void k_add_slices(Product8Args a) {
-  const int e = blockIdx.y;
-  int64_t first = 0, slices = 0;
-  {
-    // slices of the experts before, and of this one
-    const int lane = threadIdx.x & 63;
-    int64_t before = 0, mine = 0;
-    for (int f = lane; f <= e; f += 64) {
-      int64_t from = 0, to = a.m;
-      if (a.offsets) {
-        from = min(a.m, max(int64_t(0), int64_t(a.offsets[f])));
-        to = min(a.m, max(from, int64_t(a.offsets[f + 1])));
-      }
-      const int64_t parts = max(int64_t(1), (to - from + a.slice - 1) / a.slice);
-      if (f < e) before += parts;
-      else mine = parts;
+  __shared__ float quarter[SPLIT ? 4 : 1][64];
+  const int e = blockIdx.y, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  // slices of the experts before, and of this one
+  int64_t before = 0, mine = 0;
+  for (int f = lane; f <= e; f += 64) {
+    int64_t from = 0, to = a.m;
+    if (a.offsets) {
+      from = min(a.m, max(int64_t(0), int64_t(a.offsets[f])));
+      to = min(a.m, max(from, int64_t(a.offsets[f + 1])));
     }
+    const int64_t parts = max(int64_t(1), (to - from + a.slice - 1) / a.slice);
+    if (f < e) before += parts;
+    else mine = parts;
+  }
 #pragma unroll
-    for (int o = 32; o > 0; o /= 2) {
-      before += __shfl_xor(static_cast<long long>(before), o);
-      mine += __shfl_xor(static_cast<long long>(mine), o);
-    }
-    first = before;
-    slices = mine;
+  for (int o = 32; o > 0; o /= 2) {
+    before += __shfl_xor(static_cast<long long>(before), o);
+    mine += __shfl_xor(static_cast<long long>(mine), o);
   }
   const int64_t values = int64_t(a.N) * a.K, all = values + (a.dbias ? a.N : 0);
-  for (int64_t v = int64_t(blockIdx.x) * 256 + threadIdx.x; v < all; v += int64_t(gridDim.x) * 256) {
-    const bool w = v < values;
-    const int64_t stride = w ? values : a.N, at = w ? v : v - values;
-    const float* from = (w ? a.slots : a.bias_slots) + first * stride + at;
+  constexpr int kEach = SPLIT ? 64 : 256, kBy = SPLIT ? 4 : 1;
+  for (int64_t v0 = int64_t(blockIdx.x) * kEach; v0 < all; v0 += int64_t(gridDim.x) * kEach) {
+    const int64_t v = v0 + (SPLIT ? lane : int(threadIdx.x));
+    const bool weight = v < values;
+    const int64_t stride = weight ? values : a.N, at = weight ? v : v - values;
     float sum = 0.f;
-    for (int64_t s = 0; s < slices; ++s) sum += from[s * stride];
-    (w ? a.dweights : a.dbias)[e * stride + at] = sum;
+    if (v < all) {
+      int64_t s = SPLIT ? w : 0;
+      const float* from = (weight ? a.slots : a.bias_slots) + (before + s) * stride + at;
+      for (; s + 3 * kBy < mine; s += 4 * kBy, from += 4 * kBy * stride) {
+        const float t0 = from[0], t1 = from[kBy * stride], t2 = from[2 * kBy * stride], t3 = from[3 * kBy * stride];
+        sum += (t0 + t1) + (t2 + t3);
+      }
+      for (; s < mine; s += kBy, from += kBy * stride) sum += *from;
+    }
+    if constexpr (SPLIT) {
+      __syncthreads();
+      quarter[w][lane] = sum;
+      __syncthreads();
+      sum = (quarter[0][lane] + quarter[1][lane]) + (quarter[2][lane] + quarter[3][lane]);
+    }
+    if ((!SPLIT || w == 0) && v < all) (weight ? a.dweights : a.dbias)[e * stride + at] = sum;
   }
 }
 
@@ -697,13 +819,23 @@ namespace {
 int64_t items(const Product8Args& a) { return a.m / a.slice + a.E; }
 }  // namespace
 
+// Tiles of 256 x 256 where they fit the matrices about as well as
+// tiles of 128 x 128, and there is work for all CUs.
+static bool large_tiles(const Product8Args& a, int n_cu) {
+  const auto tiles = [&](int t) { return int64_t((a.N + t - 1) / t) * ((a.K + t - 1) / t); };
+  return tiles(256) * 4 * 5 <= tiles(128) * 6 && (a.m / 256) * tiles(256) >= n_cu;
+}
+
 size_t product8_weights_plan(Product8Args* a, int n_cu) {
-  const int64_t tiles = int64_t((a->N + kTile - 1) / kTile) * ((a->K + kTile - 1) / kTile);
-  // slices so that there are work-groups for every CU, of 256 rows at least
-  const int64_t want = std::max<int64_t>(1, (4 * int64_t(n_cu) + tiles - 1) / tiles);
+  const bool large = large_tiles(*a, n_cu);
+  const int tile = large ? 256 : 128;
+  const int64_t tiles = int64_t((a->N + tile - 1) / tile) * ((a->K + tile - 1) / tile);
   a->slice = a->m;
-  if (tiles * a->E < 2 * int64_t(n_cu) && want > a->E) a->slice = std::max<int64_t>(256, (a->m + want - 1) / want);
-  a->slice = std::max<int64_t>(1, (a->slice + kRows - 1) / kRows * kRows);
+  // slices of rows where the experts' tiles do not fill the CUs, one work-group each
+  // or three: as many as fit at once, each expert's last one shorter
+  const int64_t fit = int64_t(n_cu) * (large ? 1 : 3) / tiles;
+  if (tiles * a->E < n_cu) a->slice = std::max<int64_t>(256, (a->m + fit - a->E - 1) / std::max<int64_t>(1, fit - a->E));
+  a->slice = std::max<int64_t>(1, (a->slice + 63) / 64 * 64);
   if (a->slice >= a->m) return 0;
   return size_t(items(*a)) * size_t(int64_t(a->N) * a->K + a->N) * sizeof(float);
 }
@@ -717,13 +849,21 @@ void product8_workspace(Product8Args* a, unsigned char* ws) {
 }
 
 hipError_t launch_product8_weights(const Product8Args& a, int n_cu, hipStream_t s) {
-  const int tiles_n = (a.N + kTile - 1) / kTile, tiles_k = (a.K + kTile - 1) / kTile;
   const int64_t count = a.slots ? items(a) : a.E;
-  k_product_weights<<<unsigned(count * tiles_n * tiles_k), 256, 0, s>>>(a, tiles_n, tiles_k);
+  const auto run = [&](auto kernel, int tile, int threads) {
+    const int tiles_n = (a.N + tile - 1) / tile, tiles_k = (a.K + tile - 1) / tile;
+    kernel<<<unsigned(count * tiles_n * tiles_k), threads, 0, s>>>(a, tiles_n, tiles_k);
+  };
+  if (large_tiles(a, n_cu)) run(k_product_weights<4, 8, 4, 2>, 256, 512);
+  else run(k_product_weights<4, 2, 2, 4>, 128, 512);
   if (a.slots) {
     const int64_t values = int64_t(a.N) * a.K + a.N;
-    const dim3 g{unsigned(std::min<int64_t>((values + 255) / 256, int64_t(n_cu) * 8)), unsigned(a.E), 1};
-    k_add_slices<<<g, 256, 0, s>>>(a);
+    const auto blocks = [&](int64_t each) {
+      const int64_t most = std::max<int64_t>(1, int64_t(n_cu) * 8 / a.E);
+      return dim3{unsigned(std::min((values + each - 1) / each, most)), unsigned(a.E), 1};
+    };
+    if (values * a.E < int64_t(n_cu) * 1024) k_add_slices<true><<<blocks(64), 256, 0, s>>>(a);
+    else k_add_slices<false><<<blocks(256), 256, 0, s>>>(a);
   }
   return hipGetLastError();
 }
