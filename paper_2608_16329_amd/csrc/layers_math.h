@@ -18,62 +18,84 @@ typedef uint32_t U2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 
-// Values at .. at + 7 of an array of either type, those from `left` on as zero
-// (left <= 0: none is read).
+typedef float f2v __attribute__((ext_vector_type(2)));
+typedef __bf16 b2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2v{a, b}, b2v));
+}
+
+// Four values of an array of either type from `at` on, those from `left` on as
+// zero (left <= 0: none is read); and back, those before `left`.
 template <bool BF>
-__device__ __forceinline__ void load8(const void* p, int64_t at, int left, float v[8]) {
-  if (left >= 8) {
+__device__ __forceinline__ void load4at(const void* p, int64_t at, int left, float* v) {
+  if (left >= 4) {
     if (BF) {
-      const u4v h = *reinterpret_cast<const U4*>(static_cast<const uint16_t*>(p) + at);
+      const u2v h = *reinterpret_cast<const U2*>(static_cast<const uint16_t*>(p) + at);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < 2; ++q) {
         v[2 * q] = __uint_as_float(h[q] << 16);
         v[2 * q + 1] = __uint_as_float(h[q] & 0xffff0000u);
       }
     } else {
       const u4v a = *reinterpret_cast<const U4*>(static_cast<const float*>(p) + at);
-      const u4v b = *reinterpret_cast<const U4*>(static_cast<const float*>(p) + at + 4);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v[q] = __uint_as_float(a[q]);
-        v[4 + q] = __uint_as_float(b[q]);
-      }
+      for (int q = 0; q < 4; ++q) v[q] = __uint_as_float(a[q]);
     }
     return;
   }
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
+  for (int q = 0; q < 4; ++q) {
     v[q] = 0.f;
     if (q < left) v[q] = BF ? from_bf16(static_cast<const uint16_t*>(p)[at + q]) : static_cast<const float*>(p)[at + q];
   }
 }
-
 template <bool BF>
-__device__ __forceinline__ void store8(void* p, int64_t at, int left, const float v[8]) {
-  if (left >= 8) {
-    if (BF) {
-      u4v h;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) h[q] = uint32_t(to_bf16(v[2 * q])) | uint32_t(to_bf16(v[2 * q + 1])) << 16;
-      *reinterpret_cast<U4*>(static_cast<uint16_t*>(p) + at) = h;
-    } else {
-      u4v a, b;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        a[q] = __float_as_uint(v[q]);
-        b[q] = __float_as_uint(v[4 + q]);
-      }
-      *reinterpret_cast<U4*>(static_cast<float*>(p) + at) = a;
-      *reinterpret_cast<U4*>(static_cast<float*>(p) + at + 4) = b;
-    }
+__device__ __forceinline__ void store4at(void* p, int64_t at, int left, const float* v) {
+  if (left >= 4) {
+    if (BF) *reinterpret_cast<U2*>(static_cast<uint16_t*>(p) + at) = u2v{bf16x2(v[0], v[1]), bf16x2(v[2], v[3])};
+    else
+      *reinterpret_cast<U4*>(static_cast<float*>(p) + at) =
+          u4v{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
     return;
   }
 #pragma unroll
-  for (int q = 0; q < 8; ++q)
+  for (int q = 0; q < 4; ++q)
     if (q < left) {
-      if (BF) static_cast<uint16_t*>(p)[at + q] = to_bf16(v[q]);
+      if (BF) static_cast<uint16_t*>(p)[at + q] = uint16_t(bf16x2(v[q], 0.f));
       else static_cast<float*>(p)[at + q] = v[q];
     }
+}
+
+// A lane's eight values of a block of 128: from `at` on, neighbours in bfloat16, in
+// float32 four and the four that are 64 behind them, so that 16 lanes' 16-byte
+// accesses lie side by side.  `left`: values of the row from `at` on.
+template <bool BF>
+constexpr int kSecond = BF ? 4 : 64;
+template <bool BF>
+__device__ __forceinline__ void load8(const void* p, int64_t at, int left, float v[8]) {
+  if (BF && left >= 8) {
+    const u4v h = *reinterpret_cast<const U4*>(static_cast<const uint16_t*>(p) + at);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v[2 * q] = __uint_as_float(h[q] << 16);
+      v[2 * q + 1] = __uint_as_float(h[q] & 0xffff0000u);
+    }
+    return;
+  }
+  load4at<BF>(p, at, left, v);
+  load4at<BF>(p, at + kSecond<BF>, left - kSecond<BF>, v + 4);
+}
+template <bool BF>
+__device__ __forceinline__ void store8(void* p, int64_t at, int left, const float v[8]) {
+  if (BF && left >= 8) {
+    u4v h;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) h[q] = bf16x2(v[2 * q], v[2 * q + 1]);
+    *reinterpret_cast<U4*>(static_cast<uint16_t*>(p) + at) = h;
+    return;
+  }
+  store4at<BF>(p, at, left, v);
+  store4at<BF>(p, at + kSecond<BF>, left - kSecond<BF>, v + 4);
 }
 
 // The largest of 16 neighbouring lanes' values, in each of them: rotations
@@ -93,6 +115,21 @@ __device__ __forceinline__ int exponent8(uint32_t bits) {
 }
 // 2^e, -126 <= e <= 127
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float(uint32_t(e + 127) << 23); }
+// The bits of the largest finite size among eight values.
+__device__ __forceinline__ uint32_t largest8(const float v[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) top = max(top, __float_as_uint(v[q]) & 0x7fffffffu);
+  if (top >= 0x7f800000u) {     // an infinity or a NaN is among them
+    top = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const uint32_t u = __float_as_uint(v[q]) & 0x7fffffffu;
+      top = max(top, u < 0x7f800000u ? u : 0u);
+    }
+  }
+  return top;
+}
 // The bits of a finite value's size; 0 for an infinity or a NaN.
 __device__ __forceinline__ uint32_t finite_size(float v) {
   const uint32_t u = __float_as_uint(v) & 0x7fffffffu;

@@ -10,7 +10,8 @@
 //
 // Bound by memory.  16 lanes have a block, 8 values each; a wavefront has four
 // blocks, whose exponents are one 32-bit word: four of a row, or one or two each
-// of four or two rows that have no more.
+// of four or two rows that have no more.  Wavefronts that run side by side have
+// neighbouring blocks.
 #include <algorithm>
 
 #include "layers_math.h"
@@ -19,32 +20,57 @@ namespace mlip {
 namespace {
 
 // What a lane works on: row and block, the first of its eight values and how
-// many there are from there on.
+// many the row has from there on.
 struct Spot {
   int64_t row;
   int block, at, left;
   bool there;                   // the row and the block exist
 };
-template <int G>
+template <bool BF, int G>
 __device__ __forceinline__ Spot spot(int64_t row0, int quad, int64_t n, int width) {
   const int group = (threadIdx.x & 63) >> 4;
   Spot s;
   s.row = row0 + group / G;
   s.block = 4 * quad + group % G;
-  s.at = s.block * kBlock8 + 8 * (threadIdx.x & 15);
+  s.at = s.block * kBlock8 + (BF ? 8 : 4) * (threadIdx.x & 15);
   s.left = width - s.at;
   s.there = s.row < n && s.block * kBlock8 < width;
   return s;
 }
 
+// f(first row, which four blocks) for all of n rows, shared by the wavefronts.
+template <int G, typename F>
+__device__ __forceinline__ void each(int64_t n, int width, F f) {
+  const int quads = int(exps8(width) / 4);
+  const int64_t all = int64_t(gridDim.x) * 4, mine = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int64_t rows_on = all / quads;
+  const int quads_on = int(all - rows_on * quads);
+  int64_t group = mine / quads;
+  int quad = int(mine - group * quads);
+  while (group * (4 / G) < n) {
+    f(group * (4 / G), quad);
+    group += rows_on;
+    quad += quads_on;
+    if (quad >= quads) {
+      quad -= quads;
+      ++group;
+    }
+  }
+}
+
 // Writes a block's codes and exponent: all lanes of the wavefront call.
-template <int G>
+template <bool BF, int G>
 __device__ __forceinline__ void put(const Spot& s, const float v[8], uint8_t* codes, uint8_t* exps, int quad, int width, int64_t n) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int q = 0; q < 8; ++q) top = max(top, finite_size(v[q]));
-  const int e = exponent8(max16(top));
-  if (s.there) *reinterpret_cast<u2v*>(codes + s.row * codes8(width) + s.at) = encode8(v, e);
+  const int e = exponent8(max16(largest8(v)));
+  if (s.there) {
+    const u2v c = encode8(v, e);
+    uint8_t* const to = codes + s.row * codes8(width) + s.at;
+    if (BF) *reinterpret_cast<u2v*>(to) = c;
+    else {
+      *reinterpret_cast<uint32_t*>(to) = c[0];
+      *reinterpret_cast<uint32_t*>(to + kSecond<BF>) = c[1];
+    }
+  }
   uint32_t word = s.there ? uint32_t(e + 127) << (8 * (s.block & 3)) : 0u;
   if (G >= 2) word |= __shfl_xor(word, 16);
   if (G == 4) word |= __shfl_xor(word, 32);
@@ -52,9 +78,13 @@ __device__ __forceinline__ void put(const Spot& s, const float v[8], uint8_t* co
     *reinterpret_cast<uint32_t*>(exps + s.row * exps8(width) + 4 * quad) = word;
 }
 // Values of a block that was written.
+template <bool BF>
 __device__ __forceinline__ void get(const Spot& s, const uint8_t* codes, const uint8_t* exps, int width, float v[8]) {
   if (s.there) {
-    const u2v c = *reinterpret_cast<const u2v*>(codes + s.row * codes8(width) + s.at);
+    const uint8_t* const from = codes + s.row * codes8(width) + s.at;
+    u2v c;
+    if (BF) c = *reinterpret_cast<const u2v*>(from);
+    else c = u2v{*reinterpret_cast<const uint32_t*>(from), *reinterpret_cast<const uint32_t*>(from + kSecond<BF>)};
     const uint32_t e = exps[s.row * exps8(width) + s.block];
     decode8(c, __uint_as_float(e << 23), v);
   }
@@ -71,80 +101,90 @@ __device__ __forceinline__ int64_t source(const Pack8Args& a, int64_t p, int64_t
 template <bool BF, int G>
 __global__ __launch_bounds__(256) void k_pack8(Pack8Args a) {
   const int64_t end = a.order ? min(a.n, max(int64_t(0), int64_t(a.offsets[a.E]))) : a.n;
-  const int quads = int(exps8(a.width) / 4);
-  for (int64_t row0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (4 / G); row0 < end; row0 += int64_t(gridDim.x) * 4 * (4 / G))
-    for (int quad = blockIdx.y; quad < quads; quad += gridDim.y) {
-      Spot s = spot<G>(row0, quad, end, a.width);
-      const int64_t from = s.there ? source(a, s.row, end) : -1;
-      s.there = s.there && from >= 0;
-      float v[8] = {};
-      if (s.there) load8<BF>(a.x, from * a.x_stride + s.at, s.left, v);
-      put<G>(s, v, a.codes, a.exps, quad, a.width, end);
-    }
+  each<G>(end, a.width, [&](int64_t row0, int quad) {
+    Spot s = spot<BF, G>(row0, quad, end, a.width);
+    const int64_t from = s.there ? source(a, s.row, end) : -1;
+    s.there = s.there && from >= 0;
+    float v[8] = {};
+    if (s.there) load8<BF>(a.x, from * a.x_stride + s.at, s.left, v);
+    put<BF, G>(s, v, a.codes, a.exps, quad, a.width, end);
+  });
 }
 
 template <bool BF, int G>
 __global__ __launch_bounds__(256) void k_unpack8(Pack8Args a) {
-  const int quads = int(exps8(a.width) / 4);
-  for (int64_t row0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (4 / G); row0 < a.n; row0 += int64_t(gridDim.x) * 4 * (4 / G))
-    for (int quad = blockIdx.y; quad < quads; quad += gridDim.y) {
-      const Spot s = spot<G>(row0, quad, a.n, a.width);
-      float v[8];
-      get(s, a.kept, a.kept_exps, a.width, v);
-      if (s.there && s.left > 0) store8<BF>(a.out, s.row * a.width + s.at, s.left, v);
-    }
+  each<G>(a.n, a.width, [&](int64_t row0, int quad) {
+    const Spot s = spot<BF, G>(row0, quad, a.n, a.width);
+    float v[8];
+    get<BF>(s, a.kept, a.kept_exps, a.width, v);
+    if (s.there) store8<BF>(a.out, s.row * a.width + s.at, s.left, v);
+  });
 }
 
-// 1 / (1 + exp(-z)) from exp(-|z|), which does not overflow where the quotient is
-// still a number.
+// 1 / (1 + exp(-z)) from t = exp(-|z|), which does not overflow where the quotient
+// is still a number: 2^f 2^n with n + f = -|z| log2(e) in two parts, |f| <= 1/2, so
+// that t is good to 2 ulp at any z, also where it is a denormal number.
 __device__ __forceinline__ float sigmoid(float z) {
-  const float t = expf(-fabsf(z));
-  return (z < 0.f ? t : 1.f) / (1.f + t);
+  const float y = fminf(fabsf(z), 200.f);                     // (t is 0 from 104 on; an infinity has no f)
+  const float n = rintf(-y * 1.44269502f);
+  float f = fmaf(-y, 1.44269502f, -n);
+  f = fmaf(-y, 1.92596299e-8f, f);
+  const float t = ldexpf(__builtin_amdgcn_exp2f(f), int(n));
+  return (z < 0.f ? t : 1.f) * __builtin_amdgcn_rcpf(1.f + t);
+}
+
+// What is left of values in their type.
+template <bool BF>
+__device__ __forceinline__ void as_stored(float v[8]) {
+  if (BF)
+#pragma unroll
+    for (int q = 0; q < 8; q += 2) {
+      const uint32_t u = bf16x2(v[q], v[q + 1]);
+      v[q] = __uint_as_float(u << 16);
+      v[q + 1] = __uint_as_float(u & 0xffff0000u);
+    }
 }
 
 // h = r + silu(z), and z in 8 bits for the backward pass
 template <bool BF, int G>
 __global__ __launch_bounds__(256) void k_activate8(Pack8Args a) {
-  const int quads = int(exps8(a.width) / 4);
-  for (int64_t row0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (4 / G); row0 < a.n; row0 += int64_t(gridDim.x) * 4 * (4 / G))
-    for (int quad = blockIdx.y; quad < quads; quad += gridDim.y) {
-      const Spot s = spot<G>(row0, quad, a.n, a.width);
-      float z[8] = {}, h[8] = {};
-      if (s.there) {
-        load8<BF>(a.x, s.row * a.x_stride + s.at, s.left, z);
-        if (a.residual) load8<BF>(a.residual, s.row * a.residual_stride + s.at, s.left, h);
-      }
-      if (a.codes) put<G>(s, z, a.codes, a.exps, quad, a.width, a.n);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const float t = z[q] * sigmoid(z[q]);
-        h[q] = a.residual ? h[q] + t : t;
-        if (BF) h[q] = from_bf16(to_bf16(h[q]));
-      }
-      if (a.out && s.there && s.left > 0) store8<BF>(a.out, s.row * a.width + s.at, s.left, h);
-      if (a.out_codes) put<G>(s, h, a.out_codes, a.out_exps, quad, a.width, a.n);
+  each<G>(a.n, a.width, [&](int64_t row0, int quad) {
+    const Spot s = spot<BF, G>(row0, quad, a.n, a.width);
+    float z[8] = {}, h[8] = {};
+    if (s.there) {
+      load8<BF>(a.x, s.row * a.x_stride + s.at, s.left, z);
+      if (a.residual) load8<BF>(a.residual, s.row * a.residual_stride + s.at, s.left, h);
     }
+    if (a.codes) put<BF, G>(s, z, a.codes, a.exps, quad, a.width, a.n);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) h[q] = fmaf(z[q], sigmoid(z[q]), h[q]);
+    if (a.out && s.there) store8<BF>(a.out, s.row * a.width + s.at, s.left, h);
+    if (a.out_codes) {
+      as_stored<BF>(h);
+      put<BF, G>(s, h, a.out_codes, a.out_exps, quad, a.width, a.n);
+    }
+  });
 }
 
 // dz = dh silu'(z) of the z that was kept
 template <bool BF, int G>
 __global__ __launch_bounds__(256) void k_activate8_backward(Pack8Args a) {
-  const int quads = int(exps8(a.width) / 4);
-  for (int64_t row0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (4 / G); row0 < a.n; row0 += int64_t(gridDim.x) * 4 * (4 / G))
-    for (int quad = blockIdx.y; quad < quads; quad += gridDim.y) {
-      const Spot s = spot<G>(row0, quad, a.n, a.width);
-      float z[8] = {}, d[8] = {};
-      if (s.there) load8<BF>(a.x, s.row * a.x_stride + s.at, s.left, d);
-      get(s, a.kept, a.kept_exps, a.width, z);
+  each<G>(a.n, a.width, [&](int64_t row0, int quad) {
+    const Spot s = spot<BF, G>(row0, quad, a.n, a.width);
+    float z[8] = {}, d[8] = {};
+    if (s.there) load8<BF>(a.x, s.row * a.x_stride + s.at, s.left, d);
+    get<BF>(s, a.kept, a.kept_exps, a.width, z);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const float t = sigmoid(z[q]);
-        d[q] *= t * (1.f + z[q] * (1.f - t));
-        if (BF) d[q] = from_bf16(to_bf16(d[q]));
-      }
-      if (a.out && s.there && s.left > 0) store8<BF>(a.out, s.row * a.width + s.at, s.left, d);
-      if (a.out_codes) put<G>(s, d, a.out_codes, a.out_exps, quad, a.width, a.n);
+    for (int q = 0; q < 8; ++q) {
+      const float t = sigmoid(z[q]);
+      d[q] *= t * fmaf(z[q], 1.f - t, 1.f);
     }
+    if (a.out && s.there) store8<BF>(a.out, s.row * a.width + s.at, s.left, d);
+    if (a.out_codes) {
+      as_stored<BF>(d);
+      put<BF, G>(s, d, a.out_codes, a.out_exps, quad, a.width, a.n);
+    }
+  });
 }
 
 // One work-group for a block of 128 x 128 of a matrix: thread t has the 8 values
@@ -165,9 +205,12 @@ __global__ __launch_bounds__(256) void k_pack8_weights(Weights8Args a) {
     const int n = nb * kBlock8 + 16 * j + (t >> 4);
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[j][q] = 0.f;
-    if (n < a.N) load8<BF>(a.w, (e * a.N + n) * a.K + k0, a.K - k0, v[j]);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) top = max(top, finite_size(v[j][q]));
+    if (n < a.N) {
+      const int64_t at = (e * a.N + n) * a.K + k0;
+      load4at<BF>(a.w, at, a.K - k0, v[j]);
+      load4at<BF>(a.w, at + 4, a.K - k0 - 4, v[j] + 4);
+    }
+    top = max(top, largest8(v[j]));
   }
   top = max16(top);
   top = max(top, uint32_t(__shfl_xor(top, 16)));
@@ -209,9 +252,9 @@ __global__ __launch_bounds__(256) void k_pack8_weights(Weights8Args a) {
 template <typename F>
 hipError_t with_group(const Pack8Args& a, int n_cu, F run) {
   const int blocks = (a.width + kBlock8 - 1) / kBlock8, quads = (blocks + 3) / 4;
-  const int rows = blocks == 1 ? 16 : blocks == 2 ? 8 : 4;          // of a work-group
-  const int64_t x = std::max<int64_t>(1, std::min<int64_t>((a.n + rows - 1) / rows, int64_t(n_cu) * 64));
-  const dim3 g{unsigned(x), unsigned(std::min(quads, 1024)), 1};
+  const int rows = blocks == 1 ? 4 : blocks == 2 ? 2 : 1;           // of a wavefront
+  const int64_t units = (a.n + rows - 1) / rows * quads;
+  const unsigned g = unsigned(std::max<int64_t>(1, std::min<int64_t>((units + 3) / 4, int64_t(n_cu) * 64)));
   if (blocks == 1) run(std::integral_constant<int, 1>(), g);
   else if (blocks == 2) run(std::integral_constant<int, 2>(), g);
   else run(std::integral_constant<int, 4>(), g);
@@ -221,7 +264,7 @@ hipError_t with_group(const Pack8Args& a, int n_cu, F run) {
 }  // namespace
 
 #define PACK8_LAUNCH(kernel)                                                \
-  return with_group(a, n_cu, [&](auto w, dim3 g) {                          \
+  return with_group(a, n_cu, [&](auto w, unsigned g) {                          \
     if (a.bf16) kernel<true, w.value><<<g, 256, 0, s>>>(a);                 \
     else kernel<false, w.value><<<g, 256, 0, s>>>(a);                       \
   })

@@ -120,10 +120,6 @@ __device__ __forceinline__ void widen(const i8 c, float unit, bf8 v[4]) {
   }
 }
 
-typedef float f2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, bf2));
-}
 __device__ __forceinline__ u4v bf16x8(const f4 a, const f4 b) {
   return u4v{bf16x2(a[0], a[1]), bf16x2(a[2], a[3]), bf16x2(b[0], b[1]), bf16x2(b[2], b[3])};
 }
