@@ -18,13 +18,16 @@ namespace {
 
 constexpr int kPieces = 4;      // 16-byte pieces a lane has under way
 
-// A row's pieces: whole ones, and the values behind them.
+// A row's pieces of 16 bytes: the last one ends where the row does, and has some of
+// the values of the one before it again (a row of less than 16 bytes has none, and
+// its values go one a lane).
 struct Shape {
-  int pieces, tail, size;       // size of a value in bytes
+  int pieces, last, few, size;  // pieces, where the last one starts, values of a short row, bytes of a value
+  __device__ __forceinline__ int at(int c) const { return min(16 * c, last); }
 };
 __device__ __forceinline__ Shape shape(const RowsArgs& a) {
   const int size = a.bf16 ? 2 : 4, bytes = a.width * size;
-  return {bytes / 16, bytes % 16 / size, size};
+  return bytes < 16 ? Shape{0, 0, a.width, size} : Shape{(bytes + 15) / 16, bytes - 16, 0, size};
 }
 
 // Where entry `e` stands: its place, or -1 for none (and for what is no place).
@@ -51,7 +54,7 @@ __device__ __forceinline__ u4v rounded(const float* v) {
   u4v u;
 #pragma unroll
   for (int q = 0; q < 4; ++q)
-    u[q] = BF ? uint32_t(to_bf16(v[2 * q])) | uint32_t(to_bf16(v[2 * q + 1])) << 16 : __float_as_uint(v[q]);
+    u[q] = BF ? bf16x2(v[2 * q], v[2 * q + 1]) : __float_as_uint(v[q]);
   return u;
 }
 template <bool BF>
@@ -81,14 +84,14 @@ __global__ __launch_bounds__(256) void k_sort(RowsArgs a) {
       u4v v[kPieces];
 #pragma unroll
       for (int q = 0; q < kPieces; ++q)
-        if (c + q * L < f.pieces) v[q] = *reinterpret_cast<const U4*>(from + 16 * (c + q * L));
+        if (c + q * L < f.pieces) v[q] = *reinterpret_cast<const U4*>(from + f.at(c + q * L));
 #pragma unroll
       for (int q = 0; q < kPieces; ++q)
-        if (c + q * L < f.pieces) *reinterpret_cast<U4*>(to + 16 * (c + q * L)) = v[q];
+        if (c + q * L < f.pieces) *reinterpret_cast<U4*>(to + f.at(c + q * L)) = v[q];
     }
-    if (lane < f.tail) {
-      if (BF) reinterpret_cast<uint16_t*>(to)[f.pieces * 8 + lane] = reinterpret_cast<const uint16_t*>(from)[f.pieces * 8 + lane];
-      else reinterpret_cast<uint32_t*>(to)[f.pieces * 4 + lane] = reinterpret_cast<const uint32_t*>(from)[f.pieces * 4 + lane];
+    if (lane < f.few) {
+      if (BF) reinterpret_cast<uint16_t*>(to)[lane] = reinterpret_cast<const uint16_t*>(from)[lane];
+      else reinterpret_cast<uint32_t*>(to)[lane] = reinterpret_cast<const uint32_t*>(from)[lane];
     }
   }
 }
@@ -111,23 +114,22 @@ __global__ __launch_bounds__(256) void k_combine(RowsArgs a) {
         u4v v[kPieces];
 #pragma unroll
         for (int q = 0; q < kPieces; ++q)
-          if (c + q * L < f.pieces) v[q] = *reinterpret_cast<const U4*>(from + 16 * (c + q * L));
+          if (c + q * L < f.pieces) v[q] = *reinterpret_cast<const U4*>(from + f.at(c + q * L));
 #pragma unroll
         for (int q = 0; q < kPieces; ++q)
           if (c + q * L < f.pieces) add<BF>(sum[q], v[q], g);
       }
 #pragma unroll
       for (int q = 0; q < kPieces; ++q)
-        if (c + q * L < f.pieces) *reinterpret_cast<U4*>(to + 16 * (c + q * L)) = rounded<BF>(sum[q]);
+        if (c + q * L < f.pieces) *reinterpret_cast<U4*>(to + f.at(c + q * L)) = rounded<BF>(sum[q]);
     }
-    if (lane < f.tail) {
+    if (lane < f.few) {
       float sum = 0.f;
-      const int at = f.pieces * V + lane;
       for (int s = 0; s < a.K; ++s) {
         const int64_t p = place_of(a, i * a.K + s);
-        if (p >= 0) sum = fmaf(a.gates ? a.gates[i * a.K + s] : 1.f, value<BF>(a.x, p * a.x_stride + at), sum);
+        if (p >= 0) sum = fmaf(a.gates ? a.gates[i * a.K + s] : 1.f, value<BF>(a.x, p * a.x_stride + lane), sum);
       }
-      set<BF>(a.out, i * a.width + at, sum);
+      set<BF>(a.out, i * a.width + lane, sum);
     }
   }
 }
@@ -153,8 +155,8 @@ __global__ __launch_bounds__(256) void k_combine_backward(RowsArgs a) {
 #pragma unroll
           for (int q = 0; q < kPieces; ++q)
             if (c + q * L < f.pieces) {
-              d[q] = *reinterpret_cast<const U4*>(from + 16 * (c + q * L));
-              if (a.dgates) v[q] = *reinterpret_cast<const U4*>(y + 16 * (c + q * L));
+              d[q] = *reinterpret_cast<const U4*>(from + f.at(c + q * L));
+              if (a.dgates) v[q] = *reinterpret_cast<const U4*>(y + f.at(c + q * L));
             }
 #pragma unroll
           for (int q = 0; q < kPieces; ++q)
@@ -164,19 +166,20 @@ __global__ __launch_bounds__(256) void k_combine_backward(RowsArgs a) {
               if (a.dgates) {
                 float yv[V] = {};
                 add<BF>(yv, v[q], 1.f);
+                // (values that the piece before has count there)
+                const int again = (16 * (c + q * L) - f.at(c + q * L)) / f.size;
 #pragma unroll
-                for (int j = 0; j < V; ++j) dot = fmaf(dv[j], yv[j], dot);
+                for (int j = 0; j < V; ++j) dot = j >= again ? fmaf(dv[j], yv[j], dot) : dot;
               }
 #pragma unroll
               for (int j = 0; j < V; ++j) out[j] = g * dv[j];
-              *reinterpret_cast<U4*>(to + 16 * (c + q * L)) = rounded<BF>(out);
+              *reinterpret_cast<U4*>(to + f.at(c + q * L)) = rounded<BF>(out);
             }
         }
-        if (lane < f.tail) {
-          const int at = f.pieces * V + lane;
-          const float d = value<BF>(a.x, i * a.x_stride + at);
-          if (a.dgates) dot = fmaf(d, value<BF>(a.y, p * a.y_stride + at), dot);
-          set<BF>(a.out, p * a.width + at, g * d);
+        if (lane < f.few) {
+          const float d = value<BF>(a.x, i * a.x_stride + lane);
+          if (a.dgates) dot = fmaf(d, value<BF>(a.y, p * a.y_stride + lane), dot);
+          set<BF>(a.out, p * a.width + lane, g * d);
         }
       }
       if (a.dgates) {
@@ -190,7 +193,7 @@ __global__ __launch_bounds__(256) void k_combine_backward(RowsArgs a) {
 
 // Lanes of a row: 8 to 64, about kPieces pieces each.
 int lanes(const RowsArgs& a) {
-  const int pieces = a.width * (a.bf16 ? 2 : 4) / 16;
+  const int pieces = (a.width * (a.bf16 ? 2 : 4) + 15) / 16;
   int l = 8;
   while (l < 64 && l * kPieces < pieces) l *= 2;
   return l;

@@ -74,36 +74,49 @@ class _OnStream:
         return stride
 
 
+def _bytes(t, name: str, *shape):
+    _need(t.element_size() == 1 and not t.is_floating_point(), f"{name} is {t.dtype}, not uint8")
+    _need(tuple(t.shape) == shape and t.is_contiguous(), f"{name} has shape {tuple(t.shape)}, not {shape}, or is not contiguous")
+    return t
+
+
 class Rows8:
     """Places for `rows` rows of `width` values in 8 bits (mlip_pack8): codes uint8
-    [rows, width rounded up to 128s], exps uint8 [rows, blocks of 128 rounded up to fours]."""
+    [rows, width rounded up to 128s], exps uint8 [rows, blocks of 128 rounded up to
+    fours], allocated here unless given (both, contiguous)."""
 
-    def __init__(self, rows: int, width: int, *, device=None):
+    codes, exps, rows, width = (property(lambda self, k=k: self._held[k]) for k in range(4))
+
+    def __init__(self, rows: int, width: int, *, codes=None, exps=None, device=None):
         import torch
         _need(rows >= 0, f"rows is {rows}")
         _need(1 <= width <= 65536, f"width is {width}, not in 1..65536")
-        device = torch.device("cuda") if device is None else device
-        self.rows, self.width = rows, width
-        self.codes = torch.empty((rows, b.mlip_row8_codes(width)), dtype=torch.uint8, device=device)
-        self.exps = torch.empty((rows, b.mlip_row8_exps(width)), dtype=torch.uint8, device=device)
+        _need((codes is None) == (exps is None), "codes and exps go together")
+        shapes = (rows, b.mlip_row8_codes(width)), (rows, b.mlip_row8_exps(width))
+        if codes is None:
+            device = torch.device("cuda") if device is None else device
+            codes, exps = (torch.empty(s, dtype=torch.uint8, device=device) for s in shapes)
+        _need(codes.device == exps.device, f"codes are on {codes.device}, exps on {exps.device}")
+        self._held = _bytes(codes, "codes", *shapes[0]), _bytes(exps, "exps", *shapes[1]), rows, width
 
 
 class Weights8:
-    """Places for `experts` matrices [outputs, inputs] in 8 bits (mlip_pack8_weights),
-    and, with `transposed`, for their transposes, which gradients in x need."""
+    """Places for `experts` matrices [outputs, inputs] in 8 bits (mlip_pack8_weights):
+    codes and exps, and, with `transposed`, t_codes and t_exps of their transposes,
+    which gradients in x need (otherwise None)."""
+
+    codes, exps, t_codes, t_exps, experts, outputs, inputs = (property(lambda self, k=k: self._held[k]) for k in range(7))
 
     def __init__(self, experts: int, outputs: int, inputs: int, *, transposed: bool = True, device=None):
         import torch
         _need(1 <= experts <= 256, f"experts is {experts}, not in 1..256")
         _need(1 <= outputs <= 65536 and 1 <= inputs <= 65536, f"{outputs} outputs and {inputs} inputs are not in 1..65536")
         device = torch.device("cuda") if device is None else device
-        self.experts, self.outputs, self.inputs, self.transposed = experts, outputs, inputs, transposed
 
         def places(rows, width):
             return (torch.empty((experts, rows, b.mlip_row8_codes(width)), dtype=torch.uint8, device=device),
                     torch.empty((experts, (rows + 127) // 128, b.mlip_row8_exps(width)), dtype=torch.uint8, device=device))
-        self.codes, self.exps = places(outputs, inputs)
-        self.t_codes, self.t_exps = places(inputs, outputs) if transposed else (None, None)
+        self._held = (*places(outputs, inputs), *(places(inputs, outputs) if transposed else (None, None)), experts, outputs, inputs)
 
 
 class Learner(_OnStream):
@@ -237,8 +250,11 @@ class Learner(_OnStream):
     # -- wide layers of experts ----------------------------------------------------
 
     def _packed(self, r: Rows8, name: str, rows: int, width: int) -> None:
-        _need(r.codes.device == self.device, f"{name} is on {r.codes.device}, not {self.device}")
-        _need(r.rows == rows and r.width == width, f"{name} has {r.rows} rows of {r.width} values, not {rows} of {width}")
+        codes, _, has, wide = r._held
+        if has == rows and wide == width and codes.get_device() == self.device.index:
+            return
+        _need(codes.device == self.device, f"{name} is on {codes.device}, not {self.device}")
+        _need(False, f"{name} has {has} rows of {wide} values, not {rows} of {width}")
 
     def _expert_offsets(self, offsets, experts: int) -> None:
         if offsets is None:
@@ -354,7 +370,7 @@ class Learner(_OnStream):
         rows of `outputs` values, the gradient in x (mlip_product8)."""
         t = self.torch
         _need(y.dtype in self._dtypes, f"y is {y.dtype}, not float32 or bfloat16")
-        _need(not transposed or w8.transposed, "w8 has no transposes")
+        _need(not transposed or w8.t_codes is not None, "w8 has no transposes")
         n_in, n_out = (w8.outputs, w8.inputs) if transposed else (w8.inputs, w8.outputs)
         self._matrices(w8, "w8")
         self._packed(x8, "x8", x8.rows, n_in)

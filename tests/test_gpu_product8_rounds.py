@@ -27,9 +27,8 @@ def test_many_tiles(m, K, N, E, dtype):
     y = torch.full((m, N), 3.0, dtype=kind, device="cuda")
     xv, again = torch.empty_like(x), torch.full((m, N), 4.0, dtype=kind, device="cuda")
     L.unpack8(x8, xv)
-    rows = Rows8(E * N, K)
-    rows.codes = w8.codes.reshape(E * N, -1)
-    rows.exps = w8.exps.repeat_interleave(128, 1)[:, :N].reshape(E * N, -1).contiguous()
+    rows = Rows8(E * N, K, codes=w8.codes.reshape(E * N, -1),
+                 exps=w8.exps.repeat_interleave(128, 1)[:, :N].reshape(E * N, -1).contiguous())
     wv = torch.empty((E * N, K), device="cuda")
     L.unpack8(rows, wv)
     wv = wv.view(E, N, K)

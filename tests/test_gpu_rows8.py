@@ -132,9 +132,8 @@ def test_pack_weights(E, N, K, dtype):
     def read(codes, exps, width):
         """Values by the rows' reader: a matrix' exponents for each of its rows."""
         rows = codes.shape[1]
-        r = Rows8(E * rows, width)
-        r.codes = codes.reshape(E * rows, -1)
-        r.exps = exps.repeat_interleave(128, 1)[:, :rows].reshape(E * rows, -1).contiguous()
+        r = Rows8(E * rows, width, codes=codes.reshape(E * rows, -1),
+                  exps=exps.repeat_interleave(128, 1)[:, :rows].reshape(E * rows, -1).contiguous())
         got = torch.empty((E * rows, width), device="cuda")
         L.unpack8(r, got)
         return host(got).reshape(E, rows, width)
