@@ -124,24 +124,23 @@ __device__ __forceinline__ u4v bf16x8(const f4 a, const f4 b) {
   return u4v{bf16x2(a[0], a[1]), bf16x2(a[2], a[3]), bf16x2(b[0], b[1]), bf16x2(b[2], b[3])};
 }
 
-// Four neighbouring outputs of a row.
+// Four neighbouring outputs of a row, at the alignment of one.
 template <bool F32>
-__device__ __forceinline__ void put4(void* y, int64_t at, int left, const f4 v, bool whole) {
+__device__ __forceinline__ void put4(void* y, int64_t at, int left, const f4 v) {
   if (F32) {
     float* p = static_cast<float*>(y) + at;
-    if (whole && left >= 4) *reinterpret_cast<f4*>(p) = v;
+    if (left >= 4) *reinterpret_cast<U4*>(p) = __builtin_bit_cast(u4v, v);
     else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < 3; ++q)
         if (q < left) p[q] = v[q];
     }
   } else {
     uint16_t* p = static_cast<uint16_t*>(y) + at;
-    if (whole && left >= 4) {
-      *reinterpret_cast<u2v*>(p) = u2v{bf16x2(v[0], v[1]), bf16x2(v[2], v[3])};
-    } else {
+    if (left >= 4) *reinterpret_cast<U2*>(p) = u2v{bf16x2(v[0], v[1]), bf16x2(v[2], v[3])};
+    else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < 3; ++q)
         if (q < left) p[q] = to_bf16(v[q]);
     }
   }
@@ -425,7 +424,6 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
 
     // a lane has four neighbouring outputs of a row, with those of the next operand eight
     const int lane1 = anew(lane), r1 = rows0 + (lane1 & 15), g1 = lane1 >> 4;
-    const bool whole = a.N % (4 * kSide) == 0;
     using Out = std::conditional_t<F32, float, uint16_t>;
     Out* const y = static_cast<Out*>(a.y) + int64_t(tile.first) * a.N;
     if (a.bias) {
@@ -438,13 +436,16 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    // (16 bytes at the alignment of one value, whatever the outputs' number)
     const auto store = [&](int i, int j, int p, int n) {
       Out* const to = y + int64_t(p) * a.N + n;
-      if constexpr (F32) *reinterpret_cast<f4*>(to) = sum[i][j];
-      else if constexpr (STREAM) __builtin_nontemporal_store(bf16x8(sum[i][j], sum[i + 1][j]), reinterpret_cast<u4v*>(to));
-      else *reinterpret_cast<u4v*>(to) = bf16x8(sum[i][j], sum[i + 1][j]);
+      u4v v;
+      if constexpr (F32) v = __builtin_bit_cast(u4v, sum[i][j]);
+      else v = bf16x8(sum[i][j], sum[i + 1][j]);
+      if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<U4*>(to));
+      else *reinterpret_cast<U4*>(to) = v;
     };
-    const bool full = whole && tile.rows == kRowTile && tile.n0 + kColTile <= a.N;
+    const bool full = tile.rows == kRowTile && tile.n0 + kColTile <= a.N;
     if (full) {
 #pragma unroll
       for (int j = 0; j < RF; ++j) {
@@ -452,29 +453,27 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
         for (int i = 0; i < CF; i += kSide) store(i, j, r1 + 16 * j, tile.n0 + cols0 + output_of<F32>(i, 4 * g1));
         __builtin_amdgcn_sched_barrier(0);
       }
-    } else if (whole) {
-#pragma unroll
-      for (int j = 0; j < RF; ++j)
-#pragma unroll
-        for (int i = 0; i < CF; i += kSide) {
-          const int p = r1 + 16 * j, n = tile.n0 + cols0 + output_of<F32>(i, 4 * g1);
-          if (p < tile.rows && n < a.N) store(i, j, p, n);
-        }
     } else {
 #pragma unroll
-      for (int i = 0; i < CF; ++i)
+      for (int i = 0; i < CF; i += kSide) {
+        const int n = tile.n0 + cols0 + output_of<F32>(i, 4 * g1);
+        if (n + 4 * kSide <= a.N) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int n = tile.n0 + cols0 + output_of<F32>(i, 4 * g1) + q;
-          if (n < a.N)
+          for (int j = 0; j < RF; ++j)
+            if (r1 + 16 * j < tile.rows) store(i, j, r1 + 16 * j, n);
+        } else if (n < a.N) {
 #pragma unroll
-            for (int j = 0; j < RF; ++j) {
-              const int p = r1 + 16 * j;
-              if (p >= tile.rows) continue;
-              if constexpr (F32) y[int64_t(p) * a.N + n] = sum[i][j][q];
-              else y[int64_t(p) * a.N + n] = to_bf16(sum[i][j][q]);
-            }
+          for (int q = 0; q < 4 * kSide - 1; ++q)
+            if (n + q < a.N)
+#pragma unroll
+              for (int j = 0; j < RF; ++j) {
+                const int p = r1 + 16 * j;
+                if (p >= tile.rows) continue;
+                if constexpr (F32) y[int64_t(p) * a.N + n + q] = sum[i][j][q];
+                else y[int64_t(p) * a.N + n + q] = to_bf16(sum[i + q / 4][j][q % 4]);
+              }
         }
+      }
     }
     if (!more) break;
     id += slots;
@@ -488,52 +487,91 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
   }
 }
 
-// ---- few rows: 16 rows and 16 outputs, the blocks of inputs shared by wavefronts ----
+// ---- few rows: 16 RF rows and 16 outputs, the blocks of inputs shared by wavefronts ----
 
-template <bool F32>
-__global__ __launch_bounds__(256) void k_product_few(Product8Args a, int64_t row_tiles, int col_tiles) {
-  __shared__ f4 part_sum[4][64];
+// The weights are read once for every 16 RF rows, straight to registers; a wavefront
+// has every fourth block of inputs, and asks for two at once.
+template <bool F32, int RF>
+__global__ __launch_bounds__(256) void k_product_few(Product8Args a, int col_tiles) {
+  __shared__ f4 part_sum[3][RF][64];
   const int64_t id = blockIdx.x;
   const int64_t rt = id / col_tiles;
   const int n0 = int(id - rt * col_tiles) * 16;
-  const Part part = find_part(a.offsets, a.E, a.m, 16, rt, false);
+  const Part part = find_part(a.offsets, a.E, a.m, 16 * RF, rt, false);
   if (part.expert < 0) return;
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, w = uni(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, w = uni(int(threadIdx.x >> 6));
   const int64_t kp = codes8(a.K), xp = exps8(a.K);
   const int blocks = (a.K + kBlock8 - 1) / kBlock8, blocks_n = (a.N + kBlock8 - 1) / kBlock8;
-  const uint8_t* wc = a.w + (int64_t(part.expert) * a.N + min(a.N - 1, n0 + r)) * kp + 16 * g;
-  const uint8_t* we = a.w_exps + (int64_t(part.expert) * blocks_n + n0 / kBlock8) * xp;
-  const int64_t p = min(part.end - 1, part.first + r);
-  const uint8_t* xc = a.x + p * kp + 16 * g;
-  const uint8_t* xe = a.x_exps + p * xp;
-  f4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int b = w; b < blocks; b += 4) {
-    const u4v w0 = *reinterpret_cast<const u4v*>(wc + int64_t(b) * kBlock8), w1 = *reinterpret_cast<const u4v*>(wc + int64_t(b) * kBlock8 + 64);
-    const u4v x0 = *reinterpret_cast<const u4v*>(xc + int64_t(b) * kBlock8), x1 = *reinterpret_cast<const u4v*>(xc + int64_t(b) * kBlock8 + 64);
-    const uint32_t ew = we[b], ex = xe[b];
-    const i8 c = {int(w0[0]), int(w0[1]), int(w0[2]), int(w0[3]), int(w1[0]), int(w1[1]), int(w1[2]), int(w1[3])};
-    const i8 x = {int(x0[0]), int(x0[1]), int(x0[2]), int(x0[3]), int(x1[0]), int(x1[1]), int(x1[2]), int(x1[3])};
-    if constexpr (F32) {
-      bf8 cv[4], xv[4];
-      widen(c, __uint_as_float(ew << 23), cv);
-      widen(x, __uint_as_float(ex << 23), xv);
+  const uint8_t* const wc = a.w + (int64_t(part.expert) * a.N + min(a.N - 1, n0 + r)) * kp + 16 * g;
+  const uint8_t* const we = a.w_exps + (int64_t(part.expert) * blocks_n + n0 / kBlock8) * xp;
+  const uint8_t* xc[RF];
+  const uint8_t* xe[RF];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cv[s], xv[s], sum, 0, 0, 0);
-    } else {
-      sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(c, x, sum, 0, 0, 0, int(ew), 0, int(ex));
+  for (int j = 0; j < RF; ++j) {
+    const int64_t p = min(part.end - 1, part.first + 16 * j + r);
+    xc[j] = a.x + p * kp + 16 * g;
+    xe[j] = a.x_exps + p * xp;
+  }
+  f4 sum[RF];
+#pragma unroll
+  for (int j = 0; j < RF; ++j) sum[j] = f4{0.f, 0.f, 0.f, 0.f};
+  const auto codes = [](const uint8_t* from) {
+    const u4v u = *reinterpret_cast<const u4v*>(from), v = *reinterpret_cast<const u4v*>(from + 64);
+    return i8{int(u[0]), int(u[1]), int(u[2]), int(u[3]), int(v[0]), int(v[1]), int(v[2]), int(v[3])};
+  };
+  for (int b0 = w; b0 < blocks; b0 += 8) {
+    // (behind the last block the last one again, and not used)
+    i8 c[2], x[2][RF];
+    uint32_t ew[2], ex[2][RF];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int b = min(blocks - 1, b0 + 4 * h);
+      c[h] = codes(wc + int64_t(b) * kBlock8);
+      ew[h] = we[b];
+#pragma unroll
+      for (int j = 0; j < RF; ++j) {
+        x[h][j] = codes(xc[j] + int64_t(b) * kBlock8);
+        ex[h][j] = xe[j][b];
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (b0 + 4 * h >= blocks) break;
+      if constexpr (F32) {
+        bf8 cv[4];
+        widen(c[h], __uint_as_float(ew[h] << 23), cv);
+#pragma unroll
+        for (int j = 0; j < RF; ++j) {
+          bf8 xv[4];
+          widen(x[h][j], __uint_as_float(ex[h][j] << 23), xv);
+#pragma unroll
+          for (int s = 0; s < 4; ++s) sum[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cv[s], xv[s], sum[j], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < RF; ++j)
+          sum[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(c[h], x[h][j], sum[j], 0, 0, 0, int(ew[h]), 0, int(ex[h][j]));
+      }
     }
   }
-  part_sum[w][lane] = sum;
+  if (w > 0) {
+#pragma unroll
+    for (int j = 0; j < RF; ++j) part_sum[w - 1][j][lane] = sum[j];
+  }
   __syncthreads();
-  if (w != 0) return;
-  sum = (sum + part_sum[1][lane]) + (part_sum[2][lane] + part_sum[3][lane]);
+  if (w > 0) return;
   const int n = n0 + 4 * g;
+  f4 bias = {0.f, 0.f, 0.f, 0.f};
   if (a.bias) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (n + q < a.N) sum[q] += a.bias[int64_t(part.expert) * a.N + n + q];
+    for (int q = 0; q < 4; ++q) bias[q] = a.bias[int64_t(part.expert) * a.N + min(a.N - 1, n + q)];
   }
-  if (part.first + r < part.end) put4<F32>(a.y, (part.first + r) * a.N + n, a.N - n, sum, a.N % 4 == 0);
+#pragma unroll
+  for (int j = 0; j < RF; ++j) {
+    const int64_t p = part.first + 16 * j + r;
+    const f4 v = (sum[j] + part_sum[0][j][lane]) + (part_sum[1][j][lane] + part_sum[2][j][lane]) + bias;
+    if (p < part.end) put4<F32>(a.y, p * a.N + n, a.N - n, v);
+  }
 }
 
 // ---- gradients of the matrices ----------------------------------------------------
@@ -717,7 +755,7 @@ __device__ __forceinline__ void weights_tile(const Product8Args& a, const Part& 
 #pragma unroll
     for (int i = 0; i < KF; ++i) {
       const int k = kt * kK + wk + 16 * i + 4 * g;
-      put4<true>(out, int64_t(n) * a.K + k, a.K - k, sum[i][j], a.K % 4 == 0);
+      put4<true>(out, int64_t(n) * a.K + k, a.K - k, sum[i][j]);
     }
     if (BIAS && w / WN == 0 && g == 0) (a.slots ? a.bias_slots : a.dbias)[to * a.N + n] = own[j];
   }
@@ -791,12 +829,23 @@ __global__ __launch_bounds__(256) void k_add_slices(Product8Args a) {
 hipError_t launch_product8(const Product8Args& a, int n_cu, hipStream_t s) {
   // no more parts of T rows than this, whatever the experts' shares
   const auto parts = [&](int64_t t) { return a.offsets ? std::min(a.m, (a.m + int64_t(a.E) * (t - 1)) / t) : (a.m + t - 1) / t; };
-  const bool few = a.m <= int64_t(16) * a.E;
+  // Few rows: where there are not 16 for every expert, or tiles of 128 x 128 would
+  // leave seven CUs of eight without one (1,024 inputs and outputs, bfloat16: 100 rows,
+  // 8 tiles, 5.5 us against 10.2; 512 rows, 32 tiles, 8.3 against 10.3; 4,096 of both,
+  // 64 rows, 32 tiles, 16.2 against 25.0; 1,000 rows of 4,096 inputs, 64 tiles, 53 against 30).
+  const bool few = a.m <= int64_t(16) * a.E || parts(128) * ((a.N + 127) / 128) <= n_cu / 8;
   if (few) {
     const int cols = (a.N + 15) / 16;
-    const int64_t rows = parts(16);
-    if (a.bf16) k_product_few<false><<<unsigned(rows * cols), 256, 0, s>>>(a, rows, cols);
-    else k_product_few<true><<<unsigned(rows * cols), 256, 0, s>>>(a, rows, cols);
+    const auto run = [&](auto f32, auto rf) {
+      k_product_few<f32.value, rf.value><<<unsigned(parts(16 * rf.value) * cols), 256, 0, s>>>(a, cols);
+    };
+    const auto with = [&](auto f32) {
+      if (a.m <= int64_t(16) * a.E) run(f32, std::integral_constant<int, 1>());
+      else if (a.m <= int64_t(32) * a.E) run(f32, std::integral_constant<int, 2>());
+      else run(f32, std::integral_constant<int, 4>());
+    };
+    if (a.bf16) with(std::false_type());
+    else with(std::true_type());
   } else {
     // `each` work-groups a CU, as many as there is LDS for
     const auto run = [&](auto kernel, int64_t row_tile, int col_tile, int threads, int each) {
