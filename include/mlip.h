@@ -584,13 +584,15 @@ mlip_status mlip_unpack8(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, 
  * [n_experts + 1], rising; NULL with n_experts 1: all rows), and rows from
  * offsets[n_experts] on are neither read nor written.
  * mlip_product8: y_p = W_e x_p + c_e, y_dev [m][outputs] contiguous in dtype,
- * aligned to 16 bytes, bias_dev f32 [n_experts][outputs] or NULL.  With the
- * transposes and dy for x (inputs and outputs exchanged) it is the gradient in x.
+ * bias_dev f32 [n_experts][outputs] or NULL.  With the transposes and dy for x
+ * (inputs and outputs exchanged) it is the gradient in x.
  * Sums from block to block are float32.  In float32 y has the accuracy of float32
- * products of the packed values; for bf16 the 128 products of a block are added
- * up in about 16 bits below the largest of them, y being rounded to 8 bits.
- * mlip_product8_weights: dweights_dev f32 [n_experts][outputs][inputs] (aligned to
- * 16 bytes), sum_p dy_p x_p^T over the expert's rows, and, unless NULL, dbias_dev f32
+ * products of the packed values; for bf16, whose results are rounded to 8
+ * bits, the matrix instruction adds eight neighbouring products at a time with
+ * their bits below 2^-13 of the largest one cut off (rms 1.5e-5 of a sum of normally
+ * distributed values, at most 7 x 2^-13 of the largest product of each eight).
+ * mlip_product8_weights: dweights_dev f32 [n_experts][outputs][inputs],
+ * sum_p dy_p x_p^T over the expert's rows, and, unless NULL, dbias_dev f32
  * [n_experts][outputs], sum_p dy_p; 0 for experts without rows.  Float32 sums of
  * the packed values' products; dtype is not looked at beyond its range.  A NaN in
  * a row gives NaN wherever it is a factor.

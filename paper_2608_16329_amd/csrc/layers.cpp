@@ -246,8 +246,6 @@ mlip_status mlip_product8(mlip_learn* ctx, const mlip_product8_params* p, int64_
   if (m == 0) return MLIP_OK;
   if (!x_codes_dev || !x_exps_dev || !w_codes_dev || !w_exps_dev || !y_dev) return fail(ctx, MLIP_E_ARG, "NULL argument");
   if (!placed(x_codes_dev, x_exps_dev) || !placed(w_codes_dev, w_exps_dev)) return fail(ctx, MLIP_E_ARG, kPlaced);
-  // four values of a row are stored at once where rows allow it
-  if (reinterpret_cast<uintptr_t>(y_dev) % 16) return fail(ctx, MLIP_E_ARG, "y must be aligned to 16 bytes");
   Product8Args a{};
   a.m = m;
   a.E = p->n_experts;
@@ -273,7 +271,6 @@ mlip_status mlip_product8_weights(mlip_learn* ctx, const mlip_product8_params* p
   if (!dweights_dev || (m > 0 && (!dy_codes_dev || !dy_exps_dev || !x_codes_dev || !x_exps_dev)))
     return fail(ctx, MLIP_E_ARG, "NULL argument");
   if (!placed(dy_codes_dev, dy_exps_dev) || !placed(x_codes_dev, x_exps_dev)) return fail(ctx, MLIP_E_ARG, kPlaced);
-  if (reinterpret_cast<uintptr_t>(dweights_dev) % 16) return fail(ctx, MLIP_E_ARG, "dweights must be aligned to 16 bytes");
   Product8Args a{};
   a.m = m;
   a.E = p->n_experts;
