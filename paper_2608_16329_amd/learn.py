@@ -34,6 +34,7 @@ class _OnStream:
         self.torch = torch
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         self.device = self.stream.device
+        self._index = self.device.index
         self._raw = self.stream.cuda_stream
         # (the current stream's handle alone: a stream object for every call takes longer than the call's checks)
         self._current, self._device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
@@ -41,10 +42,10 @@ class _OnStream:
 
     def _run(self, call, *args) -> None:
         """The call's work after what the current stream has, and what it gets next after the call's."""
-        if self._device() != self.device.index:
+        if self._device() != self._index:
             with self.torch.cuda.device(self.device):
                 return self._run(call, *args)
-        if self._current(self.device.index) == self._raw:
+        if self._current(self._index) == self._raw:
             call(*args)
             return
         current = self.torch.cuda.current_stream(self.device)
@@ -53,7 +54,7 @@ class _OnStream:
         current.wait_stream(self.stream)
 
     def _dense(self, t, name: str, dtype, *shape):
-        if t.dtype is dtype and t.shape == shape and t.device == self.device and t.is_contiguous():
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self._index and t.is_contiguous():
             return
         _need(t.device == self.device, f"{name} is on {t.device}, not {self.device}")
         _need(t.dtype == dtype, f"{name} is {t.dtype}, not {dtype}")
@@ -62,15 +63,22 @@ class _OnStream:
 
     def _rows(self, t, name: str) -> int:
         """The values between the rows of a 2-d f32 or bf16 tensor."""
-        if t.dim() == 2 and t.dtype in self._dtypes and t.device == self.device and t.is_contiguous():
-            return t.shape[1]
-        _need(t.device == self.device, f"{name} is on {t.device}, not {self.device}")
-        _need(t.dtype in self._dtypes, f"{name} is {t.dtype}, not float32 or bfloat16")
-        _need(t.dim() == 2, f"{name} has {t.dim()} dimensions, not 2")
+        if t.dtype in self._dtypes and t.get_device() == self._index and t.is_contiguous():
+            shape = t.shape
+            if len(shape) == 2:
+                return shape[1]
+        if t.get_device() != self._index:
+            raise ValueError(f"{name} is on {t.device}, not {self.device}")
+        if t.dtype not in self._dtypes:
+            raise ValueError(f"{name} is {t.dtype}, not float32 or bfloat16")
+        if t.dim() != 2:
+            raise ValueError(f"{name} has {t.dim()} dimensions, not 2")
         n, m = t.shape
-        _need(m == 0 or t.stride(1) == 1 or m == 1, f"{name} has rows of values that are not next to each other")
+        if m > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name} has rows of values that are not next to each other")
         stride = t.stride(0) if n > 1 else m
-        _need(stride >= m, f"{name} has rows that overlap")
+        if stride < m:
+            raise ValueError(f"{name} has rows that overlap")
         return stride
 
 
@@ -251,14 +259,16 @@ class Learner(_OnStream):
 
     def _packed(self, r: Rows8, name: str, rows: int, width: int) -> None:
         codes, _, has, wide = r._held
-        if has == rows and wide == width and codes.get_device() == self.device.index:
+        if has == rows and wide == width and codes.get_device() == self._index:
             return
-        _need(codes.device == self.device, f"{name} is on {codes.device}, not {self.device}")
-        _need(False, f"{name} has {has} rows of {wide} values, not {rows} of {width}")
+        if codes.device != self.device:
+            raise ValueError(f"{name} is on {codes.device}, not {self.device}")
+        raise ValueError(f"{name} has {has} rows of {wide} values, not {rows} of {width}")
 
     def _expert_offsets(self, offsets, experts: int) -> None:
         if offsets is None:
-            _need(experts == 1, f"{experts} experts need offsets")
+            if experts != 1:
+                raise ValueError(f"{experts} experts need offsets")
         else:
             self._dense(offsets, "offsets", self.torch.int32, experts + 1)
 
@@ -287,7 +297,8 @@ class Learner(_OnStream):
         stride = self._rows(y, "y")
         _need(places.dim() == 2, "places is not 2-d")
         n, top_k = places.shape
-        _need(y.shape[0] == n * top_k, f"y has {y.shape[0]} rows, not {n} x {top_k}")
+        if y.shape[0] != n * top_k:
+            raise ValueError(f"y has {y.shape[0]} rows, not {n} x {top_k}")
         width = y.shape[1]
         self._dense(places, "places", t.int32, n, top_k)
         self._dense(out, "out", y.dtype, n, width)
@@ -304,7 +315,8 @@ class Learner(_OnStream):
         stride = self._rows(dout, "dout")
         _need(places.dim() == 2, "places is not 2-d")
         n, top_k = places.shape
-        _need(dout.shape[0] == n, f"dout has {dout.shape[0]} rows, not {n}")
+        if dout.shape[0] != n:
+            raise ValueError(f"dout has {dout.shape[0]} rows, not {n}")
         width = dout.shape[1]
         self._dense(places, "places", t.int32, n, top_k)
         self._dense(dy, "dy", dout.dtype, n * top_k, width)
@@ -315,8 +327,8 @@ class Learner(_OnStream):
             _need(y is not None, "dgates needs y")
             self._dense(dgates, "dgates", t.float32, n, top_k)
             y_stride = self._rows(y, "y")
-            _need(y.dtype == dout.dtype and tuple(y.shape) == (n * top_k, width),
-                  f"y is {y.dtype} {tuple(y.shape)}, not {dout.dtype} {(n * top_k, width)}")
+            if not (y.dtype == dout.dtype and tuple(y.shape) == (n * top_k, width)):
+                raise ValueError(f"y is {y.dtype} {tuple(y.shape)}, not {dout.dtype} {(n * top_k, width)}")
         p = self._params(b.mlip_rows_params, 1, top_k, width, self._dtypes[dout.dtype])
         self._run(b.mlip_combine_backward, self.ctx, p, n, _ptr(dout), stride, _ptr(y) if dgates is not None else None,
                   y_stride, _ptr(places), _ptr(gates), _ptr(dy), _ptr(dgates))
@@ -343,19 +355,22 @@ class Learner(_OnStream):
 
     def unpack8(self, rows8: Rows8, x) -> None:
         """The values of rows in 8 bits into x, f32 or bf16 [rows, width] (mlip_unpack8)."""
-        _need(x.dtype in self._dtypes, f"x is {x.dtype}, not float32 or bfloat16")
+        if x.dtype not in self._dtypes:
+            raise ValueError(f"x is {x.dtype}, not float32 or bfloat16")
         self._packed(rows8, "rows8", rows8.rows, rows8.width)
         self._dense(x, "x", x.dtype, rows8.rows, rows8.width)
         p = self._params(b.mlip_rows_params, 1, 1, rows8.width, self._dtypes[x.dtype])
         self._run(b.mlip_unpack8, self.ctx, p, rows8.rows, _ptr(rows8.codes), _ptr(rows8.exps), _ptr(x))
 
     def _matrices(self, w8: Weights8, name: str) -> None:
-        _need(w8.codes.device == self.device, f"{name} is on {w8.codes.device}, not {self.device}")
+        if w8.codes.device != self.device:
+            raise ValueError(f"{name} is on {w8.codes.device}, not {self.device}")
 
     def pack8_weights(self, w, w8: Weights8) -> None:
         """Matrices (f32 or bf16 [experts, outputs, inputs]) in 8 bits, and their
         transposes where w8 has places for them (mlip_pack8_weights)."""
-        _need(w.dtype in self._dtypes, f"w is {w.dtype}, not float32 or bfloat16")
+        if w.dtype not in self._dtypes:
+            raise ValueError(f"w is {w.dtype}, not float32 or bfloat16")
         self._matrices(w8, "w8")
         self._dense(w, "w", w.dtype, w8.experts, w8.outputs, w8.inputs)
         p = self._params(b.mlip_product8_params, w8.experts, w8.inputs, w8.outputs, self._dtypes[w.dtype])
@@ -369,7 +384,8 @@ class Learner(_OnStream):
         last one on left as they are.  transposed: with the transposes, [m, inputs] from
         rows of `outputs` values, the gradient in x (mlip_product8)."""
         t = self.torch
-        _need(y.dtype in self._dtypes, f"y is {y.dtype}, not float32 or bfloat16")
+        if y.dtype not in self._dtypes:
+            raise ValueError(f"y is {y.dtype}, not float32 or bfloat16")
         _need(not transposed or w8.t_codes is not None, "w8 has no transposes")
         n_in, n_out = (w8.outputs, w8.inputs) if transposed else (w8.inputs, w8.outputs)
         self._matrices(w8, "w8")
@@ -408,8 +424,8 @@ class Learner(_OnStream):
         residual_stride = width
         if residual is not None:
             residual_stride = self._rows(residual, "residual")
-            _need(residual.dtype == z.dtype and residual.shape == z.shape,
-                  f"residual is {residual.dtype} {tuple(residual.shape)}, not {z.dtype} {tuple(z.shape)}")
+            if not (residual.dtype == z.dtype and residual.shape == z.shape):
+                raise ValueError(f"residual is {residual.dtype} {tuple(residual.shape)}, not {z.dtype} {tuple(z.shape)}")
         if h is not None:
             self._dense(h, "h", z.dtype, n, width)
         for r, name in ((kept, "kept"), (h8, "h8")):
