@@ -436,43 +436,52 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    // (16 bytes at the alignment of one value, whatever the outputs' number)
-    const auto store = [&](int i, int j, int p, int n) {
+    // 16 bytes at the alignment of one value, whatever the outputs' number.  bfloat16:
+    // lanes of neighbouring rows exchange halves, so that eight of them have 64
+    // outputs of one row, a whole line, in one store.
+    const auto put = [&](const u4v v, int p, int n, bool check) {
       Out* const to = y + int64_t(p) * a.N + n;
-      u4v v;
-      if constexpr (F32) v = __builtin_bit_cast(u4v, sum[i][j]);
-      else v = bf16x8(sum[i][j], sum[i + 1][j]);
-      if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<U4*>(to));
-      else *reinterpret_cast<U4*>(to) = v;
+      if (!check || (p < tile.rows && n + 4 * kSide <= a.N)) {
+        if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<U4*>(to));
+        else *reinterpret_cast<U4*>(to) = v;
+      } else if (p < tile.rows) {
+#pragma unroll
+        for (int q = 0; q < 4 * kSide - 1; ++q)
+          if (n + q < a.N) {
+            if constexpr (F32) to[q] = __uint_as_float(v[q]);
+            else to[q] = uint16_t(v[q / 2] >> (16 * (q % 2)));
+          }
+      }
+    };
+    const auto store = [&](int j, bool check) {
+      const int n = tile.n0 + cols0;
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < CF; ++i) put(__builtin_bit_cast(u4v, sum[i][j]), r1 + 16 * j, n + output_of<true>(i, 4 * g1), check);
+      } else {
+        static_assert(CF == 4);
+        const bool odd = r1 & 1;
+        const u4v lo = bf16x8(sum[0][j], sum[1][j]), hi = bf16x8(sum[2][j], sum[3][j]);
+        u4v other;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          other[q] = uint32_t(__builtin_amdgcn_update_dpp(0, int(odd ? lo[q] : hi[q]), 0xb1, 0xf, 0xf, true));
+        put(odd ? other : lo, (r1 & ~1) + 16 * j, n + 8 * g1 + (odd ? 32 : 0), check);
+        put(odd ? hi : other, (r1 | 1) + 16 * j, n + 8 * g1 + (odd ? 32 : 0), check);
+      }
     };
     const bool full = tile.rows == kRowTile && tile.n0 + kColTile <= a.N;
     if (full) {
 #pragma unroll
       for (int j = 0; j < RF; ++j) {
-#pragma unroll
-        for (int i = 0; i < CF; i += kSide) store(i, j, r1 + 16 * j, tile.n0 + cols0 + output_of<F32>(i, 4 * g1));
+        store(j, false);
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < CF; i += kSide) {
-        const int n = tile.n0 + cols0 + output_of<F32>(i, 4 * g1);
-        if (n + 4 * kSide <= a.N) {
-#pragma unroll
-          for (int j = 0; j < RF; ++j)
-            if (r1 + 16 * j < tile.rows) store(i, j, r1 + 16 * j, n);
-        } else if (n < a.N) {
-#pragma unroll
-          for (int q = 0; q < 4 * kSide - 1; ++q)
-            if (n + q < a.N)
-#pragma unroll
-              for (int j = 0; j < RF; ++j) {
-                const int p = r1 + 16 * j;
-                if (p >= tile.rows) continue;
-                if constexpr (F32) y[int64_t(p) * a.N + n + q] = sum[i][j][q];
-                else y[int64_t(p) * a.N + n + q] = to_bf16(sum[i + q / 4][j][q % 4]);
-              }
-        }
+      for (int j = 0; j < RF; ++j) {
+        store(j, true);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     if (!more) break;
