@@ -106,18 +106,28 @@ __global__ __launch_bounds__(256) void k_combine(RowsArgs a) {
     char* to = static_cast<char*>(a.out) + i * a.width * f.size;
     for (int c = lane; c < f.pieces; c += L * kPieces) {
       float sum[kPieces][V] = {};
-      for (int s = 0; s < a.K; ++s) {
-        const int64_t p = place_of(a, i * a.K + s);
-        if (p < 0) continue;
-        const float g = a.gates ? a.gates[i * a.K + s] : 1.f;
-        const char* from = static_cast<const char*>(a.x) + p * a.x_stride * f.size;
-        u4v v[kPieces];
+      // two entries at a time, whose rows are under way together
+      for (int s = 0; s < a.K; s += 2) {
+        int64_t p[2];
+        float g[2];
 #pragma unroll
-        for (int q = 0; q < kPieces; ++q)
-          if (c + q * L < f.pieces) v[q] = *reinterpret_cast<const U4*>(from + f.at(c + q * L));
+        for (int h = 0; h < 2; ++h) {
+          p[h] = s + h < a.K ? place_of(a, i * a.K + s + h) : -1;
+          g[h] = a.gates && s + h < a.K ? a.gates[i * a.K + s + h] : 1.f;
+        }
+        u4v v[2][kPieces];
 #pragma unroll
-        for (int q = 0; q < kPieces; ++q)
-          if (c + q * L < f.pieces) add<BF>(sum[q], v[q], g);
+        for (int h = 0; h < 2; ++h) {
+          const char* const from = static_cast<const char*>(a.x) + p[h] * a.x_stride * f.size;
+#pragma unroll
+          for (int q = 0; q < kPieces; ++q)
+            if (p[h] >= 0 && c + q * L < f.pieces) v[h][q] = *reinterpret_cast<const U4*>(from + f.at(c + q * L));
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int q = 0; q < kPieces; ++q)
+            if (p[h] >= 0 && c + q * L < f.pieces) add<BF>(sum[q], v[h][q], g[h]);
       }
 #pragma unroll
       for (int q = 0; q < kPieces; ++q)

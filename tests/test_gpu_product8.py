@@ -5,7 +5,9 @@ Products of two codes are exact in float32.  float32 results: instructions of 32
 products each, whose own sums are good to 4 x 2^-23 of the sum of the sizes, and
 K / 32 additions of partial sums no larger than that, each off by at most one unit
 in the last place, 2^-23: (K / 32 + 4) 2^-23 of it, the bias one more, and one
-for each of the slices' sums of a gradient.  bfloat16 results: an instruction adds
+for each of the slices' sums of a gradient.  The bias's gradient: four sums of a
+quarter of the rows each, two rows an instruction, n / 8 roundings of half a unit:
+n / 16 of 2^-23 for n / 32.  bfloat16 results: an instruction adds
 eight neighbouring products with their bits below 2^-13 of the largest one's power
 of two cut off, 7 x 2^-13 of it for every eight; the rest as above; and half a
 step of the result, 2^-8."""
@@ -109,7 +111,7 @@ def test_gradients_of_the_matrices(case):
         n = b - a
         bound = (n / 32 + 4 + n / 256) * 2.0 ** -23
         assert (np.abs(host(dw)[e] - dv[a:b].T @ xv[a:b]) <= bound * (np.abs(dv[a:b]).T @ np.abs(xv[a:b]))).all()
-        assert (np.abs(host(db)[e] - dv[a:b].sum(0)) <= bound * np.abs(dv[a:b]).sum(0)).all()
+        assert (np.abs(host(db)[e] - dv[a:b].sum(0)) <= (bound + n / 32 * 2.0 ** -23) * np.abs(dv[a:b]).sum(0)).all()
     again = torch.full((E, N, K), 4.0, device="cuda")
     L.product8_weights(dy8, x8, again, offsets=off)
     assert torch.equal(dw, again)                             # the same bits, with and without dbias

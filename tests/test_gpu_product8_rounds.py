@@ -51,3 +51,37 @@ def test_many_tiles(m, K, N, E, dtype):
                 bound = bound + 2.0 ** -8 * want.abs() + 7 * 16 * 2.0 ** -13 * (xt @ wt.t().contiguous())
             assert bool(((y[a:b].double() - want).abs() <= bound).all()), (e, a)
     L.close()
+
+
+@pytest.mark.parametrize("m,K,N,E", [(20011, 512, 512, 3), (5003, 2048, 2048, 4), (17009, 500, 512, 70), (33333, 1000, 700, 1), (16411, 256, 2300, 9)])
+def test_gradients_in_large_tiles(m, K, N, E):
+    """Matrices whose gradients have tiles of 256 x 256, experts whose rows end within a step, NaN behind the last."""
+    import torch
+    from paper_2608_16329_amd import Learner, Rows8
+    g = torch.Generator(device="cuda").manual_seed(m)
+    x, dy = torch.randn((m, K), generator=g, device="cuda"), torch.randn((m, N), generator=g, device="cuda")
+    x[m - 7:], dy[m - 7:] = float("nan"), float("nan")
+    cuts = torch.sort(torch.randint(0, m - 7, (E - 1,), generator=g, device="cuda")).values.tolist()
+    ends = [0] + cuts + [m - 7]
+    if E > 2:
+        ends[1] = ends[2]                                     # one without rows
+    off = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    L, x8, dy8 = Learner(), Rows8(m, K), Rows8(m, N)
+    L.pack8(x, x8)
+    L.pack8(dy, dy8)
+    xv, dv = torch.empty_like(x), torch.empty_like(dy)
+    L.unpack8(x8, xv)
+    L.unpack8(dy8, dv)
+    dw, db = torch.full((E, N, K), 3.0, device="cuda"), torch.full((E, N), 3.0, device="cuda")
+    L.product8_weights(dy8, x8, dw, offsets=off, dbias=db)
+    for e in range(E):
+        a, b = ends[e], ends[e + 1]
+        xd, dd = xv[a:b].double(), dv[a:b].double()
+        bound = ((b - a) / 32 + 4 + (b - a) / 256) * 2.0 ** -23
+        want, size = dd.t().contiguous() @ xd, dd.abs().t().contiguous() @ xd.abs()
+        assert bool(((dw[e].double() - want).abs() <= bound * size).all()), e
+        assert bool(((db[e].double() - dd.sum(0)).abs() <= (bound + (b - a) / 32 * 2.0 ** -23) * dd.abs().sum(0)).all()), e
+    again = torch.full((E, N, K), 4.0, device="cuda")
+    L.product8_weights(dy8, x8, again, offsets=off)
+    assert torch.equal(dw, again)
+    L.close()
