@@ -191,9 +191,9 @@ __global__ __launch_bounds__(256) void k_activate8_backward(Pack8Args a) {
 // from 8 (t % 16) on of rows t / 16, t / 16 + 16 ..
 template <bool BF>
 __global__ __launch_bounds__(256) void k_pack8_weights(Weights8Args a) {
-  constexpr int kPitch = kBlock8 + 16;              // of a row of codes in LDS
+  constexpr int kPitch = kBlock8 / 4 + 1;           // of a row of codes in LDS, in 32-bit words
   __shared__ uint32_t tops[4];
-  __shared__ uint8_t tile[kBlock8 * kPitch];
+  __shared__ uint32_t tile[kBlock8 * kPitch];
   const int kb = blockIdx.x, nb = blockIdx.y, t = threadIdx.x;
   const int64_t e = blockIdx.z;
   const int blocks_k = (a.K + kBlock8 - 1) / kBlock8, blocks_n = (a.N + kBlock8 - 1) / kBlock8;
@@ -223,7 +223,10 @@ __global__ __launch_bounds__(256) void k_pack8_weights(Weights8Args a) {
     const int r = 16 * j + (t >> 4), n = nb * kBlock8 + r;
     const u2v c = encode8(v[j], x);
     if (a.codes && n < a.N) *reinterpret_cast<u2v*>(a.codes + (e * a.N + n) * codes8(a.K) + k0) = c;
-    if (a.codes_t) *reinterpret_cast<u2v*>(tile + r * kPitch + 8 * (t & 15)) = c;
+    if (a.codes_t) {
+      tile[r * kPitch + 2 * (t & 15)] = c[0];
+      tile[r * kPitch + 2 * (t & 15) + 1] = c[1];
+    }
   }
   // the exponent, and zeros behind the last block
   if (t < 4) {
@@ -234,18 +237,28 @@ __global__ __launch_bounds__(256) void k_pack8_weights(Weights8Args a) {
   }
   if (!a.codes_t) return;
   __syncthreads();
+  // four columns of eight rows at a time, as columns: bytes of four words change places
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int r = 16 * j + (t >> 4), k = kb * kBlock8 + r, c0 = 8 * (t & 15);
-    if (k >= a.K) continue;
-    uint32_t w[2];
+  for (int j = 0; j < 2; ++j) {
+    const int r0 = 8 * (t & 15), k4 = 16 * j + (t >> 4);
+    uint32_t w[8], col[4][2];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) w[q] = tile[(r0 + q) * kPitch + k4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      w[h] = 0;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) w[h] |= uint32_t(tile[(c0 + 4 * h + q) * kPitch + r]) << (8 * q);
+      const uint32_t* const v = w + 4 * h;
+      const uint32_t a01 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400u), a23 = __builtin_amdgcn_perm(v[3], v[2], 0x05010400u);
+      const uint32_t b01 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602u), b23 = __builtin_amdgcn_perm(v[3], v[2], 0x07030602u);
+      col[0][h] = __builtin_amdgcn_perm(a23, a01, 0x05040100u);
+      col[1][h] = __builtin_amdgcn_perm(a23, a01, 0x07060302u);
+      col[2][h] = __builtin_amdgcn_perm(b23, b01, 0x05040100u);
+      col[3][h] = __builtin_amdgcn_perm(b23, b01, 0x07060302u);
     }
-    *reinterpret_cast<u2v*>(a.codes_t + (e * a.K + k) * codes8(a.N) + nb * kBlock8 + c0) = u2v{w[0], w[1]};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int k = kb * kBlock8 + 4 * k4 + q;
+      if (k < a.K) *reinterpret_cast<u2v*>(a.codes_t + (e * a.K + k) * codes8(a.N) + nb * kBlock8 + r0) = u2v{col[q][0], col[q][1]};
+    }
   }
 }
 
