@@ -436,9 +436,9 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    // 16 bytes at the alignment of one value, whatever the outputs' number.  bfloat16:
-    // lanes of neighbouring rows exchange halves, so that eight of them have 64
-    // outputs of one row, a whole line, in one store.
+    // 16 bytes at the alignment of one value, whatever the outputs' number.  Lanes of
+    // neighbouring rows exchange halves, so that eight of them have 128 neighbouring
+    // bytes of one row, a whole line, in one store.
     const auto put = [&](const u4v v, int p, int n, bool check) {
       Out* const to = y + int64_t(p) * a.N + n;
       if (!check || (p < tile.rows && n + 4 * kSide <= a.N)) {
@@ -454,20 +454,24 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
       }
     };
     const auto store = [&](int j, bool check) {
-      const int n = tile.n0 + cols0;
-      if constexpr (F32) {
+      const bool odd = r1 & 1;
+      constexpr int kEach = 4 * kSide, kHalf = 4 * kEach;     // outputs of a lane, of a row's half line
 #pragma unroll
-        for (int i = 0; i < CF; ++i) put(__builtin_bit_cast(u4v, sum[i][j]), r1 + 16 * j, n + output_of<true>(i, 4 * g1), check);
-      } else {
-        static_assert(CF == 4);
-        const bool odd = r1 & 1;
-        const u4v lo = bf16x8(sum[0][j], sum[1][j]), hi = bf16x8(sum[2][j], sum[3][j]);
-        u4v other;
+      for (int i = 0; i < CF; i += 2 * kSide) {
+        u4v lo, hi, other;
+        if constexpr (F32) {
+          lo = __builtin_bit_cast(u4v, sum[i][j]);
+          hi = __builtin_bit_cast(u4v, sum[i + 1][j]);
+        } else {
+          lo = bf16x8(sum[i][j], sum[i + 1][j]);
+          hi = bf16x8(sum[i + 2][j], sum[i + 3][j]);
+        }
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           other[q] = uint32_t(__builtin_amdgcn_update_dpp(0, int(odd ? lo[q] : hi[q]), 0xb1, 0xf, 0xf, true));
-        put(odd ? other : lo, (r1 & ~1) + 16 * j, n + 8 * g1 + (odd ? 32 : 0), check);
-        put(odd ? hi : other, (r1 | 1) + 16 * j, n + 8 * g1 + (odd ? 32 : 0), check);
+        const int n = tile.n0 + cols0 + 16 * i + kEach * g1 + (odd ? kHalf : 0);
+        put(odd ? other : lo, (r1 & ~1) + 16 * j, n, check);
+        put(odd ? hi : other, (r1 | 1) + 16 * j, n, check);
       }
     };
     const bool full = tile.rows == kRowTile && tile.n0 + kColTile <= a.N;
@@ -861,10 +865,22 @@ hipError_t launch_product8(const Product8Args& a, int n_cu, hipStream_t s) {
       const int64_t tiles = parts(row_tile) * ((a.N + col_tile - 1) / col_tile);
       kernel<<<unsigned((std::min(tiles, int64_t(n_cu) * each) + 7) / 8 * 8), threads, 0, s>>>(a);
     };
-    if (!a.bf16) run(k_product<true, 4, 4, 2, 2>, 128, 128, 256, 2);
-    else if (parts(256) * ((a.N + 255) / 256) >= n_cu / 2)
-      run(a.m * a.N > int64_t(1) << 27 ? k_product<false, 8, 4, 2, 4, true> : k_product<false, 8, 4, 2, 4>, 256, 256, 512, 1);
-    else run(k_product<false, 4, 4, 2, 2>, 128, 128, 256, 2);
+    // Tiles of 256 x 256 read half as much for each product as tiles of 128 x 128, and
+    // are taken where half of the CUs have one (65,536 rows, 8 experts, 1,024 inputs to
+    // 4,096 outputs: bfloat16 306 us against 381, float32 591 against 693; 16,384 rows,
+    // 2,048 of both: 66 against 75 and 108 against 127; 16,000 rows, 500 of both, 126
+    // tiles, 13.0 against 12.5 and 16.0 against 16.6).  Results that are larger than the
+    // last cache, of 256 MB, go past it (65,536 x 4,096: 306 against 334 and 591 against
+    // 632; results that fit are read by what comes next).
+    const bool stream = a.m * a.N * (a.bf16 ? 2 : 4) > int64_t(1) << 28;
+    const auto with = [&](auto f32) {
+      constexpr bool kF32 = f32.value;
+      if (parts(256) * ((a.N + 255) / 256) < n_cu / 2) run(k_product<kF32, 4, 4, 2, 2>, 128, 128, 256, 2);
+      else if (stream) run(k_product<kF32, 8, 4, 2, 4, true>, 256, 256, 512, 1);
+      else run(k_product<kF32, 8, 4, 2, 4>, 256, 256, 512, 1);
+    };
+    if (a.bf16) with(std::false_type());
+    else with(std::true_type());
   }
   return hipGetLastError();
 }
