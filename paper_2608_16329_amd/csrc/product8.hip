@@ -618,7 +618,7 @@ struct Rows {
     xat = row * xpitch + (there ? piece / (kBlock8 / 16) : 0);
   }
   // Rows from step * kRows on into set s; zeros behind the part's `rows` (a buffer's
-  // loads give those behind its end).
+  // loads give those behind its end; all of the offset is in what is compared with it).
   __device__ __forceinline__ void fetch(int s, int64_t step, int64_t rows) {
     const int64_t p0 = step * kRows;
     const int left = int(max(int64_t(0), min(int64_t(kRows), rows - p0)));
@@ -626,8 +626,8 @@ struct Rows {
     const auto efrom = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(exps + p0 * xpitch), 0, max(0, left * int(xpitch) - col / kBlock8), 0x27000);
 #pragma unroll
     for (int q = 0; q < P; ++q) {
-      c[s][q] = __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(from, int(at), q * kApart * int(pitch), 0));
-      e[s][q] = __builtin_amdgcn_raw_buffer_load_b8(efrom, int(xat), q * kApart * int(xpitch), 0);
+      c[s][q] = __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(from, int(at) + q * kApart * int(pitch), 0, 0));
+      e[s][q] = __builtin_amdgcn_raw_buffer_load_b8(efrom, int(xat) + q * kApart * int(xpitch), 0, 0);
     }
   }
   // To LDS in bfloat16, without rounding: rows of 2 COLS bytes, 16 values (32 bytes) c of row p at c ^ p % 8.
@@ -903,8 +903,8 @@ size_t product8_weights_plan(Product8Args* a, int n_cu) {
   a->slice = a->m;
   // slices of rows where the experts' tiles do not fill the CUs, one work-group each
   // or three: as many as fit at once, each expert's last one shorter
-  const int64_t fit = int64_t(n_cu) * (large ? 1 : 3) / tiles;
-  if (tiles * a->E < n_cu) a->slice = std::max<int64_t>(256, (a->m + fit - a->E - 1) / std::max<int64_t>(1, fit - a->E));
+  const int64_t fit = int64_t(n_cu) * (large ? 1 : 3) / tiles, most = a->offsets ? fit - a->E : fit;
+  if (tiles * a->E < n_cu) a->slice = std::max<int64_t>(256, most > 0 ? (a->m + most - 1) / most : a->m);
   a->slice = std::max<int64_t>(1, (a->slice + 63) / 64 * 64);
   if (a->slice >= a->m) return 0;
   return size_t(items(*a)) * size_t(int64_t(a->N) * a->K + a->N) * sizeof(float);
