@@ -595,7 +595,7 @@ mlip_status mlip_unpack8(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, 
  * sum_p dy_p x_p^T over the expert's rows, and, unless NULL, dbias_dev f32
  * [n_experts][outputs], sum_p dy_p; 0 for experts without rows.  Float32 sums of
  * the packed values' products; dtype is not looked at beyond its range.  A NaN in
- * a row gives NaN wherever it is a factor.
+ * a row gives NaN wherever it is a factor.  No output may overlap an input.
  * m in [0, 2^31), n_experts 1..256, inputs and outputs 1..65536, and (m / 128 +
  * n_experts) outputs / 128, and n_experts inputs outputs / 2^14, below 2^22.
  * Errors: MLIP_E_ARG, and of mlip_product8_weights MLIP_E_STATE, MLIP_E_OOM; MLIP_E_HIP.
@@ -626,7 +626,8 @@ mlip_status mlip_product8_weights(mlip_learn* ctx, const mlip_product8_params* p
  * dz_codes_dev, dz_exps_dev are what mlip_pack8 gives for h and dz as they are
  * written, for the next product; kept_codes_dev, kept_exps_dev what it gives for z.
  * Outputs that are not wanted are NULL (kept: nothing will be differentiated).
- * silu(-infinity) is NaN.  p->n_experts and top_k are not used beyond their range.
+ * h may be z or r, and dz dh, where their rows are contiguous; apart from that no
+ * output may overlap an input.  silu(-infinity) is NaN.  p->n_experts and top_k are not used beyond their range.
  * Errors: MLIP_E_ARG, MLIP_E_HIP.
  */
 mlip_status mlip_activate8(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, const void* z_dev, int64_t z_stride,

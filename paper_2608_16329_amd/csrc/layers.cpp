@@ -54,7 +54,6 @@ RowsArgs rows_args(const mlip_rows_params* p, int64_t n) {
 Pack8Args pack_args(const mlip_rows_params* p, int64_t n) {
   Pack8Args a{};
   a.n = n;
-  a.rows = n;
   a.E = p->n_experts;
   a.K = p->top_k;
   a.width = p->width;

@@ -39,7 +39,6 @@ hipError_t launch_combine_backward(const RowsArgs& a, int n_cu, hipStream_t s);
 // Rows to and from 8 bits, and activations that keep them.
 struct Pack8Args {
   int64_t n;                  // rows that are written
-  int64_t rows;               // rows of x (n / top_k with an order)
   int E, K, width;
   bool bf16;
   const void* x;              // x, z or dh

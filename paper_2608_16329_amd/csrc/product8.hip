@@ -46,7 +46,6 @@ __device__ __forceinline__ int anew(int v) {
 struct Part {
   int expert;
   int64_t first, end;
-  int64_t begin;                // the expert's first row
 };
 // Part t of the experts' rows in parts of `rows`, each expert's from its first
 // row on.  All lanes of a wavefront call with the same t.  `whole`: every expert
@@ -54,8 +53,8 @@ struct Part {
 __device__ Part find_part(const int32_t* offsets, int E, int64_t m, int64_t rows, int64_t t, bool whole) {
   if (!offsets) {
     const int64_t first = t * rows;
-    if (first >= m && !(whole && t == 0)) return {-1, 0, 0, 0};
-    return {0, first, min(m, first + rows), 0};
+    if (first >= m && !(whole && t == 0)) return {-1, 0, 0};
+    return {0, first, min(m, first + rows)};
   }
   const int lane = threadIdx.x & 63;
   int64_t before = 0;
@@ -81,11 +80,11 @@ __device__ Part find_part(const int32_t* offsets, int E, int64_t m, int64_t rows
       const int l = __ffsll(static_cast<unsigned long long>(mine)) - 1;
       const int64_t k = t - (before + __shfl(sum, l) - __shfl(parts, l));
       const int64_t f = __shfl(int(from), l), g = __shfl(int(to), l);
-      return {uni(e0 + l), uni64(f + k * rows), uni64(min(g, f + (k + 1) * rows)), uni64(f)};
+      return {uni(e0 + l), uni64(f + k * rows), uni64(min(g, f + (k + 1) * rows))};
     }
     before += __shfl(sum, 63);
   }
-  return {-1, 0, 0, 0};
+  return {-1, 0, 0};
 }
 
 // All rows of the expert that is the rank-th largest, for at most 64 experts: long
@@ -104,8 +103,7 @@ __device__ Part sized_part(const int32_t* offsets, int E, int64_t m, int rank) {
     larger += other > mine || (other == mine && f < lane) ? 1 : 0;
   }
   const int l = uni(int(__ffsll(static_cast<unsigned long long>(__ballot(lane < E && larger == rank))) - 1));
-  const int first = __builtin_amdgcn_readlane(from, l);
-  return {l, first, __builtin_amdgcn_readlane(to, l), first};
+  return {l, __builtin_amdgcn_readlane(from, l), __builtin_amdgcn_readlane(to, l)};
 }
 
 // One operand's 32 codes of a lane as four bfloat16 operands.
@@ -811,6 +809,8 @@ __global__ __launch_bounds__(256) void k_add_slices(Product8Args a) {
     before += __shfl_xor(static_cast<long long>(before), o);
     mine += __shfl_xor(static_cast<long long>(mine), o);
   }
+  // (offsets that do not rise may ask for more than there are)
+  mine = max(int64_t(0), min(mine, a.m / a.slice + a.E - before));
   const int64_t values = int64_t(a.N) * a.K, all = values + (a.dbias ? a.N : 0);
   constexpr int kEach = SPLIT ? 64 : 256, kBy = SPLIT ? 4 : 1;
   for (int64_t v0 = int64_t(blockIdx.x) * kEach; v0 < all; v0 += int64_t(gridDim.x) * kEach) {

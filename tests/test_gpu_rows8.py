@@ -241,3 +241,24 @@ def test_more_than_2_to_the_32_values():
     L.activate8_backward(kept, tail, one)
     assert torch.equal(one, back[-64:])
     L.close()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,w", [(3, 7), (40, 129), (70, 515)])
+def test_activation_in_place(n, w, dtype):
+    """h over z or over the residual, dz over dh: bit for bit what other places get."""
+    import torch
+    from paper_2608_16329_amd import Learner, Rows8
+    rng, dtype = np.random.default_rng(w), getattr(torch, dtype)
+    z, r, dh = (tensor(values(rng, n, w), dtype) for _ in range(3))
+    L, kept, again = Learner(), Rows8(n, w), Rows8(n, w)
+    h, dz = torch.empty_like(z), torch.empty_like(z)
+    L.activate8(z, kept, h, residual=r)
+    L.activate8_backward(kept, dh, dz)
+    over_z, over_r, over_dh = z.clone(), r.clone(), dh.clone()
+    L.activate8(over_z, again, over_z, residual=r)
+    L.activate8(z, None, over_r, residual=over_r)
+    L.activate8_backward(again, over_dh, over_dh)
+    assert torch.equal(over_z, h) and torch.equal(over_r, h) and torch.equal(over_dh, dz)
+    assert torch.equal(again.codes, kept.codes) and torch.equal(again.exps, kept.exps)
+    L.close()
