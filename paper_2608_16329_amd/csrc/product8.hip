@@ -865,17 +865,24 @@ hipError_t launch_product8(const Product8Args& a, int n_cu, hipStream_t s) {
       const int64_t tiles = parts(row_tile) * ((a.N + col_tile - 1) / col_tile);
       kernel<<<unsigned((std::min(tiles, int64_t(n_cu) * each) + 7) / 8 * 8), threads, 0, s>>>(a);
     };
-    // Tiles of 256 x 256 read half as much for each product as tiles of 128 x 128, and
-    // are taken where half of the CUs have one (65,536 rows, 8 experts, 1,024 inputs to
-    // 4,096 outputs: bfloat16 306 us against 381, float32 591 against 693; 16,384 rows,
-    // 2,048 of both: 66 against 75 and 108 against 127; 16,000 rows, 500 of both, 126
-    // tiles, 13.0 against 12.5 and 16.0 against 16.6).  Results that are larger than the
-    // last cache, of 256 MB, go past it (65,536 x 4,096: 306 against 334 and 591 against
-    // 632; results that fit are read by what comes next).
+    // Tiles of 256 x 256 read half as much for each product as tiles of 128 x 128, and a
+    // CU has one of them at a time or two of those.  A round of the small ones takes
+    // about 0.6 of a round of the large ones, and the last round is seldom full; an
+    // expert's last tile is half full on average.  Small against large, in bfloat16 and
+    // float32: 65,536 rows, 8 experts, 1,024 inputs to 4,096 outputs, 33 rounds to 17,
+    // 381 us against 306 and 693 against 591; 8,192 rows, 1,024 to 2,048, 3 to 2, 35.2
+    // against 40.3 and 43.4 against 58.7; 4,096 x 4,096 x 4,096, 2 to 1, 75 against 69.
+    const auto rounds = [&](int64_t t, int at_once) {
+      const int64_t tiles = ((a.m + t - 1) / t + (a.offsets ? a.E / 2 : 0)) * ((a.N + t - 1) / t);
+      return (tiles + at_once - 1) / at_once;
+    };
+    const bool large = rounds(256, n_cu) * 5 <= rounds(128, 2 * n_cu) * 3;
+    // Results that are larger than the last cache, of 256 MB, go past it (65,536 x 4,096:
+    // 306 us against 334 and 591 against 632; results that fit are read by what comes next).
     const bool stream = a.m * a.N * (a.bf16 ? 2 : 4) > int64_t(1) << 28;
     const auto with = [&](auto f32) {
       constexpr bool kF32 = f32.value;
-      if (parts(256) * ((a.N + 255) / 256) < n_cu / 2) run(k_product<kF32, 4, 4, 2, 2>, 128, 128, 256, 2);
+      if (!large) run(k_product<kF32, 4, 4, 2, 2>, 128, 128, 256, 2);
       else if (stream) run(k_product<kF32, 8, 4, 2, 4, true>, 256, 256, 512, 1);
       else run(k_product<kF32, 8, 4, 2, 4>, 256, 256, 512, 1);
     };
