@@ -11,7 +11,12 @@
 // Bound by memory.  16 lanes have a block, 8 values each; a wavefront has four
 // blocks, whose exponents are one 32-bit word: four of a row, or one or two each
 // of four or two rows that have no more.  Wavefronts that run side by side have
-// neighbouring blocks.
+// neighbouring blocks, and float32 stores of 16 lanes are whole lines (both, and
+// conversions in hardware: 744 to 533 us of the activations below).
+// 131,072 rows of 1,024 bfloat16 values in the order of 2 of 16 experts: packing 172 us
+// (4.7 TB/s with each row read twice), unpacking 137 (5.9, partly from the last cache);
+// 65,536 rows of 4,096 bfloat16 values: silu that keeps its argument 287 us, its gradient
+// 284 (1.34 GB each, 4.7 TB/s).
 #include <algorithm>
 
 #include "layers_math.h"
@@ -188,7 +193,9 @@ __global__ __launch_bounds__(256) void k_activate8_backward(Pack8Args a) {
 }
 
 // One work-group for a block of 128 x 128 of a matrix: thread t has the 8 values
-// from 8 (t % 16) on of rows t / 16, t / 16 + 16 ..
+// from 8 (t % 16) on of rows t / 16, t / 16 + 16 ..  The transpose goes through LDS as
+// codes.  Bound by memory: 8 matrices of 4,096 x 1,024 float32 values, both ways, 45 us
+// (201 MB, 4.5 TB/s); bytes one at a time through LDS 57.
 template <bool BF>
 __global__ __launch_bounds__(256) void k_pack8_weights(Weights8Args a) {
   constexpr int kPitch = kBlock8 / 4 + 1;           // of a row of codes in LDS, in 32-bit words

@@ -9,6 +9,11 @@
 // bytes a lane.  A row has a group of 8 to 64 lanes, as many as take about four
 // pieces each, whose loads are under way together.  Sums are float32, in the
 // order of s; nothing is added up by atomics.
+// 262,144 rows of 1,024 bfloat16 values, 2 of 16 experts each: sorting 390 us, combining
+// 306 (5.3 TB/s of what is read and written; a copy of 1 GiB 5.15), combining's gradient
+// with the gates' 526 (5.1).  Sorting reads a row once for each of its experts, far
+// apart: 5.5 TB/s with both.  32,767 rows of 385 float32 values, 3 of 29 experts: 49,
+// 50 and 72 us.
 #include <algorithm>
 
 #include "layers_math.h"
@@ -201,7 +206,8 @@ __global__ __launch_bounds__(256) void k_combine_backward(RowsArgs a) {
   }
 }
 
-// Lanes of a row: 8 to 64, about kPieces pieces each.
+// Lanes of a row: 8 to 64, about kPieces pieces each (385 float32 values, 97 pieces,
+// 32 lanes: sorting, combining twice and its gradient 220 us; 16 lanes 245, 64 lanes 224).
 int lanes(const RowsArgs& a) {
   const int pieces = (a.width * (a.bf16 ? 2 : 4) + 15) / 16;
   int l = 8;
