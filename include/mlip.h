@@ -513,7 +513,7 @@ mlip_status mlip_heads(mlip_learn* ctx, const mlip_heads_params* p, int64_t n, c
  * order[p] = i top_k + s (offsets_dev, order_dev as mlip_group writes them):
  *   sorted_dev  [n top_k][width] contiguous: sorted[p] = x[order[p] / top_k] for
  *               p < offsets[n_experts]; rows from there on (entries without an
- *               expert) are left as they are
+ *               expert) are left as they are.  NULL: places alone, x is not read
  *   places_dev  int32 [n][top_k]: p, or -1 for an entry without an expert
  * mlip_combine: out_i = sum_s gates_is y[places_is] in float32, in the order of s,
  * out_dev [n][width] contiguous; entries without an expert add nothing and their

@@ -80,8 +80,9 @@ mlip_status mlip_sort(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, con
   LAYER_BEGIN(check_rows(ctx, p, n));
   if (!stride_fits(x_stride, p->width)) return fail(ctx, MLIP_E_ARG, kStride);
   if (n == 0) return MLIP_OK;
-  if (!x_dev || !offsets_dev || !order_dev || !sorted_dev || !places_dev) return fail(ctx, MLIP_E_ARG, "NULL argument");
+  if ((sorted_dev && !x_dev) || !offsets_dev || !order_dev || !places_dev) return fail(ctx, MLIP_E_ARG, "NULL argument");
   RowsArgs a = rows_args(p, n);
+  if (!sorted_dev) a.width = 1;                               // (no lanes for values)
   a.x = x_dev;
   a.x_stride = x_stride;
   a.offsets = offsets_dev;

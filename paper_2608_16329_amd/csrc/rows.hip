@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void k_sort(RowsArgs a) {
     const uint32_t entry = uint32_t(a.order[p]);
     if (entry >= a.m) continue;
     if (lane == 0) a.places[entry] = p < end ? int32_t(p) : -1;
-    if (p >= end) continue;
+    if (p >= end || !a.out) continue;
     const char* from = static_cast<const char*>(a.x) + int64_t(entry / uint32_t(a.K)) * a.x_stride * f.size;
     char* to = static_cast<char*>(a.out) + p * a.width * f.size;
     for (int c = lane; c < f.pieces; c += L * kPieces) {

@@ -275,8 +275,8 @@ class Learner(_OnStream):
     def sort(self, x, offsets, order, xs, places) -> None:
         """The rows of `x` (f32 or bf16 [n, width], rows may be apart) in the order
         that `group` found: xs (x's type) [n k, width], rows of entries without an
-        expert left as they are; places int32 [n, k], where each entry stands or -1
-        (mlip_sort).  The gradient in x is `combine` of xs' gradient."""
+        expert left as they are (None: places alone); places int32 [n, k], where each
+        entry stands or -1 (mlip_sort).  The gradient in x is `combine` of xs' gradient."""
         t = self.torch
         stride = self._rows(x, "x")
         n, width = x.shape
@@ -286,7 +286,8 @@ class Learner(_OnStream):
         self._dense(places, "places", t.int32, n, top_k)
         self._dense(offsets, "offsets", t.int32, offsets.shape[0])
         self._dense(order, "order", t.int32, n * top_k)
-        self._dense(xs, "xs", x.dtype, n * top_k, width)
+        if xs is not None:
+            self._dense(xs, "xs", x.dtype, n * top_k, width)
         p = self._params(b.mlip_rows_params, offsets.shape[0] - 1, top_k, width, self._dtypes[x.dtype])
         self._run(b.mlip_sort, self.ctx, p, n, _ptr(x), stride, _ptr(offsets), _ptr(order), _ptr(xs), _ptr(places))
 

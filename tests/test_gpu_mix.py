@@ -56,6 +56,9 @@ def test_sort_combine_and_gradients(n, w, k, E, empty, spare, dtype, weighted):
     want = host(x)[order // k]
     want[live:] = 5.0
     assert np.array_equal(host(xs), want)
+    alone = torch.full((n, k), 77, dtype=torch.int32, device="cuda")
+    L.sort(x, torch.from_numpy(offsets).cuda(), torch.from_numpy(order).cuda(), None, alone)
+    assert torch.equal(alone, places)
 
     out = torch.full((n, w), np.nan, dtype=dtype, device="cuda")
     L.combine(y, places, out, gates=gates)
