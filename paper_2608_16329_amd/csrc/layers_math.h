@@ -18,6 +18,18 @@ typedef uint32_t U2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 
+// 16 bytes from and to memory; STREAM: past what the caches hold.
+template <bool STREAM>
+__device__ __forceinline__ u4v take16(const void* from) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const U4*>(from));
+  else return *static_cast<const U4*>(from);
+}
+template <bool STREAM>
+__device__ __forceinline__ void give16(void* to, u4v v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<U4*>(to));
+  else *static_cast<U4*>(to) = v;
+}
+
 typedef float f2v __attribute__((ext_vector_type(2)));
 typedef __bf16 b2v __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
@@ -26,7 +38,7 @@ __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
 
 // Four values of an array of either type from `at` on, those from `left` on as
 // zero (left <= 0: none is read); and back, those before `left`.
-template <bool BF>
+template <bool BF, bool STREAM = false>
 __device__ __forceinline__ void load4at(const void* p, int64_t at, int left, float* v) {
   if (left >= 4) {
     if (BF) {
@@ -37,7 +49,7 @@ __device__ __forceinline__ void load4at(const void* p, int64_t at, int left, flo
         v[2 * q + 1] = __uint_as_float(h[q] & 0xffff0000u);
       }
     } else {
-      const u4v a = *reinterpret_cast<const U4*>(static_cast<const float*>(p) + at);
+      const u4v a = take16<STREAM>(static_cast<const float*>(p) + at);
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] = __uint_as_float(a[q]);
     }
@@ -49,13 +61,13 @@ __device__ __forceinline__ void load4at(const void* p, int64_t at, int left, flo
     if (q < left) v[q] = BF ? from_bf16(static_cast<const uint16_t*>(p)[at + q]) : static_cast<const float*>(p)[at + q];
   }
 }
-template <bool BF>
+template <bool BF, bool STREAM>
 __device__ __forceinline__ void store4at(void* p, int64_t at, int left, const float* v) {
   if (left >= 4) {
     if (BF) *reinterpret_cast<U2*>(static_cast<uint16_t*>(p) + at) = u2v{bf16x2(v[0], v[1]), bf16x2(v[2], v[3])};
     else
-      *reinterpret_cast<U4*>(static_cast<float*>(p) + at) =
-          u4v{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+      give16<STREAM>(static_cast<float*>(p) + at,
+                     u4v{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
     return;
   }
 #pragma unroll
@@ -71,10 +83,10 @@ __device__ __forceinline__ void store4at(void* p, int64_t at, int left, const fl
 // accesses lie side by side.  `left`: values of the row from `at` on.
 template <bool BF>
 constexpr int kSecond = BF ? 4 : 64;
-template <bool BF>
+template <bool BF, bool STREAM>
 __device__ __forceinline__ void load8(const void* p, int64_t at, int left, float v[8]) {
   if (BF && left >= 8) {
-    const u4v h = *reinterpret_cast<const U4*>(static_cast<const uint16_t*>(p) + at);
+    const u4v h = take16<STREAM>(static_cast<const uint16_t*>(p) + at);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       v[2 * q] = __uint_as_float(h[q] << 16);
@@ -82,20 +94,20 @@ __device__ __forceinline__ void load8(const void* p, int64_t at, int left, float
     }
     return;
   }
-  load4at<BF>(p, at, left, v);
-  load4at<BF>(p, at + kSecond<BF>, left - kSecond<BF>, v + 4);
+  load4at<BF, STREAM>(p, at, left, v);
+  load4at<BF, STREAM>(p, at + kSecond<BF>, left - kSecond<BF>, v + 4);
 }
-template <bool BF>
+template <bool BF, bool STREAM>
 __device__ __forceinline__ void store8(void* p, int64_t at, int left, const float v[8]) {
   if (BF && left >= 8) {
     u4v h;
 #pragma unroll
     for (int q = 0; q < 4; ++q) h[q] = bf16x2(v[2 * q], v[2 * q + 1]);
-    *reinterpret_cast<U4*>(static_cast<uint16_t*>(p) + at) = h;
+    give16<STREAM>(static_cast<uint16_t*>(p) + at, h);
     return;
   }
-  store4at<BF>(p, at, left, v);
-  store4at<BF>(p, at + kSecond<BF>, left - kSecond<BF>, v + 4);
+  store4at<BF, STREAM>(p, at, left, v);
+  store4at<BF, STREAM>(p, at + kSecond<BF>, left - kSecond<BF>, v + 4);
 }
 
 // The largest of 16 neighbouring lanes' values, in each of them: rotations

@@ -103,7 +103,7 @@ __device__ __forceinline__ int64_t source(const Pack8Args& a, int64_t p, int64_t
   return int64_t(entry) < a.n ? int64_t(entry / uint32_t(a.K)) : -1;
 }
 
-template <bool BF, int G>
+template <bool BF, int G, bool STREAM>
 __global__ __launch_bounds__(256) void k_pack8(Pack8Args a) {
   const int64_t end = a.order ? min(a.n, max(int64_t(0), int64_t(a.offsets[a.E]))) : a.n;
   each<G>(end, a.width, [&](int64_t row0, int quad) {
@@ -111,18 +111,18 @@ __global__ __launch_bounds__(256) void k_pack8(Pack8Args a) {
     const int64_t from = s.there ? source(a, s.row, end) : -1;
     s.there = s.there && from >= 0;
     float v[8] = {};
-    if (s.there) load8<BF>(a.x, from * a.x_stride + s.at, s.left, v);
+    if (s.there) load8<BF, STREAM>(a.x, from * a.x_stride + s.at, s.left, v);
     put<BF, G>(s, v, a.codes, a.exps, quad, a.width, end);
   });
 }
 
-template <bool BF, int G>
+template <bool BF, int G, bool STREAM>
 __global__ __launch_bounds__(256) void k_unpack8(Pack8Args a) {
   each<G>(a.n, a.width, [&](int64_t row0, int quad) {
     const Spot s = spot<BF, G>(row0, quad, a.n, a.width);
     float v[8];
     get<BF>(s, a.kept, a.kept_exps, a.width, v);
-    if (s.there) store8<BF>(a.out, s.row * a.width + s.at, s.left, v);
+    if (s.there) store8<BF, STREAM>(a.out, s.row * a.width + s.at, s.left, v);
   });
 }
 
@@ -151,19 +151,19 @@ __device__ __forceinline__ void as_stored(float v[8]) {
 }
 
 // h = r + silu(z), and z in 8 bits for the backward pass
-template <bool BF, int G>
+template <bool BF, int G, bool STREAM>
 __global__ __launch_bounds__(256) void k_activate8(Pack8Args a) {
   each<G>(a.n, a.width, [&](int64_t row0, int quad) {
     const Spot s = spot<BF, G>(row0, quad, a.n, a.width);
     float z[8] = {}, h[8] = {};
     if (s.there) {
-      load8<BF>(a.x, s.row * a.x_stride + s.at, s.left, z);
-      if (a.residual) load8<BF>(a.residual, s.row * a.residual_stride + s.at, s.left, h);
+      load8<BF, STREAM>(a.x, s.row * a.x_stride + s.at, s.left, z);
+      if (a.residual) load8<BF, STREAM>(a.residual, s.row * a.residual_stride + s.at, s.left, h);
     }
     if (a.codes) put<BF, G>(s, z, a.codes, a.exps, quad, a.width, a.n);
 #pragma unroll
     for (int q = 0; q < 8; ++q) h[q] = fmaf(z[q], sigmoid(z[q]), h[q]);
-    if (a.out && s.there) store8<BF>(a.out, s.row * a.width + s.at, s.left, h);
+    if (a.out && s.there) store8<BF, STREAM>(a.out, s.row * a.width + s.at, s.left, h);
     if (a.out_codes) {
       as_stored<BF>(h);
       put<BF, G>(s, h, a.out_codes, a.out_exps, quad, a.width, a.n);
@@ -172,19 +172,19 @@ __global__ __launch_bounds__(256) void k_activate8(Pack8Args a) {
 }
 
 // dz = dh silu'(z) of the z that was kept
-template <bool BF, int G>
+template <bool BF, int G, bool STREAM>
 __global__ __launch_bounds__(256) void k_activate8_backward(Pack8Args a) {
   each<G>(a.n, a.width, [&](int64_t row0, int quad) {
     const Spot s = spot<BF, G>(row0, quad, a.n, a.width);
     float z[8] = {}, d[8] = {};
-    if (s.there) load8<BF>(a.x, s.row * a.x_stride + s.at, s.left, d);
+    if (s.there) load8<BF, STREAM>(a.x, s.row * a.x_stride + s.at, s.left, d);
     get<BF>(s, a.kept, a.kept_exps, a.width, z);
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       const float t = sigmoid(z[q]);
       d[q] *= t * fmaf(z[q], 1.f - t, 1.f);
     }
-    if (a.out && s.there) store8<BF>(a.out, s.row * a.width + s.at, s.left, d);
+    if (a.out && s.there) store8<BF, STREAM>(a.out, s.row * a.width + s.at, s.left, d);
     if (a.out_codes) {
       as_stored<BF>(d);
       put<BF, G>(s, d, a.out_codes, a.out_exps, quad, a.width, a.n);
@@ -269,24 +269,35 @@ __global__ __launch_bounds__(256) void k_pack8_weights(Weights8Args a) {
   }
 }
 
+// Values that are more than the last cache, of 256 MB, holds go past it in and out: what
+// comes next would not find them there, and finds the codes (65,536 rows of 4,096 bfloat16
+// values: packing 148 us and 126 so, unpacking 141 and 120, the activation 250 and
+// 220, its gradient 252 and 203; 16,384 rows of 2,048, which stay there from call to call, 19
+// and 22, 16 and 15, 31 and 34, 33 and 38).
+bool streams(const Pack8Args& a) { return a.n * a.width * (a.bf16 ? 2 : 4) > int64_t(1) << 28; }
+
 template <typename F>
 hipError_t with_group(const Pack8Args& a, int n_cu, F run) {
   const int blocks = (a.width + kBlock8 - 1) / kBlock8, quads = (blocks + 3) / 4;
   const int rows = blocks == 1 ? 4 : blocks == 2 ? 2 : 1;           // of a wavefront
   const int64_t units = (a.n + rows - 1) / rows * quads;
   const unsigned g = unsigned(std::max<int64_t>(1, std::min<int64_t>((units + 3) / 4, int64_t(n_cu) * 64)));
-  if (blocks == 1) run(std::integral_constant<int, 1>(), g);
-  else if (blocks == 2) run(std::integral_constant<int, 2>(), g);
-  else run(std::integral_constant<int, 4>(), g);
+  const auto with = [&](auto w) {
+    if (streams(a)) run(w, std::true_type(), g);
+    else run(w, std::false_type(), g);
+  };
+  if (blocks == 1) with(std::integral_constant<int, 1>());
+  else if (blocks == 2) with(std::integral_constant<int, 2>());
+  else with(std::integral_constant<int, 4>());
   return hipGetLastError();
 }
 
 }  // namespace
 
 #define PACK8_LAUNCH(kernel)                                                \
-  return with_group(a, n_cu, [&](auto w, unsigned g) {                          \
-    if (a.bf16) kernel<true, w.value><<<g, 256, 0, s>>>(a);                 \
-    else kernel<false, w.value><<<g, 256, 0, s>>>(a);                       \
+  return with_group(a, n_cu, [&](auto w, auto t, unsigned g) {              \
+    if (a.bf16) kernel<true, w.value, t.value><<<g, 256, 0, s>>>(a);        \
+    else kernel<false, w.value, t.value><<<g, 256, 0, s>>>(a);              \
   })
 
 hipError_t launch_pack8(const Pack8Args& a, int n_cu, hipStream_t s) { PACK8_LAUNCH(k_pack8); }

@@ -73,7 +73,7 @@ __device__ __forceinline__ void set(void* p, int64_t at, float v) {
 }
 
 // One group of lanes for each place in the experts' order.
-template <bool BF, int L>
+template <bool BF, int L, bool STREAM>
 __global__ __launch_bounds__(256) void k_sort(RowsArgs a) {
   const Shape f = shape(a);
   const int lane = threadIdx.x % L;
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void k_sort(RowsArgs a) {
         if (c + q * L < f.pieces) v[q] = *reinterpret_cast<const U4*>(from + f.at(c + q * L));
 #pragma unroll
       for (int q = 0; q < kPieces; ++q)
-        if (c + q * L < f.pieces) *reinterpret_cast<U4*>(to + f.at(c + q * L)) = v[q];
+        if (c + q * L < f.pieces) give16<STREAM>(to + f.at(c + q * L), v[q]);
     }
     if (lane < f.few) {
       if (BF) reinterpret_cast<uint16_t*>(to)[lane] = reinterpret_cast<const uint16_t*>(from)[lane];
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256) void k_sort(RowsArgs a) {
 }
 
 // One group of lanes for each row.
-template <bool BF, int L>
+template <bool BF, int L, bool STREAM>
 __global__ __launch_bounds__(256) void k_combine(RowsArgs a) {
   constexpr int V = BF ? 8 : 4;
   const Shape f = shape(a);
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(256) void k_combine(RowsArgs a) {
           const char* const from = static_cast<const char*>(a.x) + p[h] * a.x_stride * f.size;
 #pragma unroll
           for (int q = 0; q < kPieces; ++q)
-            if (p[h] >= 0 && c + q * L < f.pieces) v[h][q] = *reinterpret_cast<const U4*>(from + f.at(c + q * L));
+            if (p[h] >= 0 && c + q * L < f.pieces) v[h][q] = take16<STREAM>(from + f.at(c + q * L));
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(256) void k_combine(RowsArgs a) {
       }
 #pragma unroll
       for (int q = 0; q < kPieces; ++q)
-        if (c + q * L < f.pieces) *reinterpret_cast<U4*>(to + f.at(c + q * L)) = rounded<BF>(sum[q]);
+        if (c + q * L < f.pieces) give16<STREAM>(to + f.at(c + q * L), rounded<BF>(sum[q]));
     }
     if (lane < f.few) {
       float sum = 0.f;
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void k_combine(RowsArgs a) {
 
 // One group of lanes for each row: its gradient goes to its entries' places, and
 // its products with the experts' outputs there are the gates' gradients.
-template <bool BF, int L>
+template <bool BF, int L, bool STREAM>
 __global__ __launch_bounds__(256) void k_combine_backward(RowsArgs a) {
   constexpr int V = BF ? 8 : 4;
   const Shape f = shape(a);
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256) void k_combine_backward(RowsArgs a) {
           for (int q = 0; q < kPieces; ++q)
             if (c + q * L < f.pieces) {
               d[q] = *reinterpret_cast<const U4*>(from + f.at(c + q * L));
-              if (a.dgates) v[q] = *reinterpret_cast<const U4*>(y + f.at(c + q * L));
+              if (a.dgates) v[q] = take16<STREAM>(y + f.at(c + q * L));
             }
 #pragma unroll
           for (int q = 0; q < kPieces; ++q)
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void k_combine_backward(RowsArgs a) {
               }
 #pragma unroll
               for (int j = 0; j < V; ++j) out[j] = g * dv[j];
-              *reinterpret_cast<U4*>(to + f.at(c + q * L)) = rounded<BF>(out);
+              give16<STREAM>(to + f.at(c + q * L), rounded<BF>(out));
             }
         }
         if (lane < f.few) {
@@ -216,20 +216,32 @@ int lanes(const RowsArgs& a) {
 }
 int grid(int64_t rows, int l, int n_cu) { return int(std::max<int64_t>(1, std::min<int64_t>((rows * l + 255) / 256, int64_t(n_cu) * 64))); }
 
-template <bool BF, typename F>
-void with_lanes(int l, F run) {
-  if (l == 8) run(std::integral_constant<int, 8>());
-  else if (l == 16) run(std::integral_constant<int, 16>());
-  else if (l == 32) run(std::integral_constant<int, 32>());
-  else run(std::integral_constant<int, 64>());
+// Rows in the experts' order that are more than the last cache, of 256 MB, holds go past
+// it in and out: what comes next would not find them there, and the rows of the
+// caller's order, which are read once for each expert, stay longer (262,144 rows of 1,024
+// bfloat16 values, 2 experts each: sorting 394 us and 336 so, combining 294 and 261, its
+// gradient 525 and 493; 32,767 rows of 385 float32 values, 3 each, 151 MB, called
+// again and again: 39 and 41, 30 and 39, 74 and 82).
+bool streams(const RowsArgs& a) { return a.m * a.width * (a.bf16 ? 2 : 4) > int64_t(1) << 28; }
+
+template <typename F>
+void with_lanes(int l, bool stream, F run) {
+  const auto with = [&](auto w) {
+    if (stream) run(w, std::true_type());
+    else run(w, std::false_type());
+  };
+  if (l == 8) with(std::integral_constant<int, 8>());
+  else if (l == 16) with(std::integral_constant<int, 16>());
+  else if (l == 32) with(std::integral_constant<int, 32>());
+  else with(std::integral_constant<int, 64>());
 }
 
 }  // namespace
 
-#define ROWS_LAUNCH(kernel, rows)                                                                       \
-  const int l = lanes(a), g = grid(rows, l, n_cu);                                                      \
-  if (a.bf16) with_lanes<true>(l, [&](auto w) { kernel<true, w.value><<<g, 256, 0, s>>>(a); });         \
-  else with_lanes<false>(l, [&](auto w) { kernel<false, w.value><<<g, 256, 0, s>>>(a); });              \
+#define ROWS_LAUNCH(kernel, rows)                                                                                      \
+  const int l = lanes(a), g = grid(rows, l, n_cu);                                                                     \
+  if (a.bf16) with_lanes(l, streams(a), [&](auto w, auto t) { kernel<true, w.value, t.value><<<g, 256, 0, s>>>(a); });     \
+  else with_lanes(l, streams(a), [&](auto w, auto t) { kernel<false, w.value, t.value><<<g, 256, 0, s>>>(a); });          \
   return hipGetLastError()
 
 hipError_t launch_sort(const RowsArgs& a, int n_cu, hipStream_t s) { ROWS_LAUNCH(k_sort, a.m); }

@@ -161,3 +161,37 @@ def test_more_than_2_to_the_32_bytes():
     L.combine_backward(x, xs, places, xs.zero_())
     assert torch.equal(xs[-8:], x[-8:]) and torch.equal(xs[n - 8:n], x[-8:])
     L.close()
+
+
+@pytest.mark.parametrize("n,w,k,E,dtype", [(60001, 385, 3, 9, "float32"), (50003, 1030, 3, 70, "bfloat16"), (20001, 4096, 1, 2, "float32"), (600001, 30, 4, 5, "float32")])
+def test_rows_larger_than_the_last_cache(n, w, k, E, dtype):
+    import torch
+    from paper_2608_16329_amd import Learner
+    dtype, m = getattr(torch, dtype), n * k
+    step = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x, y, dout = (torch.randn((r, w), generator=g, device="cuda").to(dtype) for r in (n, m, n))
+    experts, gates = torch.randint(-1, E, (n, k), generator=g, device="cuda", dtype=torch.int32), torch.rand((n, k), generator=g, device="cuda")
+    L = Learner()
+    offsets, order = (torch.empty(s, dtype=torch.int32, device="cuda") for s in (E + 1, m))
+    L.group(experts, offsets, order)
+    live, places = int(offsets[-1]), torch.empty((n, k), dtype=torch.int32, device="cuda")
+    xs, dy = torch.full((m, w), 5.0, dtype=dtype, device="cuda"), torch.full((m, w), 5.0, dtype=dtype, device="cuda")
+    L.sort(x, offsets, order, xs, places)
+    assert torch.equal(xs[:live], x[(order[:live] // k).long()]) and bool((xs[live:] == 5).all())
+    out, dgates = torch.empty((n, w), dtype=dtype, device="cuda"), torch.empty((n, k), device="cuda")
+    L.combine(y, places, out, gates=gates)
+    L.combine_backward(dout, y, places, dy, gates=gates, dgates=dgates)
+    for a in range(0, n, 10000):
+        p, gt = places[a:a + 10000].long(), gates[a:a + 10000].double()
+        terms = torch.where((p >= 0)[..., None], y[p.clamp(min=0)].double(), 0.0)
+        weighted = terms * gt[..., None]
+        want = weighted.sum(1)
+        assert bool(((out[a:a + 10000].double() - want).abs() <= k * 2.0 ** -24 * weighted.abs().sum(1) + step * want.abs()).all())
+        d = dout[a:a + 10000].double()
+        dots = terms * d[:, None]
+        assert bool(((dgates[a:a + 10000].double() - dots.sum(2)).abs() <= (w / 8 + 10) * 2.0 ** -24 * dots.abs().sum(2)).all())
+        want = (d[:, None] * gt[..., None])[p >= 0]
+        assert bool(((dy[p[p >= 0]].double() - want).abs() <= step * want.abs()).all())
+    assert bool((dy[live:] == 5).all())
+    L.close()

@@ -262,3 +262,38 @@ def test_activation_in_place(n, w, dtype):
     assert torch.equal(over_z, h) and torch.equal(over_r, h) and torch.equal(over_dh, dz)
     assert torch.equal(again.codes, kept.codes) and torch.equal(again.exps, kept.exps)
     L.close()
+
+
+@pytest.mark.parametrize("n,w,dtype", [(300001, 257, "float32"), (40003, 3500, "bfloat16"), (1100001, 65, "float32"), (70001, 2050, "bfloat16")])
+def test_values_larger_than_the_last_cache(n, w, dtype):
+    """All rows at once and in parts that the cache holds: the same bits."""
+    import torch
+    from paper_2608_16329_amd import Learner, Rows8
+    g, dtype = torch.Generator(device="cuda").manual_seed(n), getattr(torch, dtype)
+    z, r, dh = (torch.randn((n, w), generator=g, device="cuda").to(dtype) for _ in range(3))
+    order = torch.randperm(n, generator=g, device="cuda").to(torch.int32)
+    offsets = torch.tensor([0, n - 3], dtype=torch.int32, device="cuda")
+    L, packed, sorted8, kept, h8, dz8 = Learner(), *(Rows8(n, w) for _ in range(5))
+    h, dz, back = (torch.empty_like(z) for _ in range(3))
+    L.pack8(z, packed)
+    L.pack8(z, sorted8, offsets=offsets, order=order)
+    L.unpack8(packed, back)
+    L.activate8(z, kept, h, h8=h8, residual=r)
+    L.activate8_backward(kept, dh, dz, dz8=dz8)
+    for a in range(0, n, 30000):
+        s = slice(a, min(n, a + 30000))
+        m = s.stop - a
+        one, two, three = (Rows8(m, w) for _ in range(3))
+        u, v = torch.empty((m, w), dtype=dtype, device="cuda"), torch.empty((m, w), dtype=dtype, device="cuda")
+
+        def same_as(part, whole):
+            return torch.equal(part.codes, whole.codes[s]) and torch.equal(part.exps, whole.exps[s])
+        L.pack8(z[s], one)
+        L.unpack8(one, u)
+        assert same_as(one, packed) and torch.equal(u, back[s])
+        L.activate8(z[s], one, u, h8=two, residual=r[s])
+        L.activate8_backward(one, dh[s], v, dz8=three)
+        assert same_as(one, kept) and same_as(two, h8) and same_as(three, dz8) and torch.equal(u, h[s]) and torch.equal(v, dz[s])
+    at = order[:n - 3].long()
+    assert torch.equal(sorted8.codes[:n - 3], packed.codes[at]) and torch.equal(sorted8.exps[:n - 3], packed.exps[at])
+    L.close()
