@@ -12,11 +12,11 @@
 // blocks, whose exponents are one 32-bit word: four of a row, or one or two each
 // of four or two rows that have no more.  Wavefronts that run side by side have
 // neighbouring blocks, and float32 stores of 16 lanes are whole lines (both, and
-// conversions in hardware: 744 to 533 us of the activations below).
-// 131,072 rows of 1,024 bfloat16 values in the order of 2 of 16 experts: packing 172 us
-// (4.7 TB/s with each row read twice), unpacking 137 (5.9, partly from the last cache);
-// 65,536 rows of 4,096 bfloat16 values: silu that keeps its argument 287 us, its gradient
-// 284 (1.34 GB each, 4.7 TB/s).
+// conversions in hardware: 744 to 533 us of the two activations below).
+// 131,072 rows of 1,024 bfloat16 values in the order of 2 of 16 experts: packing 150 to
+// 161 us (5.0 TB/s with each row read twice), unpacking 118 to 128 (6.3, partly from the
+// last cache); 65,536 rows of 4,096 bfloat16 values: silu that keeps its argument 220 to
+// 228 us, its gradient 203 to 221 (1.34 GB each, 6 TB/s; 466 the two in turn on new values).
 #include <algorithm>
 
 #include "layers_math.h"

@@ -9,11 +9,11 @@
 // bytes a lane.  A row has a group of 8 to 64 lanes, as many as take about four
 // pieces each, whose loads are under way together.  Sums are float32, in the
 // order of s; nothing is added up by atomics.
-// 262,144 rows of 1,024 bfloat16 values, 2 of 16 experts each: sorting 390 us, combining
-// 306 (5.3 TB/s of what is read and written; a copy of 1 GiB 5.15), combining's gradient
-// with the gates' 526 (5.1).  Sorting reads a row once for each of its experts, far
-// apart: 5.5 TB/s with both.  32,767 rows of 385 float32 values, 3 of 29 experts: 49,
-// 50 and 72 us.
+// 262,144 rows of 1,024 bfloat16 values, 2 of 16 experts each: sorting 336 us (4.8 TB/s of
+// what is read and written, 6.4 with a row's second reading; a copy of 1 GiB 5.15),
+// combining 257 (6.3: some of it is still in the last cache), combining's gradient with
+// the gates' 493 (5.4).  32,767 rows of 385 float32 values, 3 of 29 experts: 49, 50
+// and 72 us, 39, 30 and 74 where the last cache has them.
 #include <algorithm>
 
 #include "layers_math.h"
