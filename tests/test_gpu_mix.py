@@ -163,7 +163,7 @@ def test_more_than_2_to_the_32_bytes():
     L.close()
 
 
-@pytest.mark.parametrize("n,w,k,E,dtype", [(60001, 385, 3, 9, "float32"), (50003, 1030, 3, 70, "bfloat16"), (20001, 4096, 1, 2, "float32"), (600001, 30, 4, 5, "float32")])
+@pytest.mark.parametrize("n,w,k,E,dtype", [(60001, 385, 3, 9, "float32"), (50003, 1030, 3, 70, "bfloat16"), (50003, 1031, 3, 8, "bfloat16"), (20001, 4096, 1, 2, "float32"), (600001, 30, 4, 5, "float32")])
 def test_rows_larger_than_the_last_cache(n, w, k, E, dtype):
     import torch
     from paper_2608_16329_amd import Learner

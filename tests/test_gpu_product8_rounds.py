@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("m,K,N,E", [(70000, 128, 512, 3), (70001, 200, 520, 2), (40000, 640, 1024, 1), (33000, 1300, 777, 4), (200000, 60, 260, 16),
-                                     (40001, 300, 2100, 3), (131149, 640, 1024, 5), (30011, 100, 1029, 2)])
+                                     (40001, 300, 2100, 3), (131149, 640, 1024, 5), (30011, 100, 1029, 2), (131149, 70, 1031, 2)])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_many_tiles(m, K, N, E, dtype):
     import torch

@@ -264,7 +264,7 @@ def test_activation_in_place(n, w, dtype):
     L.close()
 
 
-@pytest.mark.parametrize("n,w,dtype", [(300001, 257, "float32"), (40003, 3500, "bfloat16"), (1100001, 65, "float32"), (70001, 2050, "bfloat16")])
+@pytest.mark.parametrize("n,w,dtype", [(300001, 257, "float32"), (40003, 3500, "bfloat16"), (1100001, 65, "float32"), (70001, 2050, "bfloat16"), (70001, 2051, "bfloat16")])
 def test_values_larger_than_the_last_cache(n, w, dtype):
     """All rows at once and in parts that the cache holds: the same bits."""
     import torch
