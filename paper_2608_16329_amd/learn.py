@@ -24,6 +24,14 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _at(r):
+    """The places of a Rows8's codes and exponents."""
+    if r is None:
+        return None, None
+    codes, exps, _, _ = r._held
+    return codes.data_ptr(), exps.data_ptr()
+
+
 class _OnStream:
     """A stream of its own that is put in order with the caller's current one."""
 
@@ -60,6 +68,17 @@ class _OnStream:
         _need(t.dtype == dtype, f"{name} is {t.dtype}, not {dtype}")
         _need(tuple(t.shape) == shape, f"{name} has shape {tuple(t.shape)}, not {shape}")
         _need(t.is_contiguous(), f"{name} is not contiguous")
+
+    def _matrix(self, t, name: str):
+        """Rows, values of a row, values between rows and mlip_dtype of a 2-d f32 or bf16 tensor."""
+        kind = self._dtypes.get(t.dtype)
+        if kind is not None and t.get_device() == self._index and t.is_contiguous():
+            shape = t.shape
+            if len(shape) == 2:
+                n, m = shape
+                return n, m, m, kind
+        stride = self._rows(t, name)
+        return *t.shape, stride, kind
 
     def _rows(self, t, name: str) -> int:
         """The values between the rows of a 2-d f32 or bf16 tensor."""
@@ -278,8 +297,7 @@ class Learner(_OnStream):
         expert left as they are (None: places alone); places int32 [n, k], where each
         entry stands or -1 (mlip_sort).  The gradient in x is `combine` of xs' gradient."""
         t = self.torch
-        stride = self._rows(x, "x")
-        n, width = x.shape
+        n, width, stride, kind = self._matrix(x, "x")
         _need(places.dim() == 2, "places is not 2-d")
         _need(offsets.dim() == 1 and offsets.shape[0] >= 2, "offsets is not 1-d with at least 2 places")
         top_k = places.shape[1]
@@ -288,24 +306,23 @@ class Learner(_OnStream):
         self._dense(order, "order", t.int32, n * top_k)
         if xs is not None:
             self._dense(xs, "xs", x.dtype, n * top_k, width)
-        p = self._params(b.mlip_rows_params, offsets.shape[0] - 1, top_k, width, self._dtypes[x.dtype])
+        p = self._params(b.mlip_rows_params, offsets.shape[0] - 1, top_k, width, kind)
         self._run(b.mlip_sort, self.ctx, p, n, _ptr(x), stride, _ptr(offsets), _ptr(order), _ptr(xs), _ptr(places))
 
     def combine(self, y, places, out, *, gates=None) -> None:
         """out (y's type, [n, width]): each row's sum of the rows of `y` ([n k, width],
         rows may be apart) at its `places`, times its gates f32 [n, k] (mlip_combine)."""
         t = self.torch
-        stride = self._rows(y, "y")
+        m, width, stride, kind = self._matrix(y, "y")
         _need(places.dim() == 2, "places is not 2-d")
         n, top_k = places.shape
-        if y.shape[0] != n * top_k:
-            raise ValueError(f"y has {y.shape[0]} rows, not {n} x {top_k}")
-        width = y.shape[1]
+        if m != n * top_k:
+            raise ValueError(f"y has {m} rows, not {n} x {top_k}")
         self._dense(places, "places", t.int32, n, top_k)
         self._dense(out, "out", y.dtype, n, width)
         if gates is not None:
             self._dense(gates, "gates", t.float32, n, top_k)
-        p = self._params(b.mlip_rows_params, 1, top_k, width, self._dtypes[y.dtype])
+        p = self._params(b.mlip_rows_params, 1, top_k, width, kind)
         self._run(b.mlip_combine, self.ctx, p, n, _ptr(y), stride, _ptr(places), _ptr(gates), _ptr(out))
 
     def combine_backward(self, dout, y, places, dy, *, gates=None, dgates=None) -> None:
@@ -313,12 +330,11 @@ class Learner(_OnStream):
         they are) and, where it is given, dgates f32 [n, k], which alone needs `y`
         (otherwise None may stand there) (mlip_combine_backward)."""
         t = self.torch
-        stride = self._rows(dout, "dout")
+        rows, width, stride, kind = self._matrix(dout, "dout")
         _need(places.dim() == 2, "places is not 2-d")
         n, top_k = places.shape
-        if dout.shape[0] != n:
-            raise ValueError(f"dout has {dout.shape[0]} rows, not {n}")
-        width = dout.shape[1]
+        if rows != n:
+            raise ValueError(f"dout has {rows} rows, not {n}")
         self._dense(places, "places", t.int32, n, top_k)
         self._dense(dy, "dy", dout.dtype, n * top_k, width)
         if gates is not None:
@@ -330,7 +346,7 @@ class Learner(_OnStream):
             y_stride = self._rows(y, "y")
             if not (y.dtype == dout.dtype and tuple(y.shape) == (n * top_k, width)):
                 raise ValueError(f"y is {y.dtype} {tuple(y.shape)}, not {dout.dtype} {(n * top_k, width)}")
-        p = self._params(b.mlip_rows_params, 1, top_k, width, self._dtypes[dout.dtype])
+        p = self._params(b.mlip_rows_params, 1, top_k, width, kind)
         self._run(b.mlip_combine_backward, self.ctx, p, n, _ptr(dout), stride, _ptr(y) if dgates is not None else None,
                   y_stride, _ptr(places), _ptr(gates), _ptr(dy), _ptr(dgates))
 
@@ -339,8 +355,7 @@ class Learner(_OnStream):
         with what `group` wrote, their n top_k entries in the experts' order, rows of
         entries without an expert left as they are (mlip_pack8)."""
         t = self.torch
-        stride = self._rows(x, "x")
-        n, width = x.shape
+        n, width, stride, kind = self._matrix(x, "x")
         _need((offsets is None) == (order is None), "offsets and order go together")
         _need(order is not None or top_k == 1, "top_k is 1 without an order")
         experts = 1
@@ -350,22 +365,23 @@ class Learner(_OnStream):
             self._dense(offsets, "offsets", t.int32, experts + 1)
             self._dense(order, "order", t.int32, n * top_k)
         self._packed(rows8, "rows8", n * top_k, width)
-        p = self._params(b.mlip_rows_params, experts, top_k, width, self._dtypes[x.dtype])
-        self._run(b.mlip_pack8, self.ctx, p, n, _ptr(x), stride, _ptr(offsets), _ptr(order), _ptr(rows8.codes),
-                  _ptr(rows8.exps))
+        p = self._params(b.mlip_rows_params, experts, top_k, width, kind)
+        self._run(b.mlip_pack8, self.ctx, p, n, x.data_ptr(), stride, _ptr(offsets), _ptr(order), *_at(rows8))
 
     def unpack8(self, rows8: Rows8, x) -> None:
         """The values of rows in 8 bits into x, f32 or bf16 [rows, width] (mlip_unpack8)."""
         if x.dtype not in self._dtypes:
             raise ValueError(f"x is {x.dtype}, not float32 or bfloat16")
-        self._packed(rows8, "rows8", rows8.rows, rows8.width)
-        self._dense(x, "x", x.dtype, rows8.rows, rows8.width)
-        p = self._params(b.mlip_rows_params, 1, 1, rows8.width, self._dtypes[x.dtype])
-        self._run(b.mlip_unpack8, self.ctx, p, rows8.rows, _ptr(rows8.codes), _ptr(rows8.exps), _ptr(x))
+        _, _, n, width = rows8._held
+        self._packed(rows8, "rows8", n, width)
+        self._dense(x, "x", x.dtype, n, width)
+        p = self._params(b.mlip_rows_params, 1, 1, width, self._dtypes[x.dtype])
+        self._run(b.mlip_unpack8, self.ctx, p, n, *_at(rows8), x.data_ptr())
 
     def _matrices(self, w8: Weights8, name: str) -> None:
-        if w8.codes.device != self.device:
-            raise ValueError(f"{name} is on {w8.codes.device}, not {self.device}")
+        codes = w8._held[0]
+        if codes.get_device() != self._index:
+            raise ValueError(f"{name} is on {codes.device}, not {self.device}")
 
     def pack8_weights(self, w, w8: Weights8) -> None:
         """Matrices (f32 or bf16 [experts, outputs, inputs]) in 8 bits, and their
@@ -387,18 +403,20 @@ class Learner(_OnStream):
         t = self.torch
         if y.dtype not in self._dtypes:
             raise ValueError(f"y is {y.dtype}, not float32 or bfloat16")
-        _need(not transposed or w8.t_codes is not None, "w8 has no transposes")
-        n_in, n_out = (w8.outputs, w8.inputs) if transposed else (w8.inputs, w8.outputs)
+        codes, exps, t_codes, t_exps, experts, n_out, n_in = w8._held
+        if transposed:
+            _need(t_codes is not None, "w8 has no transposes")
+            codes, exps, n_out, n_in = t_codes, t_exps, n_in, n_out
         self._matrices(w8, "w8")
-        self._packed(x8, "x8", x8.rows, n_in)
-        self._dense(y, "y", y.dtype, x8.rows, n_out)
-        self._expert_offsets(offsets, w8.experts)
+        m = x8._held[2]
+        self._packed(x8, "x8", m, n_in)
+        self._dense(y, "y", y.dtype, m, n_out)
+        self._expert_offsets(offsets, experts)
         if bias is not None:
-            self._dense(bias, "bias", t.float32, w8.experts, n_out)
-        p = self._params(b.mlip_product8_params, w8.experts, n_in, n_out, self._dtypes[y.dtype])
-        codes, exps = (w8.t_codes, w8.t_exps) if transposed else (w8.codes, w8.exps)
-        self._run(b.mlip_product8, self.ctx, p, x8.rows, _ptr(x8.codes), _ptr(x8.exps), _ptr(codes), _ptr(exps),
-                  _ptr(offsets), _ptr(bias), _ptr(y))
+            self._dense(bias, "bias", t.float32, experts, n_out)
+        p = self._params(b.mlip_product8_params, experts, n_in, n_out, self._dtypes[y.dtype])
+        self._run(b.mlip_product8, self.ctx, p, m, *_at(x8), codes.data_ptr(), exps.data_ptr(), _ptr(offsets), _ptr(bias),
+                  y.data_ptr())
 
     def product8_weights(self, dy8: Rows8, x8: Rows8, dweights, *, offsets=None, dbias=None) -> None:
         """The matrices' gradients, f32 [experts, outputs, inputs], and dbias f32
@@ -406,22 +424,22 @@ class Learner(_OnStream):
         t = self.torch
         _need(dweights.dim() == 3, "dweights is not 3-d")
         experts, n_out, n_in = dweights.shape
-        self._packed(x8, "x8", x8.rows, n_in)
-        self._packed(dy8, "dy8", x8.rows, n_out)
+        m = x8._held[2]
+        self._packed(x8, "x8", m, n_in)
+        self._packed(dy8, "dy8", m, n_out)
         self._dense(dweights, "dweights", t.float32, experts, n_out, n_in)
         self._expert_offsets(offsets, experts)
         if dbias is not None:
             self._dense(dbias, "dbias", t.float32, experts, n_out)
         p = self._params(b.mlip_product8_params, experts, n_in, n_out, b.MLIP_F32)
-        self._run(b.mlip_product8_weights, self.ctx, p, x8.rows, _ptr(dy8.codes), _ptr(dy8.exps), _ptr(x8.codes),
-                  _ptr(x8.exps), _ptr(offsets), _ptr(dweights), _ptr(dbias))
+        self._run(b.mlip_product8_weights, self.ctx, p, m, *_at(dy8), *_at(x8), _ptr(offsets), dweights.data_ptr(),
+                  _ptr(dbias))
 
     def activate8(self, z, kept: Optional[Rows8] = None, h=None, *, h8: Optional[Rows8] = None, residual=None) -> None:
         """h = residual + silu(z) of the rows of `z` (f32 or bf16 [n, width], rows may be
         apart, residual too) into h (z's type) and, packed, h8; z itself, packed, into
         `kept` for the backward pass (mlip_activate8)."""
-        stride = self._rows(z, "z")
-        n, width = z.shape
+        n, width, stride, kind = self._matrix(z, "z")
         residual_stride = width
         if residual is not None:
             residual_stride = self._rows(residual, "residual")
@@ -429,26 +447,25 @@ class Learner(_OnStream):
                 raise ValueError(f"residual is {residual.dtype} {tuple(residual.shape)}, not {z.dtype} {tuple(z.shape)}")
         if h is not None:
             self._dense(h, "h", z.dtype, n, width)
-        for r, name in ((kept, "kept"), (h8, "h8")):
-            if r is not None:
-                self._packed(r, name, n, width)
-        p = self._params(b.mlip_rows_params, 1, 1, width, self._dtypes[z.dtype])
-        self._run(b.mlip_activate8, self.ctx, p, n, _ptr(z), stride, _ptr(residual), residual_stride, _ptr(h),
-                  _ptr(h8 and h8.codes), _ptr(h8 and h8.exps), _ptr(kept and kept.codes), _ptr(kept and kept.exps))
+        if kept is not None:
+            self._packed(kept, "kept", n, width)
+        if h8 is not None:
+            self._packed(h8, "h8", n, width)
+        p = self._params(b.mlip_rows_params, 1, 1, width, kind)
+        self._run(b.mlip_activate8, self.ctx, p, n, z.data_ptr(), stride, _ptr(residual), residual_stride, _ptr(h), *_at(h8),
+                  *_at(kept))
 
     def activate8_backward(self, kept: Rows8, dh, dz=None, *, dz8: Optional[Rows8] = None) -> None:
         """dz = dh silu'(z) with the z that was kept, into dz (dh's type, [n, width]) and,
         packed, dz8; dh's rows may be apart (mlip_activate8_backward)."""
-        stride = self._rows(dh, "dh")
-        n, width = dh.shape
+        n, width, stride, kind = self._matrix(dh, "dh")
         self._packed(kept, "kept", n, width)
         if dz is not None:
             self._dense(dz, "dz", dh.dtype, n, width)
         if dz8 is not None:
             self._packed(dz8, "dz8", n, width)
-        p = self._params(b.mlip_rows_params, 1, 1, width, self._dtypes[dh.dtype])
-        self._run(b.mlip_activate8_backward, self.ctx, p, n, _ptr(kept.codes), _ptr(kept.exps), _ptr(dh), stride, _ptr(dz),
-                  _ptr(dz8 and dz8.codes), _ptr(dz8 and dz8.exps))
+        p = self._params(b.mlip_rows_params, 1, 1, width, kind)
+        self._run(b.mlip_activate8_backward, self.ctx, p, n, *_at(kept), dh.data_ptr(), stride, _ptr(dz), *_at(dz8))
 
 
 class AdamW(_OnStream):
