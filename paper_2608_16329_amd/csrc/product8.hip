@@ -157,10 +157,13 @@ __device__ __forceinline__ void put4(void* y, int64_t at, int left, const f4 v) 
 // come to LDS as they are, without registers, while the block before is multiplied;
 // the next tile's first block comes during a tile's last step, so that only the stores
 // of the results stand between two tiles, and those of a full tile are not waited for.
-// 65,536 rows, 8 experts, 1,024 inputs to 4,096 outputs, bfloat16: 306 to 326 us (1,690
-// to 1,800 TFLOP/s), 168 MB read from memory and 525 written, the matrix instructions
+// 65,536 rows, 8 experts, 1,024 inputs to 4,096 outputs, bfloat16: 306 to 357 us (1,540
+// to 1,800 TFLOP/s, the cards differ), 168 MB read from memory and 525 written, the matrix instructions
 // busy for 35% of the cycles: a tile has eight steps only, and its results take 60 us of
 // stores; 4,096 to 1,024: 326 to 350, four rounds of tiles and a fifth of a few.
+// Four or sixteen tiles of rows beside each other instead of eight, and a higher priority
+// of wavefronts while they multiply, are within 2% (the gradients below get 8% slower
+// by that priority).
 
 // Which of a wavefront's outputs row r of its operand i of W is: the four that a
 // lane gets of each of two neighbouring operands (rows 4 g .. 4 g + 3) are eight
