@@ -29,7 +29,7 @@ namespace {
 struct Spot {
   int64_t row;
   int block, at, left;
-  bool there;                   // the row and the block exist
+  bool there;                   // the row and the block exist (and, packing, the row's entry)
 };
 template <bool BF, int G>
 __device__ __forceinline__ Spot spot(int64_t row0, int quad, int64_t n, int width) {
@@ -63,9 +63,11 @@ __device__ __forceinline__ void each(int64_t n, int width, F f) {
   }
 }
 
-// Writes a block's codes and exponent: all lanes of the wavefront call.
+// Writes a block's codes and exponent where it is there: all lanes of the wavefront
+// call.  The lane that writes a row's exponents has the first of its four blocks,
+// which a row that is there always has.
 template <bool BF, int G>
-__device__ __forceinline__ void put(const Spot& s, const float v[8], uint8_t* codes, uint8_t* exps, int quad, int width, int64_t n) {
+__device__ __forceinline__ void put(const Spot& s, const float v[8], uint8_t* codes, uint8_t* exps, int quad, int width) {
   const int e = exponent8(max16(largest8(v)));
   if (s.there) {
     const u2v c = encode8(v, e);
@@ -79,7 +81,7 @@ __device__ __forceinline__ void put(const Spot& s, const float v[8], uint8_t* co
   uint32_t word = s.there ? uint32_t(e + 127) << (8 * (s.block & 3)) : 0u;
   if (G >= 2) word |= __shfl_xor(word, 16);
   if (G == 4) word |= __shfl_xor(word, 32);
-  if ((threadIdx.x & 15) == 0 && s.block % 4 == 0 && s.row < n)
+  if ((threadIdx.x & 15) == 0 && s.block % 4 == 0 && s.there)
     *reinterpret_cast<uint32_t*>(exps + s.row * exps8(width) + 4 * quad) = word;
 }
 // Values of a block that was written.
@@ -112,7 +114,7 @@ __global__ __launch_bounds__(256) void k_pack8(Pack8Args a) {
     s.there = s.there && from >= 0;
     float v[8] = {};
     if (s.there) load8<BF, STREAM>(a.x, from * a.x_stride + s.at, s.left, v);
-    put<BF, G>(s, v, a.codes, a.exps, quad, a.width, end);
+    put<BF, G>(s, v, a.codes, a.exps, quad, a.width);
   });
 }
 
@@ -160,13 +162,13 @@ __global__ __launch_bounds__(256) void k_activate8(Pack8Args a) {
       load8<BF, STREAM>(a.x, s.row * a.x_stride + s.at, s.left, z);
       if (a.residual) load8<BF, STREAM>(a.residual, s.row * a.residual_stride + s.at, s.left, h);
     }
-    if (a.codes) put<BF, G>(s, z, a.codes, a.exps, quad, a.width, a.n);
+    if (a.codes) put<BF, G>(s, z, a.codes, a.exps, quad, a.width);
 #pragma unroll
     for (int q = 0; q < 8; ++q) h[q] = fmaf(z[q], sigmoid(z[q]), h[q]);
     if (a.out && s.there) store8<BF, STREAM>(a.out, s.row * a.width + s.at, s.left, h);
     if (a.out_codes) {
       as_stored<BF>(h);
-      put<BF, G>(s, h, a.out_codes, a.out_exps, quad, a.width, a.n);
+      put<BF, G>(s, h, a.out_codes, a.out_exps, quad, a.width);
     }
   });
 }
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(256) void k_activate8_backward(Pack8Args a) {
     if (a.out && s.there) store8<BF, STREAM>(a.out, s.row * a.width + s.at, s.left, d);
     if (a.out_codes) {
       as_stored<BF>(d);
-      put<BF, G>(s, d, a.out_codes, a.out_exps, quad, a.width, a.n);
+      put<BF, G>(s, d, a.out_codes, a.out_exps, quad, a.width);
     }
   });
 }
