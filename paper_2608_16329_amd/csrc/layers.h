@@ -55,6 +55,23 @@ struct Pack8Args {
   uint8_t* out_codes;         // of h or dz, or null
   uint8_t* out_exps;
 };
+// Whether values go past the last cache, of 256 MB, in and out: where they are more
+// than it holds, what comes next would not find them there, and finds the codes (65,536
+// rows of 4,096 bfloat16 values: packing 148 us and 126 so, unpacking 141 and 120, the
+// activation 250 and 220, its gradient 252 and 203; 16,384 rows of 2,048, which stay there
+// from call to call, 19 and 22, 16 and 15, 31 and 34, 33 and 38).
+// With an order each row is read again for each of its experts, so rows that stay there
+// together with their codes do not go past it (1,024 bfloat16 values, through the cache and
+// past it: 10,240 rows, 16 experts each, 75 us and 97, 131 and 155 with unpacking behind it;
+// 45,000 rows, 3 each, 62 and 82, 111 and 131).  Where they do not fit, the codes count, which
+// what comes next reads: 131,072 rows, 2 each, 153 and 149, 291 and 261 with unpacking; 65,536
+// rows, 4 each, 127 and 148, 280 and 259 (but 100,000 rows of 512 float32 values, 8 each, 276
+// and 390, 655 and 763: codes that do not fit by themselves gain nothing).
+inline bool pack8_streams(const Pack8Args& a) {
+  constexpr int64_t kCache = int64_t(1) << 28;
+  const int64_t values = a.n * a.width * (a.bf16 ? 2 : 4);
+  return values > kCache && (!a.order || values / a.K + a.n * (codes8(a.width) + exps8(a.width)) > kCache);
+}
 hipError_t launch_pack8(const Pack8Args& a, int n_cu, hipStream_t s);
 hipError_t launch_unpack8(const Pack8Args& a, int n_cu, hipStream_t s);
 hipError_t launch_activate8(const Pack8Args& a, int n_cu, hipStream_t s);

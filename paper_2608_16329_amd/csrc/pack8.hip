@@ -271,13 +271,6 @@ __global__ __launch_bounds__(256) void k_pack8_weights(Weights8Args a) {
   }
 }
 
-// Values that are more than the last cache, of 256 MB, holds go past it in and out: what
-// comes next would not find them there, and finds the codes (65,536 rows of 4,096 bfloat16
-// values: packing 148 us and 126 so, unpacking 141 and 120, the activation 250 and
-// 220, its gradient 252 and 203; 16,384 rows of 2,048, which stay there from call to call, 19
-// and 22, 16 and 15, 31 and 34, 33 and 38).
-bool streams(const Pack8Args& a) { return a.n * a.width * (a.bf16 ? 2 : 4) > int64_t(1) << 28; }
-
 template <typename F>
 hipError_t with_group(const Pack8Args& a, int n_cu, F run) {
   const int blocks = (a.width + kBlock8 - 1) / kBlock8, quads = (blocks + 3) / 4;
@@ -285,7 +278,7 @@ hipError_t with_group(const Pack8Args& a, int n_cu, F run) {
   const int64_t units = (a.n + rows - 1) / rows * quads;
   const unsigned g = unsigned(std::max<int64_t>(1, std::min<int64_t>((units + 3) / 4, int64_t(n_cu) * 64)));
   const auto with = [&](auto w) {
-    if (streams(a)) run(w, std::true_type(), g);
+    if (pack8_streams(a)) run(w, std::true_type(), g);
     else run(w, std::false_type(), g);
   };
   if (blocks == 1) with(std::integral_constant<int, 1>());
