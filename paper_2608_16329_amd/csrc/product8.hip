@@ -158,7 +158,7 @@ __device__ __forceinline__ void put4(void* y, int64_t at, int left, const f4 v) 
 // the next tile's first block comes during a tile's last step, so that only the stores
 // of the results stand between two tiles, and those of a full tile are not waited for.
 // 65,536 rows, 8 experts, 1,024 inputs to 4,096 outputs, bfloat16: 306 to 357 us (1,540
-// to 1,800 TFLOP/s, the cards differ), 168 MB read from memory and 525 written, the matrix instructions
+// to 1,800 TFLOP/s, the cards differ), 339 MB read past L2 and 538 written, the matrix instructions
 // busy for 35% of the cycles: a tile has eight steps only, and its results take 60 us of
 // stores; 4,096 to 1,024: 326 to 350, four rounds of tiles and a fifth of a few.
 // Four or sixteen tiles of rows beside each other instead of eight, and a higher priority
@@ -623,7 +623,7 @@ __global__ __launch_bounds__(256) void k_product_few(Product8Args a, int col_til
 // slices of them, which k_add_slices adds up in order.
 // 65,536 rows, 8 experts of 3,500 to 15,500 rows, 4,096 x 1,024: 550 to 615 us (890 to
 // 1,000 TFLOP/s; a product of 8,192 x 8,192 x 8,192 of the library's bfloat16 1,072),
-// 600 MB read from memory; 4,096 x 4,096 of one expert 1,220 TFLOP/s.  The matrix
+// 1.23 GB read past L2; 4,096 x 4,096 of one expert 1,220 TFLOP/s.  The matrix
 // instructions are busy for 42% of the cycles, LDS for 37% (bank conflicts 10%).
 // Columns laid transposed by the threads that write them were slower (851 us against
 // 627), writes without conflicts too (645 against 636), sixteen wavefronts of 64 x 64
