@@ -507,7 +507,10 @@ mlip_status mlip_heads(mlip_learn* ctx, const mlip_heads_params* p, int64_t n, c
 /*
  * Layers of experts wider than the energy heads (hidden width 64): rows are
  * brought into the experts' order, go through matrix products and activations,
- * and come back with weights.  Between the products rows are held in 8 bits.
+ * and come back with weights.  Between the products rows are held in 8 bits, so a
+ * result is a step function of its inputs, and the gradients are those of the layers
+ * without that rounding: they serve training, and values that are not differentiated
+ * again, not an energy whose derivative is to be the force on an atom.
  *
  * mlip_sort: entry i top_k + s (row i, its s-th expert) stands at place p with
  * order[p] = i top_k + s (offsets_dev, order_dev as mlip_group writes them):
@@ -556,6 +559,7 @@ mlip_status mlip_combine_backward(mlip_learn* ctx, const mlip_rows_params* p, in
  *         128, zeros behind the row's end; aligned to 16 bytes
  *   exps  uint8 [rows][mlip_row8_exps(width)], e + 127 of each block, rounded up
  *         to a multiple of four, zeros behind the last; aligned to 4 bytes
+ * (whole blocks: 64 and 129 values take 132 and 260 bytes, more than in bf16)
  * mlip_pack8 packs n rows, or, with offsets_dev and order_dev (both or neither),
  * their entries in the experts' order as mlip_sort would write them: n top_k rows,
  * those from offsets[n_experts] on left as they are.  mlip_unpack8 writes the
@@ -594,7 +598,8 @@ mlip_status mlip_unpack8(mlip_learn* ctx, const mlip_rows_params* p, int64_t n, 
  * mlip_product8_weights: dweights_dev f32 [n_experts][outputs][inputs],
  * sum_p dy_p x_p^T over the expert's rows, and, unless NULL, dbias_dev f32
  * [n_experts][outputs], sum_p dy_p; 0 for experts without rows.  Float32 sums of
- * the packed values' products; dtype is not looked at beyond its range.  A NaN in
+ * the packed values' products, in dbias of the packed values (a caller who has dy
+ * in more bits may sum that instead); dtype is not looked at beyond its range.  A NaN in
  * a row gives NaN wherever it is a factor.  No output may overlap an input.
  * m in [0, 2^31), n_experts 1..256, inputs and outputs 1..65536, and (m / 128 +
  * n_experts) outputs / 128, and n_experts inputs outputs / 2^14, below 2^22.

@@ -8,15 +8,20 @@
 // 2^(e - 6)).  A matrix shares e over 128 x 128 values, so that its transpose
 // has the same values.
 //
-// Bound by memory.  16 lanes have a block, 8 values each; a wavefront has four
-// blocks, whose exponents are one 32-bit word: four of a row, or one or two each
-// of four or two rows that have no more.  Wavefronts that run side by side have
-// neighbouring blocks, and float32 stores of 16 lanes are whole lines (both, and
-// conversions in hardware: 744 to 533 us of the two activations below).
-// 131,072 rows of 1,024 bfloat16 values in the order of 2 of 16 experts: packing 150 to
+// Bound by memory, activations by vector instructions about as much.  16 lanes have a
+// block, 8 values each; a wavefront has four blocks, whose exponents are one 32-bit
+// word: four of a row, or one or two each of four or two rows that have no more.
+// Wavefronts that run side by side have neighbouring blocks, and float32 stores of 16
+// lanes are whole lines (both, and conversions in hardware: 744 to 533 us of the two
+// activations below).
+// 131,072 rows of 1,024 bfloat16 values in the order of 2 of 16 experts: packing 147 to
 // 161 us (5.0 TB/s with each row read twice), unpacking 118 to 128 (6.3, partly from the
-// last cache); 65,536 rows of 4,096 bfloat16 values: silu that keeps its argument 220 to
-// 228 us, its gradient 203 to 221 (1.34 GB each, 6 TB/s; 466 the two in turn on new values).
+// last cache).  65,536 rows of 4,096 bfloat16 values, the last 50 of 100 launches on normally
+// distributed values: silu that keeps its argument 237 us (225 to 250), its gradient 215
+// (1.34 GB each, 5.7 and 6.3 TB/s; 458 to 466 the two in turn); the first dozen launches, before the
+// clock has settled, 214 to 300.  With results in 8 bits instead, 1.07 GB, 256 and 248: the maxima
+// and the encoding bring the vector instructions to 172 and 159 million, and these, at four
+// cycles each, fill the SIMDs (136 and 124 million without).
 #include <algorithm>
 
 #include "layers_math.h"

@@ -156,7 +156,8 @@ __device__ __forceinline__ void put4(void* y, int64_t at, int left, const f4 v) 
 // A work-group takes tiles in turn.  A step is one block of 128 inputs: its codes
 // come to LDS as they are, without registers, while the block before is multiplied;
 // the next tile's first block comes during a tile's last step, so that only the stores
-// of the results stand between two tiles, and those of a full tile are not waited for.
+// of the results stand between two tiles, and those of a full tile are not waited for
+// until the next one's first step ends.
 // 65,536 rows, 8 experts, 1,024 inputs to 4,096 outputs, bfloat16: 306 to 357 us (1,540
 // to 1,800 TFLOP/s, the cards differ), 339 MB read past L2 and 538 written, the matrix instructions
 // busy for 35% of the cycles: a tile has eight steps only, and its results take 60 us of
@@ -522,8 +523,6 @@ __global__ __launch_bounds__(64 * WR * WC) void k_product(Product8Args a) {
 }
 
 // ---- few rows: 16 RF rows and 16 outputs, the blocks of inputs shared by wavefronts ----
-
-// ---- few rows -----------------------------------------------------------------------
 //
 // Bound by the weights, that is by memory or, for a row or two, by latency: they are
 // read once for every 16 RF rows, straight to registers; a work-group has 16 outputs,
@@ -612,8 +611,7 @@ __global__ __launch_bounds__(256) void k_product_few(Product8Args a, int col_til
   }
 }
 
-// ---- gradients of the matrices ----------------------------------------------------
-
+// ---- gradients of the matrices ------------------------------------------------------
 //
 // The sum runs over rows, and an operand's values of one column are those of
 // consecutive rows: rows go to LDS as they come, in bfloat16 (codes times their row's
@@ -699,7 +697,9 @@ __device__ __forceinline__ bf8 columns(const unsigned char* lds, int lane_at, in
         (__attribute__((address_space(3))) s4*)(lds + (lane_at ^ (32 * i)) + 16 * s * (2 * COLS)));
   return __builtin_bit_cast(bf8, s8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]});
 }
-// Where a lane's first four values of a wavefront's columns are (first a multiple of 64 columns).
+// Where a lane's first four values of a wavefront's columns are.  `first` is a multiple
+// of the wavefront's columns, a power of two of them, so that 16 i more of them is an
+// exclusive or with 32 i bytes.
 template <int COLS>
 __device__ __forceinline__ int columns_at(int first) {
   const int lane = threadIdx.x & 63, p = 4 * (lane >> 4) + ((lane & 15) >> 2);
@@ -890,6 +890,8 @@ hipError_t launch_product8(const Product8Args& a, int n_cu, hipStream_t s) {
   // leave seven CUs of eight without one (1,024 inputs and outputs, bfloat16: 100 rows,
   // 8 tiles, 5.5 us against 10.2; 512 rows, 32 tiles, 8.3 against 10.3; 4,096 of both,
   // 64 rows, 32 tiles, 16.2 against 25.0; 1,000 rows of 4,096 inputs, 64 tiles, 53 against 30).
+  // The experts' own sizes are not known here: 4,096 rows at one of 256 experts, 1,024 inputs
+  // and outputs, take 93 us (101 with even shares), one expert's own 4,096 rows 11.
   const bool few = a.m <= int64_t(16) * a.E || parts(128) * ((a.N + 127) / 128) <= n_cu / 8;
   if (few) {
     const int cols = (a.N + 15) / 16;
@@ -923,6 +925,9 @@ hipError_t launch_product8(const Product8Args& a, int n_cu, hipStream_t s) {
     const bool large = rounds(256, n_cu) * 5 <= rounds(128, 2 * n_cu) * 3;
     // Results that are larger than the last cache, of 256 MB, go past it (65,536 x 4,096:
     // 306 us against 334 and 591 against 632; results that fit are read by what comes next).
+    // Those of 128 x 128 tiles do not: most are narrow, and parts of lines cost more past the
+    // cache (float32, 4,300,000 x 33: 1,353 us through it, 1,432 past it; 300,000 x 257: 160 and
+    // 197; 128 bfloat16 outputs, whole lines: 2,200,000 rows 238 and 232, 1,200,000 of 128 inputs 108 and 80).
     const bool stream = a.m * a.N * (a.bf16 ? 2 : 4) > int64_t(1) << 28;
     const auto with = [&](auto f32) {
       constexpr bool kF32 = f32.value;
@@ -958,7 +963,10 @@ size_t product8_weights_plan(Product8Args* a, int n_cu) {
   // slices of rows where the experts' tiles do not fill the CUs, one work-group each
   // or, of the small ones, two: as many as fit at once, each expert's last one shorter
   // (30,001 rows, 6 experts, 321 x 385: 41, 36 and 40 us with one, two and three, 131
-  // without slices; 16,384 rows, 2,048 x 2,048: 152 with one, 169 with two, 444 without)
+  // without slices; 16,384 rows, 2,048 x 2,048: 152 with one, 169 with two, 444 without).
+  // The experts' own sizes are not known here: with slices they hardly matter (262,144 rows, 64
+  // experts, 256 x 256: 73 to 75 us), without them the largest one's tiles end late (512 x 512:
+  // 159 us with even shares, 237, 348 and 634 where the largest has 2, 3 and 6 times the mean)
   const int64_t fit = int64_t(n_cu) * (large ? 1 : 2) / tiles, most = a->offsets ? fit - a->E : fit;
   if (tiles * a->E < n_cu) a->slice = std::max<int64_t>(256, most > 0 ? (a->m + most - 1) / most : a->m);
   a->slice = std::max<int64_t>(1, (a->slice + 63) / 64 * 64);
